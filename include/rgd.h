@@ -19,6 +19,12 @@
  *   rgd_soft_gate           its soft variant (the appendix ablation, Alg. 2),
  *   rgd_residual_precheck   the residual-stream classifier that lets a prompt
  *                           skip the probe (App. A), once per prompt.
+ * A step whose rows decode several drafted tokens at once has beside them:
+ *   rgd_w4_matvec           products of a few rows with 4-bit weights, as an
+ *                           output matrix or a draft model keeps them,
+ *   rgd_verify_draft        drafted tokens against the target's probabilities,
+ *   rgd_cache_*             the pages of the KV cache: reserved and written for
+ *                           new tokens, forked, trimmed, copied and compacted.
  *
  * Conventions for every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller unless a comment
@@ -60,6 +66,7 @@ extern "C" {
 #define RGD_DEV_BAD_TOKEN 2     /* negative probe token that is not the stop token: skipped */
 #define RGD_DEV_WAIT_TIMEOUT 4  /* a bounded wait on a copy gave up; outputs of that block are missing */
 #define RGD_DEV_BAD_PARAM 8     /* temperature < 0 or not finite, min_p outside [0, 1], or non-finite logits max */
+#define RGD_DEV_NO_PAGE 16      /* the pool has fewer free pages than rgd_cache_reserve was asked for */
 
 /* logits element types */
 #define RGD_F32 0
@@ -383,6 +390,175 @@ int rgd_soft_gate(const rgd_trie* trie, int32_t groups, int32_t rows_per_group, 
 int rgd_residual_precheck(int32_t groups, int32_t d, int32_t dtype, const void* h, const float* w, float bias,
                           float theta, int32_t rows_per_group, float* prob_out, rgd_gate_state* state,
                           uint8_t* row_active, int32_t* dev_status, rgd_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Verification of drafted tokens                                             */
+/* ------------------------------------------------------------------------ */
+
+/* Bytes of device workspace rgd_verify_draft needs (0 on a negative argument). */
+size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
+
+/* Row r has n = n_draft[r] drafted tokens d_0 .. d_{n-1} (a draft model's, a
+ * phrase list's, the refusal trie's own continuation) and the target's logits at
+ * the n + 1 positions they lead to: position k follows the row's prefix and d_0 ..
+ * d_{k-1}.  Sample rows (as in rgd_sample_head): with p_k and q_k the target's and
+ * the draft's softmax(l / T) over their min-p kept sets {l >= c}, c = fl32(l_max +
+ * fl32(T ln p_min)), in order of k
+ *   d_k is accepted if accept_u[r, k] q_k(d_k) < p_k(d_k);
+ *   at the first that is not, the row's last token is drawn from max(0, p_k - q_k)
+ *   (from p_k should that be 0 everywhere); if all are accepted it is drawn from p_n:
+ *   token = the smallest i whose cumulative weight exceeds draw_u[r] times their sum.
+ * The tokens that come out are distributed as p, whatever the draft.  Greedy rows
+ * (is_probe or temperature 0): d_k is accepted if it is the argmax (lowest index on
+ * ties), and the last token is the argmax; draft_logits, min_p and the uniforms are
+ * not read.
+ *   target_logits  [rows, max_draft + 1] rows of vocab logits, target_stride elements
+ *                  apart (>= vocab), dtype RGD_F32 or RGD_BF16
+ *   draft_logits   [rows, max_draft] rows of vocab logits of the same dtype,
+ *                  draft_stride elements apart; NULL: every draft was certain
+ *                  (q_k(d_k) = 1).  Rows that start on 16 bytes are read by bulk copies
+ *   draft_tokens   int32 [rows, max_draft]; one outside [0, vocab) sets
+ *                  RGD_DEV_BAD_TOKEN, is rejected, and the draw there is from p_k
+ *   n_draft        int32 [rows], in [0, max_draft]; NULL: max_draft each
+ *   is_probe       uint8 [rows] or NULL; temperature, min_p float [rows]
+ *   accept_u       float [rows, max_draft], draw_u float [rows]: independent
+ *                  uniforms in [0, 1)
+ *   row_active     uint8 [rows] or NULL (all active)
+ *   token_out      int32 [rows, max_draft + 1]: the accepted drafts, the last token,
+ *                  then -1; all -1 for inactive and rejected rows
+ *   accepted_out   int32 [rows]: accepted drafts (0 for inactive and rejected rows);
+ *                  token_out[r] holds accepted_out[r] + 1 tokens
+ *   accept_prob    float [rows, max_draft] or NULL: min(1, p_k(d_k) / q_k(d_k)) of
+ *                  every drafted position (1 or 0 in greedy rows), whether the row
+ *                  gets there or not; 0 past n_draft
+ *   workspace      rgd_verify_draft_workspace_size() bytes, 4-byte aligned, zero-filled
+ *                  before its first use; a call leaves the row counts at its start at
+ *                  zero again unless it reports RGD_DEV_WAIT_TIMEOUT (zero-fill it
+ *                  then, and where rows grows).  Calls that share it must not overlap
+ * A row with n_draft, temperature, min_p or a uniform out of range, or with a
+ * position it gets to whose largest logit is not finite, is rejected and sets
+ * RGD_DEV_BAD_PARAM.  NaN logits have no weight.  Weights are 2^((l - l_max)
+ * log2(e)/T) in fp32, rounded to multiples of 2^-31 and summed exactly, so the
+ * outputs do not depend on how a call is cut.  RGD_ERR_UNSUPPORTED when a position's
+ * one or two rows take more than about 3.5 MB.  One kernel on `stream`. */
+int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, int32_t dtype, const void* target_logits,
+                     int64_t target_stride, const void* draft_logits, int64_t draft_stride,
+                     const int32_t* draft_tokens, const int32_t* n_draft, const uint8_t* is_probe,
+                     const float* temperature, const float* min_p, const float* accept_u, const float* draw_u,
+                     const uint8_t* row_active, int32_t* token_out, int32_t* accepted_out, float* accept_prob,
+                     void* workspace, size_t workspace_bytes, int32_t* dev_status, rgd_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Products with 4-bit weights                                                */
+/* ------------------------------------------------------------------------ */
+
+/* y[i, j] = sum_k x[i, k] W[j, k],  W[j, k] = (q[j, k] - z[j, k / G]) s[j, k / G],
+ * for a few rows of activations (m up to some tens; any m is right).
+ *   x        bf16 [m, k]
+ *   weights  uint8 [n, ceil(k / 2)]: q in 4 bits, the even k in the low half of its
+ *            byte; the last high half of an odd k is not read as a weight
+ *   scales   [n, ceil(k / G)], scale_dtype RGD_F32 or RGD_BF16, finite; G = group_size
+ *            = 32, 64 or 128; the last group of a row may be short
+ *   zeros    uint8 [n, ceil(k / G)], 0 to 15, or NULL (8 everywhere)
+ *   y        [m] rows of n elements, y_stride elements apart (>= n; the rest of a row
+ *            is left alone), out_dtype RGD_F32 or RGD_BF16
+ * Products of bf16 activations with the whole numbers q - z are exact and are summed,
+ * and scaled group by group, in fp32; the result is rounded once.  One kernel on
+ * `stream`. */
+int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size, const rgd_bf16* x, const uint8_t* weights,
+                  int32_t scale_dtype, const void* scales, const uint8_t* zeros, int32_t out_dtype, void* y,
+                  int64_t y_stride, rgd_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Pages of the KV cache                                                      */
+/* ------------------------------------------------------------------------ */
+
+/* The pools of a paged cache: for every layer K and V bf16 [num_pages, Hkv,
+ * page_size, D] as rgd_prefix_decode_attn reads them (layer l of k_pages starts at
+ * k_pages + l * layer_stride).  Page i stands for the same tokens in every layer.
+ * page_refs, device int32 [num_pages], counts the rows whose table lists a page; a page
+ * is free exactly if its count is 0.  Whoever fills a table by other means sets the
+ * counts too. */
+typedef struct {
+  int32_t num_layers;    /* >= 1, at most 4096                                      */
+  int32_t num_pages;     /* pages in each pool                                      */
+  int32_t num_kv_heads;  /* Hkv, at most 4096                                       */
+  int32_t page_size;     /* tokens per page: 16                                     */
+  int32_t head_dim;      /* D: a multiple of 8, at most 1024                        */
+  int32_t reserved;      /* must be 0                                               */
+  int64_t layer_stride;  /* elements from a layer's pool to the next; 0: no gap     */
+} rgd_cache_shape;
+
+/* Bytes of device workspace rgd_cache_reserve (for up to `rows` rows) and
+ * rgd_cache_compact need; 16-byte aligned, its contents do not matter.  Calls that
+ * share it must not overlap.  0 on an invalid shape. */
+size_t rgd_cache_workspace_size(const rgd_cache_shape* shape, int32_t rows);
+
+/* Makes room for n_new[r] tokens after the length[r] that row r has: every page that
+ * tokens length .. length + n_new - 1 fall into is the row's own afterwards.  A table
+ * entry < 0 there gets a free page; a page that other rows list too (count > 1) is
+ * replaced by a free page, into which the row's tokens in it (length % page_size of
+ * them) are copied in every layer.  Free pages are taken in order of their number,
+ * by rows in order and within a row by column.
+ *   block_table  int32 [rows, max_pages], updated; length, n_new int32 [rows]
+ *   row_active   uint8 [rows] or NULL (all); other rows are left alone
+ *   page_refs    updated; k_pages, v_pages every layer's pools
+ *   row_ok       uint8 [rows] or NULL: 1 where an active row has its room, else 0
+ * Where the pool runs out, a row whose pages and those of the rows before it (those
+ * refused included) exceed the free pages is left as it was, and RGD_DEV_NO_PAGE is
+ * set.  A row of a negative length or n_new, or past the table, or with an entry >=
+ * num_pages there, is left as it was and sets RGD_DEV_BAD_PAGE.  Two kernels. */
+int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int32_t max_pages, int32_t* block_table,
+                      const int32_t* length, const int32_t* n_new, const uint8_t* row_active, int32_t* page_refs,
+                      rgd_bf16* k_pages, rgd_bf16* v_pages, uint8_t* row_ok, void* workspace, size_t workspace_bytes,
+                      int32_t* dev_status, rgd_stream_t stream);
+
+/* Writes one layer's keys and values of new tokens into reserved pages: token i <
+ * n_new[r] of row r becomes token length[r] + i of the row (the lengths stay the
+ * caller's to raise).
+ *   k_new, v_new  bf16, the Hkv x D values of (r, i) at r * row_stride + i *
+ *                 token_stride elements (both multiples of 8): views of a fused
+ *                 projection's output do
+ *   n_new         int32 [rows], at most max_new
+ *   row_active    uint8 [rows] or NULL: rows to write (rgd_cache_reserve's row_ok)
+ * A token whose page is not listed is skipped and sets RGD_DEV_BAD_PAGE. */
+int rgd_cache_write(const rgd_cache_shape* shape, int32_t layer, int32_t rows, int32_t max_new, const rgd_bf16* k_new,
+                    const rgd_bf16* v_new, int64_t row_stride, int64_t token_stride, const int32_t* n_new,
+                    int32_t max_pages, const int32_t* block_table, const int32_t* length, const uint8_t* row_active,
+                    rgd_bf16* k_pages, rgd_bf16* v_pages, int32_t* dev_status, rgd_stream_t stream);
+
+/* Gives back every page of a row that lies wholly past its length (all of them at
+ * length 0): entries from ceil(length / page_size) on become -1 and their counts fall
+ * by one.  After rejected drafts, with the lengths raised by what was accepted; for
+ * rows that have ended, with length 0.  Rows with row_active 0 are left alone. */
+int rgd_cache_trim(int32_t rows, int32_t max_pages, int32_t num_pages, int32_t* block_table, const int32_t* length,
+                   const uint8_t* row_active, int32_t* page_refs, int32_t* dev_status, rgd_stream_t stream);
+
+/* Makes row child[i] a copy of row parent[i]: the parent's length and the pages of its
+ * tokens, shared (their counts rise by one; nothing is copied until one of them
+ * writes, see rgd_cache_reserve).  A child's row is overwritten: trim it to length 0
+ * first.  No row may be a child twice, or a child and a parent, in one call.  A pair
+ * outside [0, rows) is skipped and sets RGD_DEV_BAD_PAGE. */
+int rgd_cache_fork(int32_t pairs, const int32_t* parent, const int32_t* child, int32_t rows, int32_t max_pages,
+                   int32_t num_pages, int32_t* block_table, int32_t* length, int32_t* page_refs, int32_t* dev_status,
+                   rgd_stream_t stream);
+
+/* Copies page src[i] onto page dst[i] for i < n, keys and values in every layer (device
+ * int32 arrays; no target may be another pair's source or target).  A pair outside
+ * the pool is skipped and sets RGD_DEV_BAD_PAGE. */
+int rgd_cache_copy(const rgd_cache_shape* shape, int32_t n, const int32_t* src, const int32_t* dst, rgd_bf16* k_pages,
+                   rgd_bf16* v_pages, int32_t* dev_status, rgd_stream_t stream);
+
+/* Moves the pages in use to the front of the pool.  With L pages in use, the i-th of
+ * them at or above L goes to the i-th free page below L, in every layer; the counts
+ * move along and the entries of up to two tables (int32 [rows, max_pages]; NULL: none;
+ * every table of the pool has to be given) are renumbered.  *num_live (device) = L: pages
+ * from L on are free afterwards.  An entry that names a free page at or above L becomes
+ * -1 and sets RGD_DEV_BAD_PAGE.  Two kernels. */
+int rgd_cache_compact(const rgd_cache_shape* shape, int32_t rows_a, int32_t max_pages_a, int32_t* block_table_a,
+                      int32_t rows_b, int32_t max_pages_b, int32_t* block_table_b, int32_t* page_refs,
+                      rgd_bf16* k_pages, rgd_bf16* v_pages, int32_t* num_live, void* workspace,
+                      size_t workspace_bytes, int32_t* dev_status, rgd_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(HERE, "librgd.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "rgd.h")
 
 RGD_OK, RGD_ERR_INVALID_ARG, RGD_ERR_CUDA, RGD_ERR_UNSUPPORTED = 0, 1, 2, 3
-RGD_DEV_BAD_PAGE, RGD_DEV_BAD_TOKEN, RGD_DEV_WAIT_TIMEOUT, RGD_DEV_BAD_PARAM = 1, 2, 4, 8
+RGD_DEV_BAD_PAGE, RGD_DEV_BAD_TOKEN, RGD_DEV_WAIT_TIMEOUT, RGD_DEV_BAD_PARAM, RGD_DEV_NO_PAGE = 1, 2, 4, 8, 16
 RGD_F32, RGD_BF16 = 0, 1
 RGD_PENDING, RGD_REFUSAL, RGD_NON_REFUSAL = 0, 1, 2
 
@@ -34,6 +34,12 @@ class AttnShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "num_groups", "rows_per_group", "num_q_heads", "num_kv_heads", "head_dim", "page_size",
         "num_pages", "max_prompt_pages", "max_suffix_pages", "num_ctas", "reserved")]
+
+
+class CacheShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "num_layers", "num_pages", "num_kv_heads", "page_size", "head_dim", "reserved")] + [
+            ("layer_stride", ctypes.c_int64)]
 
 
 class GateState(ctypes.Structure):
@@ -71,6 +77,20 @@ _SIGNATURES = {
     "rgd_residual_precheck": (ctypes.c_int, [_I32, _I32, _I32, _P, _P, _F, _F, _I32, _P, _P, _P, _P, _P]),
     "rgd_soft_gate": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _P, _I64, _I32, _F, _I32, _I32, _I32, _P, _P,
                                      _P, _P, _P, _P]),
+    "rgd_verify_draft_workspace_size": (_SZ, [_I32, _I32]),
+    "rgd_verify_draft": (ctypes.c_int, [_I32, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P,
+                                        _P, _P, _P, _P, _SZ, _P, _P]),
+    "rgd_w4_matvec": (ctypes.c_int, [_I32, _I32, _I32, _I32, _P, _P, _I32, _P, _P, _I32, _P, _I64, _P]),
+    "rgd_cache_workspace_size": (_SZ, [ctypes.POINTER(CacheShape), _I32]),
+    "rgd_cache_reserve": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                         _SZ, _P, _P]),
+    "rgd_cache_write": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _I32, _I32, _P, _P, _I64, _I64, _P, _I32, _P,
+                                       _P, _P, _P, _P, _P, _P]),
+    "rgd_cache_trim": (ctypes.c_int, [_I32, _I32, _I32, _P, _P, _P, _P, _P, _P]),
+    "rgd_cache_fork": (ctypes.c_int, [_I32, _P, _P, _I32, _I32, _I32, _P, _P, _P, _P, _P]),
+    "rgd_cache_copy": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _P, _P, _P, _P, _P, _P]),
+    "rgd_cache_compact": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _I32, _P, _I32, _I32, _P, _P, _P, _P, _P,
+                                         _P, _SZ, _P, _P]),
 }
 
 
@@ -419,6 +439,189 @@ def rgd_soft_gate(trie: Trie, groups: int, rows_per_group: int, logits, row_stri
         _ptr(token_out, "token_out", torch.int32, numel=G),
         _ptr(mass_out, "mass_out", torch.float32, optional=True, numel=G),
         _ptr(dev_status, "dev_status", torch.int32, optional=True, numel=1), _stream(stream)))
+
+
+_DTYPE = None  # torch dtype -> RGD_F32 / RGD_BF16, once torch is needed
+
+
+def _dtype_of(t, name: str) -> int:
+    global _DTYPE
+    if _DTYPE is None:
+        import torch
+        _DTYPE = {torch.float32: RGD_F32, torch.bfloat16: RGD_BF16}
+    code = _DTYPE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32 or bfloat16")
+    return code
+
+
+def rgd_verify_draft_workspace_size(rows: int, max_draft: int) -> int:
+    n = load_library().rgd_verify_draft_workspace_size(int(rows), int(max_draft))
+    if n == 0:
+        raise RgdError(RGD_ERR_INVALID_ARG, load_library().rgd_last_error_string().decode())
+    return int(n)
+
+
+def _bytes_of(workspace) -> int:
+    return workspace.numel() * workspace.element_size() if hasattr(workspace, "numel") else 0
+
+
+def rgd_verify_draft(target_logits, draft_logits, draft_tokens, n_draft, is_probe, temperature, min_p, accept_u, draw_u,
+                     row_active, token_out, accepted_out, accept_prob, workspace, vocab: Optional[int] = None,
+                     dev_status=None, stream=None) -> None:
+    """``target_logits`` [rows, max_draft + 1, W] and ``draft_logits`` [rows, max_draft, W'] (or None: certain
+    drafts), of which the first ``vocab`` of every row are logits (default: W)."""
+    import torch
+    if target_logits.dim() != 3 or target_logits.shape[1] < 1:
+        raise ValueError("target_logits must be [rows, max_draft + 1, vocab]")
+    rows, positions, width = target_logits.shape
+    draft = positions - 1
+    dtype = _dtype_of(target_logits, "target_logits")
+    draft_width = width
+    if draft_logits is not None:
+        if draft_logits.dim() != 3 or draft_logits.shape[0] != rows or draft_logits.shape[1] != draft:
+            raise ValueError("draft_logits must be [rows, max_draft, vocab]")
+        draft_width = draft_logits.shape[2]
+    i32, f32, u8 = torch.int32, torch.float32, torch.uint8
+    _check(_call(load_library().rgd_verify_draft,
+        rows, draft, width if vocab is None else int(vocab), dtype, _ptr(target_logits, "target_logits"), width,
+        _ptr(draft_logits, "draft_logits", target_logits.dtype, optional=True), draft_width,
+        _ptr(draft_tokens, "draft_tokens", i32, optional=draft == 0, numel=rows * draft),
+        _ptr(n_draft, "n_draft", i32, optional=True, numel=rows),
+        _ptr(is_probe, "is_probe", u8, optional=True, numel=rows),
+        _ptr(temperature, "temperature", f32, numel=rows), _ptr(min_p, "min_p", f32, numel=rows),
+        _ptr(accept_u, "accept_u", f32, optional=draft == 0, numel=rows * draft),
+        _ptr(draw_u, "draw_u", f32, numel=rows), _ptr(row_active, "row_active", u8, optional=True, numel=rows),
+        _ptr(token_out, "token_out", i32, numel=rows * positions), _ptr(accepted_out, "accepted_out", i32, numel=rows),
+        _ptr(accept_prob, "accept_prob", f32, optional=True, numel=rows * draft),
+        _ptr(workspace, "workspace"), _bytes_of(workspace),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_w4_matvec(x, weights, scales, zeros, group_size: int, y, stream=None) -> None:
+    """``y`` [m, W >= n] gets ``x`` [m, k] times the 4-bit ``weights`` [n, ceil(k / 2)] in its first n columns."""
+    import torch
+    if x.dim() != 2 or weights.dim() != 2 or y.dim() != 2:
+        raise ValueError("x must be [m, k], weights [n, ceil(k / 2)] and y [m, n]")
+    m, k = x.shape
+    n, group = weights.shape[0], int(group_size)
+    if weights.shape[1] != (k + 1) // 2:
+        raise ValueError(f"weights holds rows of {weights.shape[1]} bytes, {k} weights take {(k + 1) // 2}")
+    if y.shape[0] != m or y.shape[1] < n:
+        raise ValueError(f"y must be [{m}, {n}] (or wider)")
+    groups = -(-k // group) if group > 0 else 0
+    _check(_call(load_library().rgd_w4_matvec,
+        m, n, k, group, _ptr(x, "x", torch.bfloat16), _ptr(weights, "weights", torch.uint8),
+        _dtype_of(scales, "scales"), _ptr(scales, "scales", numel=n * groups),
+        _ptr(zeros, "zeros", torch.uint8, optional=True, numel=n * groups), _dtype_of(y, "y"), _ptr(y, "y"),
+        y.shape[1], _stream(stream)))
+
+
+def rgd_cache_workspace_size(shape: CacheShape, rows: int) -> int:
+    n = load_library().rgd_cache_workspace_size(ctypes.byref(shape), int(rows))
+    if n == 0:
+        raise RgdError(RGD_ERR_INVALID_ARG, load_library().rgd_last_error_string().decode())
+    return int(n)
+
+
+def _pool_numel(shape: CacheShape) -> int:
+    pool = shape.num_pages * shape.num_kv_heads * shape.page_size * shape.head_dim
+    return pool + max(shape.num_layers - 1, 0) * (shape.layer_stride or pool)
+
+
+def _table_size(block_table, name: str = "block_table"):
+    if block_table.dim() != 2:
+        raise ValueError(f"{name} must be [rows, max_pages]")
+    return block_table.shape
+
+
+def rgd_cache_reserve(shape: CacheShape, block_table, length, n_new, row_active, page_refs, k_pages, v_pages, row_ok,
+                      workspace, dev_status=None, stream=None) -> None:
+    import torch
+    rows, cols = _table_size(block_table)
+    i32, u8, pool = torch.int32, torch.uint8, _pool_numel(shape)
+    _check(_call(load_library().rgd_cache_reserve,
+        ctypes.byref(shape), rows, cols, _ptr(block_table, "block_table", i32), _ptr(length, "length", i32, numel=rows),
+        _ptr(n_new, "n_new", i32, numel=rows), _ptr(row_active, "row_active", u8, optional=True, numel=rows),
+        _ptr(page_refs, "page_refs", i32, numel=shape.num_pages),
+        _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
+        _ptr(row_ok, "row_ok", u8, optional=True, numel=rows), _ptr(workspace, "workspace"), _bytes_of(workspace),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+def _new_tokens(t, name: str, shape: CacheShape):
+    """[rows, max_new, Hkv, D] whose last two dimensions are dense; its rows and tokens may be strided."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be a bfloat16 tensor")
+    if t.dim() != 4 or t.shape[2] != shape.num_kv_heads or t.shape[3] != shape.head_dim:
+        raise ValueError(f"{name} must be [rows, max_new, num_kv_heads, head_dim]")
+    if t.numel() and (t.stride(3) != 1 or t.stride(2) != shape.head_dim):
+        raise ValueError(f"{name}: heads and head_dim must be dense")
+    return t.data_ptr() if t.is_cuda else _HostTensor(name)
+
+
+def rgd_cache_write(shape: CacheShape, layer: int, k_new, v_new, n_new, block_table, length, row_active, k_pages,
+                    v_pages, dev_status=None, stream=None) -> None:
+    """``k_new`` and ``v_new`` [rows, max_new, Hkv, D] have the same strides; views of a fused projection do."""
+    import torch
+    rows, cols = _table_size(block_table)
+    k, v = _new_tokens(k_new, "k_new", shape), _new_tokens(v_new, "v_new", shape)
+    if k_new.shape[0] != rows or v_new.shape != k_new.shape or v_new.stride() != k_new.stride():
+        raise ValueError("k_new and v_new must have block_table's rows and the same shape and strides")
+    i32, pool = torch.int32, _pool_numel(shape)
+    _check(_call(load_library().rgd_cache_write,
+        ctypes.byref(shape), int(layer), rows, k_new.shape[1], k, v, k_new.stride(0), k_new.stride(1),
+        _ptr(n_new, "n_new", i32, numel=rows), cols, _ptr(block_table, "block_table", i32),
+        _ptr(length, "length", i32, numel=rows), _ptr(row_active, "row_active", torch.uint8, optional=True, numel=rows),
+        _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_cache_trim(block_table, length, row_active, page_refs, dev_status=None, stream=None) -> None:
+    import torch
+    rows, cols = _table_size(block_table)
+    i32 = torch.int32
+    _check(_call(load_library().rgd_cache_trim,
+        rows, cols, page_refs.numel(), _ptr(block_table, "block_table", i32), _ptr(length, "length", i32, numel=rows),
+        _ptr(row_active, "row_active", torch.uint8, optional=True, numel=rows), _ptr(page_refs, "page_refs", i32),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_cache_fork(parent, child, block_table, length, page_refs, dev_status=None, stream=None) -> None:
+    import torch
+    rows, cols = _table_size(block_table)
+    i32, pairs = torch.int32, parent.numel()
+    _check(_call(load_library().rgd_cache_fork,
+        pairs, _ptr(parent, "parent", i32), _ptr(child, "child", i32, numel=pairs), rows, cols, page_refs.numel(),
+        _ptr(block_table, "block_table", i32), _ptr(length, "length", i32, numel=rows),
+        _ptr(page_refs, "page_refs", i32), _ptr(dev_status, "dev_status", i32, optional=True, numel=1),
+        _stream(stream)))
+
+
+def rgd_cache_copy(shape: CacheShape, src, dst, k_pages, v_pages, dev_status=None, stream=None) -> None:
+    import torch
+    i32, n, pool = torch.int32, src.numel(), _pool_numel(shape)
+    _check(_call(load_library().rgd_cache_copy,
+        ctypes.byref(shape), n, _ptr(src, "src", i32), _ptr(dst, "dst", i32, numel=n),
+        _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_cache_compact(shape: CacheShape, block_table_a, block_table_b, page_refs, k_pages, v_pages, num_live, workspace,
+                      dev_status=None, stream=None) -> None:
+    """Both tables may be None; every table of the pool has to be given."""
+    import torch
+    i32, pool = torch.int32, _pool_numel(shape)
+    ra, ca = (0, 0) if block_table_a is None else _table_size(block_table_a, "block_table_a")
+    rb, cb = (0, 0) if block_table_b is None else _table_size(block_table_b, "block_table_b")
+    _check(_call(load_library().rgd_cache_compact,
+        ctypes.byref(shape), ra, ca, _ptr(block_table_a, "block_table_a", i32, optional=True), rb, cb,
+        _ptr(block_table_b, "block_table_b", i32, optional=True),
+        _ptr(page_refs, "page_refs", i32, numel=shape.num_pages),
+        _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
+        _ptr(num_live, "num_live", i32, numel=1), _ptr(workspace, "workspace"), _bytes_of(workspace),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
 
 
 def new_gate_state(groups: int, device="cuda"):

@@ -1,0 +1,586 @@
+// The paged KV cache's own operations: pages for new tokens (with a copy of a shared
+// page before it is written), the tokens' keys and values into them, rows forked and
+// trimmed, pages copied, and the pool compacted.
+//
+// A page is free exactly if its count in page_refs is 0, and an allocation takes the
+// free page of the lowest number.  So there is no free list that could disagree with the
+// counts, giving a page back is one atomic decrement, in any order, and every result is
+// a function of the tables and counts alone.  The price is a look through the counts
+// when pages are needed.
+#include <algorithm>
+#include <cmath>
+
+#include "common.h"
+#include "ptx.cuh"
+
+namespace rgd {
+namespace {
+
+constexpr int kPageSize = 16;
+constexpr int kPlanThreads = 1024;
+constexpr int kCopyThreads = 256;
+
+struct CacheView {
+  int32_t layers, pages, heads, dim;
+  int64_t layer_stride;  // elements between a layer's pool and the next
+};
+
+__device__ __forceinline__ void begin_dependent() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+__device__ __forceinline__ void flag(int32_t* dev_status, int32_t bit) {
+  if (dev_status) atomicOr(dev_status, bit);
+}
+
+// Exclusive prefix sum over the block's threads, and the total.
+__device__ __forceinline__ int32_t block_scan(int32_t v, int32_t* part, int32_t& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int32_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  __syncthreads();  // (part may still be read from the scan before)
+  if (lane == 31) part[warp] = incl;
+  __syncthreads();
+  int32_t w = part[lane];
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int32_t x = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += x;
+  }
+  total = __shfl_sync(0xffffffffu, w, 31);
+  const int32_t before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+  return incl - v + (warp ? before : 0);
+}
+
+// ---------------------------------------------------------------------------
+// pages for new tokens
+// ---------------------------------------------------------------------------
+struct ReserveParams {
+  int32_t rows, cols, pages;
+  int32_t* table;
+  const int32_t* length;
+  const int32_t* n_new;
+  const uint8_t* row_active;
+  int32_t* refs;
+  uint8_t* row_ok;
+  int32_t* num_copies;  // workspace: copies to make, then source, target and slots of each
+  int32_t* src;
+  int32_t* dst;
+  int32_t* slots;
+  int32_t* need;   // workspace [rows]: where the row's pages start among all needed (-1: the row is wrong)
+  int32_t* fresh;  // workspace [pages]: the free pages in order, as many as are needed
+  int32_t* dev_status;
+};
+
+// A row's columns that its new tokens fall into; false where there is nothing to reserve or the row is wrong.
+__device__ __forceinline__ bool new_columns(const ReserveParams& p, int r, int32_t& len, int32_t& first, int32_t& last,
+                                            bool& bad) {
+  bad = false;
+  if (p.row_active && !p.row_active[r]) return false;
+  len = p.length[r];
+  const int32_t n = p.n_new[r];
+  bad = len < 0 || n < 0 || (int64_t)len + n > (int64_t)p.cols * kPageSize;
+  if (bad || n == 0) return false;
+  first = len / kPageSize;
+  last = (len + n + kPageSize - 1) / kPageSize;
+  return true;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) reserve_kernel(const ReserveParams p) {
+  __shared__ int32_t part[32];
+  __shared__ int32_t copies;
+  begin_dependent();
+  const int tid = threadIdx.x;
+  if (tid == 0) copies = 0;
+  // how many pages each row needs, and where they start among all
+  int32_t needed = 0;
+  for (int base = 0; base < p.rows; base += kPlanThreads) {
+    const int r = base + tid;
+    int32_t len, first, last, k = 0;
+    bool bad = false;
+    if (r < p.rows && new_columns(p, r, len, first, last, bad)) {
+      for (int j = first; j < last; ++j) {
+        const int32_t page = p.table[(int64_t)r * p.cols + j];
+        bad = bad || page >= p.pages;
+        k += page < 0 || (page < p.pages && p.refs[page] > 1);
+      }
+    }
+    if (bad) {
+      flag(p.dev_status, RGD_DEV_BAD_PAGE);
+      k = 0;
+    }
+    int32_t total;
+    const int32_t at = needed + block_scan(k, part, total);
+    if (r < p.rows) p.need[r] = bad ? -1 : at;  // (where its pages start among all)
+    needed += total;
+  }
+  // the free pages of the lowest numbers
+  int32_t found = 0;
+  for (int64_t base = 0; base < p.pages && found < needed; base += kPlanThreads * 4) {
+    int32_t mine[4];
+    int32_t k = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t i = base + tid * 4 + e;
+      mine[e] = i < p.pages ? p.refs[i] : 1;
+      k += mine[e] == 0;
+    }
+    int32_t total;
+    int32_t at = found + block_scan(k, part, total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (mine[e] == 0) p.fresh[at++] = (int32_t)(base + tid * 4 + e);
+    found += total;
+  }
+  __syncthreads();
+  // the rows' pages, in order, as far as they go; pages given up are noted, so that no
+  // count changes while rows still read them
+  for (int r = tid; r < p.rows; r += kPlanThreads) {
+    int32_t at = p.need[r], len, first, last;
+    bool bad, ok = (!p.row_active || p.row_active[r]) && at >= 0;
+    if (ok && new_columns(p, r, len, first, last, bad)) {
+      int32_t* row = p.table + (int64_t)r * p.cols;
+      int32_t k = 0;
+      for (int j = first; j < last; ++j) k += row[j] < 0 || p.refs[row[j]] > 1;
+      ok = at + k <= found;
+      if (!ok) flag(p.dev_status, RGD_DEV_NO_PAGE);
+      for (int j = first; ok && j < last; ++j) {
+        const int32_t old = row[j];
+        if (old >= 0 && p.refs[old] <= 1) continue;
+        const int32_t page = p.fresh[at++];
+        if (old >= 0) {
+          const int32_t i = atomicAdd(&copies, 1);
+          p.src[i] = old;
+          p.dst[i] = page;
+          p.slots[i] = j == first ? len % kPageSize : 0;
+        }
+        row[j] = page;
+        p.refs[page] = 1;
+      }
+    }
+    if (p.row_ok) p.row_ok[r] = ok;
+  }
+  __syncthreads();
+  for (int i = tid; i < copies; i += kPlanThreads) atomicSub(p.refs + p.src[i], 1);
+  if (tid == 0) *p.num_copies = copies;
+}
+
+// ---------------------------------------------------------------------------
+// copies of pages
+// ---------------------------------------------------------------------------
+struct CopyParams {
+  CacheView c;
+  uint16_t* pool[2];  // keys, values
+  const int32_t* count;  // copies to make (NULL: n)
+  int32_t n;
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* slots;  // leading slots of each to copy (NULL: all)
+  int32_t* dev_status;
+  // compaction: tables whose entries at or above *live move as `place` says
+  const int32_t* live;
+  const int32_t* place;
+  int32_t* table[2];
+  int64_t entries[2];
+};
+
+// A warp copies one (page, layer, pool, head): up to 16 x D elements, contiguous on both
+// sides, all loads before the stores.
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const CopyParams p) {
+  begin_dependent();
+  const int lane = threadIdx.x & 31;
+  const int64_t warps = (int64_t)gridDim.x * (kCopyThreads / 32);
+  const int64_t w0 = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  if (p.live) {
+    const int32_t live = *p.live;
+    for (int k = 0; k < 2; ++k)
+      for (int64_t i = w0 * 32 + lane; i < p.entries[k]; i += warps * 32) {
+        const int32_t e = p.table[k][i];
+        if (e < live) continue;
+        const int32_t to = e < p.c.pages ? p.place[e] : -1;
+        if (to < 0) flag(p.dev_status, RGD_DEV_BAD_PAGE);
+        p.table[k][i] = to;
+      }
+  }
+  const int32_t n = p.count ? *p.count : p.n;
+  const int per_page = p.c.layers * 2 * p.c.heads;
+  for (int64_t w = w0; w < (int64_t)n * per_page; w += warps) {
+    const int32_t i = (int32_t)(w / per_page), part = (int32_t)(w % per_page);
+    const int32_t head = part % p.c.heads, pool = part / p.c.heads % 2, layer = part / p.c.heads / 2;
+    const int32_t s = p.src[i], d = p.dst[i];
+    if (s < 0 || s >= p.c.pages || d < 0 || d >= p.c.pages) {
+      flag(p.dev_status, RGD_DEV_BAD_PAGE);
+      continue;
+    }
+    const int32_t vecs = (p.slots ? p.slots[i] : kPageSize) * p.c.dim / 8;
+    uint16_t* base = p.pool[pool] + layer * p.c.layer_stride;
+    const int64_t page = (int64_t)kPageSize * p.c.dim;
+    const uint4* from = reinterpret_cast<const uint4*>(base + ((int64_t)s * p.c.heads + head) * page);
+    uint4* to = reinterpret_cast<uint4*>(base + ((int64_t)d * p.c.heads + head) * page);
+    for (int v = lane; v < vecs; v += 32 * 8) {
+      uint4 x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (v + k * 32 < vecs) x[k] = from[v + k * 32];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (v + k * 32 < vecs) to[v + k * 32] = x[k];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// keys and values of new tokens
+// ---------------------------------------------------------------------------
+struct WriteParams {
+  CacheView c;
+  uint16_t* pool[2];
+  const uint16_t* fresh[2];
+  int64_t row_stride, token_stride;
+  int32_t rows, tokens, cols;
+  const int32_t* n_new;
+  const int32_t* table;
+  const int32_t* length;
+  const uint8_t* row_ok;
+  int32_t* dev_status;
+};
+
+// A warp writes one token's keys and values.
+__global__ void __launch_bounds__(kCopyThreads) write_kernel(const WriteParams p) {
+  begin_dependent();
+  const int lane = threadIdx.x & 31;
+  const int64_t w = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  const int32_t r = (int32_t)(w / p.tokens), i = (int32_t)(w % p.tokens);
+  if (r >= p.rows || i >= p.n_new[r] || (p.row_ok && !p.row_ok[r])) return;
+  const int64_t pos = (int64_t)p.length[r] + i;
+  const int32_t page = pos >= 0 && pos < (int64_t)p.cols * kPageSize ? p.table[(int64_t)r * p.cols + pos / kPageSize] : -1;
+  if (page < 0 || page >= p.c.pages) {
+    if (lane == 0) flag(p.dev_status, RGD_DEV_BAD_PAGE);
+    return;
+  }
+  const int32_t per = p.c.dim / 8, vecs = p.c.heads * per;
+  const int64_t at = r * p.row_stride + i * p.token_stride;
+  const uint4* k = reinterpret_cast<const uint4*>(p.fresh[0] + at);
+  const uint4* v = reinterpret_cast<const uint4*>(p.fresh[1] + at);
+  const int64_t to = ((int64_t)page * p.c.heads * kPageSize + pos % kPageSize) * per;
+#pragma unroll 4
+  for (int x = lane; x < vecs; x += 32) {
+    const int32_t h = x / per;
+    const int64_t o = to + (int64_t)h * kPageSize * per + (x - h * per);
+    reinterpret_cast<uint4*>(p.pool[0])[o] = k[x];
+    reinterpret_cast<uint4*>(p.pool[1])[o] = v[x];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// pages taken up and given back with rows
+// ---------------------------------------------------------------------------
+// A warp per row gives back its pages past the row's length.
+__global__ void __launch_bounds__(kCopyThreads)
+    trim_kernel(int32_t rows, int32_t cols, int32_t pages, int32_t* table, const int32_t* length, const uint8_t* row_active,
+                int32_t* refs, int32_t* dev_status) {
+  begin_dependent();
+  const int r = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5);
+  if (r >= rows || (row_active && !row_active[r])) return;
+  const int32_t len = length[r];
+  if (len < 0) {
+    flag(dev_status, RGD_DEV_BAD_PAGE);
+    return;
+  }
+  for (int64_t j = ((int64_t)len + kPageSize - 1) / kPageSize + (threadIdx.x & 31); j < cols; j += 32) {
+    int32_t* e = table + (int64_t)r * cols + j;
+    const int32_t page = *e;
+    if (page < 0) continue;
+    if (page < pages) atomicSub(refs + page, 1);
+    else flag(dev_status, RGD_DEV_BAD_PAGE);
+    *e = -1;
+  }
+}
+
+// A warp per pair gives the child the parent's pages and length.
+__global__ void __launch_bounds__(kCopyThreads)
+    fork_kernel(int32_t n, int32_t rows, int32_t cols, int32_t pages, const int32_t* parent, const int32_t* child,
+                int32_t* table, int32_t* length, int32_t* refs, int32_t* dev_status) {
+  begin_dependent();
+  const int i = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (i >= n) return;
+  const int32_t a = parent[i], b = child[i];
+  const int32_t len = a >= 0 && a < rows ? length[a] : -1;
+  if (b < 0 || b >= rows || a == b || len < 0 || len > (int64_t)cols * kPageSize) {
+    flag(dev_status, RGD_DEV_BAD_PAGE);
+    return;
+  }
+  const int32_t held = (int32_t)(((int64_t)len + kPageSize - 1) / kPageSize);
+  for (int j = lane; j < cols; j += 32) {
+    const int32_t page = j < held ? table[(int64_t)a * cols + j] : -1;
+    if (page >= 0 && page < pages) atomicAdd(refs + page, 1);
+    else if (j < held) flag(dev_status, RGD_DEV_BAD_PAGE);
+    table[(int64_t)b * cols + j] = page;
+  }
+  if (lane == 0) length[b] = len;
+}
+
+// ---------------------------------------------------------------------------
+// the pool compacted
+// ---------------------------------------------------------------------------
+// The i-th page in use at or above the number of pages in use moves to the i-th free page
+// below it: the fewest moves, and no target is a source.
+__global__ void __launch_bounds__(kPlanThreads)
+    compact_kernel(int32_t pages, int32_t* refs, int32_t* num_live, int32_t* num_moves, int32_t* src, int32_t* dst,
+                   int32_t* place) {
+  __shared__ int32_t part[32];
+  begin_dependent();
+  const int tid = threadIdx.x;
+  int32_t live = 0;
+  for (int64_t base = 0; base < pages; base += kPlanThreads) {
+    int32_t total;
+    block_scan(base + tid < pages && refs[base + tid] > 0, part, total);
+    live += total;
+  }
+  int32_t movers = 0, holes = 0;
+  for (int64_t base = 0; base < pages; base += kPlanThreads) {
+    const int64_t i = base + tid;
+    const bool used = i < pages && refs[i] > 0;
+    const bool mover = used && i >= live, hole = i < live && !used;
+    int32_t total;
+    int32_t at = movers + block_scan(mover, part, total);
+    movers += total;
+    if (mover) src[at] = (int32_t)i;
+    at = holes + block_scan(hole, part, total);
+    holes += total;
+    if (hole) dst[at] = (int32_t)i;
+    if (i >= live && i < pages) place[i] = -1;
+  }
+  __syncthreads();
+  for (int i = tid; i < movers; i += kPlanThreads) {
+    place[src[i]] = dst[i];
+    refs[dst[i]] = refs[src[i]];
+    refs[src[i]] = 0;
+  }
+  if (tid == 0) {
+    *num_live = live;
+    *num_moves = movers;
+  }
+}
+
+int check_shape(const char* fn, const rgd_cache_shape* s, CacheView& c) {
+  RGD_CHECK_ARG(s != nullptr, "%s: shape is NULL", fn);
+  RGD_CHECK_ARG(s->num_layers >= 1 && s->num_pages >= 1 && s->num_kv_heads >= 1 && s->head_dim >= 1,
+                "%s: num_layers/num_pages/num_kv_heads/head_dim must be >= 1", fn);
+  RGD_CHECK_ARG(s->reserved == 0, "%s: reserved must be 0", fn);
+  if (s->page_size != kPageSize) return set_error(RGD_ERR_UNSUPPORTED, "%s: page_size must be 16", fn);
+  if (s->head_dim % 8 != 0 || s->head_dim > 1024)
+    return set_error(RGD_ERR_UNSUPPORTED, "%s: head_dim must be a multiple of 8, at most 1024", fn);
+  if (s->num_kv_heads > 4096 || s->num_layers > 4096)
+    return set_error(RGD_ERR_UNSUPPORTED, "%s: at most 4096 heads and layers", fn);
+  const int64_t pool = (int64_t)s->num_pages * s->num_kv_heads * kPageSize * s->head_dim;
+  RGD_CHECK_ARG(s->layer_stride == 0 || (s->layer_stride >= pool && s->layer_stride % 8 == 0),
+                "%s: layer_stride must be 0 or a multiple of 8 no smaller than a layer's pool", fn);
+  c = CacheView{s->num_layers, s->num_pages, s->num_kv_heads, s->head_dim, s->layer_stride ? s->layer_stride : pool};
+  return RGD_OK;
+}
+
+int blocks_for(int64_t warps) { return (int)((warps + kCopyThreads / 32 - 1) / (kCopyThreads / 32)); }
+
+int launch_copies(const CopyParams& p, int64_t most, cudaStream_t st) {
+  const int64_t warps = std::max(most * p.c.layers * 2 * p.c.heads, (p.entries[0] + p.entries[1] + 31) / 32);
+  const int grid = (int)std::min<int64_t>(blocks_for(std::max<int64_t>(warps, 1)), 152 * 8);
+  const cudaError_t e = launch_dependent(copy_kernel, grid, kCopyThreads, 0, st, p);
+  return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache copy launch");
+}
+
+}  // namespace
+}  // namespace rgd
+
+using namespace rgd;
+
+extern "C" size_t rgd_cache_workspace_size(const rgd_cache_shape* shape, int32_t rows) {
+  clear_error();
+  CacheView c;
+  if (check_shape("rgd_cache_workspace_size", shape, c)) return 0;
+  if (rows < 0) {
+    set_error(RGD_ERR_INVALID_ARG, "rgd_cache_workspace_size: rows < 0");
+    return 0;
+  }
+  return 256 + 4 * (4 * (size_t)c.pages + (size_t)rows);
+}
+
+extern "C" int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int32_t max_pages, int32_t* block_table,
+                                 const int32_t* length, const int32_t* n_new, const uint8_t* row_active,
+                                 int32_t* page_refs, rgd_bf16* k_pages, rgd_bf16* v_pages, uint8_t* row_ok,
+                                 void* workspace, size_t workspace_bytes, int32_t* dev_status, rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_cache_reserve";
+  CacheView c;
+  if (int rc = check_shape(fn, shape, c)) return rc;
+  RGD_CHECK_ARG(rows >= 0 && max_pages >= 1, "%s: bad rows/max_pages", fn);
+  if (rows == 0) return RGD_OK;
+  RGD_CHECK_ARG(block_table && length && n_new && page_refs && k_pages && v_pages && workspace,
+                "%s: block_table/length/n_new/page_refs/k_pages/v_pages/workspace must be non-NULL", fn);
+  RGD_CHECK_ARG(aligned16(k_pages) && aligned16(v_pages) && aligned16(workspace),
+                "%s: k_pages/v_pages/workspace must be 16-byte aligned", fn);
+  RGD_CHECK_ARG(workspace_bytes >= rgd_cache_workspace_size(shape, rows), "%s: workspace too small", fn);
+  RGD_CHECK_ARG(max_pages <= 0x7fffffff / kPageSize, "%s: max_pages too large", fn);
+  cudaStream_t st = (cudaStream_t)stream;
+  int32_t* ws = static_cast<int32_t*>(workspace);
+  ReserveParams p{};
+  p.rows = rows;
+  p.cols = max_pages;
+  p.pages = c.pages;
+  p.table = block_table;
+  p.length = length;
+  p.n_new = n_new;
+  p.row_active = row_active;
+  p.refs = page_refs;
+  p.row_ok = row_ok;
+  p.num_copies = ws;
+  p.src = ws + 64;
+  p.dst = p.src + c.pages;
+  p.slots = p.dst + c.pages;
+  p.fresh = p.slots + c.pages;
+  p.need = p.fresh + c.pages;
+  p.dev_status = dev_status;
+  const cudaError_t e = launch_dependent(reserve_kernel, 1, kPlanThreads, 0, st, p);
+  if (e != cudaSuccess) return cuda_error(e, "cache reserve launch");
+  CopyParams q{};
+  q.c = c;
+  q.pool[0] = k_pages;
+  q.pool[1] = v_pages;
+  q.count = p.num_copies;
+  q.src = p.src;
+  q.dst = p.dst;
+  q.slots = p.slots;
+  q.dev_status = dev_status;
+  return launch_copies(q, rows, st);
+}
+
+extern "C" int rgd_cache_write(const rgd_cache_shape* shape, int32_t layer, int32_t rows, int32_t max_new,
+                               const rgd_bf16* k_new, const rgd_bf16* v_new, int64_t row_stride, int64_t token_stride,
+                               const int32_t* n_new, int32_t max_pages, const int32_t* block_table,
+                               const int32_t* length, const uint8_t* row_active, rgd_bf16* k_pages, rgd_bf16* v_pages,
+                               int32_t* dev_status, rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_cache_write";
+  CacheView c;
+  if (int rc = check_shape(fn, shape, c)) return rc;
+  RGD_CHECK_ARG(rows >= 0 && max_new >= 0 && max_pages >= 1, "%s: bad rows/max_new/max_pages", fn);
+  RGD_CHECK_ARG(layer >= 0 && layer < c.layers, "%s: layer outside [0, num_layers)", fn);
+  RGD_CHECK_ARG(row_stride >= 0 && token_stride >= 0, "%s: strides must not be negative", fn);
+  if (rows == 0 || max_new == 0) return RGD_OK;
+  RGD_CHECK_ARG(k_new && v_new && n_new && block_table && length && k_pages && v_pages,
+                "%s: k_new/v_new/n_new/block_table/length/k_pages/v_pages must be non-NULL", fn);
+  RGD_CHECK_ARG(aligned16(k_new) && aligned16(v_new) && aligned16(k_pages) && aligned16(v_pages) &&
+                    row_stride % 8 == 0 && token_stride % 8 == 0,
+                "%s: tensors must be 16-byte aligned and strides multiples of 8 elements", fn);
+  RGD_CHECK_ARG((int64_t)rows * max_new <= 0x7fffffff, "%s: too many tokens", fn);
+  WriteParams p{};
+  p.c = c;
+  p.pool[0] = k_pages + layer * c.layer_stride;
+  p.pool[1] = v_pages + layer * c.layer_stride;
+  p.fresh[0] = k_new;
+  p.fresh[1] = v_new;
+  p.row_stride = row_stride;
+  p.token_stride = token_stride;
+  p.rows = rows;
+  p.tokens = max_new;
+  p.cols = max_pages;
+  p.n_new = n_new;
+  p.table = block_table;
+  p.length = length;
+  p.row_ok = row_active;
+  p.dev_status = dev_status;
+  const cudaError_t e =
+      launch_dependent(write_kernel, blocks_for((int64_t)rows * max_new), kCopyThreads, 0, (cudaStream_t)stream, p);
+  return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache write launch");
+}
+
+extern "C" int rgd_cache_trim(int32_t rows, int32_t max_pages, int32_t num_pages, int32_t* block_table,
+                              const int32_t* length, const uint8_t* row_active, int32_t* page_refs,
+                              int32_t* dev_status, rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_cache_trim";
+  RGD_CHECK_ARG(rows >= 0 && max_pages >= 1 && num_pages >= 1, "%s: bad rows/max_pages/num_pages", fn);
+  if (rows == 0) return RGD_OK;
+  RGD_CHECK_ARG(block_table && length && page_refs, "%s: block_table/length/page_refs must be non-NULL", fn);
+  const cudaError_t e = launch_dependent(trim_kernel, blocks_for(rows), kCopyThreads, 0, (cudaStream_t)stream, rows,
+                                         max_pages, num_pages, block_table, length, row_active, page_refs, dev_status);
+  return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache trim launch");
+}
+
+extern "C" int rgd_cache_fork(int32_t pairs, const int32_t* parent, const int32_t* child, int32_t rows,
+                              int32_t max_pages, int32_t num_pages, int32_t* block_table, int32_t* length,
+                              int32_t* page_refs, int32_t* dev_status, rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_cache_fork";
+  RGD_CHECK_ARG(pairs >= 0 && rows >= 0 && max_pages >= 1 && num_pages >= 1, "%s: bad pairs/rows/max_pages/num_pages", fn);
+  if (pairs == 0) return RGD_OK;
+  RGD_CHECK_ARG(parent && child && block_table && length && page_refs,
+                "%s: parent/child/block_table/length/page_refs must be non-NULL", fn);
+  const cudaError_t e = launch_dependent(fork_kernel, blocks_for(pairs), kCopyThreads, 0, (cudaStream_t)stream, pairs,
+                                         rows, max_pages, num_pages, parent, child, block_table, length, page_refs,
+                                         dev_status);
+  return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache fork launch");
+}
+
+extern "C" int rgd_cache_copy(const rgd_cache_shape* shape, int32_t n, const int32_t* src, const int32_t* dst,
+                              rgd_bf16* k_pages, rgd_bf16* v_pages, int32_t* dev_status, rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_cache_copy";
+  CacheView c;
+  if (int rc = check_shape(fn, shape, c)) return rc;
+  RGD_CHECK_ARG(n >= 0, "%s: n < 0", fn);
+  if (n == 0) return RGD_OK;
+  RGD_CHECK_ARG(src && dst && k_pages && v_pages, "%s: src/dst/k_pages/v_pages must be non-NULL", fn);
+  RGD_CHECK_ARG(aligned16(k_pages) && aligned16(v_pages), "%s: k_pages/v_pages must be 16-byte aligned", fn);
+  CopyParams q{};
+  q.c = c;
+  q.pool[0] = k_pages;
+  q.pool[1] = v_pages;
+  q.n = n;
+  q.src = src;
+  q.dst = dst;
+  q.dev_status = dev_status;
+  return launch_copies(q, n, (cudaStream_t)stream);
+}
+
+extern "C" int rgd_cache_compact(const rgd_cache_shape* shape, int32_t rows_a, int32_t max_pages_a,
+                                 int32_t* block_table_a, int32_t rows_b, int32_t max_pages_b, int32_t* block_table_b,
+                                 int32_t* page_refs, rgd_bf16* k_pages, rgd_bf16* v_pages, int32_t* num_live,
+                                 void* workspace, size_t workspace_bytes, int32_t* dev_status, rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_cache_compact";
+  CacheView c;
+  if (int rc = check_shape(fn, shape, c)) return rc;
+  RGD_CHECK_ARG(rows_a >= 0 && rows_b >= 0 && max_pages_a >= 0 && max_pages_b >= 0, "%s: bad rows/max_pages", fn);
+  RGD_CHECK_ARG(page_refs && k_pages && v_pages && num_live && workspace,
+                "%s: page_refs/k_pages/v_pages/num_live/workspace must be non-NULL", fn);
+  const int64_t na = block_table_a ? (int64_t)rows_a * max_pages_a : 0, nb = block_table_b ? (int64_t)rows_b * max_pages_b : 0;
+  RGD_CHECK_ARG(aligned16(k_pages) && aligned16(v_pages) && aligned16(workspace),
+                "%s: k_pages/v_pages/workspace must be 16-byte aligned", fn);
+  RGD_CHECK_ARG(workspace_bytes >= rgd_cache_workspace_size(shape, 0), "%s: workspace too small", fn);
+  cudaStream_t st = (cudaStream_t)stream;
+  int32_t* ws = static_cast<int32_t*>(workspace);
+  CopyParams q{};
+  q.c = c;
+  q.pool[0] = k_pages;
+  q.pool[1] = v_pages;
+  int32_t *src = ws + 64, *dst = src + c.pages, *place = dst + c.pages;
+  const cudaError_t e =
+      launch_dependent(compact_kernel, 1, kPlanThreads, 0, st, c.pages, page_refs, num_live, ws, src, dst, place);
+  if (e != cudaSuccess) return cuda_error(e, "cache compact launch");
+  q.count = ws;
+  q.src = src;
+  q.dst = dst;
+  q.dev_status = dev_status;
+  q.live = num_live;
+  q.place = place;
+  q.table[0] = block_table_a;
+  q.table[1] = block_table_b;
+  q.entries[0] = na;
+  q.entries[1] = nb;
+  return launch_copies(q, c.pages, st);
+}
