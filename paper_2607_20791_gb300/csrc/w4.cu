@@ -34,6 +34,8 @@ constexpr int kW4Threads = kW4Warps * 32;
 constexpr int kChunk = 128;      // weights of a row per chunk
 constexpr int kAhead = 4;        // chunks in flight per warp
 constexpr int kTileRows = 16;
+constexpr int kMaxK = 1 << 24;
+constexpr int kNoChunk = kMaxK / kChunk;  // past every row's end
 constexpr int kUnit = 512;       // bytes of x per MMA step: 8 rows, 32 weights
 constexpr int kW4Smem = 112 * 1024;  // of a CTA at most: two to an SM
 // Tiles whose sums are kept while k goes in blocks, for 8 NT rows of x.
@@ -68,12 +70,19 @@ __device__ __forceinline__ uint32_t weights2(uint32_t word, int p, uint32_t bias
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// What a lane holds of a chunk: 32 weights of rows g and g + 8, and one group's scale and zero of each.
+// What a lane holds of a chunk: 32 weights of rows g and g + 8, and one group's scale and
+// zero of each, as they lie in memory (a load must not be waited for before its use).
 struct Chunk {
   uint4 q[2];
-  float s[2];
-  uint32_t z[2];
+  uint32_t s[2], z[2];
 };
+
+// 16 bytes that no other block reads.
+__device__ __forceinline__ uint4 load_once(const uint8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 
 // 16 bytes from any address: the five words they lie in, shifted.  A word that ends past
 // the buffer is put together from its bytes.
@@ -94,26 +103,38 @@ __device__ __forceinline__ uint4 load_unaligned(const uint8_t* w, int64_t at, in
                     __funnelshift_r(u[3], u[4], sh));
 }
 
-template <bool kSmallGroups, bool kAligned>
-__device__ __forceinline__ void load_chunk(const W4Params& p, Chunk& c, int tile, int chunk, int lane) {
-  const int t = lane & 3;
+// Where a lane's rows of a tile lie.
+struct Rows {
+  int64_t w[2];  // byte of the lane's first 16 of chunk 0
+  int64_t g[2];  // first group
+};
+__device__ __forceinline__ void at_tile(const W4Params& p, Rows& r, int tile, int lane) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int64_t n = min(tile * kTileRows + (lane >> 2) + 8 * h, p.n - 1);  // (rows past the last are not written)
-    const int64_t off = (int64_t)chunk * (kChunk / 2) + t * 16;
+    const int n = min(tile * kTileRows + (lane >> 2) + 8 * h, p.n - 1);  // (rows past the last are not written)
+    r.w[h] = n * p.row_bytes + (lane & 3) * 16;
+    r.g[h] = (int64_t)n * p.groups;
+  }
+}
+
+template <bool kSmallGroups, bool kAligned>
+__device__ __forceinline__ void load_chunk(const W4Params& p, Chunk& c, const Rows& r, int chunk, int lane) {
+  const int off = chunk * (kChunk / 2);
+  // (a group of the whole chunk is every lane's, also of those past the row's end)
+  const int k = chunk * kChunk + (kSmallGroups ? (lane & 3) * 32 : 0);
+  const bool some = k < p.k, all = off + (lane & 3) * 16 < (int)p.row_bytes;
+  const int group = k >> p.group_shift;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
     c.q[h] = make_uint4(0, 0, 0, 0);
-    c.s[h] = 0.f;
-    c.z[h] = 0x43084308u;
-    // (a group of the whole chunk is every lane's, also of those past the row's end)
-    const int64_t k = kSmallGroups ? off * 2 : (int64_t)chunk * kChunk;
-    if (k >= p.k) continue;
-    const int64_t g = n * p.groups + (k >> p.group_shift);
-    c.s[h] = p.scale_f32 ? __ldg(static_cast<const float*>(p.scales) + g)
-                         : __uint_as_float((uint32_t)__ldg(static_cast<const uint16_t*>(p.scales) + g) << 16);
-    if (p.zeros) c.z[h] = 0x43004300u + 0x00010001u * (__ldg(p.zeros + g) & 15u);
-    if (off >= p.row_bytes) continue;
-    if (kAligned) c.q[h] = __ldg(reinterpret_cast<const uint4*>(p.w + n * p.row_bytes + off));
-    else c.q[h] = load_unaligned(p.w, n * p.row_bytes + off, p.total_bytes);
+    c.s[h] = 0;
+    c.z[h] = 8;
+    if (all) c.q[h] = kAligned ? load_once(p.w + r.w[h] + off) : load_unaligned(p.w, r.w[h] + off, p.total_bytes);
+    if (some) {
+      if (p.scale_f32) c.s[h] = __ldg(static_cast<const uint32_t*>(p.scales) + r.g[h] + group);
+      else c.s[h] = __ldg(static_cast<const uint16_t*>(p.scales) + r.g[h] + group);
+      if (p.zeros) c.z[h] = __ldg(p.zeros + r.g[h] + group);
+    }
   }
 }
 
@@ -136,18 +157,20 @@ __device__ __forceinline__ void transpose_quad(uint4& v, int t) {
 
 // Adds a chunk's products to the sums of its tile.
 template <int NT, bool kSmallGroups>
-__device__ __forceinline__ void multiply_chunk(Chunk& c, const uint8_t* xs, float (&acc)[NT][4], int lane) {
+__device__ __forceinline__ void multiply_chunk(Chunk& c, const uint8_t* xs, float (&acc)[NT][4], int scale_shift, int lane) {
   if (kSmallGroups) {
     transpose_quad(c.q[0], lane & 3);
     transpose_quad(c.q[1], lane & 3);
   }
+  const float sc[2] = {__uint_as_float(c.s[0] << scale_shift), __uint_as_float(c.s[1] << scale_shift)};
+  const uint32_t zc[2] = {0x43004300u + 0x00010001u * (c.z[0] & 15u), 0x43004300u + 0x00010001u * (c.z[1] & 15u)};
   float sum[NT][4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t lo = j == 0 ? c.q[0].x : j == 1 ? c.q[0].y : j == 2 ? c.q[0].z : c.q[0].w;
     const uint32_t hi = j == 0 ? c.q[1].x : j == 1 ? c.q[1].y : j == 2 ? c.q[1].z : c.q[1].w;
-    float s0 = c.s[0], s1 = c.s[1];
-    uint32_t z0 = c.z[0], z1 = c.z[1];
+    float s0 = sc[0], s1 = sc[1];
+    uint32_t z0 = zc[0], z1 = zc[1];
     if (kSmallGroups) {  // (the group of these 32 weights is lane j's of the quad)
       const int from = (lane & ~3) | j;
       s0 = __shfl_sync(0xffffffffu, s0, from);
@@ -219,6 +242,7 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_kernel(const W4Params p) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tiles = (p.n + kTileRows - 1) / kTileRows;
   const int mine = (tiles - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;  // this CTA's tiles, gridDim apart
+  const int scale_shift = p.scale_f32 ? 0 : 16;
   int flip = 0;
   for (int m0 = 0; m0 < p.m; m0 += 8 * NT) {
     for (int first = 0; first < mine; first += kBatch) {
@@ -230,16 +254,15 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_kernel(const W4Params p) {
         const int items = batch * per;
         Chunk c[kAhead];
         int lt = 0, lc = 0;  // the next chunk to load: tile of the batch, chunk of the tile
+        Rows rows;
+        at_tile(p, rows, (int)blockIdx.x + first * (int)gridDim.x, lane);
         auto load = [&](Chunk& into) {
-          if (lt < batch) {
-            const int chunk = lc * kW4Warps + warp;
-            load_chunk<kSmallGroups, kAligned>(p, into, (int)blockIdx.x + (first + lt) * (int)gridDim.x,
-                                 chunk < chunks ? chunk0 + chunk : 0x1000000, lane);
-          }
-          if (++lc == per) {
-            lc = 0;
-            ++lt;
-          }
+          const int chunk = lc * kW4Warps + warp;
+          load_chunk<kSmallGroups, kAligned>(p, into, rows, lt < batch && chunk < chunks ? chunk0 + chunk : kNoChunk, lane);
+          if (++lc < per) return;
+          lc = 0;
+          ++lt;
+          at_tile(p, rows, (int)blockIdx.x + (first + lt) * (int)gridDim.x, lane);
         };
 #pragma unroll
         for (int s = 0; s < kAhead; ++s) load(c[s]);
@@ -254,7 +277,7 @@ __global__ void __launch_bounds__(kW4Threads, 2) w4_kernel(const W4Params p) {
 #pragma unroll
           for (int s = 0; s < kAhead; ++s) {
             if (it + s >= items) break;
-            multiply_chunk<NT, kSmallGroups>(c[s], xs + (int64_t)(at * kW4Warps + warp) * 4 * NT * kUnit, acc, lane);
+            multiply_chunk<NT, kSmallGroups>(c[s], xs + (int64_t)(at * kW4Warps + warp) * 4 * NT * kUnit, acc, scale_shift, lane);
             load(c[s]);
             if (++at < per) continue;
             // the tile's sums: this warp's, then all of them
@@ -336,7 +359,7 @@ extern "C" int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size
   clear_error();
   const char* fn = "rgd_w4_matvec";
   RGD_CHECK_ARG(m >= 0 && n >= 0 && k >= 1, "%s: bad m/n/k", fn);
-  RGD_CHECK_ARG(k <= 1 << 24, "%s: k too large", fn);
+  RGD_CHECK_ARG(k <= kMaxK, "%s: k too large", fn);
   RGD_CHECK_ARG(group_size == 32 || group_size == 64 || group_size == 128, "%s: group_size must be 32, 64 or 128", fn);
   RGD_CHECK_ARG((scale_dtype == RGD_F32 || scale_dtype == RGD_BF16) && (out_dtype == RGD_F32 || out_dtype == RGD_BF16),
                 "%s: scale_dtype and out_dtype must be RGD_F32 or RGD_BF16", fn);
