@@ -1,0 +1,31 @@
+// Shared between the 4-bit products' host side and their kernel's instantiations.
+#pragma once
+
+#include "common.h"
+
+namespace rgd {
+
+constexpr int kW4MaxK = 1 << 24;
+
+struct W4Params {
+  int32_t m, n, k, groups;
+  int32_t group_shift;   // log2 of the group size
+  int32_t block_chunks;  // chunks of a block of k (a multiple of split)
+  int32_t blocks;        // blocks of k
+  int32_t split;         // warps of a group
+  int32_t batch;         // tiles of a group between which k may go in blocks
+  const uint16_t* x;
+  const uint8_t* w;
+  const uint8_t* scales;
+  const uint8_t* zeros;
+  void* y;
+  int64_t row_bytes, y_stride, total_bytes;
+  int32_t scale_bytes, out_f32, x_vec;
+};
+
+// Launches the kernel for up to 8, 16 and 32 rows of x at a time.
+int launch_w4_n8(W4Params& p, cudaStream_t st);
+int launch_w4_n16(W4Params& p, cudaStream_t st);
+int launch_w4_n32(W4Params& p, cudaStream_t st);
+
+}  // namespace rgd

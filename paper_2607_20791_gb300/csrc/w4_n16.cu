@@ -1,0 +1,8 @@
+// The 4-bit products' kernel for 9 to 16 rows of x (a translation unit each, compiled in parallel).
+#include "w4_kernel.cuh"
+
+namespace rgd {
+
+int launch_w4_n16(W4Params& p, cudaStream_t st) { return launch_w4<2>(p, st); }
+
+}  // namespace rgd

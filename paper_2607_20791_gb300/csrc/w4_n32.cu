@@ -1,0 +1,8 @@
+// The 4-bit products' kernel for more than 16 rows of x (a translation unit each, compiled in parallel).
+#include "w4_kernel.cuh"
+
+namespace rgd {
+
+int launch_w4_n32(W4Params& p, cudaStream_t st) { return launch_w4<4>(p, st); }
+
+}  // namespace rgd
