@@ -463,11 +463,12 @@ int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, int32_t dty
  *   y        [m] rows of n elements, y_stride elements apart (>= n; the rest of a row
  *            is left alone), out_dtype RGD_F32 or RGD_BF16
  * Products of bf16 activations with the whole numbers q - z are exact and are summed,
- * and scaled group by group, in fp32; the result is rounded once.  One kernel on
- * `stream`. */
+ * and scaled group by group, in fp32; the result is rounded once.  dev_status gets
+ * RGD_DEV_WAIT_TIMEOUT when a bounded wait on a copy gave up; y is then not valid.  One
+ * kernel on `stream`. */
 int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size, const rgd_bf16* x, const uint8_t* weights,
                   int32_t scale_dtype, const void* scales, const uint8_t* zeros, int32_t out_dtype, void* y,
-                  int64_t y_stride, rgd_stream_t stream);
+                  int64_t y_stride, int32_t* dev_status, rgd_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Pages of the KV cache                                                      */

@@ -80,7 +80,7 @@ _SIGNATURES = {
     "rgd_verify_draft_workspace_size": (_SZ, [_I32, _I32]),
     "rgd_verify_draft": (ctypes.c_int, [_I32, _I32, _I32, _I32, _P, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P,
                                         _P, _P, _P, _P, _SZ, _P, _P]),
-    "rgd_w4_matvec": (ctypes.c_int, [_I32, _I32, _I32, _I32, _P, _P, _I32, _P, _P, _I32, _P, _I64, _P]),
+    "rgd_w4_matvec": (ctypes.c_int, [_I32, _I32, _I32, _I32, _P, _P, _I32, _P, _P, _I32, _P, _I64, _P, _P]),
     "rgd_cache_workspace_size": (_SZ, [ctypes.POINTER(CacheShape), _I32]),
     "rgd_cache_reserve": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                          _SZ, _P, _P]),
@@ -498,7 +498,7 @@ def rgd_verify_draft(target_logits, draft_logits, draft_tokens, n_draft, is_prob
         _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
 
 
-def rgd_w4_matvec(x, weights, scales, zeros, group_size: int, y, stream=None) -> None:
+def rgd_w4_matvec(x, weights, scales, zeros, group_size: int, y, dev_status=None, stream=None) -> None:
     """``y`` [m, W >= n] gets ``x`` [m, k] times the 4-bit ``weights`` [n, ceil(k / 2)] in its first n columns."""
     import torch
     if x.dim() != 2 or weights.dim() != 2 or y.dim() != 2:
@@ -514,7 +514,7 @@ def rgd_w4_matvec(x, weights, scales, zeros, group_size: int, y, stream=None) ->
         m, n, k, group, _ptr(x, "x", torch.bfloat16), _ptr(weights, "weights", torch.uint8),
         _dtype_of(scales, "scales"), _ptr(scales, "scales", numel=n * groups),
         _ptr(zeros, "zeros", torch.uint8, optional=True, numel=n * groups), _dtype_of(y, "y"), _ptr(y, "y"),
-        y.shape[1], _stream(stream)))
+        y.shape[1], _ptr(dev_status, "dev_status", torch.int32, optional=True, numel=1), _stream(stream)))
 
 
 def rgd_cache_workspace_size(shape: CacheShape, rows: int) -> int:

@@ -1,5 +1,6 @@
 // Error reporting shared by all entry points.
 #include <cstring>
+#include <mutex>
 
 #include "common.h"
 
@@ -16,6 +17,20 @@ int set_error(int code, const char* fmt, ...) {
 }
 
 void clear_error() { g_error[0] = '\0'; }
+
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
+            cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
+  });
+  return fn;
+}
 
 }  // namespace rgd
 

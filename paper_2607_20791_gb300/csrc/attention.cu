@@ -16,20 +16,6 @@ namespace {
 constexpr int kTicketSlots = 8192;  // job counters at the start of every workspace (at least)
 constexpr float kLog2e = 1.4426950408889634f;
 
-PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  static std::once_flag once;
-  std::call_once(once, [] {
-    void* ptr = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ptr);
-  });
-  return fn;
-}
-
 // The K or V pool ([rows][D] bf16) for copies of whole 16-token page-head tiles, one
 // box each, with the 128-byte swizzle (16-byte chunk index XOR row index mod 8).
 // V: 64 columns x 16 rows x D/64 halves, so a tile lands half-major.  K: 64 columns x
@@ -38,7 +24,7 @@ PFN_cuTensorMapEncodeTiled_v12000 get_encode_fn() {
 // operand per half although each page is one box (with a box per half the K
 // producer's issue, ~75 cycles a box, was twice the V producer's).
 int make_kv_map(CUtensorMap* map, const void* base, int64_t rows, int D, bool is_k) {
-  auto fn = get_encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
   const cuuint32_t halves = (cuuint32_t)(D / 64);
   const cuuint64_t row = (cuuint64_t)D * 2;

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <cudaTypedefs.h>
 
 #include <atomic>
 #include <cstdarg>
@@ -21,6 +22,9 @@ inline int cuda_error(cudaError_t e, const char* what) {
 }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// The driver's cuTensorMapEncodeTiled (NULL where it is missing).
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
 
 // Launches a kernel as a programmatic dependent of the previous kernel on the
 // stream: it is scheduled while that kernel finishes, and waits for it

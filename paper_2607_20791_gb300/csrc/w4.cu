@@ -5,7 +5,8 @@ using namespace rgd;
 
 extern "C" int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size, const rgd_bf16* x,
                              const uint8_t* weights, int32_t scale_dtype, const void* scales, const uint8_t* zeros,
-                             int32_t out_dtype, void* y, int64_t y_stride, rgd_stream_t stream) {
+                             int32_t out_dtype, void* y, int64_t y_stride, int32_t* dev_status,
+                             rgd_stream_t stream) {
   clear_error();
   const char* fn = "rgd_w4_matvec";
   RGD_CHECK_ARG(m >= 0 && n >= 0 && k >= 1, "%s: bad m/n/k", fn);
@@ -36,6 +37,7 @@ extern "C" int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size
   p.scale_bytes = scale_dtype == RGD_F32 ? 4 : 2;
   p.out_f32 = out_dtype == RGD_F32;
   p.x_vec = k % 8 == 0;
+  p.dev_status = dev_status;
   cudaStream_t st = (cudaStream_t)stream;
   return m <= 8 ? launch_w4_n8(p, st) : m <= 16 ? launch_w4_n16(p, st) : launch_w4_n32(p, st);
 }

@@ -21,6 +21,7 @@ struct W4Params {
   void* y;
   int64_t row_bytes, y_stride, total_bytes;
   int32_t scale_bytes, out_f32, x_vec;
+  int32_t* dev_status;
 };
 
 // Launches the kernel for up to 8, 16 and 32 rows of x at a time.

@@ -3,11 +3,12 @@
 //
 // The weights are read once; everything else is small.  A tile is 32 rows of W (16 above
 // 16 rows of x); the warps of its group take the 128-weight chunks of those rows in turn,
-// so that together they read contiguous bytes of a row.  A chunk is one 16-byte
-// asynchronous copy a lane and 8 rows (lane 4g + t: rows g, g + 8, ..., bytes 16t ..) into the
-// lane's own place in shared memory, 4 KB a warp ahead of their use, and 8
-// mma.m16n8k16 with the weights as A for every 16 of its rows and 8 rows of x: one row
-// costs the same as eight, and the tensor pipe does the sums over k in fp32.
+// so that together they read contiguous bytes of a row.  A chunk is one
+// TMA box of 64 bytes by the tile's rows into the warp's own ring in shared memory, 4 KB
+// ahead of its use, read 16 bytes a lane (lane 4g + t: rows g, g + 8, ..., bytes 16t ..), and
+// 8 mma.m16n8k16 with the weights as A for every 16 of its rows and 8 rows of x: one row
+// costs the same as eight, and the tensor pipe does the sums over k in fp32.  (Rows off
+// 16 bytes come by 4-byte asynchronous copies.)
 //
 // Which k a lane's A elements stand for is free as long as B agrees, so a lane feeds the
 // 8 nibbles of a 32-bit word as they lie: nibbles p and p + 4 are the two halves of
@@ -35,9 +36,8 @@ namespace rgd {
 namespace {
 
 constexpr int kChunk = 128;  // weights of a row per chunk
-constexpr int kNoChunk = kW4MaxK / kChunk;  // past every row's end
 constexpr int kUnit = 512;   // bytes of x per MMA step: 8 rows, 32 weights
-constexpr int kW4Smem = 226 * 1024;
+constexpr int kW4Smem = 226 * 1024;  // (of 227; the barriers take the rest)
 
 // For 8 NT rows of x: warps of a block, groups of 16 rows of W in a tile, chunks in flight.
 template <int NT>
@@ -64,70 +64,52 @@ __device__ __forceinline__ uint32_t weights2(uint32_t word, int p, uint32_t bias
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-
-// A chunk's scales and zeros, of one group of each of a lane's rows, as they lie in memory (a
-// load must not be waited for before its use).
-template <int R, bool kZeros>
-struct Scales {
-  uint32_t s[R], z[kZeros ? R : 1];
-};
-
-// Where a lane's rows of a tile lie: row g of the tile, and how many of its rows g, g + 8, ... there are.
-struct Rows {
-  const uint8_t* w;  // the lane's first 16 bytes of chunk 0
-  int64_t group;     // the row's first group
-  int32_t count;
-};
-template <int R>
-__device__ __forceinline__ Rows rows_of(const W4Params& p, int tile, int lane) {
-  const int64_t n = (int64_t)tile * (8 * R) + (lane >> 2);
-  Rows r;
-  r.count = n < p.n ? (int)min((p.n - n + 7) / 8, (int64_t)R) : 0;
-  r.w = p.w + n * p.row_bytes + (lane & 3) * 16;
-  r.group = n * p.groups;
-  return r;
+__device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+               "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
+               : "memory");
 }
 
-// Starts the copy of a lane's part of a chunk into the ring slot at `to`.  Nothing is
-// read past the weights' end: a copy's bytes there are filled with zeros.
-template <int R, bool kSmallGroups, bool kAligned, bool kZeros>
-__device__ __forceinline__ void load_chunk(const W4Params& p, Scales<R, kZeros>& c, uint32_t to, const Rows& r, int chunk,
-                                           int lane) {
-  const int off = chunk * (kChunk / 2);
-  // (a group of the whole chunk is every lane's, also of those past the row's end)
-  const int k = chunk * kChunk + (kSmallGroups ? (lane & 3) * 32 : 0);
-  const int some = k < p.k ? r.count : 0, all = off + (lane & 3) * 16 < (int)p.row_bytes ? r.count : 0;
-  const uint8_t* w = r.w + off;
-  const int64_t g = r.group + (k >> p.group_shift);
-  const uint8_t* s = p.scales + g * p.scale_bytes;
-  const int64_t row_step = 8 * p.row_bytes;
-  const int group_step = 8 * p.groups, scale_step = group_step * p.scale_bytes;
+// A chunk's scales and zeros as they lie in memory (a load must not be waited for before its
+// use).  Lane i has those of row i of the tile (of row i - 16 for the second half of k in a
+// tile of 16 rows): one, or one for every 32 weights where groups are smaller.
+template <int NL, bool kZeros>
+struct Scales {
+  uint32_t s[NL], z[kZeros ? NL : 1];
+};
+
+template <int kRows, int NL, bool kSmallGroups, bool kZeros>
+__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const uint8_t* row_scales,
+                                            const uint8_t* row_zeros, int chunk, int lane) {
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    int g = (chunk * kChunk + (kSmallGroups ? (lane / kRows * NL + i) * 32 : 0)) >> p.group_shift;
+    if (kSmallGroups) g = min(g, p.groups - 1);  // (weights past the row's end meet zeros of x)
+    if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(row_scales) + g);
+    else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(row_scales) + g);
+    if (kZeros) c.z[i] = __ldg(row_zeros + g);
+  }
+}
+
+// Rows off 16 bytes: starts the copies of the words that hold the lane's 16 bytes of rows
+// g, g + 8, ... of a chunk.  Nothing is read past the weights' end or for rows past the
+// last: those bytes are filled with zeros.
+template <int R>
+__device__ __forceinline__ void copy_words(const W4Params& p, uint32_t to, int tile, int chunk, int lane) {
+  const int64_t n = (int64_t)tile * (8 * R) + (lane >> 2);
+  const int off = chunk * (kChunk / 2) + (lane & 3) * 16;
 #pragma unroll
   for (int h = 0; h < R; ++h) {
-    const uint8_t* src = w + h * row_step;
-    if (kAligned) {
-      copy16(to + h * 512 + lane * 16, h < all ? src : p.w, h < all ? 16 : 0);
-    } else {
-      const int64_t at = (h < all ? src - p.w : 0) & ~int64_t(3);
+    const bool has = n + 8 * h < p.n && off < (int)p.row_bytes;
+    const int64_t at = (has ? (n + 8 * h) * p.row_bytes + off : 0) & ~int64_t(3);
 #pragma unroll
-      for (int i = 0; i < 5; ++i) {
-        const int64_t left = p.total_bytes - (at + 4 * i);
-        const int bytes = h >= all || left <= 0 ? 0 : left < 4 ? (int)left : 4;
-        copy4(to + h * 640 + i * 128 + lane * 4, p.w + (bytes ? at + 4 * i : 0), bytes);
-      }
-    }
-    c.s[h] = 0;
-    if (kZeros) c.z[h] = 0;
-    if (h < some) {
-      if (p.scale_bytes == 2) c.s[h] = __ldg(reinterpret_cast<const uint16_t*>(s + (int64_t)h * scale_step));
-      else c.s[h] = __ldg(reinterpret_cast<const uint32_t*>(s + (int64_t)h * scale_step));
-      if (kZeros) c.z[h] = __ldg(p.zeros + g + (int64_t)h * group_step);
+    for (int i = 0; i < 5; ++i) {
+      const int64_t left = p.total_bytes - (at + 4 * i);
+      const int bytes = !has || left <= 0 ? 0 : left < 4 ? (int)left : 4;
+      copy4(to + h * 640 + i * 128 + lane * 4, p.w + (bytes ? at + 4 * i : 0), bytes);
     }
   }
 }
@@ -160,27 +142,29 @@ __device__ __forceinline__ void transpose_quad(uint4& v, int t) {
   v = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Adds the products of 16 rows' chunk (a lane's weights of rows g and g + 8) to their sums.
-template <int NT, bool kSmallGroups>
-__device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, float s0, float s1, uint32_t z0, uint32_t z1,
-                                              const uint8_t* xs, float (&acc)[NT][4], int lane) {
+// Adds the products of 16 rows' chunk (a lane's weights of rows g and g + 8, rows `sub` ..
+// of the tile) to their sums.  s and z: the tile's scales and biases by lane.
+template <int NT, int kRows, int NL, bool kSmallGroups, bool kZeros>
+__device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, const float (&s)[NL], const uint32_t (&z)[kZeros ? NL : 1],
+                                              int sub, const uint8_t* xs, float (&acc)[NT][4], int lane) {
   if (kSmallGroups) {
     transpose_quad(q0, lane & 3);
     transpose_quad(q1, lane & 3);
   }
-  float sum[NT][4];
+  float sum[NT][4], t0 = 0.f, t1 = 0.f;
+  uint32_t b0 = 0x43084308u, b1 = 0x43084308u;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t lo = j == 0 ? q0.x : j == 1 ? q0.y : j == 2 ? q0.z : q0.w;
     const uint32_t hi = j == 0 ? q1.x : j == 1 ? q1.y : j == 2 ? q1.z : q1.w;
-    float t0 = s0, t1 = s1;
-    uint32_t b0 = z0, b1 = z1;
-    if (kSmallGroups) {  // (the group of these 32 weights is lane j's of the quad)
-      const int from = (lane & ~3) | j;
-      t0 = __shfl_sync(0xffffffffu, s0, from);
-      t1 = __shfl_sync(0xffffffffu, s1, from);
-      b0 = __shfl_sync(0xffffffffu, z0, from);
-      b1 = __shfl_sync(0xffffffffu, z1, from);
+    if (kSmallGroups || j == 0) {
+      const int from = sub + (lane >> 2) + (kSmallGroups ? j / NL * kRows : 0), i = kSmallGroups ? j % NL : 0;
+      t0 = __shfl_sync(0xffffffffu, s[i], from);
+      t1 = __shfl_sync(0xffffffffu, s[i], from + 8);
+      if (kZeros) {
+        b0 = __shfl_sync(0xffffffffu, z[kZeros ? i : 0], from);
+        b1 = __shfl_sync(0xffffffffu, z[kZeros ? i : 0], from + 8);
+      }
     }
     uint32_t a[4], b[4];
 #pragma unroll
@@ -209,27 +193,38 @@ __device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, float s0, floa
 // A block of x into shared memory, 8 numbers a lane and step, in the order of the nibbles.
 template <int NT, bool kSmallGroups>
 __device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int chunk0, int chunks, int m0) {
-  for (int u = threadIdx.x; u < chunks * 4 * NT * 32; u += kWarps<NT> * 32) {
-    const int lane = u & 31, i = (u >> 5) % NT, j = (u >> 5) / NT & 3, c = (u >> 5) / (NT * 4);
-    const int t = lane & 3, m = m0 + i * 8 + (lane >> 2);
-    const int64_t k = (int64_t)(chunk0 + c) * kChunk + (kSmallGroups ? j * 32 + t * 8 : t * 32 + j * 8);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (m < p.m && k < p.k) {
-      const uint16_t* src = p.x + (int64_t)m * p.k + k;
-      uint16_t e[8];
-      if (p.x_vec) {  // (k is then a multiple of 8)
-        const uint4 r = __ldg(reinterpret_cast<const uint4*>(src));
-        const uint32_t q[4] = {r.x, r.y, r.z, r.w};
+  constexpr int kThreads = kWarps<NT> * 32, kBatch = 8;  // (loads in flight)
+  const int units = chunks * 4 * NT * 32;
+  for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kBatch) {
+    uint4 r[kBatch];
 #pragma unroll
-        for (int b = 0; b < 8; ++b) e[b] = (uint16_t)(b & 1 ? q[b / 2] >> 16 : q[b / 2] & 0xffffu);
-      } else {
+    for (int f = 0; f < kBatch; ++f) {
+      const int u = u0 + f * kThreads;
+      const int lane = u & 31, i = (u >> 5) % NT, j = (u >> 5) / NT & 3, c = (u >> 5) / (NT * 4);
+      const int t = lane & 3, m = m0 + i * 8 + (lane >> 2);
+      const int k = (chunk0 + c) * kChunk + (kSmallGroups ? j * 32 + t * 8 : t * 32 + j * 8);
+      r[f] = make_uint4(0, 0, 0, 0);
+      if (u < units && m < p.m && k < p.k) {
+        const uint16_t* src = p.x + (int64_t)m * p.k + k;
+        if (p.x_vec) {  // (k is then a multiple of 8)
+          r[f] = __ldg(reinterpret_cast<const uint4*>(src));
+        } else {
+          uint16_t e[8];
 #pragma unroll
-        for (int b = 0; b < 8; ++b) e[b] = k + b < p.k ? __ldg(src + b) : 0;
+          for (int b = 0; b < 8; ++b) e[b] = k + b < p.k ? __ldg(src + b) : 0;
+          r[f] = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16,
+                            e[6] | (uint32_t)e[7] << 16);
+        }
       }
-      v = make_uint4(e[0] | (uint32_t)e[4] << 16, e[1] | (uint32_t)e[5] << 16, e[2] | (uint32_t)e[6] << 16,
-                     e[3] | (uint32_t)e[7] << 16);
     }
-    *reinterpret_cast<uint4*>(xs + (int64_t)u * 16) = v;
+#pragma unroll
+    for (int f = 0; f < kBatch; ++f) {
+      const int u = u0 + f * kThreads;
+      if (u < units)
+        *reinterpret_cast<uint4*>(xs + (int64_t)u * 16) =
+            make_uint4(__byte_perm(r[f].x, r[f].z, 0x5410), __byte_perm(r[f].x, r[f].z, 0x7632),
+                       __byte_perm(r[f].y, r[f].w, 0x5410), __byte_perm(r[f].y, r[f].w, 0x7632));
+    }
   }
 }
 
@@ -238,7 +233,7 @@ __device__ __forceinline__ void group_barrier(int group, int warps) {
   asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
 }
 
-// Shared memory: every warp's sums of a tile, the sums kept between blocks of k, the warps' rings, x.
+// Shared memory: the warps' rings, every warp's sums of a tile, the sums kept between blocks of k, x.
 template <int NT, bool kAligned>
 struct Layout {
   static constexpr int kRows = 16 * kSub<NT>;   // of a tile
@@ -249,16 +244,24 @@ struct Layout {
 };
 
 template <int NT, bool kSmallGroups, bool kAligned, bool kZeros>
-__global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p) {
+__global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
   using L = Layout<NT, kAligned>;
-  constexpr int kSums = L::kSums, kRows = L::kRows, R = kRows / 8, A = kAhead<NT>;
-  extern __shared__ __align__(16) uint8_t dyn[];
+  constexpr int kSums = L::kSums, kRows = L::kRows, R = kRows / 8, A = kAhead<NT>, NL = kSmallGroups ? kRows / 8 : 1;
+  extern __shared__ __align__(128) uint8_t dyn[];
+  __shared__ uint64_t landed[kWarps<NT>][A];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int S = p.split, groups = kWarps<NT> / S, group = warp / S, member = warp % S;
-  float* part = reinterpret_cast<float*>(dyn) + group * S * kSums;  // [S][kSums]
-  const uint8_t* ring = dyn + L::kPart + warp * A * L::kSlot;
-  float* kept = reinterpret_cast<float*>(dyn + L::kPart + L::kRing) + group * p.batch * kSums;  // [batch][kSums]
-  uint8_t* xs = dyn + L::kPart + L::kRing + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
+  const uint8_t* ring = dyn + warp * A * L::kSlot;
+  float* part = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;                   // [S][kSums]
+  float* kept = reinterpret_cast<float*>(dyn + L::kRing + L::kPart) + group * p.batch * kSums;  // [batch][kSums]
+  uint8_t* xs = dyn + L::kRing + L::kPart + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
+  if (kAligned && lane == 0) {
+#pragma unroll
+    for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], 1);
+    fence_mbar_init();
+    fence_proxy_async_smem();
+  }
+  __syncwarp();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tiles = (p.n + kRows - 1) / kRows;
@@ -268,32 +271,51 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
   const int most = (int)blockIdx.x < tiles ? (tiles - (int)blockIdx.x + stride - 1) / stride : 0;  // of any group here
   const int scale_shift = p.scale_bytes == 2 ? 16 : 0;
   const uint32_t ring_at = smem_u32(ring);
+  uint32_t parity = 0;  // of each slot's barrier
+  int flying = 0, lost = 0;  // copies on their way, and the slot of the oldest once a wait has given up
+  bool alive = true;    // no wait has given up
   for (int m0 = 0; m0 < p.m; m0 += 8 * NT) {
     for (int first = 0; first < most; first += p.batch) {
       const int batch = max(0, min(p.batch, mine - first));
       for (int kb = 0; kb < p.blocks; ++kb) {
         const int chunk0 = kb * p.block_chunks;
         const int chunks = min(p.block_chunks, (p.k + kChunk - 1) / kChunk - chunk0);
-        const int per = (chunks + S - 1) / S;  // chunks of a warp and tile
-        const int items = batch * per;
-        Scales<R, kZeros> c[A];
-        int lt = 0, lc = member;  // the next chunk to load: tile of the batch, chunk of the tile
-        Rows rows = rows_of<R>(p, tile0 + first * stride, lane);
-        auto load = [&](Scales<R, kZeros>& into, int s) {
-          load_chunk<R, kSmallGroups, kAligned, kZeros>(p, into, ring_at + s * L::kSlot, rows,
-                                                        lt < batch && lc < chunks ? chunk0 + lc : kNoChunk, lane);
-          asm volatile("cp.async.commit_group;" ::: "memory");
+        const int per = (chunks - member + S - 1) / S;  // chunks of this warp and a tile (none: the group's others have them)
+        const int items = batch * max(per, 1);
+        Scales<NL, kZeros> c[A];
+        // the next chunk to load, its tile, and the scales and zeros of the lane's row (of the last row for those past it)
+        int lt = 0, lc = member, load_tile = tile0 + first * stride;
+        const uint8_t *row_scales, *row_zeros;
+        auto at_row = [&] {
+          const int64_t g = min((int64_t)load_tile * kRows + lane % kRows, (int64_t)p.n - 1) * p.groups;
+          row_scales = p.scales + g * p.scale_bytes;
+          row_zeros = p.zeros + g;
+        };
+        at_row();
+        auto load = [&](Scales<NL, kZeros>& into, int s) {
+          if (lt < batch && lc < chunks) {
+            if (!kAligned) {
+              copy_words<R>(p, ring_at + s * L::kSlot, load_tile, chunk0 + lc, lane);
+            } else if (lane == 0 && alive) {
+              mbar_arrive_expect_tx(&landed[warp][s], L::kSlot);
+              copy_box(ring_at + s * L::kSlot, &map, (chunk0 + lc) * (kChunk / 2), load_tile * kRows, &landed[warp][s]);
+            }
+            if (kAligned && alive) ++flying;
+            load_scales<kRows, NL, kSmallGroups, kZeros>(p, into, row_scales, row_zeros, chunk0 + lc, lane);
+          }
+          if (!kAligned) asm volatile("cp.async.commit_group;" ::: "memory");
           lc += S;
-          if (lc < per * S) return;
+          if (lc < chunks) return;
           lc = member;
           ++lt;
-          rows = rows_of<R>(p, tile0 + (first + lt) * stride, lane);
+          load_tile += stride;
+          at_row();
         };
 #pragma unroll
         for (int s = 0; s < A; ++s) load(c[s], s);
         if (p.blocks > 1 || first == 0) {
           __syncthreads();  // (the x of the block before is no longer read)
-          stage_x<NT, kSmallGroups>(p, xs, chunk0, per * S, m0);
+          stage_x<NT, kSmallGroups>(p, xs, chunk0, chunks, m0);
           __syncthreads();
         }
         float acc[kSub<NT>][NT][4] = {};
@@ -302,26 +324,43 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
 #pragma unroll
           for (int s = 0; s < A; ++s) {
             if (it + s >= items) break;
-            uint32_t shift = 0;  // (the same for all of a lane's rows, which are 8 apart)
-            if (!kAligned)
-              shift = (uint32_t)(((int64_t)(tile0 + (first + tile) * stride) * kRows + (lane >> 2)) * p.row_bytes & 3) * 8;
-            asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copy of the chunk has landed
-            uint4 q[R];
+            if (at < chunks) {
+              uint32_t shift = 0;  // (the same for all of a lane's rows, which are 8 apart)
+              if (kAligned) {
+                if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
+                  if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
+                  alive = false;  // (no more copies; those on their way are waited for at the end)
+                  lost = s;
+                }
+                if (alive) {
+                  parity ^= 1u << s;
+                  --flying;
+                }
+              } else {
+                asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copies of the chunk have landed
+                shift = (uint32_t)(((int64_t)(tile0 + (first + tile) * stride) * kRows + (lane >> 2)) * p.row_bytes & 3) * 8;
+              }
+              uint4 q[R];
 #pragma unroll
-            for (int h = 0; h < R; ++h) q[h] = chunk_row<kAligned>(ring + s * L::kSlot, h, shift, lane);
-            const Scales<R, kZeros> now = c[s];
-            load(c[s], s);  // (over what this lane has just read)
+              for (int h = 0; h < R; ++h) q[h] = chunk_row<kAligned>(ring + s * L::kSlot, h, shift, lane);
+              float sc[NL];
+              uint32_t z[kZeros ? NL : 1];
 #pragma unroll
-            for (int b = 0; b < kSub<NT>; ++b) {
-              const int h = 2 * b;
-              multiply_rows<NT, kSmallGroups>(
-                  q[h], q[h + 1], __uint_as_float(now.s[h] << scale_shift), __uint_as_float(now.s[h + 1] << scale_shift),
-                  kZeros ? 0x43004300u + 0x00010001u * (now.z[kZeros ? h : 0] & 15u) : 0x43084308u,
-                  kZeros ? 0x43004300u + 0x00010001u * (now.z[kZeros ? h + 1 : 0] & 15u) : 0x43084308u,
-                  xs + (int64_t)at * 4 * NT * kUnit, acc[b], lane);
+              for (int i = 0; i < NL; ++i) {
+                sc[i] = __uint_as_float(c[s].s[i] << scale_shift);
+                if (kZeros) z[i] = 0x43004300u + 0x00010001u * (c[s].z[i] & 15u);
+              }
+              __syncwarp();
+              load(c[s], s);  // (over what the warp has just read)
+#pragma unroll
+              for (int b = 0; b < kSub<NT>; ++b)
+                multiply_rows<NT, kRows, NL, kSmallGroups, kZeros>(q[2 * b], q[2 * b + 1], sc, z, 16 * b,
+                                                                   xs + (int64_t)at * 4 * NT * kUnit, acc[b], lane);
+            } else {
+              load(c[s], s);
             }
             at += S;
-            if (at < per * S) continue;
+            if (at < chunks) continue;
             // the tile's sums: this warp's, once the group has read those of the tile before, then all of them
             group_barrier(group, S);
             float* mp = part + member * kSums + (lane & 3) * 2 * kRows + (lane >> 2);
@@ -356,7 +395,9 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
       }
     }
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!kAligned) asm volatile("cp.async.wait_all;" ::: "memory");
+  if (!alive)
+    for (int i = 0; i < flying; ++i) mbar_wait(&landed[warp][(lost + i) % A], (parity >> (lost + i) % A) & 1u);
 }
 
 template <int NT, bool kSmallGroups, bool kAligned, bool kZeros>
@@ -391,7 +432,18 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
     p.blocks = (chunks + p.block_chunks - 1) / p.block_chunks;
     smem = L::kPart + L::kRing + p.batch * groups * sums + p.block_chunks * x_bytes;
   }
-  const cudaError_t e = launch_dependent(k, std::min(tiles, sms), W * 32, smem, st, p);
+  CUtensorMap map = {};
+  if (kAligned) {
+    const auto encode = tensor_map_encoder();
+    if (!encode) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
+    const cuuint64_t dims[2] = {(cuuint64_t)p.row_bytes, (cuuint64_t)p.n}, strides[1] = {(cuuint64_t)p.row_bytes};
+    const cuuint32_t box[2] = {kChunk / 2, L::kRows}, ones[2] = {1, 1};
+    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p.w), dims, strides, box, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+  }
+  const cudaError_t e = launch_dependent(k, std::min(tiles, sms), W * 32, smem, st, p, map);
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "w4 launch");
 }
 
