@@ -35,17 +35,20 @@
 namespace rgd {
 namespace {
 
-constexpr int kChunk = 128;  // weights of a row per chunk
+constexpr int kPart = 128;   // weights of a row that a lane's quad holds at a time
 constexpr int kUnit = 512;   // bytes of x per MMA step: 8 rows, 32 weights
 constexpr int kW4Smem = 226 * 1024;  // (of 227; the barriers take the rest)
 
-// For 8 NT rows of x: warps of a block, groups of 16 rows of W in a tile, chunks in flight.
-template <int NT>
-constexpr int kWarps = NT == 1 ? 24 : 16;
+constexpr int kWarps = 16;   // of a block
+// For 8 NT rows of x: groups of 16 rows of W in a tile, 128-weight parts of a chunk, chunks in flight.
 template <int NT>
 constexpr int kSub = NT == 4 ? 1 : 2;
 template <int NT>
+constexpr int kParts = NT == 1 ? 2 : 1;
+template <int NT>
 constexpr int kAhead = NT == 4 ? 4 : 2;
+template <int NT>
+constexpr int kChunk = kPart * kParts<NT>;
 // Bytes of 8 rows of a chunk in a warp's ring; rows off 16 bytes come as the five words that hold a lane's 16 bytes.
 template <bool kAligned>
 constexpr int kPiece = kAligned ? 512 : 640;
@@ -57,11 +60,18 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Nibbles p and p + 4 of a word as bf16 q - z (bias: 128 + z twice).
-__device__ __forceinline__ uint32_t weights2(uint32_t word, int p, uint32_t bias) {
-  const uint32_t u = ((word >> (4 * p)) & 0x000f000fu) | 0x43004300u;
+// Nibbles p and p + 4 of a word as bf16 q - z (bias: 128 + z twice).  `magic` is 0x43004300 in a
+// register, so that mask and exponent go in by one instruction.
+__device__ __forceinline__ uint32_t weights2(uint32_t word, int p, uint32_t magic, uint32_t bias) {
+  uint32_t u;
+  asm("lop3.b32 %0, %1, 0x000f000f, %2, 0xea;" : "=r"(u) : "r"(word >> (4 * p)), "r"(magic));
   const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&bias));
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t exponent_bits() {
+  uint32_t m;
+  asm volatile("mov.b32 %0, 0x43004300;" : "=r"(m));
+  return m;
 }
 
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
@@ -75,19 +85,20 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
 
 // A chunk's scales and zeros as they lie in memory (a load must not be waited for before its
 // use).  Lane i has those of row i of the tile (of row i - 16 for the second half of k in a
-// tile of 16 rows): one, or one for every 32 weights where groups are smaller.
+// tile of 16 rows): one of every 128 weights, or of every 32 where groups are smaller.
 template <int NL, bool kZeros>
 struct Scales {
   uint32_t s[NL], z[kZeros ? NL : 1];
 };
 
-template <int kRows, int NL, bool kSmallGroups, bool kZeros>
+template <int kRows, int kParts, int NL, bool kSmallGroups, bool kZeros>
 __device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const uint8_t* row_scales,
                                             const uint8_t* row_zeros, int chunk, int lane) {
+  constexpr int kEach = NL / kParts;
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    int g = (chunk * kChunk + (kSmallGroups ? (lane / kRows * NL + i) * 32 : 0)) >> p.group_shift;
-    if (kSmallGroups) g = min(g, p.groups - 1);  // (weights past the row's end meet zeros of x)
+    const int k = (chunk * kParts + i / kEach) * kPart + (kSmallGroups ? (lane / kRows * kEach + i % kEach) * 32 : 0);
+    const int g = min(k >> p.group_shift, p.groups - 1);  // (weights past the row's end meet zeros of x)
     if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(row_scales) + g);
     else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(row_scales) + g);
     if (kZeros) c.z[i] = __ldg(row_zeros + g);
@@ -95,12 +106,12 @@ __device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros
 }
 
 // Rows off 16 bytes: starts the copies of the words that hold the lane's 16 bytes of rows
-// g, g + 8, ... of a chunk.  Nothing is read past the weights' end or for rows past the
+// g, g + 8, ... of a part.  Nothing is read past the weights' end or for rows past the
 // last: those bytes are filled with zeros.
 template <int R>
-__device__ __forceinline__ void copy_words(const W4Params& p, uint32_t to, int tile, int chunk, int lane) {
+__device__ __forceinline__ void copy_words(const W4Params& p, uint32_t to, int tile, int part, int lane) {
   const int64_t n = (int64_t)tile * (8 * R) + (lane >> 2);
-  const int off = chunk * (kChunk / 2) + (lane & 3) * 16;
+  const int off = part * (kPart / 2) + (lane & 3) * 16;
 #pragma unroll
   for (int h = 0; h < R; ++h) {
     const bool has = n + 8 * h < p.n && off < (int)p.row_bytes;
@@ -143,10 +154,11 @@ __device__ __forceinline__ void transpose_quad(uint4& v, int t) {
 }
 
 // Adds the products of 16 rows' chunk (a lane's weights of rows g and g + 8, rows `sub` ..
-// of the tile) to their sums.  s and z: the tile's scales and biases by lane.
+// of the tile) to their sums.  s and z: the tile's scales and biases by lane, the chunk's part's
+// from `first` on.
 template <int NT, int kRows, int NL, bool kSmallGroups, bool kZeros>
 __device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, const float (&s)[NL], const uint32_t (&z)[kZeros ? NL : 1],
-                                              int sub, const uint8_t* xs, float (&acc)[NT][4], int lane) {
+                                              int first, int sub, const uint8_t* xs, float (&acc)[NT][4], uint32_t magic, int lane) {
   if (kSmallGroups) {
     transpose_quad(q0, lane & 3);
     transpose_quad(q1, lane & 3);
@@ -158,7 +170,8 @@ __device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, const float (&
     const uint32_t lo = j == 0 ? q0.x : j == 1 ? q0.y : j == 2 ? q0.z : q0.w;
     const uint32_t hi = j == 0 ? q1.x : j == 1 ? q1.y : j == 2 ? q1.z : q1.w;
     if (kSmallGroups || j == 0) {
-      const int from = sub + (lane >> 2) + (kSmallGroups ? j / NL * kRows : 0), i = kSmallGroups ? j % NL : 0;
+      constexpr int kEach = NL / kParts<NT>;
+      const int from = sub + (lane >> 2) + (kSmallGroups ? j / kEach * kRows : 0), i = first + (kSmallGroups ? j % kEach : 0);
       t0 = __shfl_sync(0xffffffffu, s[i], from);
       t1 = __shfl_sync(0xffffffffu, s[i], from + 8);
       if (kZeros) {
@@ -169,8 +182,8 @@ __device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, const float (&
     uint32_t a[4], b[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      a[q] = weights2(lo, q, b0);
-      b[q] = weights2(hi, q, b1);
+      a[q] = weights2(lo, q, magic, b0);
+      b[q] = weights2(hi, q, magic, b1);
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
@@ -192,9 +205,9 @@ __device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, const float (&
 
 // A block of x into shared memory, 8 numbers a lane and step, in the order of the nibbles.
 template <int NT, bool kSmallGroups>
-__device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int chunk0, int chunks, int m0) {
-  constexpr int kThreads = kWarps<NT> * 32, kBatch = 8;  // (loads in flight)
-  const int units = chunks * 4 * NT * 32;
+__device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int part0, int parts, int m0) {
+  constexpr int kThreads = kWarps * 32, kBatch = 8;  // (loads in flight)
+  const int units = parts * 4 * NT * 32;
   for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kBatch) {
     uint4 r[kBatch];
 #pragma unroll
@@ -202,7 +215,7 @@ __device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int chun
       const int u = u0 + f * kThreads;
       const int lane = u & 31, i = (u >> 5) % NT, j = (u >> 5) / NT & 3, c = (u >> 5) / (NT * 4);
       const int t = lane & 3, m = m0 + i * 8 + (lane >> 2);
-      const int k = (chunk0 + c) * kChunk + (kSmallGroups ? j * 32 + t * 8 : t * 32 + j * 8);
+      const int k = (part0 + c) * kPart + (kSmallGroups ? j * 32 + t * 8 : t * 32 + j * 8);
       r[f] = make_uint4(0, 0, 0, 0);
       if (u < units && m < p.m && k < p.k) {
         const uint16_t* src = p.x + (int64_t)m * p.k + k;
@@ -238,23 +251,25 @@ template <int NT, bool kAligned>
 struct Layout {
   static constexpr int kRows = 16 * kSub<NT>;   // of a tile
   static constexpr int kSums = kRows * 8 * NT;
-  static constexpr int kPart = kWarps<NT> * kSums * 4;
-  static constexpr int kSlot = 2 * kSub<NT> * kPiece<kAligned>;
-  static constexpr int kRing = kWarps<NT> * kAhead<NT> * kSlot;
+  static constexpr int kJoin = kWarps * kSums * 4;
+  static constexpr int kPartBytes = 2 * kSub<NT> * kPiece<kAligned>;
+  static constexpr int kSlot = kParts<NT> * kPartBytes;
+  static constexpr int kRing = kWarps * kAhead<NT> * kSlot;
 };
 
 template <int NT, bool kSmallGroups, bool kAligned, bool kZeros>
-__global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
+__global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
   using L = Layout<NT, kAligned>;
-  constexpr int kSums = L::kSums, kRows = L::kRows, R = kRows / 8, A = kAhead<NT>, NL = kSmallGroups ? kRows / 8 : 1;
+  constexpr int kSums = L::kSums, kRows = L::kRows, R = kRows / 8, A = kAhead<NT>, P = kParts<NT>;
+  constexpr int NL = P * (kSmallGroups ? kRows / 8 : 1);
   extern __shared__ __align__(128) uint8_t dyn[];
-  __shared__ uint64_t landed[kWarps<NT>][A];
+  __shared__ uint64_t landed[kWarps][A];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int S = p.split, groups = kWarps<NT> / S, group = warp / S, member = warp % S;
+  const int S = p.split, groups = kWarps / S, group = warp / S, member = warp % S;
   const uint8_t* ring = dyn + warp * A * L::kSlot;
   float* part = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;                   // [S][kSums]
-  float* kept = reinterpret_cast<float*>(dyn + L::kRing + L::kPart) + group * p.batch * kSums;  // [batch][kSums]
-  uint8_t* xs = dyn + L::kRing + L::kPart + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
+  float* kept = reinterpret_cast<float*>(dyn + L::kRing + L::kJoin) + group * p.batch * kSums;  // [batch][kSums]
+  uint8_t* xs = dyn + L::kRing + L::kJoin + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
   if (kAligned && lane == 0) {
 #pragma unroll
     for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], 1);
@@ -270,7 +285,7 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
   const int mine = tile0 < tiles ? (tiles - tile0 + stride - 1) / stride : 0;
   const int most = (int)blockIdx.x < tiles ? (tiles - (int)blockIdx.x + stride - 1) / stride : 0;  // of any group here
   const int scale_shift = p.scale_bytes == 2 ? 16 : 0;
-  const uint32_t ring_at = smem_u32(ring);
+  const uint32_t ring_at = smem_u32(ring), magic = exponent_bits();
   uint32_t parity = 0;  // of each slot's barrier
   int flying = 0, lost = 0;  // copies on their way, and the slot of the oldest once a wait has given up
   bool alive = true;    // no wait has given up
@@ -279,7 +294,7 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
       const int batch = max(0, min(p.batch, mine - first));
       for (int kb = 0; kb < p.blocks; ++kb) {
         const int chunk0 = kb * p.block_chunks;
-        const int chunks = min(p.block_chunks, (p.k + kChunk - 1) / kChunk - chunk0);
+        const int chunks = min(p.block_chunks, (p.k + kChunk<NT> - 1) / kChunk<NT> - chunk0);
         const int per = (chunks - member + S - 1) / S;  // chunks of this warp and a tile (none: the group's others have them)
         const int items = batch * max(per, 1);
         Scales<NL, kZeros> c[A];
@@ -295,13 +310,17 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
         auto load = [&](Scales<NL, kZeros>& into, int s) {
           if (lt < batch && lc < chunks) {
             if (!kAligned) {
-              copy_words<R>(p, ring_at + s * L::kSlot, load_tile, chunk0 + lc, lane);
+              for (int c2 = 0; c2 < P; ++c2)
+                copy_words<R>(p, ring_at + s * L::kSlot + c2 * L::kPartBytes, load_tile, (chunk0 + lc) * P + c2, lane);
             } else if (lane == 0 && alive) {
               mbar_arrive_expect_tx(&landed[warp][s], L::kSlot);
-              copy_box(ring_at + s * L::kSlot, &map, (chunk0 + lc) * (kChunk / 2), load_tile * kRows, &landed[warp][s]);
+#pragma unroll
+              for (int c2 = 0; c2 < P; ++c2)  // (a part past the row's end is filled with zeros)
+                copy_box(ring_at + s * L::kSlot + c2 * L::kPartBytes, &map, ((chunk0 + lc) * P + c2) * (kPart / 2),
+                         load_tile * kRows, &landed[warp][s]);
             }
             if (kAligned && alive) ++flying;
-            load_scales<kRows, NL, kSmallGroups, kZeros>(p, into, row_scales, row_zeros, chunk0 + lc, lane);
+            load_scales<kRows, P, NL, kSmallGroups, kZeros>(p, into, row_scales, row_zeros, chunk0 + lc, lane);
           }
           if (!kAligned) asm volatile("cp.async.commit_group;" ::: "memory");
           lc += S;
@@ -315,7 +334,7 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
         for (int s = 0; s < A; ++s) load(c[s], s);
         if (p.blocks > 1 || first == 0) {
           __syncthreads();  // (the x of the block before is no longer read)
-          stage_x<NT, kSmallGroups>(p, xs, chunk0, chunks, m0);
+          stage_x<NT, kSmallGroups>(p, xs, chunk0 * P, chunks * P, m0);
           __syncthreads();
         }
         float acc[kSub<NT>][NT][4] = {};
@@ -340,9 +359,12 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
                 asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copies of the chunk have landed
                 shift = (uint32_t)(((int64_t)(tile0 + (first + tile) * stride) * kRows + (lane >> 2)) * p.row_bytes & 3) * 8;
               }
-              uint4 q[R];
+              uint4 q[P][R];
 #pragma unroll
-              for (int h = 0; h < R; ++h) q[h] = chunk_row<kAligned>(ring + s * L::kSlot, h, shift, lane);
+              for (int c2 = 0; c2 < P; ++c2)
+#pragma unroll
+                for (int h = 0; h < R; ++h)
+                  q[c2][h] = chunk_row<kAligned>(ring + s * L::kSlot + c2 * L::kPartBytes, h, shift, lane);
               float sc[NL];
               uint32_t z[kZeros ? NL : 1];
 #pragma unroll
@@ -353,9 +375,12 @@ __global__ void __launch_bounds__(kWarps<NT> * 32, 1) w4_kernel(const W4Params p
               __syncwarp();
               load(c[s], s);  // (over what the warp has just read)
 #pragma unroll
-              for (int b = 0; b < kSub<NT>; ++b)
-                multiply_rows<NT, kRows, NL, kSmallGroups, kZeros>(q[2 * b], q[2 * b + 1], sc, z, 16 * b,
-                                                                   xs + (int64_t)at * 4 * NT * kUnit, acc[b], lane);
+              for (int c2 = 0; c2 < P; ++c2)
+#pragma unroll
+                for (int b = 0; b < kSub<NT>; ++b)
+                  multiply_rows<NT, kRows, NL, kSmallGroups, kZeros>(q[c2][2 * b], q[c2][2 * b + 1], sc, z, c2 * (NL / P), 16 * b,
+                                                                     xs + (int64_t)(at * P + c2) * 4 * NT * kUnit, acc[b],
+                                                                     magic, lane);
             } else {
               load(c[s], s);
             }
@@ -406,38 +431,38 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
   using L = Layout<NT, kAligned>;
   auto k = w4_kernel<NT, kSmallGroups, kAligned, kZeros>;
   if (int rc = ensure_smem(k, kW4Smem, done)) return rc;
-  constexpr int W = kWarps<NT>, sms = 152;
+  constexpr int W = kWarps, sms = 152;
   constexpr int sums = L::kSums * 4;        // bytes
-  constexpr int x_bytes = 4 * NT * kUnit;   // of a chunk
-  constexpr int room = kW4Smem - L::kPart - L::kRing;
+  constexpr int x_bytes = 4 * kParts<NT> * NT * kUnit;  // of a chunk
+  constexpr int room = kW4Smem - L::kJoin - L::kRing;
   const int tiles = (p.n + L::kRows - 1) / L::kRows;
-  const int chunks = (p.k + kChunk - 1) / kChunk;
+  const int chunks = (p.k + kChunk<NT> - 1) / kChunk<NT>;
   static_assert(room / 4 >= W / 4 * sums, "a tile of each group must be kept");
   static_assert(room - room / 4 >= x_bytes * 4, "a block of k must fit");
-  // a block of a group's width of k has to fit; 24 and 16 are whole blocks, 12, 8 and 4 divide them
+  // (a block of a group's width of k has to fit)
   int S = tiles <= sms ? W : tiles <= 4 * sms ? 8 : 4;
-  while (S * x_bytes > room - room / 4) S = S > 12 ? (W == 24 ? 12 : 8) : S > 8 ? 8 : 4;
+  while (S * x_bytes > room - room / 4) S /= 2;
   p.split = S;
   const int groups = W / S;
   const int whole = (chunks + S - 1) / S * S;
   p.blocks = 1;
   p.block_chunks = whole;
   p.batch = 0x3fffffff;
-  int smem = L::kPart + L::kRing + whole * x_bytes;
+  int smem = L::kJoin + L::kRing + whole * x_bytes;
   if (whole > room / x_bytes) {  // blocks of k, as even as they come: a quarter of the room keeps sums
     p.batch = std::max(1, room / 4 / (groups * sums));
     const int fits = (room - p.batch * groups * sums) / (x_bytes * S) * S;
     p.blocks = (chunks + fits - 1) / fits;
     p.block_chunks = ((chunks + p.blocks - 1) / p.blocks + S - 1) / S * S;
     p.blocks = (chunks + p.block_chunks - 1) / p.block_chunks;
-    smem = L::kPart + L::kRing + p.batch * groups * sums + p.block_chunks * x_bytes;
+    smem = L::kJoin + L::kRing + p.batch * groups * sums + p.block_chunks * x_bytes;
   }
   CUtensorMap map = {};
   if (kAligned) {
     const auto encode = tensor_map_encoder();
     if (!encode) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
     const cuuint64_t dims[2] = {(cuuint64_t)p.row_bytes, (cuuint64_t)p.n}, strides[1] = {(cuuint64_t)p.row_bytes};
-    const cuuint32_t box[2] = {kChunk / 2, L::kRows}, ones[2] = {1, 1};
+    const cuuint32_t box[2] = {kPart / 2, L::kRows}, ones[2] = {1, 1};
     const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p.w), dims, strides, box, ones,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
