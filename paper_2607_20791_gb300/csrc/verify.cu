@@ -21,6 +21,8 @@
 // rounding is what a sum in fp32 does to a small weight too: it loses at most 2^-32 of
 // the largest weight, 3e-5 of the sum in the worst case over 131072 tokens, where each
 // is below 2.4e-10 of the largest.
+#include <cuda_bf16.h>
+
 #include <algorithm>
 #include <cmath>
 
@@ -105,6 +107,136 @@ __device__ __forceinline__ uint32_t whole(float w) {
   return __float_as_uint(fmaf(w, 0x1p31f, 0x1p23f)) - 0x4b000000u;
 }
 
+// Two fp32 values in one 64-bit register, and arithmetic on both at once.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t word_sum(uint64_t v) { return (uint32_t)v + (uint32_t)(v >> 32); }
+
+// A lane's sum of whole(w), exact for up to 512 numbers.  Small ones (w <= 2^-8) are added
+// as the bits of w 2^31 + 2^23.  Others go in two halves, w = a 2^-15 + r with a the
+// nearest whole number, and w 2^31 = a 2^16 + r 2^31, both again read off the bits of a sum
+// (2^23, and 1.5 2^23 for r's sign).  Conversions to integers would take the special
+// function unit's time, which the exponentials need.
+struct WholeSum {
+  uint32_t low = 0, a = 0, b = 0;
+  __device__ void small(uint64_t w2) {
+    low += word_sum(fma2(w2, pair(0x1p31f, 0x1p31f), pair(0x1p23f, 0x1p23f))) - 2u * 0x4b000000u;
+  }
+  __device__ void any(uint64_t w2) {
+    const uint64_t h = fma2(w2, pair(0x1p15f, 0x1p15f), pair(0x1p23f, 0x1p23f));
+    const uint64_t n = add2(h, pair(-0x1p23f, -0x1p23f));
+    const uint64_t r = fma2(n, pair(-0x1p-15f, -0x1p-15f), w2);
+    a += word_sum(h) - 2u * 0x4b000000u;
+    b += word_sum(fma2(r, pair(0x1p31f, 0x1p31f), pair(0x1.8p23f, 0x1.8p23f))) - 2u * 0x4b400000u;
+  }
+  __device__ uint64_t total() const { return (uint64_t)low + ((uint64_t)a << 16) + (uint64_t)(int64_t)(int32_t)b; }
+};
+
+// 16 bytes of logits: pairs of them, their maximum, and whether any is at or above a bound.
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int kPairs = 2;
+  using Max = float;
+  struct Bound {
+    float v;
+    __device__ explicit Bound(float x) : v(x) {}
+  };
+  __device__ static Max lowest() { return -INFINITY; }
+  __device__ static Max max_of(const uint4& w, Max m) {
+    return fmaxf(fmaxf(fmaxf(fmaxf(m, __uint_as_float(w.x)), __uint_as_float(w.y)), __uint_as_float(w.z)), __uint_as_float(w.w));
+  }
+  __device__ static float value(Max m) { return m; }
+  __device__ static bool reaches(Max m, const Bound& b) { return m >= b.v; }
+  __device__ static void get(const uint4& w, int i, float& a, float& b) {
+    a = __uint_as_float(i ? w.z : w.x);
+    b = __uint_as_float(i ? w.w : w.y);
+  }
+};
+template <>
+struct Vec<__nv_bfloat16> {
+  static constexpr int kPairs = 4;
+  using Max = __nv_bfloat162;
+  // (a bf16 is >= an fp32 bound exactly if it is >= the bound rounded up to bf16)
+  struct Bound {
+    __nv_bfloat162 v;
+    __device__ explicit Bound(float x) : v(__bfloat162bfloat162(__float2bfloat16_ru(x))) {}
+  };
+  __device__ static __nv_bfloat162 b2(uint32_t u) { return *reinterpret_cast<const __nv_bfloat162*>(&u); }
+  __device__ static Max lowest() { return b2(0xff80ff80u); }
+  __device__ static Max max_of(const uint4& w, Max m) {  // (NaN never wins, as with fmaxf)
+    return __hmax2(__hmax2(__hmax2(b2(w.x), b2(w.y)), __hmax2(b2(w.z), b2(w.w))), m);
+  }
+  __device__ static float value(Max m) {
+    const uint32_t u = *reinterpret_cast<const uint32_t*>(&m);
+    return fmaxf(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  }
+  __device__ static bool reaches(Max m, const Bound& b) { return __hge2_mask(m, b.v) != 0; }
+  __device__ static void get(const uint4& w, int i, float& a, float& b) {
+    const uint32_t u = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    a = __uint_as_float(u << 16);
+    b = __uint_as_float(u & 0xffff0000u);
+  }
+};
+
+// The sum of a share's weights, in whole multiples of 2^-31.
+template <typename T>
+__device__ __forceinline__ uint64_t sum_weights(const uint4* v, int mine, const Side& side, int lane) {
+  using V = Vec<T>;
+  WholeSum sum;
+  const bool open = side.cut == -INFINITY;  // no truncation
+  const typename V::Bound cut(side.cut), big(side.top - 8.001f / side.kexp);  // (below `big` a weight is under 2^-8)
+  const uint64_t top = pair(-side.top, -side.top), kexp = pair(side.kexp, side.kexp);
+  for (int i = lane; i < mine; i += 32) {
+    const uint4 w = v[i];
+    const typename V::Max m = V::max_of(w, V::lowest());
+    if (!open && !V::reaches(m, cut)) continue;
+    const bool small = open && !V::reaches(m, big);
+#pragma unroll
+    for (int e = 0; e < V::kPairs; ++e) {
+      float a, b;
+      V::get(w, e, a, b);
+      unpair(mul2(add2(pair(a, b), top), kexp), a, b);
+      // (2^-200 is 0; NaN and -inf end there too)
+      if (open) {
+        a = fmaxf(a, -200.f);
+        b = fmaxf(b, -200.f);
+      } else {
+        float la, lb;
+        V::get(w, e, la, lb);
+        a = la >= side.cut ? a : -200.f;
+        b = lb >= side.cut ? b : -200.f;
+      }
+      const uint64_t w2 = pair(ex2_approx(a), ex2_approx(b));
+      if (small) sum.small(w2);
+      else sum.any(w2);
+    }
+  }
+  return sum.total();
+}
+
 __device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -140,9 +272,9 @@ __device__ void finish_unit(const VerifyParams& p, int row, int pos, int n, int3
   int last = 0;
   if (lane == 0) {
     res[pos] = result;
-    __threadfence();
-    last = atomicAdd(p.count + row, 1) == n;
-    __threadfence();
+    int32_t old;
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(p.count + row) : "memory");
+    last = old == n;
   }
   if (!__shfl_sync(0xffffffffu, last, 0)) return;
   __syncwarp();
@@ -257,19 +389,12 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
   __syncwarp();
 
   // Pass 1: the maxima (NaN never wins).
-  float tm = -INFINITY, qm = -INFINITY;
-  for (int i = lane; i < mine; i += 32) {
-    const uint4 a = tv[i];
-#pragma unroll
-    for (int e = 0; e < E; ++e) tm = fmaxf(tm, elem<T>(a, e));
-  }
-  if (two) {
-    for (int i = lane; i < mine; i += 32) {
-      const uint4 a = qv[i];
-#pragma unroll
-      for (int e = 0; e < E; ++e) qm = fmaxf(qm, elem<T>(a, e));
-    }
-  }
+  using V = Vec<T>;
+  typename V::Max tmax = V::lowest(), qmax = V::lowest();
+  for (int i = lane; i < mine; i += 32) tmax = V::max_of(tv[i], tmax);
+  if (two)
+    for (int i = lane; i < mine; i += 32) qmax = V::max_of(qv[i], qmax);
+  float tm = V::value(tmax), qm = V::value(qmax);
   tm = warp_max(tm);
   if (two) qm = warp_max(qm);
   cluster_wait();  // every CTA of the cluster has started
@@ -301,6 +426,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
     uint32_t best = 0xffffffffu;
     for (int i = lane; i < mine && best == 0xffffffffu; i += 32) {
       const uint4 a = tv[i];
+      if (V::value(V::max_of(a, V::lowest())) != t.top) continue;
 #pragma unroll
       for (int e = E - 1; e >= 0; --e)
         if (elem<T>(a, e) == t.top) best = (uint32_t)(v0 + i) * E + e;
@@ -323,19 +449,8 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
   t.kexp = q.kexp = fminf(__fdiv_rn(1.4426950408889634f, temp), 3e38f);  // (finite: 0 times it is 0)
   t.cut = __fadd_rn(t.top, sh.theta);
   q.cut = __fadd_rn(q.top, sh.theta);
-  uint64_t ts = 0, qs = 0;
-  for (int i = lane; i < mine; i += 32) {
-    const uint4 a = tv[i];
-#pragma unroll
-    for (int e = 0; e < E; ++e) ts += whole(t.weight(elem<T>(a, e)));
-  }
-  if (two) {
-    for (int i = lane; i < mine; i += 32) {
-      const uint4 a = qv[i];
-#pragma unroll
-      for (int e = 0; e < E; ++e) qs += whole(q.weight(elem<T>(a, e)));
-    }
-  }
+  uint64_t ts = sum_weights<T>(tv, mine, t, lane), qs = 0;
+  if (two) qs = sum_weights<T>(qv, mine, q, lane);
   ts = warp_sum(ts);
   if (two) qs = warp_sum(qs);
   if (lane < (int)csize) {
@@ -367,17 +482,28 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
     }
     // Pass 3: the sums of max(0, p - q); a certain draft takes its own token's p alone.
     if (d_in) {
-      uint64_t rs = 0;
+      WholeSum rest;
+      const typename V::Bound cut(t.cut);
       for (int i = lane; i < mine; i += 32) {
         const uint4 a = tv[i];
+        if (!V::reaches(V::max_of(a, V::lowest()), cut)) continue;  // (p is 0 there)
         const uint4 b = two ? qv[i] : a;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float pe = t.prob(elem<T>(a, e));
-          const float qe = two ? q.prob(elem<T>(b, e)) : (v0 + i) * E + e == d ? 1.f : 0.f;
-          rs += whole(fmaxf(pe - qe, 0.f));
+        for (int e = 0; e < V::kPairs; ++e) {
+          float x, y, u0 = 0.f, u1 = 0.f;
+          V::get(a, e, x, y);
+          if (two) {
+            V::get(b, e, u0, u1);
+            u0 = q.prob(u0);
+            u1 = q.prob(u1);
+          } else {
+            u0 = (v0 + i) * E + 2 * e == d ? 1.f : 0.f;
+            u1 = (v0 + i) * E + 2 * e + 1 == d ? 1.f : 0.f;
+          }
+          rest.any(pair(fmaxf(t.prob(x) - u0, 0.f), fmaxf(t.prob(y) - u1, 0.f)));
         }
       }
+      uint64_t rs = rest.total();
       rs = warp_sum(rs);
       if (lane < (int)csize) push(&sh.sum[2][slot], rs, lane);
       cluster_exchange();
