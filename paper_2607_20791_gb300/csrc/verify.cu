@@ -7,14 +7,21 @@
 // which leaves the emitted tokens distributed as if each were drawn from p.
 //
 // One thread-block cluster of C CTAs handles one position (a "unit": the target's row
-// and, for k < n, the draft's).  Both rows are read from HBM once, into shared memory,
-// each warp's contiguous share by a bulk copy of its own.  Three passes follow, with one
-// exchange over the cluster after each:
-//   1 the two maxima (a greedy row needs the argmax only);
-//   2 the sums of the kept weights, and with them p(d), q(d) and the acceptance;
-//   3 where the draft is rejected, the sums of max(0, p - q).
-// A draw then picks the warp by prefix sums over the cluster and that warp searches its
-// own share.  The last unit of a row to finish joins the row's results.
+// and, for k < n, the draft's), every warp a contiguous share of each row:
+//   1 the two maxima, a stream from HBM (a greedy row then needs the argmax only).  A
+//     lane keeps the maximum of every group of its vectors;
+//   2 the sums of the kept weights, and with them p(d), q(d) and the acceptance.  The rows
+//     were just read and lie in L2, and only vectors whose group reaches the cutoff are
+//     read again: under min-p a few, without truncation all;
+//   3 where the draft is rejected, the sums of max(0, p - q), likewise.
+// Each is joined over the CTA's warps in shared memory and over the cluster by one 8-byte
+// push from every CTA into every CTA.  A draw then picks the CTA and the warp by prefix
+// sums and that warp searches its own share.  The last unit of a row to finish joins the
+// row's results.
+//
+// Rows held in shared memory instead were read from HBM no less, but 152 SMs hold 64 such
+// pairs of rows, each for three exchanges over its cluster: a third of the copy rate with
+// every CTA's memory loaded once, less with two buffers each.
 //
 // Sums are exact in any order, and so is every token, whatever the cluster's size: a
 // weight 2^x <= 1 is rounded once to a whole number of 2^-31 and summed in 64 bits.  The
@@ -33,10 +40,9 @@ namespace rgd {
 namespace {
 
 constexpr int kVerifyWarps = 8;
-constexpr int kVerifyThreads = kVerifyWarps * 32;
+constexpr int kVerifyThreads = (kVerifyWarps + 1) * 32;  // (the last warp looks after the parameters)
+constexpr int kGroups = kVerifyWarps;  // groups of a warp's vectors, and loads in flight per lane
 constexpr int kVerifyCluster = 16;                           // CTAs of a unit at most
-constexpr int kSlots = kVerifyCluster * kVerifyWarps;        // warps of a unit at most
-constexpr int kVerifySmem = 220 * 1024;                      // rows' bytes in one CTA at most
 constexpr int32_t kTaken = -1, kRejectedRow = -2;            // results of a unit other than a token
 
 struct VerifyParams {
@@ -44,8 +50,7 @@ struct VerifyParams {
   const uint8_t* draft;  // NULL: every draft was certain
   int64_t target_stride, draft_stride;  // bytes
   int32_t rows, max_draft, vocab;
-  int32_t wvec;  // 16-byte vectors of a row per warp (a multiple of 32)
-  int32_t copy_target, copy_draft;  // the rows start on 16 bytes: bulk copies
+  int32_t depth;  // stripes of 32 vectors in a group: a warp's share is kGroups depth stripes
   const int32_t* tokens;
   const int32_t* n_draft;
   const uint8_t* is_probe;
@@ -63,10 +68,11 @@ struct VerifyParams {
 };
 
 struct VerifyShared {
-  uint64_t sum[3][kSlots];   // pushed by every warp of the cluster: target's and draft's weights, the rest
-  float top[2][kSlots];      // ... and the maxima
-  uint64_t copied[kVerifyWarps];
-  float theta;
+  // of this CTA's warps, and pushed by every CTA of the cluster into every other
+  float warp_top[2][kVerifyWarps], top[2][kVerifyCluster];
+  uint64_t warp_sum[3][kVerifyWarps], sum[3][kVerifyCluster];  // target's and draft's weights, max(0, p - q)
+  uint64_t group_sum[kVerifyWarps];  // of the groups of the share that a draw falls into
+  float theta, tl, ql;  // T ln p_min, the drafted token's logits
 };
 
 // Element i of a 16-byte vector.
@@ -81,12 +87,6 @@ __device__ __forceinline__ float elem<__nv_bfloat16>(const uint4& w, int i) {
   const uint32_t u = (i >> 1) == 0 ? w.x : (i >> 1) == 1 ? w.y : (i >> 1) == 2 ? w.z : w.w;
   return __uint_as_float((i & 1) ? (u & 0xffff0000u) : (u << 16));
 }
-template <typename T>
-__device__ __forceinline__ T neg_inf();
-template <>
-__device__ __forceinline__ float neg_inf<float>() { return -INFINITY; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 neg_inf<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80u); }
 template <typename T>
 __device__ __forceinline__ float one_logit(const uint8_t* row, int32_t i) {
   return (float)reinterpret_cast<const T*>(row)[i];
@@ -133,17 +133,17 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
 }
 __device__ __forceinline__ uint32_t word_sum(uint64_t v) { return (uint32_t)v + (uint32_t)(v >> 32); }
 
-// A lane's sum of whole(w), exact for up to 512 numbers.  Small ones (w <= 2^-8) are added
-// as the bits of w 2^31 + 2^23.  Others go in two halves, w = a 2^-15 + r with a the
-// nearest whole number, and w 2^31 = a 2^16 + r 2^31, both again read off the bits of a sum
-// (2^23, and 1.5 2^23 for r's sign).  Conversions to integers would take the special
+// A lane's sum of whole(w), exact for up to 512 numbers.  Those of a vector below 2^-8 are
+// added as the bits of w 2^31 + 2^23.  Others go in two halves, w = a 2^-15 + r with a
+// the nearest whole number, and w 2^31 = a 2^16 + r 2^31, both again read off the bits of a
+// sum (2^23, and 1.5 2^23 for r's sign).  Conversions to integers would take the special
 // function unit's time, which the exponentials need.
 struct WholeSum {
   uint32_t low = 0, a = 0, b = 0;
   __device__ void small(uint64_t w2) {
     low += word_sum(fma2(w2, pair(0x1p31f, 0x1p31f), pair(0x1p23f, 0x1p23f))) - 2u * 0x4b000000u;
   }
-  __device__ void any(uint64_t w2) {
+  __device__ void add(uint64_t w2) {
     const uint64_t h = fma2(w2, pair(0x1p15f, 0x1p15f), pair(0x1p23f, 0x1p23f));
     const uint64_t n = add2(h, pair(-0x1p23f, -0x1p23f));
     const uint64_t r = fma2(n, pair(-0x1p-15f, -0x1p-15f), w2);
@@ -165,6 +165,7 @@ struct Vec<float> {
     __device__ explicit Bound(float x) : v(x) {}
   };
   __device__ static Max lowest() { return -INFINITY; }
+  __device__ static uint4 nothing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
   __device__ static Max max_of(const uint4& w, Max m) {
     return fmaxf(fmaxf(fmaxf(fmaxf(m, __uint_as_float(w.x)), __uint_as_float(w.y)), __uint_as_float(w.z)), __uint_as_float(w.w));
   }
@@ -186,6 +187,7 @@ struct Vec<__nv_bfloat16> {
   };
   __device__ static __nv_bfloat162 b2(uint32_t u) { return *reinterpret_cast<const __nv_bfloat162*>(&u); }
   __device__ static Max lowest() { return b2(0xff80ff80u); }
+  __device__ static uint4 nothing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
   __device__ static Max max_of(const uint4& w, Max m) {  // (NaN never wins, as with fmaxf)
     return __hmax2(__hmax2(__hmax2(b2(w.x), b2(w.y)), __hmax2(b2(w.z), b2(w.w))), m);
   }
@@ -201,46 +203,10 @@ struct Vec<__nv_bfloat16> {
   }
 };
 
-// The sum of a share's weights, in whole multiples of 2^-31.
-template <typename T>
-__device__ __forceinline__ uint64_t sum_weights(const uint4* v, int mine, const Side& side, int lane) {
-  using V = Vec<T>;
-  WholeSum sum;
-  const bool open = side.cut == -INFINITY;  // no truncation
-  const typename V::Bound cut(side.cut), big(side.top - 8.001f / side.kexp);  // (below `big` a weight is under 2^-8)
-  const uint64_t top = pair(-side.top, -side.top), kexp = pair(side.kexp, side.kexp);
-  for (int i = lane; i < mine; i += 32) {
-    const uint4 w = v[i];
-    const typename V::Max m = V::max_of(w, V::lowest());
-    if (!open && !V::reaches(m, cut)) continue;
-    const bool small = open && !V::reaches(m, big);
-#pragma unroll
-    for (int e = 0; e < V::kPairs; ++e) {
-      float a, b;
-      V::get(w, e, a, b);
-      unpair(mul2(add2(pair(a, b), top), kexp), a, b);
-      // (2^-200 is 0; NaN and -inf end there too)
-      if (open) {
-        a = fmaxf(a, -200.f);
-        b = fmaxf(b, -200.f);
-      } else {
-        float la, lb;
-        V::get(w, e, la, lb);
-        a = la >= side.cut ? a : -200.f;
-        b = lb >= side.cut ? b : -200.f;
-      }
-      const uint64_t w2 = pair(ex2_approx(a), ex2_approx(b));
-      if (small) sum.small(w2);
-      else sum.any(w2);
-    }
-  }
-  return sum.total();
-}
-
+// Sum over the warp of numbers below 2^54, in two halves.
 __device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
+  const uint32_t low = __reduce_add_sync(0xffffffffu, (uint32_t)v & 0x7ffffffu);
+  return low + ((uint64_t)__reduce_add_sync(0xffffffffu, (uint32_t)(v >> 27)) << 27);
 }
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
@@ -248,25 +214,167 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
+// A warp's share of a row in global memory, as vectors of E elements from its first on: those
+// read whole, and the last one element by element where the row does not end with it (or
+// does not start on 16 bytes: then every vector comes as the 4-byte words it lies in, and
+// a whole one's last word may reach past the row).
+template <typename T, bool kAligned>
+struct Share {
+  static constexpr int E = 16 / (int)sizeof(T);
+  const uint8_t* at;
+  int32_t n, whole;
+  __device__ Share(const uint8_t* row, int64_t e0, int64_t count) {
+    n = (int32_t)max(int64_t(0), count);
+    at = n ? row + e0 * (int64_t)sizeof(T) : row;
+    whole = kAligned ? n / E : n ? (n - 1) / E : 0;
+  }
+  __device__ uint4 get(int i) const {
+    const uint8_t* p = at + (int64_t)i * 16;
+    if (kAligned) return __ldg(reinterpret_cast<const uint4*>(p));
+    uint32_t u[5];
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 3);
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(p - off);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = __ldg(w + k);
+    u[4] = E == 8 && off ? __ldg(w + 4) : 0;  // (only where it holds an element of the vector)
+    if (E == 4) return make_uint4(u[0], u[1], u[2], u[3]);
+    return make_uint4(__funnelshift_r(u[0], u[1], 8 * off), __funnelshift_r(u[1], u[2], 8 * off),
+                      __funnelshift_r(u[2], u[3], 8 * off), __funnelshift_r(u[3], u[4], 8 * off));
+  }
+  // The last vector, in the lane whose turn it is; elements past the row's end read as -inf.
+  __device__ uint4 rest(int lane) const {
+    uint4 w = Vec<T>::nothing();
+    if (n == whole * E || (whole & 31) != lane) return w;
+    uint32_t* u = &w.x;
+#pragma unroll
+    for (int k = 0; k < E; ++k) {
+      if (whole * E + k >= n) continue;
+      const uint8_t* p = at + (int64_t)(whole * E + k) * (int)sizeof(T);
+      if (E == 4) u[k] = __ldg(reinterpret_cast<const uint32_t*>(p));
+      else u[k >> 1] = __byte_perm(u[k >> 1], __ldg(reinterpret_cast<const uint16_t*>(p)), (k & 1) ? 0x5410 : 0x3254);
+    }
+    return w;
+  }
+};
+
+// What a lane keeps of its part of a share: the maxima of its groups (group g: its
+// vectors of stripes g depth .. of the share) and the last vector.
+template <typename T>
+struct Kept {
+  typename Vec<T>::Max group[kGroups];
+  uint4 rest;
+};
+
+template <typename T, bool kAligned>
+__device__ __forceinline__ float find_maxima(const Share<T, kAligned>& v, Kept<T>& kept, int depth, int lane) {
+  using V = Vec<T>;
+  kept.rest = v.rest(lane);
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) kept.group[g] = V::lowest();
+#pragma unroll 1
+  for (int s = 0; s < depth; ++s) {
+    uint4 w[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int i = (g * depth + s) * 32 + lane;
+      w[g] = V::nothing();
+      if (i < v.whole) w[g] = v.get(i);
+    }
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) kept.group[g] = V::max_of(w[g], kept.group[g]);
+  }
+  float m = V::value(V::max_of(kept.rest, V::lowest()));
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) m = fmaxf(m, V::value(kept.group[g]));
+  return warp_max(m);
+}
+
+// Walks a lane's vectors of the groups in `mask`; next() gives -1 after the last.
+struct Walk {
+  uint32_t mask;
+  int depth, whole, lane, s;
+  __device__ Walk(uint32_t mask, int depth, int whole, int lane) : mask(mask), depth(depth), whole(whole), lane(lane), s(0) {}
+  __device__ int next() {
+    if (!mask) return -1;
+    const int i = ((__ffs(mask) - 1) * depth + s) * 32 + lane;
+    if (++s == depth) {
+      s = 0;
+      mask &= mask - 1;
+    }
+    if (i < whole) return i;
+    mask = 0;  // (everything further is past the end too)
+    return -1;
+  }
+};
+
+// The groups whose maximum reaches a bound.
+template <typename T>
+__device__ __forceinline__ uint32_t groups_reaching(const Kept<T>& kept, float bound) {
+  using V = Vec<T>;
+  const typename V::Bound b(bound);
+  uint32_t mask = 0;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) mask |= V::reaches(kept.group[g], b) ? 1u << g : 0u;
+  return mask;
+}
+
+// The weights of a vector, added to a sum (NaN and -inf have none).  kOpen: no truncation.
+template <typename T, bool kOpen>
+__device__ __forceinline__ void add_weights(const uint4& w, const Side& side, const typename Vec<T>::Bound& big, WholeSum& sum) {
+  using V = Vec<T>;
+  const uint64_t top = pair(-side.top, -side.top), kexp = pair(side.kexp, side.kexp);
+  uint64_t w2[V::kPairs];
+#pragma unroll
+  for (int e = 0; e < V::kPairs; ++e) {
+    float a, b, x, y;
+    V::get(w, e, a, b);
+    unpair(mul2(add2(pair(a, b), top), kexp), x, y);
+    x = kOpen ? fmaxf(x, -200.f) : a >= side.cut ? x : -200.f;  // (2^-200 is 0)
+    y = kOpen ? fmaxf(y, -200.f) : b >= side.cut ? y : -200.f;
+    w2[e] = pair(ex2_approx(x), ex2_approx(y));
+  }
+  if (kOpen && !V::reaches(V::max_of(w, V::lowest()), big)) {
+#pragma unroll
+    for (int e = 0; e < V::kPairs; ++e) sum.small(w2[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V::kPairs; ++e) sum.add(w2[e]);
+  }
+}
+
+// The sum of a warp's weights, in whole multiples of 2^-31.
+template <typename T, bool kOpen, bool kAligned>
+__device__ __forceinline__ uint64_t sum_weights(const Share<T, kAligned>& v, const Kept<T>& kept, const Side& side, int depth,
+                                                int lane) {
+  using V = Vec<T>;
+  const typename V::Bound big(side.top - 8.001f / side.kexp);  // (below it a weight is under 2^-8)
+  WholeSum sum;
+  Walk walk(kOpen ? (1u << kGroups) - 1 : groups_reaching(kept, side.cut), depth, v.whole, lane);
+  uint4 w = kept.rest, w1 = V::nothing(), w2 = w1;
+  int i1 = walk.next(), i2 = walk.next();
+  if (i1 >= 0) w1 = v.get(i1);
+  if (i2 >= 0) w2 = v.get(i2);
+#pragma unroll 1
+  for (;;) {  // (two vectors are on their way while one is worked on)
+    const int i3 = walk.next();
+    uint4 w3 = V::nothing();
+    if (i3 >= 0) w3 = v.get(i3);
+    add_weights<T, kOpen>(w, side, big, sum);
+    if (i1 < 0) break;
+    w = w1, w1 = w2, w2 = w3;
+    i1 = i2, i2 = i3;
+  }
+  return warp_sum(sum.total());
+}
+
 __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ void push(const uint64_t* slot, uint64_t v, uint32_t rank) {
-  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(peer_addr(smem_u32(slot), rank)), "l"(v) : "memory");
-}
-__device__ __forceinline__ void push(const float* slot, float v, uint32_t rank) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(smem_u32(slot), rank)), "f"(v) : "memory");
-}
-// What was pushed before is seen by every CTA of the cluster after it.
-__device__ __forceinline__ void cluster_exchange() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 
 // The whole warp: a row's finished unit is counted, and the last one to finish writes the row.
-__device__ void finish_unit(const VerifyParams& p, int row, int pos, int n, int32_t result) {
+__device__ __noinline__ void finish_unit(const VerifyParams& p, int row, int pos, int n, int32_t result) {
   const int lane = threadIdx.x & 31;
   int32_t* res = p.result + (int64_t)row * (p.max_draft + 1);
   int last = 0;
@@ -300,28 +408,22 @@ __device__ void finish_unit(const VerifyParams& p, int row, int pos, int n, int3
   }
 }
 
-// One warp's share of one row into shared memory; elements past the row's end read as
-// -inf.  Bulk copies where the row starts on 16 bytes.
-template <typename T>
-__device__ __forceinline__ uint32_t fetch_share(uint4* dst, const uint8_t* row, int32_t vocab, int32_t v0, int32_t wvec,
-                                                bool bulk, uint64_t* bar, int lane) {
-  constexpr int E = 16 / (int)sizeof(T);
-  const int32_t e0 = v0 * E;                                   // first element
-  const int32_t ne = min(max(vocab - e0, 0), wvec * E);        // elements of the row here
-  const int32_t nv = bulk ? ne / E : 0;
-  if (lane == 0 && nv) bulk_load(dst, row + (int64_t)e0 * sizeof(T), (uint32_t)nv * 16, bar);
-  T* d = reinterpret_cast<T*>(dst);
-  const T* s = reinterpret_cast<const T*>(row) + e0;
-  const int32_t end = (ne + E - 1) / E * E;  // whole vectors
-#pragma unroll 8
-  for (int32_t i = nv * E + lane; i < end; i += 32) d[i] = i < ne ? s[i] : neg_inf<T>();
-  return (uint32_t)nv * 16;
+// What the CTAs pushed before is seen by the whole cluster after it.
+__device__ __forceinline__ void cluster_exchange() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void push(const uint64_t* slot, uint64_t v, uint32_t rank) {
+  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(peer_addr(smem_u32(slot), rank)), "l"(v) : "memory");
+}
+__device__ __forceinline__ void push(const float* slot, float v, uint32_t rank) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(smem_u32(slot), rank)), "f"(v) : "memory");
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyParams p) {
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyParams p) {
   constexpr int E = 16 / (int)sizeof(T);
-  extern __shared__ __align__(16) uint8_t dyn[];
+  using V = Vec<T>;
   __shared__ VerifyShared sh;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t rank, csize, unit;
@@ -333,15 +435,14 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
   asm volatile("griddepcontrol.wait;" ::: "memory");
   // The row's parameters; every thread of the cluster takes the same decisions.
   const bool active = !p.row_active || p.row_active[row];
-  const float temp = p.temperature[row], min_p = p.min_p[row];
+  const float temp = p.temperature[row], min_p = p.min_p[row], draw_u = p.draw_u[row];
   const bool greedy = (p.is_probe && p.is_probe[row]) || temp == 0.f;
   const int n = p.n_draft ? p.n_draft[row] : K;
-  const float draw_u = p.draw_u[row];
   bool good = n >= 0 && n <= K;
   if (!greedy) good = good && temp > 0.f && temp < INFINITY && min_p >= 0.f && min_p <= 1.f && draw_u >= 0.f && draw_u < 1.f;
-  const bool leader = rank == 0 && warp == 0;
-  const bool has_draft = good && pos < n;
-  if (leader && lane == 0 && pos < K && p.accept_prob && !(active && has_draft)) p.accept_prob[(int64_t)row * K + pos] = 0.f;
+  const bool leader = rank == 0 && warp == 0, has_draft = active && good && pos < n;
+  float* prob = pos < K && p.accept_prob ? p.accept_prob + (int64_t)row * K + pos : nullptr;
+  if (leader && lane == 0 && prob && !has_draft) *prob = 0.f;
   if (!active || !good) {
     if (leader && pos == 0) {
       for (int i = lane; i <= K; i += 32) p.token_out[(int64_t)row * (K + 1) + i] = -1;
@@ -353,69 +454,51 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
     return;
   }
   if (pos > n) return;
+  cluster_arrive_relaxed();
   const int32_t d = has_draft ? p.tokens[(int64_t)row * K + pos] : -1;
   const bool d_in = d >= 0 && d < p.vocab;  // (a draft outside the vocabulary is rejected, q = 0 everywhere)
   const float u = has_draft && !greedy ? p.accept_u[(int64_t)row * K + pos] : 0.f;
   const bool two = p.draft != nullptr && has_draft && !greedy;
-  const uint8_t* trow = p.target + ((int64_t)row * (K + 1) + pos) * p.target_stride;
-  const uint8_t* qrow = two ? p.draft + ((int64_t)row * K + pos) * p.draft_stride : nullptr;
+  const int64_t trow = ((int64_t)row * (K + 1) + pos) * p.target_stride, qrow = ((int64_t)row * K + pos) * p.draft_stride;
 
-  // This warp's share, and its place among the cluster's warps (in index order).
-  const int slot = (int)rank * kVerifyWarps + warp, slots = (int)csize * kVerifyWarps;
-  const int32_t v0 = slot * p.wvec;
-  const int32_t mine = min(max((p.vocab + E - 1) / E - v0, 0), p.wvec);  // its vectors
-  uint4* tv = reinterpret_cast<uint4*>(dyn) + (int64_t)warp * p.wvec;
-  uint4* qv = reinterpret_cast<uint4*>(dyn) + (int64_t)(kVerifyWarps + warp) * p.wvec;
-  uint64_t* bar = &sh.copied[warp];
-  if (lane == 0) {
-    mbar_init(bar, 1);
-    fence_mbar_init();
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  }
-  __syncwarp();
-  cluster_arrive_relaxed();
-  uint32_t bytes = fetch_share<T>(tv, trow, p.vocab, v0, p.wvec, p.copy_target, bar, lane);
-  if (two) bytes += fetch_share<T>(qv, qrow, p.vocab, v0, p.wvec, p.copy_draft, bar, lane);
-  if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
-  const float td = d_in && !greedy ? one_logit<T>(trow, d) : 0.f;
-  const float qd = d_in && two ? one_logit<T>(qrow, d) : 0.f;
-  if (threadIdx.x == 0) sh.theta = (float)((double)temp * log((double)min_p));
-  __syncwarp();
-  bool copied = mbar_wait(bar, 0);
-  if (!copied) {
-    if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
-    copied = mbar_wait(bar, 0);  // (the copy in flight, before this block may end)
-  }
-  __syncwarp();
+  // This warp's share (none for the last warp), in the order of the elements over the cluster.
+  const bool worker = warp < kVerifyWarps;
+  const int64_t share = (int64_t)kGroups * p.depth * 32 * E;
+  const int64_t e0 = ((int64_t)rank * kVerifyWarps + warp) * share;
+  const int64_t count = worker ? min(share, p.vocab - e0) : 0;
+  const Share<T, kAligned> tv(p.target + trow, e0, count);
+  const Share<T, kAligned> qv(two ? p.draft + qrow : p.target + trow, e0, two ? count : 0);
 
   // Pass 1: the maxima (NaN never wins).
-  using V = Vec<T>;
-  typename V::Max tmax = V::lowest(), qmax = V::lowest();
-  for (int i = lane; i < mine; i += 32) tmax = V::max_of(tv[i], tmax);
-  if (two)
-    for (int i = lane; i < mine; i += 32) qmax = V::max_of(qv[i], qmax);
-  float tm = V::value(tmax), qm = V::value(qmax);
-  tm = warp_max(tm);
-  if (two) qm = warp_max(qm);
+  if (!worker && lane == 0) {
+    sh.tl = d_in && !greedy ? one_logit<T>(p.target + trow, d) : 0.f;
+    sh.ql = d_in && two ? one_logit<T>(p.draft + qrow, d) : 0.f;
+    sh.theta = (float)((double)temp * log((double)min_p));
+  }
+  Kept<T> tkept, qkept;
+  {
+    const float tm = find_maxima(tv, tkept, p.depth, lane);
+    const float qm = find_maxima(qv, qkept, two ? p.depth : 0, lane);
+    if (worker && lane == 0) {
+      sh.warp_top[0][warp] = tm;
+      sh.warp_top[1][warp] = qm;
+    }
+  }
+  __syncthreads();
   cluster_wait();  // every CTA of the cluster has started
-  if (lane < (int)csize) {
-    push(&sh.top[0][slot], tm, lane);
-    if (two) push(&sh.top[1][slot], qm, lane);
+  if (warp < 2) {
+    const float m = warp_max(sh.warp_top[warp][lane % kVerifyWarps]);
+    if (lane < (int)csize) push(&sh.top[warp][rank], m, lane);
   }
   cluster_exchange();
   Side t, q;
-  t.top = q.top = -INFINITY;
-  for (int i = lane; i < slots; i += 32) {
-    t.top = fmaxf(t.top, sh.top[0][i]);
-    if (two) q.top = fmaxf(q.top, sh.top[1][i]);
-  }
-  t.top = warp_max(t.top);
-  if (two) q.top = warp_max(q.top);
-  const bool finite = fabsf(t.top) < INFINITY && (!two || fabsf(q.top) < INFINITY) && (!has_draft || greedy || (u >= 0.f && u < 1.f));
-  if (!finite) {
+  t.top = warp_max(sh.top[0][lane % csize]);
+  q.top = warp_max(sh.top[1][lane % csize]);
+  if (!two) q.top = 0.f;
+  if (!(fabsf(t.top) < INFINITY && fabsf(q.top) < INFINITY && u >= 0.f && u < 1.f)) {
     if (leader) {
       if (lane == 0 && p.dev_status) atomicOr(p.dev_status, RGD_DEV_BAD_PARAM);
-      if (lane == 0 && has_draft && p.accept_prob) p.accept_prob[(int64_t)row * K + pos] = 0.f;
+      if (lane == 0 && prob) *prob = 0.f;
       finish_unit(p, row, pos, n, kRejectedRow);
     }
     return;
@@ -424,58 +507,67 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
 
   if (greedy) {  // the lowest index of the largest logit
     uint32_t best = 0xffffffffu;
-    for (int i = lane; i < mine && best == 0xffffffffu; i += 32) {
-      const uint4 a = tv[i];
-      if (V::value(V::max_of(a, V::lowest())) != t.top) continue;
+    auto look = [&](const uint4& w, int i) {
 #pragma unroll
       for (int e = E - 1; e >= 0; --e)
-        if (elem<T>(a, e) == t.top) best = (uint32_t)(v0 + i) * E + e;
-    }
+        if (elem<T>(w, e) == t.top) best = min(best, (uint32_t)e0 + i * E + e);
+    };
+    Walk walk(groups_reaching(tkept, t.top), p.depth, tv.whole, lane);
+#pragma unroll 1
+    for (int i = walk.next(); i >= 0; i = walk.next()) look(tv.get(i), i);
+    look(tkept.rest, tv.whole);
     best = __reduce_min_sync(0xffffffffu, best);
-    if (lane == 0) push(&sh.sum[0][slot], best, 0);
+    if (worker && lane == 0) sh.warp_sum[0][warp] = best;
+    __syncthreads();
+    if (warp == 0) {
+      best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.warp_sum[0][lane % kVerifyWarps]);
+      if (lane == 0) push(&sh.sum[0][rank], best, 0);
+    }
     cluster_exchange();
     if (leader) {
-      uint32_t b = 0xffffffffu;
-      for (int i = lane; i < slots; i += 32) b = min(b, (uint32_t)sh.sum[0][i]);
-      b = __reduce_min_sync(0xffffffffu, b);
-      const bool same = has_draft && (int32_t)b == d;
-      if (lane == 0 && has_draft && p.accept_prob) p.accept_prob[(int64_t)row * K + pos] = same ? 1.f : 0.f;
-      finish_unit(p, row, pos, n, same ? kTaken : (int32_t)b);
+      best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.sum[0][lane % csize]);
+      const bool same = has_draft && (int32_t)best == d;
+      if (lane == 0 && prob && has_draft) *prob = same ? 1.f : 0.f;
+      finish_unit(p, row, pos, n, same ? kTaken : (int32_t)best);
     }
     return;
   }
+
+  // A sum of every warp over the cluster: by warp for the CTA's own, by CTA for all.
+  auto join = [&](int which, uint64_t mine) {
+    if (worker && lane == 0) sh.warp_sum[which][warp] = mine;
+  };
+  auto exchange = [&](int first, int last) {
+    __syncthreads();
+    if (warp >= first && warp <= last) {
+      const uint64_t v = warp_sum(lane < kVerifyWarps ? sh.warp_sum[warp][lane] : 0);
+      if (lane < (int)csize) push(&sh.sum[warp][rank], v, lane);
+    }
+    cluster_exchange();
+  };
+  auto over_cluster = [&](int which) { return warp_sum(lane < (int)csize ? sh.sum[which][lane] : 0); };
 
   // Pass 2: the sums of the weights.
   t.kexp = q.kexp = fminf(__fdiv_rn(1.4426950408889634f, temp), 3e38f);  // (finite: 0 times it is 0)
   t.cut = __fadd_rn(t.top, sh.theta);
   q.cut = __fadd_rn(q.top, sh.theta);
-  uint64_t ts = sum_weights<T>(tv, mine, t, lane), qs = 0;
-  if (two) qs = sum_weights<T>(qv, mine, q, lane);
-  ts = warp_sum(ts);
-  if (two) qs = warp_sum(qs);
-  if (lane < (int)csize) {
-    push(&sh.sum[0][slot], ts, lane);
-    if (two) push(&sh.sum[1][slot], qs, lane);
+  if (sh.theta == -INFINITY) {
+    join(0, sum_weights<T, true>(tv, tkept, t, p.depth, lane));
+    if (two) join(1, sum_weights<T, true>(qv, qkept, q, p.depth, lane));
+  } else {
+    join(0, sum_weights<T, false>(tv, tkept, t, p.depth, lane));
+    if (two) join(1, sum_weights<T, false>(qv, qkept, q, p.depth, lane));
   }
-  cluster_exchange();
-  uint64_t tz = 0, qz = 0;
-  for (int i = lane; i < slots; i += 32) {
-    tz += sh.sum[0][i];
-    if (two) qz += sh.sum[1][i];
-  }
-  tz = warp_sum(tz);
-  t.inv = __fdiv_rn(1.f, __ull2float_rn(tz) * 0x1p-31f);
-  if (two) {
-    qz = warp_sum(qz);
-    q.inv = __fdiv_rn(1.f, __ull2float_rn(qz) * 0x1p-31f);
-  }
+  exchange(0, two ? 1 : 0);
+  uint64_t total = over_cluster(0);
+  t.inv = __fdiv_rn(1.f, __ull2float_rn(total) * 0x1p-31f);
+  if (two) q.inv = __fdiv_rn(1.f, __ull2float_rn(over_cluster(1)) * 0x1p-31f);
   int which = 0;  // the sums that the draw goes by: the target's weights, or the rest
   if (has_draft) {
-    const float pd = d_in ? t.prob(td) : 0.f;
-    const float qp = !d_in ? 0.f : two ? q.prob(qd) : 1.f;
+    const float pd = d_in ? t.prob(sh.tl) : 0.f;
+    const float qp = !d_in ? 0.f : two ? q.prob(sh.ql) : 1.f;
     const bool taken = d_in && __fmul_rn(u, qp) < pd;
-    if (leader && lane == 0 && p.accept_prob)
-      p.accept_prob[(int64_t)row * K + pos] = qp > 0.f ? fminf(__fdiv_rn(pd, qp), 1.f) : pd > 0.f ? 1.f : 0.f;
+    if (leader && lane == 0 && prob) *prob = qp > 0.f ? fminf(__fdiv_rn(pd, qp), 1.f) : pd > 0.f ? 1.f : 0.f;
     if (taken) {
       if (leader) finish_unit(p, row, pos, n, kTaken);
       return;
@@ -483,112 +575,138 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(const VerifyPara
     // Pass 3: the sums of max(0, p - q); a certain draft takes its own token's p alone.
     if (d_in) {
       WholeSum rest;
-      const typename V::Bound cut(t.cut);
-      for (int i = lane; i < mine; i += 32) {
-        const uint4 a = tv[i];
-        if (!V::reaches(V::max_of(a, V::lowest()), cut)) continue;  // (p is 0 there)
-        const uint4 b = two ? qv[i] : a;
+      auto add = [&](const uint4& a, const uint4& c, int i) {
 #pragma unroll
         for (int e = 0; e < V::kPairs; ++e) {
-          float x, y, u0 = 0.f, u1 = 0.f;
+          float x, y, q0, q1;
           V::get(a, e, x, y);
-          if (two) {
-            V::get(b, e, u0, u1);
-            u0 = q.prob(u0);
-            u1 = q.prob(u1);
-          } else {
-            u0 = (v0 + i) * E + 2 * e == d ? 1.f : 0.f;
-            u1 = (v0 + i) * E + 2 * e + 1 == d ? 1.f : 0.f;
-          }
-          rest.any(pair(fmaxf(t.prob(x) - u0, 0.f), fmaxf(t.prob(y) - u1, 0.f)));
+          V::get(c, e, q0, q1);
+          const int32_t at = (int32_t)e0 + i * E + 2 * e;
+          q0 = two ? q.prob(q0) : at == d ? 1.f : 0.f;
+          q1 = two ? q.prob(q1) : at + 1 == d ? 1.f : 0.f;
+          rest.add(pair(fmaxf(t.prob(x) - q0, 0.f), fmaxf(t.prob(y) - q1, 0.f)));
         }
+      };
+      Walk walk(groups_reaching(tkept, t.cut), p.depth, tv.whole, lane);  // (p is 0 elsewhere)
+      uint4 a = tkept.rest, c = two ? qkept.rest : a;
+      int i = tv.whole, ahead = walk.next();
+#pragma unroll 1
+      for (;;) {
+        uint4 a1 = V::nothing(), c1 = a1;
+        if (ahead >= 0) {
+          a1 = tv.get(ahead);
+          if (two) c1 = qv.get(ahead);
+        }
+        add(a, c, i);
+        if (ahead < 0) break;
+        i = ahead;
+        ahead = walk.next();
+        a = a1, c = c1;
       }
-      uint64_t rs = rest.total();
-      rs = warp_sum(rs);
-      if (lane < (int)csize) push(&sh.sum[2][slot], rs, lane);
-      cluster_exchange();
-      uint64_t rz = 0;
-      for (int i = lane; i < slots; i += 32) rz += sh.sum[2][i];
-      if (warp_sum(rz) > 0) which = 2;  // (p and q may be equal but for rounding: then p itself)
+      join(2, warp_sum(rest.total()));
+      exchange(2, 2);
+      const uint64_t rz = over_cluster(2);
+      if (rz > 0) {  // (p and q may be equal but for rounding: then p itself)
+        which = 2;
+        total = rz;
+      }
     }
   }
 
-  // The draw: the warp whose share holds the mark, by prefix sums over the cluster's warps.
-  uint64_t total = 0, before = 0;
-  for (int i = lane; i < slots; i += 32) {
-    total += sh.sum[which][i];
-    before += i < slot ? sh.sum[which][i] : 0;
-  }
-  total = warp_sum(total);
-  before = warp_sum(before);
+  // The draw: the CTA, then the share, that holds the mark; every warp of the CTA takes one
+  // group of that share, and the one whose group holds the mark finds the element.
   const uint64_t mark = (uint64_t)((double)draw_u * (double)total);
-  const uint64_t here = sh.sum[which][slot];
-  if (!(before <= mark && mark < before + here)) return;
-  for (int base = 0; base < mine; base += 32) {
-    const int i = base + lane;
-    uint32_t w[E];
-    uint64_t s = 0;
-    const uint4 a = i < mine ? tv[i] : make_uint4(0, 0, 0, 0);
-    const uint4 b = two && i < mine ? qv[i] : a;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float x = t.weight(elem<T>(a, e));
-      if (which == 2) {
-        const float qe = two ? q.prob(elem<T>(b, e)) : (v0 + i) * E + e == d ? 1.f : 0.f;
-        x = fmaxf(__fmul_rn(x, t.inv) - qe, 0.f);
+  uint64_t before = warp_sum(lane < (int)rank ? sh.sum[which][lane] : 0);
+  if (!(before <= mark && mark < before + sh.sum[which][rank])) return;
+  int owner = 0;
+  for (; owner + 1 < kVerifyWarps && before + sh.warp_sum[which][owner] <= mark; ++owner) before += sh.warp_sum[which][owner];
+  const int64_t o0 = ((int64_t)rank * kVerifyWarps + owner) * share, left = min(share, p.vocab - o0);
+  const Share<T, kAligned> ot(p.target + trow, o0, left), oq(two ? p.draft + qrow : p.target + trow, o0, two ? left : 0);
+  uint64_t group = 0;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {  // the groups' sums, then the element
+#pragma unroll 1
+    for (int s = 0; s < (worker ? p.depth : 0); ++s) {
+      const int i = (warp * p.depth + s) * 32 + lane;
+      uint4 a = V::nothing(), c = a;
+      if (i < ot.whole) {
+        a = ot.get(i);
+        if (two) c = oq.get(i);
+      } else if (i == ot.whole) {
+        a = ot.rest(lane);
+        if (two) c = oq.rest(lane);
       }
-      w[e] = i < mine ? whole(x) : 0u;
-      s += w[e];
-    }
-    uint64_t incl = s;
+      uint32_t w[E];
+      uint64_t sum = 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint64_t v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += v;
-    }
-    const uint32_t hit = __ballot_sync(0xffffffffu, before + incl > mark);
-    if (hit) {
-      const int at = __ffs(hit) - 1;
-      uint64_t c = before + incl - s;
-      int32_t token = 0;
-#pragma unroll
-      for (int e = E - 1; e >= 0; --e) {
-        uint64_t upto = c;
-#pragma unroll
-        for (int f = 0; f <= e; ++f) upto += w[f];
-        if (upto > mark) token = (v0 + i) * E + e;
+      for (int e = 0; e < E; ++e) {
+        float x = t.weight(elem<T>(a, e));
+        if (which == 2) {
+          const float qe = two ? q.prob(elem<T>(c, e)) : o0 + i * E + e == d ? 1.f : 0.f;
+          x = fmaxf(__fmul_rn(x, t.inv) - qe, 0.f);
+        }
+        w[e] = whole(x);
+        sum += w[e];
       }
-      finish_unit(p, row, pos, n, __shfl_sync(0xffffffffu, token, at));
-      return;
+      const uint64_t stripe = warp_sum(sum);
+      if (pass == 0) {
+        group += stripe;
+      } else if (mark < before + stripe) {
+        uint64_t upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+          if (lane >= o) upto += v;
+        }
+        upto += before;
+        const int at = __ffs(__ballot_sync(0xffffffffu, upto > mark)) - 1;
+        int32_t token = 0;
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e) {  // (from behind: the first element whose sum up to it exceeds the mark stays)
+          if (upto > mark) token = (int32_t)o0 + i * E + e;
+          upto -= w[e];
+        }
+        finish_unit(p, row, pos, n, __shfl_sync(0xffffffffu, token, at));
+        return;
+      } else {
+        before += stripe;
+      }
     }
-    before += __shfl_sync(0xffffffffu, incl, 31);
+    if (pass == 1) return;
+    if (worker && lane == 0) sh.group_sum[warp] = group;
+    __syncthreads();
+    if (!worker) return;
+    before += warp_sum(lane < warp ? sh.group_sum[lane] : 0);
+    if (!(before <= mark && mark < before + group)) return;
   }
 }
 
-template <typename T>
-int launch_verify(VerifyParams& p, bool two, cudaStream_t st) {
-  static std::atomic<bool> done[kMaxDevices];
-  auto k = verify_kernel<T>;
-  if (int rc = ensure_smem(k, kVerifySmem, done)) return rc;
+template <typename T, bool kAligned>
+int launch_verify(VerifyParams& p, cudaStream_t st) {
+  static std::atomic<bool> wide[kMaxDevices];  // clusters of 16 are allowed
+  auto k = verify_kernel<T, kAligned>;
   const int64_t nvec = ((int64_t)p.vocab * sizeof(T) + 15) / 16;
   const int64_t units = (int64_t)p.rows * (p.max_draft + 1);
-  auto share = [&](int c) { return (int)((nvec + (int64_t)c * kVerifyWarps * 32 - 1) / ((int64_t)c * kVerifyWarps * 32)) * 32; };
-  auto bytes = [&](int c) { return (int64_t)share(c) * kVerifyWarps * 16 * (two ? 2 : 1); };
-  // CTAs of a unit: three to an SM, so that one's passes run behind another's copies; more
-  // where the units alone do not fill the SMs.
+  auto depth = [&](int c) { return (int)((nvec + (int64_t)c * kVerifyWarps * kGroups * 32 - 1) / ((int64_t)c * kVerifyWarps * kGroups * 32)); };
+  // CTAs of a unit: one pass over a CTA's share should be a few loads deep; more CTAs where
+  // the units alone do not fill the SMs.
   int c = 1;
-  while (c < kVerifyCluster && (bytes(c) > 72 * 1024 || (units * c < 304 && share(c) > 32))) c *= 2;
-  if (bytes(c) > kVerifySmem)
-    return set_error(RGD_ERR_UNSUPPORTED, "rgd_verify_draft: vocab %d too large", p.vocab);
+  while (c < 8 && depth(c) > 1) c *= 2;
+  while (c < kVerifyCluster && units * c < 304 && depth(c) > 1) c *= 2;
   if (c > 8) {
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return cuda_error(e, "verify attributes");
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+    if (dev >= kMaxDevices || !wide[dev].load(std::memory_order_acquire)) {
+      e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return cuda_error(e, "verify attributes");
+      if (dev < kMaxDevices) wide[dev].store(true, std::memory_order_release);
+    }
   }
-  p.wvec = share(c);
+  p.depth = depth(c);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * c));
   cfg.blockDim = dim3(kVerifyThreads);
-  cfg.dynamicSmemBytes = (size_t)bytes(c);
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -636,6 +754,8 @@ extern "C" int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, 
   RGD_CHECK_ARG(aligned16(target_logits) && aligned16(draft_logits), "%s: logits must be 16-byte aligned", fn);
   RGD_CHECK_ARG((reinterpret_cast<uintptr_t>(workspace) & 3u) == 0, "%s: workspace must be 4-byte aligned", fn);
   RGD_CHECK_ARG(workspace_bytes >= rgd_verify_draft_workspace_size(rows, max_draft), "%s: workspace too small", fn);
+  // (a lane has at most 512 of them then, and its sums are exact)
+  if (vocab > 1 << 20) return set_error(RGD_ERR_UNSUPPORTED, "%s: vocab %d too large (max %d)", fn, vocab, 1 << 20);
   if ((int64_t)rows * ((int64_t)max_draft + 1) > 0x7fffffff / kVerifyCluster)
     return set_error(RGD_ERR_UNSUPPORTED, "%s: too many positions", fn);
   const int es = dtype == RGD_F32 ? 4 : 2;
@@ -647,8 +767,6 @@ extern "C" int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, 
   p.rows = rows;
   p.max_draft = max_draft;
   p.vocab = vocab;
-  p.copy_target = p.target_stride % 16 == 0;
-  p.copy_draft = p.draft_stride % 16 == 0;
   p.tokens = draft_tokens;
   p.n_draft = n_draft;
   p.is_probe = is_probe;
@@ -663,7 +781,8 @@ extern "C" int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, 
   p.count = static_cast<int32_t*>(workspace);
   p.result = p.count + rows;
   p.dev_status = dev_status;
-  const bool two = p.draft != nullptr;
-  return dtype == RGD_F32 ? launch_verify<float>(p, two, (cudaStream_t)stream)
-                          : launch_verify<__nv_bfloat16>(p, two, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool aligned = p.target_stride % 16 == 0 && (!p.draft || p.draft_stride % 16 == 0);
+  if (dtype == RGD_F32) return aligned ? launch_verify<float, true>(p, st) : launch_verify<float, false>(p, st);
+  return aligned ? launch_verify<__nv_bfloat16, true>(p, st) : launch_verify<__nv_bfloat16, false>(p, st);
 }
