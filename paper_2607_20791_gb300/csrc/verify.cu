@@ -41,7 +41,7 @@ namespace {
 
 constexpr int kVerifyWarps = 8;
 constexpr int kVerifyThreads = (kVerifyWarps + 1) * 32;  // (the last warp looks after the parameters)
-constexpr int kGroups = kVerifyWarps;  // groups of a warp's vectors, and loads in flight per lane
+constexpr int kGroups = 4;  // groups of a warp's vectors, and loads in flight per lane
 constexpr int kVerifyCluster = 16;                           // CTAs of a unit at most
 constexpr int32_t kTaken = -1, kRejectedRow = -2;            // results of a unit other than a token
 
@@ -71,9 +71,69 @@ struct VerifyShared {
   // of this CTA's warps, and pushed by every CTA of the cluster into every other
   float warp_top[2][kVerifyWarps], top[2][kVerifyCluster];
   uint64_t warp_sum[3][kVerifyWarps], sum[3][kVerifyCluster];  // target's and draft's weights, max(0, p - q)
-  uint64_t group_sum[kVerifyWarps];  // of the groups of the share that a draw falls into
+  uint64_t part_sum[kVerifyWarps];  // of the parts of the share that a draw falls into
   float theta, tl, ql;  // T ln p_min, the drafted token's logits
 };
+
+// T ln p rounded to fp32, p in [0, 1].  FP64 is slow on this part (CUDA's log took 3 us of a
+// call on its own), so the logarithm is taken in pairs of floats, to about 2^-44: p = 2^k m
+// with m in [sqrt(1/2), sqrt(2)), ln m = 2 atanh(s) = 2 (s + s^3/3 + s^5/5 + ...) with
+// s = (m - 1) / (m + 1).
+struct Float2 {
+  float hi, lo;
+};
+__device__ __forceinline__ Float2 sum_of(float a, float b) {  // exactly (Knuth)
+  const float s = __fadd_rn(a, b), bb = __fsub_rn(s, a);
+  return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, bb)), __fsub_rn(b, bb))};
+}
+__device__ __forceinline__ Float2 product_of(float a, float b) {  // exactly
+  const float h = __fmul_rn(a, b);
+  return {h, __fmaf_rn(a, b, -h)};
+}
+__device__ __forceinline__ Float2 add(Float2 a, Float2 b) {
+  const Float2 s = sum_of(a.hi, b.hi);
+  return sum_of(s.hi, __fadd_rn(s.lo, __fadd_rn(a.lo, b.lo)));
+}
+__device__ __forceinline__ Float2 mul(Float2 a, Float2 b) {
+  const Float2 h = product_of(a.hi, b.hi);
+  return sum_of(h.hi, __fadd_rn(h.lo, __fmaf_rn(a.hi, b.lo, __fmul_rn(a.lo, b.hi))));
+}
+__device__ __forceinline__ float scaled_log(float temp, float p) {
+  if (p == 0.f) return -INFINITY;
+  int k = 0;
+  if (p < 0x1p-100f) {  // (subnormals too)
+    p *= 0x1p60f;
+    k = -60;
+  }
+  const uint32_t bits = __float_as_uint(p);
+  k += (int)(bits >> 23) - 127;
+  float m = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+  if (m > 1.4142135f) {
+    m *= 0.5f;
+    ++k;
+  }
+  const float a = m - 1.f;  // (exact)
+  const Float2 b = sum_of(m, 1.f);
+  const float q = __fdiv_rn(a, b.hi);
+  const float r = __fmaf_rn(-q, b.lo, __fmaf_rn(-q, b.hi, a));
+  const Float2 s = sum_of(q, __fdiv_rn(r, b.hi)), z = mul(s, s);
+  // 1/3 + z/5 + z^2/7 + ... + z^8/19, z <= 0.0295: the last terms need fewer digits
+  float tail = 1.f / 19.f;
+  tail = __fmaf_rn(tail, z.hi, 1.f / 17.f);
+  tail = __fmaf_rn(tail, z.hi, 1.f / 15.f);
+  tail = __fmaf_rn(tail, z.hi, 1.f / 13.f);
+  tail = __fmaf_rn(tail, z.hi, 1.f / 11.f);
+  Float2 c = add(mul({tail, 0.f}, z), {(float)(1.0 / 9), (float)(1.0 / 9 - (double)(float)(1.0 / 9))});
+  c = add(mul(c, z), {(float)(1.0 / 7), (float)(1.0 / 7 - (double)(float)(1.0 / 7))});
+  c = add(mul(c, z), {(float)(1.0 / 5), (float)(1.0 / 5 - (double)(float)(1.0 / 5))});
+  c = add(mul(c, z), {(float)(1.0 / 3), (float)(1.0 / 3 - (double)(float)(1.0 / 3))});
+  Float2 l = add(s, mul(s, mul(c, z)));
+  l = {2.f * l.hi, 2.f * l.lo};
+  constexpr double kLn2 = 0.69314718055994530942;
+  l = add(mul({(float)k, 0.f}, {(float)kLn2, (float)(kLn2 - (double)(float)kLn2)}), l);
+  const Float2 v = product_of(l.hi, temp);
+  return __fadd_rn(v.hi, __fmaf_rn(l.lo, temp, v.lo));
+}
 
 // Element i of a 16-byte vector.
 template <typename T>
@@ -131,26 +191,26 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-__device__ __forceinline__ uint32_t word_sum(uint64_t v) { return (uint32_t)v + (uint32_t)(v >> 32); }
 
-// A lane's sum of whole(w), exact for up to 512 numbers.  Those of a vector below 2^-8 are
-// added as the bits of w 2^31 + 2^23.  Others go in two halves, w = a 2^-15 + r with a
-// the nearest whole number, and w 2^31 = a 2^16 + r 2^31, both again read off the bits of a
-// sum (2^23, and 1.5 2^23 for r's sign).  Conversions to integers would take the special
-// function unit's time, which the exponentials need.
+// A lane's sum of whole(w), exact for up to 2^16 numbers.  They go in two halves, w = a 2^-15 +
+// r with a the nearest whole number, and w 2^31 = a 2^16 + r 2^31, both read off the bits
+// of a sum (2^23, and 1.5 2^23 for r's sign).  Conversions to integers would take the
+// special function unit's time, which the exponentials need.
 struct WholeSum {
-  uint32_t low = 0, a = 0, b = 0;
-  __device__ void small(uint64_t w2) {
-    low += word_sum(fma2(w2, pair(0x1p31f, 0x1p31f), pair(0x1p23f, 0x1p23f))) - 2u * 0x4b000000u;
-  }
+  uint32_t a = 0, b = 0, pairs = 0;
   __device__ void add(uint64_t w2) {
     const uint64_t h = fma2(w2, pair(0x1p15f, 0x1p15f), pair(0x1p23f, 0x1p23f));
     const uint64_t n = add2(h, pair(-0x1p23f, -0x1p23f));
     const uint64_t r = fma2(n, pair(-0x1p-15f, -0x1p-15f), w2);
-    a += word_sum(h) - 2u * 0x4b000000u;
-    b += word_sum(fma2(r, pair(0x1p31f, 0x1p31f), pair(0x1.8p23f, 0x1.8p23f))) - 2u * 0x4b400000u;
+    const uint64_t l = fma2(r, pair(0x1p31f, 0x1p31f), pair(0x1.8p23f, 0x1.8p23f));
+    a += (uint32_t)h + (uint32_t)(h >> 32);
+    b += (uint32_t)l + (uint32_t)(l >> 32);
   }
-  __device__ uint64_t total() const { return (uint64_t)low + ((uint64_t)a << 16) + (uint64_t)(int64_t)(int32_t)b; }
+  __device__ void count(int n) { pairs += n; }  // of the calls of add()
+  __device__ uint64_t total() const {
+    const uint32_t high = a - pairs * (2u * 0x4b000000u), low = b - pairs * (2u * 0x4b400000u);
+    return ((uint64_t)high << 16) + (uint64_t)(int64_t)(int32_t)low;
+  }
 };
 
 // 16 bytes of logits: pairs of them, their maximum, and whether any is at or above a bound.
@@ -175,6 +235,12 @@ struct Vec<float> {
     a = __uint_as_float(i ? w.z : w.x);
     b = __uint_as_float(i ? w.w : w.y);
   }
+  // The same, those below a bound (and NaN) as -inf.
+  __device__ static void get_from(const uint4& w, int i, const Bound& c, float& a, float& b) {
+    get(w, i, a, b);
+    a = a >= c.v ? a : -INFINITY;
+    b = b >= c.v ? b : -INFINITY;
+  }
 };
 template <>
 struct Vec<__nv_bfloat16> {
@@ -198,6 +264,13 @@ struct Vec<__nv_bfloat16> {
   __device__ static bool reaches(Max m, const Bound& b) { return __hge2_mask(m, b.v) != 0; }
   __device__ static void get(const uint4& w, int i, float& a, float& b) {
     const uint32_t u = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    a = __uint_as_float(u << 16);
+    b = __uint_as_float(u & 0xffff0000u);
+  }
+  __device__ static void get_from(const uint4& w, int i, const Bound& c, float& a, float& b) {
+    uint32_t u = i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w;
+    const uint32_t m = __hge2_mask(b2(u), c.v);
+    u = (u & m) | (0xff80ff80u & ~m);
     a = __uint_as_float(u << 16);
     b = __uint_as_float(u & 0xffff0000u);
   }
@@ -318,51 +391,60 @@ __device__ __forceinline__ uint32_t groups_reaching(const Kept<T>& kept, float b
   return mask;
 }
 
-// The weights of a vector, added to a sum (NaN and -inf have none).  kOpen: no truncation.
-template <typename T, bool kOpen>
-__device__ __forceinline__ void add_weights(const uint4& w, const Side& side, const typename Vec<T>::Bound& big, WholeSum& sum) {
+// The kept weights of a vector, added to a sum (NaN and -inf have none).
+template <typename T>
+__device__ __forceinline__ void add_weights(const uint4& w, const Side& side, const typename Vec<T>::Bound& cut, WholeSum& sum) {
   using V = Vec<T>;
   const uint64_t top = pair(-side.top, -side.top), kexp = pair(side.kexp, side.kexp);
-  uint64_t w2[V::kPairs];
 #pragma unroll
   for (int e = 0; e < V::kPairs; ++e) {
-    float a, b, x, y;
-    V::get(w, e, a, b);
-    unpair(mul2(add2(pair(a, b), top), kexp), x, y);
-    x = kOpen ? fmaxf(x, -200.f) : a >= side.cut ? x : -200.f;  // (2^-200 is 0)
-    y = kOpen ? fmaxf(y, -200.f) : b >= side.cut ? y : -200.f;
-    w2[e] = pair(ex2_approx(x), ex2_approx(y));
+    float a, b;
+    V::get_from(w, e, cut, a, b);
+    unpair(mul2(add2(pair(a, b), top), kexp), a, b);
+    sum.add(pair(ex2_approx(a), ex2_approx(b)));
   }
-  if (kOpen && !V::reaches(V::max_of(w, V::lowest()), big)) {
-#pragma unroll
-    for (int e = 0; e < V::kPairs; ++e) sum.small(w2[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < V::kPairs; ++e) sum.add(w2[e]);
-  }
+  sum.count(V::kPairs);
 }
 
 // The sum of a warp's weights, in whole multiples of 2^-31.
-template <typename T, bool kOpen, bool kAligned>
+template <typename T, bool kAligned>
 __device__ __forceinline__ uint64_t sum_weights(const Share<T, kAligned>& v, const Kept<T>& kept, const Side& side, int depth,
                                                 int lane) {
   using V = Vec<T>;
-  const typename V::Bound big(side.top - 8.001f / side.kexp);  // (below it a weight is under 2^-8)
+  const typename V::Bound cut(side.cut);
+  const uint32_t mask = groups_reaching(kept, side.cut);
   WholeSum sum;
-  Walk walk(kOpen ? (1u << kGroups) - 1 : groups_reaching(kept, side.cut), depth, v.whole, lane);
-  uint4 w = kept.rest, w1 = V::nothing(), w2 = w1;
-  int i1 = walk.next(), i2 = walk.next();
-  if (i1 >= 0) w1 = v.get(i1);
-  if (i2 >= 0) w2 = v.get(i2);
+  uint4 w = kept.rest;
+  if (__popc(__reduce_and_sync(0xffffffffu, mask)) > kGroups / 2) {  // most of it: all of it, in order
+    constexpr int kFlight = 4;
 #pragma unroll 1
-  for (;;) {  // (two vectors are on their way while one is worked on)
-    const int i3 = walk.next();
-    uint4 w3 = V::nothing();
-    if (i3 >= 0) w3 = v.get(i3);
-    add_weights<T, kOpen>(w, side, big, sum);
-    if (i1 < 0) break;
-    w = w1, w1 = w2, w2 = w3;
-    i1 = i2, i2 = i3;
+    for (int i = lane; i < v.whole; i += 32 * kFlight) {
+      uint4 x[kFlight];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        x[k] = V::nothing();
+        if (i + 32 * k < v.whole) x[k] = v.get(i + 32 * k);
+      }
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) add_weights<T>(x[k], side, cut, sum);
+    }
+    add_weights<T>(w, side, cut, sum);
+  } else {  // the groups that reach the cutoff, two vectors on their way while one is worked on
+    Walk walk(mask, depth, v.whole, lane);
+    uint4 w1 = V::nothing(), w2 = w1;
+    int i1 = walk.next(), i2 = walk.next();
+    if (i1 >= 0) w1 = v.get(i1);
+    if (i2 >= 0) w2 = v.get(i2);
+#pragma unroll 1
+    for (;;) {
+      const int i3 = walk.next();
+      uint4 w3 = V::nothing();
+      if (i3 >= 0) w3 = v.get(i3);
+      add_weights<T>(w, side, cut, sum);
+      if (i1 < 0) break;
+      w = w1, w1 = w2, w2 = w3;
+      i1 = i2, i2 = i3;
+    }
   }
   return warp_sum(sum.total());
 }
@@ -421,7 +503,7 @@ __device__ __forceinline__ void push(const float* slot, float v, uint32_t rank) 
 }
 
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyParams p) {
   constexpr int E = 16 / (int)sizeof(T);
   using V = Vec<T>;
   __shared__ VerifyShared sh;
@@ -473,7 +555,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
   if (!worker && lane == 0) {
     sh.tl = d_in && !greedy ? one_logit<T>(p.target + trow, d) : 0.f;
     sh.ql = d_in && two ? one_logit<T>(p.draft + qrow, d) : 0.f;
-    sh.theta = (float)((double)temp * log((double)min_p));
+    sh.theta = scaled_log(temp, min_p);
   }
   Kept<T> tkept, qkept;
   {
@@ -551,13 +633,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
   t.kexp = q.kexp = fminf(__fdiv_rn(1.4426950408889634f, temp), 3e38f);  // (finite: 0 times it is 0)
   t.cut = __fadd_rn(t.top, sh.theta);
   q.cut = __fadd_rn(q.top, sh.theta);
-  if (sh.theta == -INFINITY) {
-    join(0, sum_weights<T, true>(tv, tkept, t, p.depth, lane));
-    if (two) join(1, sum_weights<T, true>(qv, qkept, q, p.depth, lane));
-  } else {
-    join(0, sum_weights<T, false>(tv, tkept, t, p.depth, lane));
-    if (two) join(1, sum_weights<T, false>(qv, qkept, q, p.depth, lane));
-  }
+  join(0, sum_weights(tv, tkept, t, p.depth, lane));
+  if (two) join(1, sum_weights(qv, qkept, q, p.depth, lane));
   exchange(0, two ? 1 : 0);
   uint64_t total = over_cluster(0);
   t.inv = __fdiv_rn(1.f, __ull2float_rn(total) * 0x1p-31f);
@@ -586,6 +663,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
           q1 = two ? q.prob(q1) : at + 1 == d ? 1.f : 0.f;
           rest.add(pair(fmaxf(t.prob(x) - q0, 0.f), fmaxf(t.prob(y) - q1, 0.f)));
         }
+        rest.count(V::kPairs);
       };
       Walk walk(groups_reaching(tkept, t.cut), p.depth, tv.whole, lane);  // (p is 0 elsewhere)
       uint4 a = tkept.rest, c = two ? qkept.rest : a;
@@ -613,8 +691,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
     }
   }
 
-  // The draw: the CTA, then the share, that holds the mark; every warp of the CTA takes one
-  // group of that share, and the one whose group holds the mark finds the element.
+  // The draw: the CTA, then the share, that holds the mark; every warp of the CTA takes a part
+  // of that share, and the one whose part holds the mark finds the element.
   const uint64_t mark = (uint64_t)((double)draw_u * (double)total);
   uint64_t before = warp_sum(lane < (int)rank ? sh.sum[which][lane] : 0);
   if (!(before <= mark && mark < before + sh.sum[which][rank])) return;
@@ -622,12 +700,13 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
   for (; owner + 1 < kVerifyWarps && before + sh.warp_sum[which][owner] <= mark; ++owner) before += sh.warp_sum[which][owner];
   const int64_t o0 = ((int64_t)rank * kVerifyWarps + owner) * share, left = min(share, p.vocab - o0);
   const Share<T, kAligned> ot(p.target + trow, o0, left), oq(two ? p.draft + qrow : p.target + trow, o0, two ? left : 0);
-  uint64_t group = 0;
+  const int stripes = (kGroups * p.depth + kVerifyWarps - 1) / kVerifyWarps;  // of a part
+  uint64_t part = 0;
 #pragma unroll 1
-  for (int pass = 0; pass < 2; ++pass) {  // the groups' sums, then the element
+  for (int pass = 0; pass < 2; ++pass) {  // the parts' sums, then the element
 #pragma unroll 1
-    for (int s = 0; s < (worker ? p.depth : 0); ++s) {
-      const int i = (warp * p.depth + s) * 32 + lane;
+    for (int s = 0; s < (worker ? stripes : 0); ++s) {
+      const int i = (warp * stripes + s) * 32 + lane;
       uint4 a = V::nothing(), c = a;
       if (i < ot.whole) {
         a = ot.get(i);
@@ -650,7 +729,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
       }
       const uint64_t stripe = warp_sum(sum);
       if (pass == 0) {
-        group += stripe;
+        part += stripe;
       } else if (mark < before + stripe) {
         uint64_t upto = sum;
 #pragma unroll
@@ -673,11 +752,11 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
       }
     }
     if (pass == 1) return;
-    if (worker && lane == 0) sh.group_sum[warp] = group;
+    if (worker && lane == 0) sh.part_sum[warp] = part;
     __syncthreads();
     if (!worker) return;
-    before += warp_sum(lane < warp ? sh.group_sum[lane] : 0);
-    if (!(before <= mark && mark < before + group)) return;
+    before += warp_sum(lane < warp ? sh.part_sum[lane] : 0);
+    if (!(before <= mark && mark < before + part)) return;
   }
 }
 
