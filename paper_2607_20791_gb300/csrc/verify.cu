@@ -41,7 +41,8 @@ namespace {
 
 constexpr int kVerifyWarps = 8;
 constexpr int kVerifyThreads = (kVerifyWarps + 1) * 32;  // (the last warp looks after the parameters)
-constexpr int kGroups = 4;  // groups of a warp's vectors, and loads in flight per lane
+constexpr int kGroups = 16;  // groups of a lane's vectors whose maxima it keeps
+constexpr int kFlight = 4;   // loads in flight per lane
 constexpr int kVerifyCluster = 16;                           // CTAs of a unit at most
 constexpr int32_t kTaken = -1, kRejectedRow = -2;            // results of a unit other than a token
 
@@ -50,7 +51,7 @@ struct VerifyParams {
   const uint8_t* draft;  // NULL: every draft was certain
   int64_t target_stride, draft_stride;  // bytes
   int32_t rows, max_draft, vocab;
-  int32_t depth;  // stripes of 32 vectors in a group: a warp's share is kGroups depth stripes
+  int32_t stripes;  // of 32 vectors, in a warp's share
   const int32_t* tokens;
   const int32_t* n_draft;
   const uint8_t* is_probe;
@@ -229,7 +230,9 @@ struct Vec<float> {
   __device__ static Max max_of(const uint4& w, Max m) {
     return fmaxf(fmaxf(fmaxf(fmaxf(m, __uint_as_float(w.x)), __uint_as_float(w.y)), __uint_as_float(w.z)), __uint_as_float(w.w));
   }
+  __device__ static Max max_of(Max a, Max b, Max c) { return fmaxf(fmaxf(a, b), c); }
   __device__ static float value(Max m) { return m; }
+  __device__ static __nv_bfloat162 up(Max a, Max b) { return {__float2bfloat16_ru(a), __float2bfloat16_ru(b)}; }
   __device__ static bool reaches(Max m, const Bound& b) { return m >= b.v; }
   __device__ static void get(const uint4& w, int i, float& a, float& b) {
     a = __uint_as_float(i ? w.z : w.x);
@@ -256,6 +259,10 @@ struct Vec<__nv_bfloat16> {
   __device__ static uint4 nothing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
   __device__ static Max max_of(const uint4& w, Max m) {  // (NaN never wins, as with fmaxf)
     return __hmax2(__hmax2(__hmax2(b2(w.x), b2(w.y)), __hmax2(b2(w.z), b2(w.w))), m);
+  }
+  __device__ static Max max_of(Max a, Max b, Max c) { return __hmax2(__hmax2(a, b), c); }
+  __device__ static __nv_bfloat162 up(Max a, Max b) {  // the larger half of each
+    return __hmax2(__lows2bfloat162(a, b), __highs2bfloat162(a, b));
   }
   __device__ static float value(Max m) {
     const uint32_t u = *reinterpret_cast<const uint32_t*>(&m);
@@ -330,65 +337,74 @@ struct Share {
   }
 };
 
-// What a lane keeps of its part of a share: the maxima of its groups (group g: its
-// vectors of stripes g depth .. of the share) and the last vector.
-template <typename T>
+// What a lane keeps of its part of a share: the maxima of its groups (group g: its vectors
+// of stripes g, g + kGroups, ...) rounded up to bf16, two to a word, and the last vector.
 struct Kept {
-  typename Vec<T>::Max group[kGroups];
+  uint32_t group[kGroups / 2];
   uint4 rest;
 };
 
 template <typename T, bool kAligned>
-__device__ __forceinline__ float find_maxima(const Share<T, kAligned>& v, Kept<T>& kept, int depth, int lane) {
+__device__ __forceinline__ float find_maxima(const Share<T, kAligned>& v, Kept& kept, int stripes, int lane) {
   using V = Vec<T>;
   kept.rest = v.rest(lane);
+  typename V::Max all = V::max_of(kept.rest, V::lowest());
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) kept.group[g] = V::lowest();
+  for (int g = 0; g < kGroups / 2; ++g) kept.group[g] = 0xff80ff80u;
 #pragma unroll 1
-  for (int s = 0; s < depth; ++s) {
-    uint4 w[kGroups];
+  for (int s = 0; s < stripes; s += kGroups) {
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const int i = (g * depth + s) * 32 + lane;
-      w[g] = V::nothing();
-      if (i < v.whole) w[g] = v.get(i);
+    for (int g = 0; g < kGroups; g += kFlight) {
+      if (s + g >= stripes) break;
+      uint4 w[kFlight];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        const int i = (s + g + k) * 32 + lane;
+        w[k] = V::nothing();
+        if (i < v.whole) w[k] = v.get(i);
+      }
+#pragma unroll
+      for (int k = 0; k < kFlight; k += 2) {
+        const typename V::Max m0 = V::max_of(w[k], V::lowest()), m1 = V::max_of(w[k + 1], V::lowest());
+        all = V::max_of(m0, m1, all);
+        const __nv_bfloat162 m = __hmax2(V::up(m0, m1), *reinterpret_cast<const __nv_bfloat162*>(&kept.group[(g + k) / 2]));
+        kept.group[(g + k) / 2] = *reinterpret_cast<const uint32_t*>(&m);
+      }
     }
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) kept.group[g] = V::max_of(w[g], kept.group[g]);
   }
-  float m = V::value(V::max_of(kept.rest, V::lowest()));
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) m = fmaxf(m, V::value(kept.group[g]));
-  return warp_max(m);
+  return warp_max(V::value(all));
 }
 
 // Walks a lane's vectors of the groups in `mask`; next() gives -1 after the last.
 struct Walk {
   uint32_t mask;
-  int depth, whole, lane, s;
-  __device__ Walk(uint32_t mask, int depth, int whole, int lane) : mask(mask), depth(depth), whole(whole), lane(lane), s(0) {}
+  int stripes, whole, lane, s;
+  __device__ Walk(uint32_t mask, int stripes, int whole, int lane)
+      : mask(mask), stripes(stripes), whole(whole), lane(lane) {
+    s = __ffs(mask) - 1;
+  }
   __device__ int next() {
-    if (!mask) return -1;
-    const int i = ((__ffs(mask) - 1) * depth + s) * 32 + lane;
-    if (++s == depth) {
-      s = 0;
-      mask &= mask - 1;
+    while (mask) {
+      const int i = s * 32 + lane;
+      s += kGroups;
+      if (s >= stripes) {
+        mask &= mask - 1;
+        s = mask ? __ffs(mask) - 1 : 0;
+      }
+      if (i < whole) return i;
     }
-    if (i < whole) return i;
-    mask = 0;  // (everything further is past the end too)
     return -1;
   }
 };
 
-// The groups whose maximum reaches a bound.
-template <typename T>
-__device__ __forceinline__ uint32_t groups_reaching(const Kept<T>& kept, float bound) {
-  using V = Vec<T>;
-  const typename V::Bound b(bound);
+// The groups whose maximum may reach a bound.
+__device__ __forceinline__ uint32_t groups_reaching(const Kept& kept, float bound) {
+  const __nv_bfloat162 b = __bfloat162bfloat162(__float2bfloat16_ru(bound));  // (bf16 maxima: see Vec's Bound)
   uint32_t mask = 0;
 #pragma unroll
-  for (int g = 0; g < kGroups; ++g) mask |= V::reaches(kept.group[g], b) ? 1u << g : 0u;
-  return mask;
+  for (int g = 0; g < kGroups; g += 2)
+    mask |= (__hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&kept.group[g / 2]), b) & 0x00020001u) << g;
+  return (mask | mask >> 16) & ((1u << kGroups) - 1);
 }
 
 // The kept weights of a vector, added to a sum (NaN and -inf have none).
@@ -408,15 +424,17 @@ __device__ __forceinline__ void add_weights(const uint4& w, const Side& side, co
 
 // The sum of a warp's weights, in whole multiples of 2^-31.
 template <typename T, bool kAligned>
-__device__ __forceinline__ uint64_t sum_weights(const Share<T, kAligned>& v, const Kept<T>& kept, const Side& side, int depth,
+__device__ __forceinline__ uint64_t sum_weights(const Share<T, kAligned>& v, const Kept& kept, const Side& side, int stripes,
                                                 int lane) {
   using V = Vec<T>;
   const typename V::Bound cut(side.cut);
   const uint32_t mask = groups_reaching(kept, side.cut);
   WholeSum sum;
   uint4 w = kept.rest;
-  if (__popc(__reduce_and_sync(0xffffffffu, mask)) > kGroups / 2) {  // most of it: all of it, in order
-    constexpr int kFlight = 4;
+  // (a step of the walk below costs about 1.7 vectors in order, and the warp takes as many as
+  // its busiest lane)
+  const int steps = (int)__reduce_max_sync(0xffffffffu, (uint32_t)__popc(mask)) * ((stripes + kGroups - 1) / kGroups);
+  if (7 * steps > 4 * stripes) {  // all of the share, in order
 #pragma unroll 1
     for (int i = lane; i < v.whole; i += 32 * kFlight) {
       uint4 x[kFlight];
@@ -430,7 +448,7 @@ __device__ __forceinline__ uint64_t sum_weights(const Share<T, kAligned>& v, con
     }
     add_weights<T>(w, side, cut, sum);
   } else {  // the groups that reach the cutoff, two vectors on their way while one is worked on
-    Walk walk(mask, depth, v.whole, lane);
+    Walk walk(mask, stripes, v.whole, lane);
     uint4 w1 = V::nothing(), w2 = w1;
     int i1 = walk.next(), i2 = walk.next();
     if (i1 >= 0) w1 = v.get(i1);
@@ -503,7 +521,7 @@ __device__ __forceinline__ void push(const float* slot, float v, uint32_t rank) 
 }
 
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyParams p) {
   constexpr int E = 16 / (int)sizeof(T);
   using V = Vec<T>;
   __shared__ VerifyShared sh;
@@ -545,7 +563,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
 
   // This warp's share (none for the last warp), in the order of the elements over the cluster.
   const bool worker = warp < kVerifyWarps;
-  const int64_t share = (int64_t)kGroups * p.depth * 32 * E;
+  const int64_t share = (int64_t)p.stripes * 32 * E;
   const int64_t e0 = ((int64_t)rank * kVerifyWarps + warp) * share;
   const int64_t count = worker ? min(share, p.vocab - e0) : 0;
   const Share<T, kAligned> tv(p.target + trow, e0, count);
@@ -557,10 +575,10 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     sh.ql = d_in && two ? one_logit<T>(p.draft + qrow, d) : 0.f;
     sh.theta = scaled_log(temp, min_p);
   }
-  Kept<T> tkept, qkept;
+  Kept tkept, qkept;
   {
-    const float tm = find_maxima(tv, tkept, p.depth, lane);
-    const float qm = find_maxima(qv, qkept, two ? p.depth : 0, lane);
+    const float tm = find_maxima(tv, tkept, p.stripes, lane);
+    const float qm = find_maxima(qv, qkept, two ? p.stripes : 0, lane);
     if (worker && lane == 0) {
       sh.warp_top[0][warp] = tm;
       sh.warp_top[1][warp] = qm;
@@ -594,7 +612,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
       for (int e = E - 1; e >= 0; --e)
         if (elem<T>(w, e) == t.top) best = min(best, (uint32_t)e0 + i * E + e);
     };
-    Walk walk(groups_reaching(tkept, t.top), p.depth, tv.whole, lane);
+    Walk walk(groups_reaching(tkept, t.top), p.stripes, tv.whole, lane);
 #pragma unroll 1
     for (int i = walk.next(); i >= 0; i = walk.next()) look(tv.get(i), i);
     look(tkept.rest, tv.whole);
@@ -633,8 +651,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   t.kexp = q.kexp = fminf(__fdiv_rn(1.4426950408889634f, temp), 3e38f);  // (finite: 0 times it is 0)
   t.cut = __fadd_rn(t.top, sh.theta);
   q.cut = __fadd_rn(q.top, sh.theta);
-  join(0, sum_weights(tv, tkept, t, p.depth, lane));
-  if (two) join(1, sum_weights(qv, qkept, q, p.depth, lane));
+  join(0, sum_weights(tv, tkept, t, p.stripes, lane));
+  if (two) join(1, sum_weights(qv, qkept, q, p.stripes, lane));
   exchange(0, two ? 1 : 0);
   uint64_t total = over_cluster(0);
   t.inv = __fdiv_rn(1.f, __ull2float_rn(total) * 0x1p-31f);
@@ -665,7 +683,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
         }
         rest.count(V::kPairs);
       };
-      Walk walk(groups_reaching(tkept, t.cut), p.depth, tv.whole, lane);  // (p is 0 elsewhere)
+      Walk walk(groups_reaching(tkept, t.cut), p.stripes, tv.whole, lane);  // (p is 0 elsewhere)
       uint4 a = tkept.rest, c = two ? qkept.rest : a;
       int i = tv.whole, ahead = walk.next();
 #pragma unroll 1
@@ -700,7 +718,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   for (; owner + 1 < kVerifyWarps && before + sh.warp_sum[which][owner] <= mark; ++owner) before += sh.warp_sum[which][owner];
   const int64_t o0 = ((int64_t)rank * kVerifyWarps + owner) * share, left = min(share, p.vocab - o0);
   const Share<T, kAligned> ot(p.target + trow, o0, left), oq(two ? p.draft + qrow : p.target + trow, o0, two ? left : 0);
-  const int stripes = (kGroups * p.depth + kVerifyWarps - 1) / kVerifyWarps;  // of a part
+  const int stripes = (p.stripes + kVerifyWarps - 1) / kVerifyWarps;  // of a part
   uint64_t part = 0;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {  // the parts' sums, then the element
@@ -766,12 +784,17 @@ int launch_verify(VerifyParams& p, cudaStream_t st) {
   auto k = verify_kernel<T, kAligned>;
   const int64_t nvec = ((int64_t)p.vocab * sizeof(T) + 15) / 16;
   const int64_t units = (int64_t)p.rows * (p.max_draft + 1);
-  auto depth = [&](int c) { return (int)((nvec + (int64_t)c * kVerifyWarps * kGroups * 32 - 1) / ((int64_t)c * kVerifyWarps * kGroups * 32)); };
-  // CTAs of a unit: one pass over a CTA's share should be a few loads deep; more CTAs where
-  // the units alone do not fill the SMs.
+  auto stripes = [&](int c) { return (int)((nvec + (int64_t)c * kVerifyWarps * 32 - 1) / ((int64_t)c * kVerifyWarps * 32)); };
+  // CTAs of a unit.  A CTA pays for three exchanges however little it reads, and reads
+  // nothing meanwhile: its warps' shares are up to 40 stripes (20 KB), and shorter (16) only
+  // to have some three CTAs for each that fits the SMs at once (456), so that they are at
+  // different stages.  Measured: 400 units of 2 x 128256 bf16 46 us with 4, 52 with 2, 62 with
+  // 8; 2048 of 152064 216 us with 2, 234 with 4, 338 with 8; 192 of 262144 fp32 64 us with 8,
+  // 80 with 4.  Few units are cut further until the SMs have two CTAs each.
   int c = 1;
-  while (c < 8 && depth(c) > 1) c *= 2;
-  while (c < kVerifyCluster && units * c < 304 && depth(c) > 1) c *= 2;
+  while (c < kVerifyCluster && stripes(c) > 40) c *= 2;
+  while (c < kVerifyCluster && units * c < 3 * 456 && stripes(2 * c) >= 16) c *= 2;
+  while (c < kVerifyCluster && units * c < 304 && stripes(c) > 2) c *= 2;
   if (c > 8) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -782,7 +805,7 @@ int launch_verify(VerifyParams& p, cudaStream_t st) {
       if (dev < kMaxDevices) wide[dev].store(true, std::memory_order_release);
     }
   }
-  p.depth = depth(c);
+  p.stripes = stripes(c);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(units * c));
   cfg.blockDim = dim3(kVerifyThreads);
