@@ -179,13 +179,21 @@ def _ptr(t, name: str, dtype=None, optional: bool = False, numel: Optional[int] 
     return t.data_ptr()
 
 
+_raw_stream = None  # (current device, its current stream), once asked for: without a Stream object 2 us less
+
+
 def _stream(stream) -> Optional[int]:
+    global _raw_stream
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream[1](_raw_stream[0]())
         import torch
         try:
-            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (without a Stream object: 2 us less)
-            if raw is not None:
-                return raw(torch.cuda.current_device())
+            torch.cuda.current_device()  # (initialises CUDA)
+            raw = (getattr(torch._C, "_cuda_getDevice", None), getattr(torch._C, "_cuda_getCurrentRawStream", None))
+            if None not in raw:
+                _raw_stream = raw
+                return raw[1](raw[0]())
             return torch.cuda.current_stream().cuda_stream
         except (RuntimeError, AssertionError):  # no CUDA device: the call is refused or fails in CUDA
             return None
