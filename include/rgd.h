@@ -416,7 +416,7 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *                  apart (>= vocab), dtype RGD_F32 or RGD_BF16
  *   draft_logits   [rows, max_draft] rows of vocab logits of the same dtype,
  *                  draft_stride elements apart; NULL: every draft was certain
- *                  (q_k(d_k) = 1).  Rows that start on 16 bytes are read by bulk copies
+ *                  (q_k(d_k) = 1).  Rows that all start on 16 bytes are read fastest
  *   draft_tokens   int32 [rows, max_draft]; one outside [0, vocab) sets
  *                  RGD_DEV_BAD_TOKEN, is rejected, and the draw there is from p_k
  *   n_draft        int32 [rows], in [0, max_draft]; NULL: max_draft each
@@ -432,15 +432,15 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *                  every drafted position (1 or 0 in greedy rows), whether the row
  *                  gets there or not; 0 past n_draft
  *   workspace      rgd_verify_draft_workspace_size() bytes, 4-byte aligned, zero-filled
- *                  before its first use; a call leaves the row counts at its start at
- *                  zero again unless it reports RGD_DEV_WAIT_TIMEOUT (zero-fill it
- *                  then, and where rows grows).  Calls that share it must not overlap
+ *                  before its first use; a call leaves it all zero again, so one sized
+ *                  for the largest call serves calls of any shape.  Calls that share
+ *                  it must not overlap
  * A row with n_draft, temperature, min_p or a uniform out of range, or with a
  * position it gets to whose largest logit is not finite, is rejected and sets
  * RGD_DEV_BAD_PARAM.  NaN logits have no weight.  Weights are 2^((l - l_max)
  * log2(e)/T) in fp32, rounded to multiples of 2^-31 and summed exactly, so the
- * outputs do not depend on how a call is cut.  RGD_ERR_UNSUPPORTED when a position's
- * one or two rows take more than about 3.5 MB.  One kernel on `stream`. */
+ * outputs do not depend on how a call is cut.  RGD_ERR_UNSUPPORTED above a vocab of
+ * 2^20.  One kernel on `stream`. */
 int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, int32_t dtype, const void* target_logits,
                      int64_t target_stride, const void* draft_logits, int64_t draft_stride,
                      const int32_t* draft_tokens, const int32_t* n_draft, const uint8_t* is_probe,

@@ -21,6 +21,9 @@ Decoding") and the published definitions it relies on:
 * ``precheck``   -- the residual-stream classifier of App. A: a d + 1 logistic
   readout per prompt and the skip rule p <= theta, applied to the gate state.
 
+* ``drafting``   -- what a step with drafted tokens adds: verification against the
+  target's probabilities, products with 4-bit weights, the cache's pages.
+
 Only ``tests/``, ``__graft_entry__.smoke()`` and ``bench.py``'s CPU-baseline /
 reference legs may import this package.  The product library never calls it and
 shares no code with it; the two meet only through the seeded input generators.

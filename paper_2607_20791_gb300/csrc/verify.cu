@@ -498,6 +498,8 @@ __device__ __noinline__ void finish_unit(const VerifyParams& p, int row, int pos
       break;
     }
   }
+  __syncwarp();
+  for (int i = lane; i <= n; i += 32) res[i] = 0;  // (the workspace is all zero again: its next call may have another shape)
   const bool good = token != kRejectedRow;
   for (int i = lane; i <= p.max_draft; i += 32)
     p.token_out[(int64_t)row * (p.max_draft + 1) + i] =
