@@ -2,27 +2,30 @@
 // W[n, k] = (q[n, k] - z[n, k / G]) s[n, k / G], q packed two to a byte along k.
 //
 // The weights are read once; everything else is small.  A tile is 32 rows of W (16 above
-// 16 rows of x); the warps of its group take the 128-weight chunks of those rows in turn,
-// so that together they read contiguous bytes of a row.  A chunk is one
-// TMA box of 64 bytes by the tile's rows into the warp's own ring in shared memory, 4 KB
-// ahead of its use, read 16 bytes a lane (lane 4g + t: rows g, g + 8, ..., bytes 16t ..), and
-// 8 mma.m16n8k16 with the weights as A for every 16 of its rows and 8 rows of x: one row
-// costs the same as eight, and the tensor pipe does the sums over k in fp32.  (Rows off
-// 16 bytes come by 4-byte asynchronous copies.)
+// 16 rows of x); the warps of its group take the chunks of those rows (256 weights for up
+// to 8 rows of x, else 128) in turn, so that together they read contiguous bytes of a row.
+// A chunk comes by TMA boxes of 64 bytes by the tile's rows into the warp's own ring in
+// shared memory, 4 to 8 KB ahead of its use.  Every 128 weights are 8 mma.m16n8k16 with the
+// weights as A for every 16 rows of W and 8 rows of x: one row of x costs the same as
+// eight, and the tensor pipe does the sums over k in fp32.
 //
 // Which k a lane's A elements stand for is free as long as B agrees, so a lane feeds the
 // 8 nibbles of a 32-bit word as they lie: nibbles p and p + 4 are the two halves of
 // (word >> 4p) & 0x000f000f, and with 0x4300 over each (bf16 128) they are the bf16
 // numbers 128 + q.  128 + z taken from them leaves q - z exactly.  x lies in shared memory
-// in that order, one 16-byte load a lane for two MMAs.  With groups of 128 the four words
-// of a 16-byte copy share a scale and go in as they are; with smaller groups an MMA's k
-// must stay within 32 weights, so the quad's 4 x 4 words are transposed first.  A group's
-// sum is scaled in fp32 after its last MMA.
+// in that order, one 16-byte load a lane for two MMAs.  With groups of 128 a lane of a quad
+// has 16 bytes of a row in one load.  With smaller ones an MMA's k must stay within 32
+// weights: its quad reads a word each of the same 16 bytes, from boxes swizzled by 64 bytes
+// so that the warp's 32 words lie in 32 banks.  A group's sum is scaled in fp32 after its
+// last MMA.
 //
-// One block of 24 warps (16 above 8 rows of x) fills an SM, so that x lies there once.  Its
-// warps form groups of S that share a tile and whose sums meet in shared memory: few tiles
-// want a wide group, many a narrow one, whose joins cost less.  Where x does not fit, k goes
-// in blocks, with the sums of a group's tiles kept in shared memory between them.
+// Rows off 16 bytes have no box: a bulk copy a row brings the whole 16-byte vectors that
+// hold its part of a chunk, and a lane's word is cut from the two it lies in.
+//
+// One block of 16 warps fills an SM, so that x lies there once.  Its warps form groups of S
+// that share a tile and whose sums meet in shared memory: few tiles want a wide group, many
+// a narrow one, whose joins cost less.  Where x does not fit, k goes in blocks, with the sums
+// of a group's tiles kept in shared memory between them.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -35,12 +38,11 @@
 namespace rgd {
 namespace {
 
-constexpr int kPart = 128;   // weights of a row that a lane's quad holds at a time
-constexpr int kUnit = 512;   // bytes of x per MMA step: 8 rows, 32 weights
+constexpr int kPart = 128;           // weights of a row that a lane's quad works on together
 constexpr int kW4Smem = 226 * 1024;  // (of 227; the barriers take the rest)
+constexpr int kWarps = 16;           // of a block
 
-constexpr int kWarps = 16;   // of a block
-// For 8 NT rows of x: groups of 16 rows of W in a tile, 128-weight parts of a chunk, chunks in flight.
+// For 8 NT rows of x: groups of 16 rows of W in a tile, parts of a chunk, chunks in flight.
 template <int NT>
 constexpr int kSub = NT == 4 ? 1 : 2;
 template <int NT>
@@ -49,15 +51,34 @@ template <int NT>
 constexpr int kAhead = NT == 4 ? 4 : 2;
 template <int NT>
 constexpr int kChunk = kPart * kParts<NT>;
-// Bytes of 8 rows of a chunk in a warp's ring; rows off 16 bytes come as the five words that hold a lane's 16 bytes.
-template <bool kAligned>
-constexpr int kPiece = kAligned ? 512 : 640;
+
+// Shared memory: the warps' rings, every warp's sums of a tile, the sums kept between blocks of
+// k, the warps' scales (where groups are small), x.  GS: steps of 32 weights in a group.
+template <int NT, int GS, bool kAligned>
+struct Layout {
+  static constexpr int kRows = 16 * kSub<NT>;  // of a tile
+  static constexpr int kSums = kRows * 8 * NT;
+  static constexpr int kJoin = kWarps * kSums * 4;
+  static constexpr int kPitch = kAligned ? 64 : kParts<NT> * 64 + 16;            // from a row to the next
+  static constexpr int kSlot = kRows * (kAligned ? kParts<NT> * 64 : kPitch);    // of a chunk
+  static constexpr int kRing = kWarps * kAhead<NT> * kSlot;
+  static constexpr int kGroups = 4 / GS;                                         // of a part
+  static constexpr int kScales = GS == 4 ? 0 : kParts<NT> * kRows * kGroups * 4;  // bytes of a warp
+  static constexpr int kFixed = kRing + kJoin + kWarps * kScales;
+};
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same from zero.
+__device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                               uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // Nibbles p and p + 4 of a word as bf16 q - z (bias: 128 + z twice).  `magic` is 0x43004300 in a
@@ -74,9 +95,6 @@ __device__ __forceinline__ uint32_t exponent_bits() {
   return m;
 }
 
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint64_t* bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar))
@@ -84,138 +102,83 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
 }
 
 // A chunk's scales and zeros as they lie in memory (a load must not be waited for before its
-// use).  Lane i has those of row i of the tile (of row i - 16 for the second half of k in a
-// tile of 16 rows): one of every 128 weights, or of every 32 where groups are smaller.
+// use).  Lane i has those of row i of the tile (in a tile of 16 rows, lanes i and i + 16 half
+// of row i's each): one of every 128 weights, or one of every group.
 template <int NL, bool kZeros>
 struct Scales {
   uint32_t s[NL], z[kZeros ? NL : 1];
 };
 
-template <int kRows, int kParts, int NL, bool kSmallGroups, bool kZeros>
+template <int kRows, int kEach, int GS, int NL, bool kZeros>
 __device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const uint8_t* row_scales,
-                                            const uint8_t* row_zeros, int chunk, int lane) {
-  constexpr int kEach = NL / kParts;
+                                            const uint8_t* row_zeros, int part, int lane) {
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    const int k = (chunk * kParts + i / kEach) * kPart + (kSmallGroups ? (lane / kRows * kEach + i % kEach) * 32 : 0);
-    const int g = min(k >> p.group_shift, p.groups - 1);  // (weights past the row's end meet zeros of x)
+    const int step = GS == 4 ? 0 : (lane / kRows * kEach + i % kEach) * GS;
+    const int g = min(((part + i / kEach) * kPart + step * 32) >> p.group_shift, p.groups - 1);  // (past the row's end x is zero)
     if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(row_scales) + g);
     else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(row_scales) + g);
     if (kZeros) c.z[i] = __ldg(row_zeros + g);
   }
 }
 
-// Rows off 16 bytes: starts the copies of the words that hold the lane's 16 bytes of rows
-// g, g + 8, ... of a part.  Nothing is read past the weights' end or for rows past the
-// last: those bytes are filled with zeros.
-template <int R>
-__device__ __forceinline__ void copy_words(const W4Params& p, uint32_t to, int tile, int part, int lane) {
-  const int64_t n = (int64_t)tile * (8 * R) + (lane >> 2);
-  const int off = part * (kPart / 2) + (lane & 3) * 16;
+// Adds the products of a part of 16 rows (lo and hi: a lane's words of rows g and g + 8 by step)
+// to their sums.  s: the groups' scales of those rows; z: their zeros, a byte each.
+template <int NT, int GS, bool kZeros>
+__device__ __forceinline__ void multiply_rows(const uint32_t (&lo)[4], const uint32_t (&hi)[4], const float (&s0)[4 / GS],
+                                              const float (&s1)[4 / GS], uint32_t z0, uint32_t z1, const uint8_t* xs, int unit,
+                                              bool has_x, float (&acc)[NT][4], uint32_t magic) {
 #pragma unroll
-  for (int h = 0; h < R; ++h) {
-    const bool has = n + 8 * h < p.n && off < (int)p.row_bytes;
-    const int64_t at = (has ? (n + 8 * h) * p.row_bytes + off : 0) & ~int64_t(3);
-#pragma unroll
-    for (int i = 0; i < 5; ++i) {
-      const int64_t left = p.total_bytes - (at + 4 * i);
-      const int bytes = !has || left <= 0 ? 0 : left < 4 ? (int)left : 4;
-      copy4(to + h * 640 + i * 128 + lane * 4, p.w + (bytes ? at + 4 * i : 0), bytes);
+  for (int g = 0; g < 4 / GS; ++g) {
+    uint32_t b0 = 0x43084308u, b1 = 0x43084308u;
+    if (kZeros) {
+      b0 = 0x43004300u + 0x00010001u * (z0 >> (8 * g) & 15u);
+      b1 = 0x43004300u + 0x00010001u * (z1 >> (8 * g) & 15u);
     }
-  }
-}
-
-// A lane's 32 weights of row h out of the ring.  `shift`: bits that the row's bytes lie past a word's start.
-template <bool kAligned>
-__device__ __forceinline__ uint4 chunk_row(const uint8_t* slot, int h, uint32_t shift, int lane) {
-  if (kAligned) return *reinterpret_cast<const uint4*>(slot + h * 512 + lane * 16);
-  uint32_t u[5];
+    float sum[NT][4];
 #pragma unroll
-  for (int i = 0; i < 5; ++i) u[i] = *reinterpret_cast<const uint32_t*>(slot + h * 640 + i * 128 + lane * 4);
-  return make_uint4(__funnelshift_r(u[0], u[1], shift), __funnelshift_r(u[1], u[2], shift),
-                    __funnelshift_r(u[2], u[3], shift), __funnelshift_r(u[3], u[4], shift));
-}
-
-// The quad's 4 x 4 words transposed: lane t gets word t of each of its lanes.
-__device__ __forceinline__ void transpose_quad(uint4& v, int t) {
-  uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  const bool odd = t & 1, high = t & 2;
+    for (int s = 0; s < GS; ++s) {
+      const int j = g * GS + s;
+      uint32_t a[4], b[4];
 #pragma unroll
-  for (int i = 0; i < 4; i += 2) {  // words i and i + 1 with lane ^ 1
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? w[i] : w[i + 1], 1);
-    (odd ? w[i] : w[i + 1]) = other;
-  }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {  // words i and i + 2 with lane ^ 2
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, high ? w[i] : w[i + 2], 2);
-    (high ? w[i] : w[i + 2]) = other;
-  }
-  v = make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// Adds the products of 16 rows' chunk (a lane's weights of rows g and g + 8, rows `sub` ..
-// of the tile) to their sums.  s and z: the tile's scales and biases by lane, the chunk's part's
-// from `first` on.
-template <int NT, int kRows, int NL, bool kSmallGroups, bool kZeros>
-__device__ __forceinline__ void multiply_rows(uint4 q0, uint4 q1, const float (&s)[NL], const uint32_t (&z)[kZeros ? NL : 1],
-                                              int first, int sub, const uint8_t* xs, float (&acc)[NT][4], uint32_t magic, int lane) {
-  if (kSmallGroups) {
-    transpose_quad(q0, lane & 3);
-    transpose_quad(q1, lane & 3);
-  }
-  float sum[NT][4], t0 = 0.f, t1 = 0.f;
-  uint32_t b0 = 0x43084308u, b1 = 0x43084308u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t lo = j == 0 ? q0.x : j == 1 ? q0.y : j == 2 ? q0.z : q0.w;
-    const uint32_t hi = j == 0 ? q1.x : j == 1 ? q1.y : j == 2 ? q1.z : q1.w;
-    if (kSmallGroups || j == 0) {
-      constexpr int kEach = NL / kParts<NT>;
-      const int from = sub + (lane >> 2) + (kSmallGroups ? j / kEach * kRows : 0), i = first + (kSmallGroups ? j % kEach : 0);
-      t0 = __shfl_sync(0xffffffffu, s[i], from);
-      t1 = __shfl_sync(0xffffffffu, s[i], from + 8);
-      if (kZeros) {
-        b0 = __shfl_sync(0xffffffffu, z[kZeros ? i : 0], from);
-        b1 = __shfl_sync(0xffffffffu, z[kZeros ? i : 0], from + 8);
+      for (int q = 0; q < 4; ++q) {
+        a[q] = weights2(lo[j], q, magic, b0);
+        b[q] = weights2(hi[j], q, magic, b1);
       }
-    }
-    uint32_t a[4], b[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      a[q] = weights2(lo, q, magic, b0);
-      b[q] = weights2(hi, q, magic, b1);
+      for (int i = 0; i < NT; ++i) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (NT > 1 || has_x) x = *reinterpret_cast<const uint4*>(xs + (j * NT + i) * unit);
+        if (s == 0) mma16816_first(sum[i], a[0], b[0], a[1], b[1], x.x, x.y);
+        else mma16816(sum[i], a[0], b[0], a[1], b[1], x.x, x.y);
+        mma16816(sum[i], a[2], b[2], a[3], b[3], x.z, x.w);
+      }
     }
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-      if (kSmallGroups || j == 0)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[i][e] = 0.f;
-      const uint4 x = *reinterpret_cast<const uint4*>(xs + (j * NT + i) * kUnit + lane * 16);
-      mma16816(sum[i], a[0], b[0], a[1], b[1], x.x, x.y);
-      mma16816(sum[i], a[2], b[2], a[3], b[3], x.z, x.w);
-      if (kSmallGroups || j == 3) {
-        acc[i][0] = fmaf(t0, sum[i][0], acc[i][0]);
-        acc[i][1] = fmaf(t0, sum[i][1], acc[i][1]);
-        acc[i][2] = fmaf(t1, sum[i][2], acc[i][2]);
-        acc[i][3] = fmaf(t1, sum[i][3], acc[i][3]);
-      }
+      acc[i][0] = fmaf(s0[g], sum[i][0], acc[i][0]);
+      acc[i][1] = fmaf(s0[g], sum[i][1], acc[i][1]);
+      acc[i][2] = fmaf(s1[g], sum[i][2], acc[i][2]);
+      acc[i][3] = fmaf(s1[g], sum[i][3], acc[i][3]);
     }
   }
 }
 
-// A block of x into shared memory, 8 numbers a lane and step, in the order of the nibbles.
-template <int NT, bool kSmallGroups>
+// A block of x into shared memory: for every part and step the 8 numbers of each row and lane
+// of a quad, in the order of the nibbles; x_rows rows (a power of two up to 8) of every 8.
+template <int NT, bool kTurned>
 __device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int part0, int parts, int m0) {
   constexpr int kThreads = kWarps * 32, kBatch = 8;  // (loads in flight)
-  const int units = parts * 4 * NT * 32;
+  const int lanes = 2 + p.x_shift;                   // log2 of the lanes that have x
+  const int units = (parts * 4 * NT) << lanes;
   for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kBatch) {
     uint4 r[kBatch];
 #pragma unroll
     for (int f = 0; f < kBatch; ++f) {
-      const int u = u0 + f * kThreads;
-      const int lane = u & 31, i = (u >> 5) % NT, j = (u >> 5) / NT & 3, c = (u >> 5) / (NT * 4);
-      const int t = lane & 3, m = m0 + i * 8 + (lane >> 2);
-      const int k = (part0 + c) * kPart + (kSmallGroups ? j * 32 + t * 8 : t * 32 + j * 8);
+      const int u = u0 + f * kThreads, v = u >> lanes;
+      const int i = v % NT, j = v / NT & 3, c = v / (NT * 4);
+      const int t = u & 3, m = m0 + i * 8 + (u >> 2 & ((1 << p.x_shift) - 1));
+      const int k = (part0 + c) * kPart + (kTurned ? j * 32 + t * 8 : t * 32 + j * 8);
       r[f] = make_uint4(0, 0, 0, 0);
       if (u < units && m < p.m && k < p.k) {
         const uint16_t* src = p.x + (int64_t)m * p.k + k;
@@ -246,33 +209,24 @@ __device__ __forceinline__ void group_barrier(int group, int warps) {
   asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
 }
 
-// Shared memory: the warps' rings, every warp's sums of a tile, the sums kept between blocks of k, x.
-template <int NT, bool kAligned>
-struct Layout {
-  static constexpr int kRows = 16 * kSub<NT>;   // of a tile
-  static constexpr int kSums = kRows * 8 * NT;
-  static constexpr int kJoin = kWarps * kSums * 4;
-  static constexpr int kPartBytes = 2 * kSub<NT> * kPiece<kAligned>;
-  static constexpr int kSlot = kParts<NT> * kPartBytes;
-  static constexpr int kRing = kWarps * kAhead<NT> * kSlot;
-};
-
-template <int NT, bool kSmallGroups, bool kAligned, bool kZeros>
+template <int NT, int GS, bool kAligned, bool kZeros>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
-  using L = Layout<NT, kAligned>;
+  using L = Layout<NT, GS, kAligned>;
+  constexpr bool kTurned = GS < 4 || !kAligned;  // a quad's words are of the same 16 bytes
   constexpr int kSums = L::kSums, kRows = L::kRows, R = kRows / 8, A = kAhead<NT>, P = kParts<NT>;
-  constexpr int NL = P * (kSmallGroups ? kRows / 8 : 1);
-  extern __shared__ __align__(128) uint8_t dyn[];
+  constexpr int kEach = GS == 4 ? 1 : L::kGroups * kRows / 32, NL = P * kEach;  // scales of a lane and part, and chunk
+  extern __shared__ __align__(1024) uint8_t dyn[];
   __shared__ uint64_t landed[kWarps][A];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane & 3;
   const int S = p.split, groups = kWarps / S, group = warp / S, member = warp % S;
   const uint8_t* ring = dyn + warp * A * L::kSlot;
-  float* part = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;                   // [S][kSums]
-  float* kept = reinterpret_cast<float*>(dyn + L::kRing + L::kJoin) + group * p.batch * kSums;  // [batch][kSums]
-  uint8_t* xs = dyn + L::kRing + L::kJoin + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
-  if (kAligned && lane == 0) {
+  float* join = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;  // [S][kSums]
+  float* scales = reinterpret_cast<float*>(dyn + L::kRing + L::kJoin + warp * L::kScales);  // [P][kRows][kGroups]
+  float* kept = reinterpret_cast<float*>(dyn + L::kFixed) + group * p.batch * kSums;        // [batch][kSums]
+  uint8_t* xs = dyn + L::kFixed + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
+  if (lane == 0) {
 #pragma unroll
-    for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], 1);
+    for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], kAligned ? 1 : kRows);
     fence_mbar_init();
     fence_proxy_async_smem();
   }
@@ -286,9 +240,22 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   const int most = (int)blockIdx.x < tiles ? (tiles - (int)blockIdx.x + stride - 1) / stride : 0;  // of any group here
   const int scale_shift = p.scale_bytes == 2 ? 16 : 0;
   const uint32_t ring_at = smem_u32(ring), magic = exponent_bits();
-  uint32_t parity = 0;  // of each slot's barrier
+  const int unit = 64 << p.x_shift;                                            // bytes of x of a step and 8 rows
+  const bool has_x = (lane >> 2) < (1 << p.x_shift);
+  const uint8_t* my_x = xs + (has_x ? lane * 16 : 0);
+  // where a lane's words of a part lie: of row g, by step
+  uint32_t word_at[4], cut[R];
+  {
+    const int g = lane >> 2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) word_at[j] = kAligned ? g * 64 + ((j ^ (g >> 1 & 3)) << 4) + t * 4 : g * L::kPitch + j * 16 + t * 4;
+#pragma unroll
+    for (int h = 0; h < R; ++h)  // (rows off 16 bytes: where their first byte lies in its vector; tiles start on one)
+      cut[h] = kAligned ? 0 : (uint32_t)(((int64_t)(g + 8 * h) * p.row_bytes) & 15);
+  }
+  uint32_t parity = 0;       // of each slot's barrier
   int flying = 0, lost = 0;  // copies on their way, and the slot of the oldest once a wait has given up
-  bool alive = true;    // no wait has given up
+  bool alive = true;         // no wait has given up
   for (int m0 = 0; m0 < p.m; m0 += 8 * NT) {
     for (int first = 0; first < most; first += p.batch) {
       const int batch = max(0, min(p.batch, mine - first));
@@ -309,20 +276,31 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
         at_row();
         auto load = [&](Scales<NL, kZeros>& into, int s) {
           if (lt < batch && lc < chunks) {
-            if (!kAligned) {
-              for (int c2 = 0; c2 < P; ++c2)
-                copy_words<R>(p, ring_at + s * L::kSlot + c2 * L::kPartBytes, load_tile, (chunk0 + lc) * P + c2, lane);
-            } else if (lane == 0 && alive) {
-              mbar_arrive_expect_tx(&landed[warp][s], L::kSlot);
+            const int part = (chunk0 + lc) * P;
+            if (alive) {
+              ++flying;
+              if (kAligned && lane == 0) {
+                mbar_arrive_expect_tx(&landed[warp][s], L::kSlot);
 #pragma unroll
-              for (int c2 = 0; c2 < P; ++c2)  // (a part past the row's end is filled with zeros)
-                copy_box(ring_at + s * L::kSlot + c2 * L::kPartBytes, &map, ((chunk0 + lc) * P + c2) * (kPart / 2),
-                         load_tile * kRows, &landed[warp][s]);
+                for (int c2 = 0; c2 < P; ++c2)  // (what lies past a row's end or the last row is filled with zeros)
+                  copy_box(ring_at + s * L::kSlot + c2 * kRows * 64, &map, (part + c2) * (kPart / 2), load_tile * kRows,
+                           &landed[warp][s]);
+              }
+              if (!kAligned && lane < kRows) {
+                // the vectors that hold the row's part, as far as they lie within the weights; the last
+                // bytes of those by themselves
+                const int64_t n = (int64_t)load_tile * kRows + lane;
+                const int64_t from = (n * p.row_bytes + (int64_t)part * (kPart / 2)) & ~int64_t(15);
+                const int64_t to = n < p.n && (int64_t)part * (kPart / 2) < p.row_bytes ? min(from + L::kPitch, p.total_bytes) : from;
+                const int64_t whole = max(from, min(to, p.total_bytes & ~int64_t(15)));
+                uint8_t* dst = const_cast<uint8_t*>(ring) + s * L::kSlot + lane * L::kPitch;
+                if (whole > from) bulk_load(dst, p.w + from, (uint32_t)(whole - from), &landed[warp][s]);
+                for (int64_t b = whole; b < to; ++b) dst[b - from] = p.w[b];
+                mbar_arrive_expect_tx(&landed[warp][s], (uint32_t)(whole - from));
+              }
             }
-            if (kAligned && alive) ++flying;
-            load_scales<kRows, P, NL, kSmallGroups, kZeros>(p, into, row_scales, row_zeros, chunk0 + lc, lane);
+            load_scales<kRows, kEach, GS, NL, kZeros>(p, into, row_scales, row_zeros, part, lane);
           }
-          if (!kAligned) asm volatile("cp.async.commit_group;" ::: "memory");
           lc += S;
           if (lc < chunks) return;
           lc = member;
@@ -334,7 +312,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
         for (int s = 0; s < A; ++s) load(c[s], s);
         if (p.blocks > 1 || first == 0) {
           __syncthreads();  // (the x of the block before is no longer read)
-          stage_x<NT, kSmallGroups>(p, xs, chunk0 * P, chunks * P, m0);
+          stage_x<NT, kTurned>(p, xs, chunk0 * P, chunks * P, m0);
           __syncthreads();
         }
         float acc[kSub<NT>][NT][4] = {};
@@ -344,43 +322,76 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
           for (int s = 0; s < A; ++s) {
             if (it + s >= items) break;
             if (at < chunks) {
-              uint32_t shift = 0;  // (the same for all of a lane's rows, which are 8 apart)
-              if (kAligned) {
-                if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
-                  if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
-                  alive = false;  // (no more copies; those on their way are waited for at the end)
-                  lost = s;
-                }
-                if (alive) {
-                  parity ^= 1u << s;
-                  --flying;
-                }
-              } else {
-                asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copies of the chunk have landed
-                shift = (uint32_t)(((int64_t)(tile0 + (first + tile) * stride) * kRows + (lane >> 2)) * p.row_bytes & 3) * 8;
+              if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
+                if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
+                alive = false;  // (no more copies; those on their way are waited for at the end)
+                lost = s;
               }
-              uint4 q[P][R];
+              if (alive) {
+                parity ^= 1u << s;
+                --flying;
+              }
+              uint32_t q[P][R][4];
 #pragma unroll
               for (int c2 = 0; c2 < P; ++c2)
 #pragma unroll
-                for (int h = 0; h < R; ++h)
-                  q[c2][h] = chunk_row<kAligned>(ring + s * L::kSlot + c2 * L::kPartBytes, h, shift, lane);
+                for (int h = 0; h < R; ++h) {
+                  const uint8_t* slot = ring + s * L::kSlot;
+                  if (!kTurned) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(slot + c2 * kRows * 64 + h * 512 + lane * 16);
+                    q[c2][h][0] = v.x, q[c2][h][1] = v.y, q[c2][h][2] = v.z, q[c2][h][3] = v.w;
+                  } else if (kAligned) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                      q[c2][h][j] = *reinterpret_cast<const uint32_t*>(slot + c2 * kRows * 64 + h * 512 + word_at[j]);
+                  } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                      const uint32_t* w = reinterpret_cast<const uint32_t*>(slot + c2 * 64 + h * 8 * L::kPitch + word_at[j] + (cut[h] & ~3u));
+                      q[c2][h][j] = __funnelshift_r(w[0], w[1], 8 * (cut[h] & 3));
+                    }
+                  }
+                }
+              // the lane's scales, as numbers; where groups are small through shared memory to the lanes of the rows
               float sc[NL];
-              uint32_t z[kZeros ? NL : 1];
+              uint32_t z[P] = {};
 #pragma unroll
               for (int i = 0; i < NL; ++i) {
                 sc[i] = __uint_as_float(c[s].s[i] << scale_shift);
-                if (kZeros) z[i] = 0x43004300u + 0x00010001u * (c[s].z[i] & 15u);
+                if (kZeros) z[i / kEach] |= (c[s].z[i] & 15u) << (8 * ((kRows == 32 || GS == 4 ? 0 : lane / kRows * kEach) + i % kEach));
               }
+              if (GS < 4) {
+#pragma unroll
+                for (int i = 0; i < NL; ++i)
+                  scales[(i / kEach * kRows + lane % kRows) * L::kGroups + lane / kRows * kEach + i % kEach] = sc[i];
+              }
+              if (kZeros && kRows == 16 && GS < 4)
+#pragma unroll
+                for (int c2 = 0; c2 < P; ++c2) z[c2] |= __shfl_xor_sync(0xffffffffu, z[c2], 16);
               __syncwarp();
               load(c[s], s);  // (over what the warp has just read)
 #pragma unroll
               for (int c2 = 0; c2 < P; ++c2)
 #pragma unroll
-                for (int b = 0; b < kSub<NT>; ++b)
-                  multiply_rows<NT, kRows, NL, kSmallGroups, kZeros>(q[c2][2 * b], q[c2][2 * b + 1], sc, z, c2 * (NL / P), 16 * b,
-                                                                     xs + (int64_t)(at * P + c2) * 4 * NT * kUnit, acc[b],
-                                                                     magic, lane);
+                for (int b = 0; b < kSub<NT>; ++b) {
+                  const int row = 16 * b + (lane >> 2);
+                  float s0[L::kGroups], s1[L::kGroups];
+                  if (GS == 4) {
+                    s0[0] = __shfl_sync(0xffffffffu, sc[c2], row);
+                    s1[0] = __shfl_sync(0xffffffffu, sc[c2], row + 8);
+                  } else {
+#pragma unroll
+                    for (int g = 0; g < L::kGroups; ++g) {
+                      s0[g] = scales[(c2 * kRows + row) * L::kGroups + g];
+                      s1[g] = scales[(c2 * kRows + row + 8) * L::kGroups + g];
+                    }
+                  }
+                  const uint32_t z0 = kZeros ? __shfl_sync(0xffffffffu, z[c2], row) : 0;
+                  const uint32_t z1 = kZeros ? __shfl_sync(0xffffffffu, z[c2], row + 8) : 0;
+                  multiply_rows<NT, GS, kZeros>(q[c2][2 * b], q[c2][2 * b + 1], s0, s1, z0, z1,
+                                                my_x + (int64_t)(at * P + c2) * 4 * NT * unit, unit, has_x, acc[b], magic);
+                }
+              if (GS < 4) __syncwarp();  // (the scales have been read)
             } else {
               load(c[s], s);
             }
@@ -388,7 +399,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
             if (at < chunks) continue;
             // the tile's sums: this warp's, once the group has read those of the tile before, then all of them
             group_barrier(group, S);
-            float* mp = part + member * kSums + (lane & 3) * 2 * kRows + (lane >> 2);
+            float* mp = join + member * kSums + t * 2 * kRows + (lane >> 2);
 #pragma unroll
             for (int b = 0; b < kSub<NT>; ++b)
 #pragma unroll
@@ -402,7 +413,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
             for (int o = member * 32 + lane; o < kSums; o += S * 32) {
               float v = kb > 0 ? kept[tile * kSums + o] : 0.f;
 #pragma unroll 4
-              for (int w = 0; w < S; ++w) v += part[w * kSums + o];
+              for (int w = 0; w < S; ++w) v += join[w * kSums + o];
               if (kb + 1 < p.blocks) {
                 kept[tile * kSums + o] = v;
                 continue;
@@ -420,25 +431,26 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
       }
     }
   }
-  if (!kAligned) asm volatile("cp.async.wait_all;" ::: "memory");
   if (!alive)
     for (int i = 0; i < flying; ++i) mbar_wait(&landed[warp][(lost + i) % A], (parity >> (lost + i) % A) & 1u);
 }
 
-template <int NT, bool kSmallGroups, bool kAligned, bool kZeros>
+template <int NT, int GS, bool kAligned, bool kZeros>
 int launch_w4_as(W4Params& p, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
-  using L = Layout<NT, kAligned>;
-  auto k = w4_kernel<NT, kSmallGroups, kAligned, kZeros>;
+  using L = Layout<NT, GS, kAligned>;
+  auto k = w4_kernel<NT, GS, kAligned, kZeros>;
   if (int rc = ensure_smem(k, kW4Smem, done)) return rc;
   constexpr int W = kWarps, sms = 152;
-  constexpr int sums = L::kSums * 4;        // bytes
-  constexpr int x_bytes = 4 * kParts<NT> * NT * kUnit;  // of a chunk
-  constexpr int room = kW4Smem - L::kJoin - L::kRing;
+  constexpr int sums = L::kSums * 4;  // bytes
+  constexpr int room = kW4Smem - L::kFixed;
+  static_assert(room / 4 >= W / 4 * sums, "a tile of each group must be kept");
+  static_assert(room - room / 4 >= 4 * 4 * kParts<NT> * NT * 512, "a block of k must fit");
+  // rows of x that are kept of every 8: a power of two
+  p.x_shift = NT > 1 || p.m > 4 ? 3 : p.m > 2 ? 2 : p.m > 1 ? 1 : 0;
+  const int x_bytes = 4 * kParts<NT> * NT * (64 << p.x_shift);  // of a chunk
   const int tiles = (p.n + L::kRows - 1) / L::kRows;
   const int chunks = (p.k + kChunk<NT> - 1) / kChunk<NT>;
-  static_assert(room / 4 >= W / 4 * sums, "a tile of each group must be kept");
-  static_assert(room - room / 4 >= x_bytes * 4, "a block of k must fit");
   // (a block of a group's width of k has to fit)
   int S = tiles <= sms ? W : tiles <= 4 * sms ? 8 : 4;
   while (S * x_bytes > room - room / 4) S /= 2;
@@ -448,14 +460,14 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
   p.blocks = 1;
   p.block_chunks = whole;
   p.batch = 0x3fffffff;
-  int smem = L::kJoin + L::kRing + whole * x_bytes;
+  int smem = L::kFixed + whole * x_bytes;
   if (whole > room / x_bytes) {  // blocks of k, as even as they come: a quarter of the room keeps sums
     p.batch = std::max(1, room / 4 / (groups * sums));
     const int fits = (room - p.batch * groups * sums) / (x_bytes * S) * S;
     p.blocks = (chunks + fits - 1) / fits;
     p.block_chunks = ((chunks + p.blocks - 1) / p.blocks + S - 1) / S * S;
     p.blocks = (chunks + p.block_chunks - 1) / p.block_chunks;
-    smem = L::kJoin + L::kRing + p.batch * groups * sums + p.block_chunks * x_bytes;
+    smem = L::kFixed + p.batch * groups * sums + p.block_chunks * x_bytes;
   }
   CUtensorMap map = {};
   if (kAligned) {
@@ -464,24 +476,23 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
     const cuuint64_t dims[2] = {(cuuint64_t)p.row_bytes, (cuuint64_t)p.n}, strides[1] = {(cuuint64_t)p.row_bytes};
     const cuuint32_t box[2] = {kPart / 2, L::kRows}, ones[2] = {1, 1};
     const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p.w), dims, strides, box, ones,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, GS == 4 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   }
   const cudaError_t e = launch_dependent(k, std::min(tiles, sms), W * 32, smem, st, p, map);
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "w4 launch");
 }
 
-template <int NT, bool kSmallGroups, bool kAligned>
-int launch_w4_zeros(W4Params& p, cudaStream_t st) {
-  return p.zeros ? launch_w4_as<NT, kSmallGroups, kAligned, true>(p, st)
-                 : launch_w4_as<NT, kSmallGroups, kAligned, false>(p, st);
+template <int NT, int GS>
+int launch_w4_steps(W4Params& p, cudaStream_t st) {
+  if (p.row_bytes % 16 == 0) return p.zeros ? launch_w4_as<NT, GS, true, true>(p, st) : launch_w4_as<NT, GS, true, false>(p, st);
+  return p.zeros ? launch_w4_as<NT, GS, false, true>(p, st) : launch_w4_as<NT, GS, false, false>(p, st);
 }
 template <int NT>
 int launch_w4(W4Params& p, cudaStream_t st) {
-  const bool small = p.group_shift < 7, aligned = p.row_bytes % 16 == 0;
-  if (small) return aligned ? launch_w4_zeros<NT, true, true>(p, st) : launch_w4_zeros<NT, true, false>(p, st);
-  return aligned ? launch_w4_zeros<NT, false, true>(p, st) : launch_w4_zeros<NT, false, false>(p, st);
+  return p.group_shift == 5 ? launch_w4_steps<NT, 1>(p, st)
+                            : p.group_shift == 6 ? launch_w4_steps<NT, 2>(p, st) : launch_w4_steps<NT, 4>(p, st);
 }
 
 }  // namespace
