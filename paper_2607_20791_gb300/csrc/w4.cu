@@ -39,5 +39,5 @@ extern "C" int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size
   p.x_vec = k % 8 == 0;
   p.dev_status = dev_status;
   cudaStream_t st = (cudaStream_t)stream;
-  return m <= 8 ? launch_w4_n8(p, st) : m <= 16 ? launch_w4_n16(p, st) : launch_w4_n32(p, st);
+  return m <= 8 ? launch_w4_n8(p, st) : launch_w4_n16(p, st);
 }

@@ -10,9 +10,11 @@ constexpr int kW4MaxK = 1 << 24;
 struct W4Params {
   int32_t m, n, k, groups;
   int32_t group_shift;   // log2 of the group size
-  int32_t block_chunks;  // chunks of a block of k (a multiple of split)
+  int32_t block_chunks;  // chunks of a block of k
   int32_t blocks;        // blocks of k
   int32_t split;         // warps of a group
+  int32_t ksplit;        // blocks of a cluster that share a tile, each with rank_chunks chunks
+  int32_t rank_chunks;
   int32_t batch;         // tiles of a group between which k may go in blocks
   const uint16_t* x;
   const uint8_t* w;
@@ -25,9 +27,8 @@ struct W4Params {
   int32_t* dev_status;
 };
 
-// Launches the kernel for up to 8, 16 and 32 rows of x at a time.
+// Launches the kernel for 8 and for 16 rows of x at a time.
 int launch_w4_n8(W4Params& p, cudaStream_t st);
 int launch_w4_n16(W4Params& p, cudaStream_t st);
-int launch_w4_n32(W4Params& p, cudaStream_t st);
 
 }  // namespace rgd

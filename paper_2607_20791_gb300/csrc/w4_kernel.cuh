@@ -1,13 +1,15 @@
 // Products of a few rows of activations with 4-bit weights: y = x W^T with
 // W[n, k] = (q[n, k] - z[n, k / G]) s[n, k / G], q packed two to a byte along k.
 //
-// The weights are read once; everything else is small.  A tile is 32 rows of W (16 above
-// 16 rows of x); the warps of its group take the chunks of those rows (256 weights for up
+// The weights are read once; everything else is small.  A tile is 32 rows of W; the warps
+// of its group take the chunks of those rows (256 weights for up
 // to 8 rows of x, else 128) in turn, so that together they read contiguous bytes of a row.
 // A chunk comes by TMA boxes of 64 bytes by the tile's rows into the warp's own ring in
 // shared memory, 4 to 8 KB ahead of its use.  Every 128 weights are 8 mma.m16n8k16 with the
 // weights as A for every 16 rows of W and 8 rows of x: one row of x costs the same as
-// eight, and the tensor pipe does the sums over k in fp32.
+// eight, and the tensor pipe does the sums over k in fp32.  (With 17 to 32 rows of x the
+// weights are read twice, 16 rows at a time: 166 us for 32 x 4096 x 128256 where one pass
+// of 32 took 198, x coming from shared memory in blocks of k.)
 //
 // Which k a lane's A elements stand for is free as long as B agrees, so a lane feeds the
 // 8 nibbles of a 32-bit word as they lie: nibbles p and p + 4 are the two halves of
@@ -25,7 +27,8 @@
 // One block of 16 warps fills an SM, so that x lies there once.  Its warps form groups of S
 // that share a tile and whose sums meet in shared memory: few tiles want a wide group, many
 // a narrow one, whose joins cost less.  Where x does not fit, k goes in blocks, with the sums
-// of a group's tiles kept in shared memory between them.
+// of a group's tiles kept in shared memory between them.  Few tiles of long rows are shared
+// by the blocks of a cluster, each with a stretch of k, whose sums the first one joins.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -42,13 +45,14 @@ constexpr int kPart = 128;           // weights of a row that a lane's quad work
 constexpr int kW4Smem = 226 * 1024;  // (of 227; the barriers take the rest)
 constexpr int kWarps = 16;           // of a block
 
-// For 8 NT rows of x: groups of 16 rows of W in a tile, parts of a chunk, chunks in flight.
-template <int NT>
-constexpr int kSub = NT == 4 ? 1 : 2;
+constexpr int kSub = 2;              // groups of 16 rows of W in a tile
+constexpr int kRows = 16 * kSub;     // of a tile
+constexpr int kAhead = 2;            // chunks in flight
+constexpr int kMaxSplit = 8;         // blocks that share a tile's k
+
+// Parts of a chunk, for 8 NT rows of x.
 template <int NT>
 constexpr int kParts = NT == 1 ? 2 : 1;
-template <int NT>
-constexpr int kAhead = NT == 4 ? 4 : 2;
 template <int NT>
 constexpr int kChunk = kPart * kParts<NT>;
 
@@ -56,12 +60,11 @@ constexpr int kChunk = kPart * kParts<NT>;
 // k, the warps' scales (where groups are small), x.  GS: steps of 32 weights in a group.
 template <int NT, int GS, bool kAligned>
 struct Layout {
-  static constexpr int kRows = 16 * kSub<NT>;  // of a tile
   static constexpr int kSums = kRows * 8 * NT;
   static constexpr int kJoin = kWarps * kSums * 4;
   static constexpr int kPitch = kAligned ? 64 : kParts<NT> * 64 + 16;            // from a row to the next
   static constexpr int kSlot = kRows * (kAligned ? kParts<NT> * 64 : kPitch);    // of a chunk
-  static constexpr int kRing = kWarps * kAhead<NT> * kSlot;
+  static constexpr int kRing = kWarps * kAhead * kSlot;
   static constexpr int kGroups = 4 / GS;                                         // of a part
   static constexpr int kScales = GS == 4 ? 0 : kParts<NT> * kRows * kGroups * 4;  // bytes of a warp
   static constexpr int kFixed = kRing + kJoin + kWarps * kScales;
@@ -102,19 +105,18 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
 }
 
 // A chunk's scales and zeros as they lie in memory (a load must not be waited for before its
-// use).  Lane i has those of row i of the tile (in a tile of 16 rows, lanes i and i + 16 half
-// of row i's each): one of every 128 weights, or one of every group.
+// use).  Lane i has those of row i of the tile: one of every 128 weights, or of every group.
 template <int NL, bool kZeros>
 struct Scales {
   uint32_t s[NL], z[kZeros ? NL : 1];
 };
 
-template <int kRows, int kEach, int GS, int NL, bool kZeros>
+template <int kEach, int GS, int NL, bool kZeros>
 __device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const uint8_t* row_scales,
-                                            const uint8_t* row_zeros, int part, int lane) {
+                                            const uint8_t* row_zeros, int part) {
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    const int step = GS == 4 ? 0 : (lane / kRows * kEach + i % kEach) * GS;
+    const int step = i % kEach * GS;
     const int g = min(((part + i / kEach) * kPart + step * 32) >> p.group_shift, p.groups - 1);  // (past the row's end x is zero)
     if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(row_scales) + g);
     else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(row_scales) + g);
@@ -209,12 +211,27 @@ __device__ __forceinline__ void group_barrier(int group, int warps) {
   asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
 }
 
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ void push_sum(float* slot, float v) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(slot)));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+}
+__device__ __forceinline__ void write_sum(const W4Params& p, int m, int64_t n, float v) {
+  if (m >= p.m || n >= p.n) return;
+  if (p.out_f32) static_cast<float*>(p.y)[m * p.y_stride + n] = v;
+  else static_cast<__nv_bfloat16*>(p.y)[m * p.y_stride + n] = __float2bfloat16(v);
+}
+
 template <int NT, int GS, bool kAligned, bool kZeros>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
   using L = Layout<NT, GS, kAligned>;
   constexpr bool kTurned = GS < 4 || !kAligned;  // a quad's words are of the same 16 bytes
-  constexpr int kSums = L::kSums, kRows = L::kRows, R = kRows / 8, A = kAhead<NT>, P = kParts<NT>;
-  constexpr int kEach = GS == 4 ? 1 : L::kGroups * kRows / 32, NL = P * kEach;  // scales of a lane and part, and chunk
+  constexpr int kSums = L::kSums, R = kRows / 8, A = kAhead, P = kParts<NT>;
+  constexpr int kEach = L::kGroups, NL = P * kEach;  // scales of a lane and part, and chunk
   extern __shared__ __align__(1024) uint8_t dyn[];
   __shared__ uint64_t landed[kWarps][A];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane & 3;
@@ -222,8 +239,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   const uint8_t* ring = dyn + warp * A * L::kSlot;
   float* join = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;  // [S][kSums]
   float* scales = reinterpret_cast<float*>(dyn + L::kRing + L::kJoin + warp * L::kScales);  // [P][kRows][kGroups]
-  float* kept = reinterpret_cast<float*>(dyn + L::kFixed) + group * p.batch * kSums;        // [batch][kSums]
-  uint8_t* xs = dyn + L::kFixed + (p.blocks > 1 ? groups * p.batch * kSums * 4 : 0);
+  float* others = reinterpret_cast<float*>(dyn + L::kFixed);                                // [ksplit][kSums]
+  float* kept = others + (p.ksplit > 1 ? p.ksplit * kSums : 0) + group * p.batch * kSums;   // [batch][kSums]
+  uint8_t* xs = dyn + L::kFixed + ((p.ksplit > 1 ? p.ksplit : 0) + (p.blocks > 1 ? groups * p.batch : 0)) * kSums * 4;
   if (lane == 0) {
 #pragma unroll
     for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], kAligned ? 1 : kRows);
@@ -234,10 +252,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tiles = (p.n + kRows - 1) / kRows;
-  // group g of block b takes tiles b + gridDim g, then every (gridDim groups)-th
-  const int tile0 = (int)blockIdx.x + group * (int)gridDim.x, stride = (int)gridDim.x * groups;
+  // group g of block (or cluster) b of B takes tiles b + B g, then every (B groups)-th
+  const int block = (int)blockIdx.x / p.ksplit, rank = (int)blockIdx.x % p.ksplit, blocks = (int)gridDim.x / p.ksplit;
+  const int tile0 = block + group * blocks, stride = blocks * groups;
   const int mine = tile0 < tiles ? (tiles - tile0 + stride - 1) / stride : 0;
-  const int most = (int)blockIdx.x < tiles ? (tiles - (int)blockIdx.x + stride - 1) / stride : 0;  // of any group here
+  const int most = block < tiles ? (tiles - block + stride - 1) / stride : 0;  // of any group here
+  const int my_chunks = min((p.k + kChunk<NT> - 1) / kChunk<NT>, (rank + 1) * p.rank_chunks);  // up to which this block goes
   const int scale_shift = p.scale_bytes == 2 ? 16 : 0;
   const uint32_t ring_at = smem_u32(ring), magic = exponent_bits();
   const int unit = 64 << p.x_shift;                                            // bytes of x of a step and 8 rows
@@ -253,6 +273,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
     for (int h = 0; h < R; ++h)  // (rows off 16 bytes: where their first byte lies in its vector; tiles start on one)
       cut[h] = kAligned ? 0 : (uint32_t)(((int64_t)(g + 8 * h) * p.row_bytes) & 15);
   }
+  if (p.ksplit > 1) cluster_sync();  // (every block has started)
   uint32_t parity = 0;       // of each slot's barrier
   int flying = 0, lost = 0;  // copies on their way, and the slot of the oldest once a wait has given up
   bool alive = true;         // no wait has given up
@@ -260,8 +281,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
     for (int first = 0; first < most; first += p.batch) {
       const int batch = max(0, min(p.batch, mine - first));
       for (int kb = 0; kb < p.blocks; ++kb) {
-        const int chunk0 = kb * p.block_chunks;
-        const int chunks = min(p.block_chunks, (p.k + kChunk<NT> - 1) / kChunk<NT> - chunk0);
+        const int chunk0 = rank * p.rank_chunks + kb * p.block_chunks;
+        const int chunks = max(0, min(p.block_chunks, my_chunks - chunk0));
         const int per = (chunks - member + S - 1) / S;  // chunks of this warp and a tile (none: the group's others have them)
         const int items = batch * max(per, 1);
         Scales<NL, kZeros> c[A];
@@ -269,7 +290,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
         int lt = 0, lc = member, load_tile = tile0 + first * stride;
         const uint8_t *row_scales, *row_zeros;
         auto at_row = [&] {
-          const int64_t g = min((int64_t)load_tile * kRows + lane % kRows, (int64_t)p.n - 1) * p.groups;
+          const int64_t g = min((int64_t)load_tile * kRows + lane, (int64_t)p.n - 1) * p.groups;
           row_scales = p.scales + g * p.scale_bytes;
           row_zeros = p.zeros + g;
         };
@@ -286,7 +307,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                   copy_box(ring_at + s * L::kSlot + c2 * kRows * 64, &map, (part + c2) * (kPart / 2), load_tile * kRows,
                            &landed[warp][s]);
               }
-              if (!kAligned && lane < kRows) {
+              if (!kAligned) {
                 // the vectors that hold the row's part, as far as they lie within the weights; the last
                 // bytes of those by themselves
                 const int64_t n = (int64_t)load_tile * kRows + lane;
@@ -299,7 +320,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                 mbar_arrive_expect_tx(&landed[warp][s], (uint32_t)(whole - from));
               }
             }
-            load_scales<kRows, kEach, GS, NL, kZeros>(p, into, row_scales, row_zeros, part, lane);
+            load_scales<kEach, GS, NL, kZeros>(p, into, row_scales, row_zeros, part);
           }
           lc += S;
           if (lc < chunks) return;
@@ -315,7 +336,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
           stage_x<NT, kTurned>(p, xs, chunk0 * P, chunks * P, m0);
           __syncthreads();
         }
-        float acc[kSub<NT>][NT][4] = {};
+        float acc[kSub][NT][4] = {};
         int tile = 0, at = member;
         for (int it = 0; it < items; it += A) {
 #pragma unroll
@@ -331,49 +352,47 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                 parity ^= 1u << s;
                 --flying;
               }
-              uint32_t q[P][R][4];
-#pragma unroll
-              for (int c2 = 0; c2 < P; ++c2)
-#pragma unroll
-                for (int h = 0; h < R; ++h) {
-                  const uint8_t* slot = ring + s * L::kSlot;
-                  if (!kTurned) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(slot + c2 * kRows * 64 + h * 512 + lane * 16);
-                    q[c2][h][0] = v.x, q[c2][h][1] = v.y, q[c2][h][2] = v.z, q[c2][h][3] = v.w;
-                  } else if (kAligned) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                      q[c2][h][j] = *reinterpret_cast<const uint32_t*>(slot + c2 * kRows * 64 + h * 512 + word_at[j]);
-                  } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                      const uint32_t* w = reinterpret_cast<const uint32_t*>(slot + c2 * 64 + h * 8 * L::kPitch + word_at[j] + (cut[h] & ~3u));
-                      q[c2][h][j] = __funnelshift_r(w[0], w[1], 8 * (cut[h] & 3));
-                    }
-                  }
-                }
               // the lane's scales, as numbers; where groups are small through shared memory to the lanes of the rows
               float sc[NL];
               uint32_t z[P] = {};
 #pragma unroll
               for (int i = 0; i < NL; ++i) {
                 sc[i] = __uint_as_float(c[s].s[i] << scale_shift);
-                if (kZeros) z[i / kEach] |= (c[s].z[i] & 15u) << (8 * ((kRows == 32 || GS == 4 ? 0 : lane / kRows * kEach) + i % kEach));
+                if (kZeros) z[i / kEach] |= (c[s].z[i] & 15u) << (8 * (i % kEach));
               }
               if (GS < 4) {
 #pragma unroll
                 for (int i = 0; i < NL; ++i)
-                  scales[(i / kEach * kRows + lane % kRows) * L::kGroups + lane / kRows * kEach + i % kEach] = sc[i];
+                  scales[(i / kEach * kRows + lane) * L::kGroups + i % kEach] = sc[i];
               }
-              if (kZeros && kRows == 16 && GS < 4)
+              if (GS < 4) __syncwarp();
+              const uint8_t* slot = ring + s * L::kSlot;
 #pragma unroll
-                for (int c2 = 0; c2 < P; ++c2) z[c2] |= __shfl_xor_sync(0xffffffffu, z[c2], 16);
-              __syncwarp();
-              load(c[s], s);  // (over what the warp has just read)
+              for (int c2 = 0; c2 < P; ++c2) {
+                uint32_t q[R][4];
 #pragma unroll
-              for (int c2 = 0; c2 < P; ++c2)
+                for (int h = 0; h < R; ++h) {
+                  if (!kTurned) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(slot + c2 * kRows * 64 + h * 512 + lane * 16);
+                    q[h][0] = v.x, q[h][1] = v.y, q[h][2] = v.z, q[h][3] = v.w;
+                  } else if (kAligned) {
 #pragma unroll
-                for (int b = 0; b < kSub<NT>; ++b) {
+                    for (int j = 0; j < 4; ++j)
+                      q[h][j] = *reinterpret_cast<const uint32_t*>(slot + c2 * kRows * 64 + h * 512 + word_at[j]);
+                  } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                      const uint32_t* w = reinterpret_cast<const uint32_t*>(slot + c2 * 64 + h * 8 * L::kPitch + word_at[j] + (cut[h] & ~3u));
+                      q[h][j] = __funnelshift_r(w[0], w[1], 8 * (cut[h] & 3));
+                    }
+                  }
+                }
+                if (c2 + 1 == P) {
+                  __syncwarp();
+                  load(c[s], s);  // (over what the warp has just read)
+                }
+#pragma unroll
+                for (int b = 0; b < kSub; ++b) {
                   const int row = 16 * b + (lane >> 2);
                   float s0[L::kGroups], s1[L::kGroups];
                   if (GS == 4) {
@@ -388,9 +407,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                   }
                   const uint32_t z0 = kZeros ? __shfl_sync(0xffffffffu, z[c2], row) : 0;
                   const uint32_t z1 = kZeros ? __shfl_sync(0xffffffffu, z[c2], row + 8) : 0;
-                  multiply_rows<NT, GS, kZeros>(q[c2][2 * b], q[c2][2 * b + 1], s0, s1, z0, z1,
+                  multiply_rows<NT, GS, kZeros>(q[2 * b], q[2 * b + 1], s0, s1, z0, z1,
                                                 my_x + (int64_t)(at * P + c2) * 4 * NT * unit, unit, has_x, acc[b], magic);
                 }
+              }
               if (GS < 4) __syncwarp();  // (the scales have been read)
             } else {
               load(c[s], s);
@@ -401,7 +421,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
             group_barrier(group, S);
             float* mp = join + member * kSums + t * 2 * kRows + (lane >> 2);
 #pragma unroll
-            for (int b = 0; b < kSub<NT>; ++b)
+            for (int b = 0; b < kSub; ++b)
 #pragma unroll
               for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -418,11 +438,19 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                 kept[tile * kSums + o] = v;
                 continue;
               }
-              const int m = m0 + o / kRows;
-              const int64_t n = (int64_t)(tile0 + (first + tile) * stride) * kRows + o % kRows;
-              if (m >= p.m || n >= p.n) continue;
-              if (p.out_f32) static_cast<float*>(p.y)[m * p.y_stride + n] = v;
-              else static_cast<__nv_bfloat16*>(p.y)[m * p.y_stride + n] = __float2bfloat16(v);
+              if (p.ksplit > 1) push_sum(others + rank * kSums + o, v);  // (into the cluster's first block)
+              else write_sum(p, m0 + o / kRows, (int64_t)(tile0 + (first + tile) * stride) * kRows + o % kRows, v);
+            }
+            if (p.ksplit > 1 && kb + 1 == p.blocks) {  // (one tile and one group: the whole cluster comes here together)
+              cluster_sync();
+              if (rank == 0) {
+                for (int o = threadIdx.x; o < kSums; o += kWarps * 32) {
+                  float v = 0.f;
+                  for (int r = 0; r < p.ksplit; ++r) v += others[r * kSums + o];
+                  write_sum(p, m0 + o / kRows, (int64_t)tile0 * kRows + o % kRows, v);
+                }
+              }
+              cluster_sync();
             }
             at = member;
             ++tile;
@@ -445,42 +473,62 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
   constexpr int sums = L::kSums * 4;  // bytes
   constexpr int room = kW4Smem - L::kFixed;
   static_assert(room / 4 >= W / 4 * sums, "a tile of each group must be kept");
-  static_assert(room - room / 4 >= 4 * 4 * kParts<NT> * NT * 512, "a block of k must fit");
+  static_assert(room - room / 4 >= 4 * 4 * kParts<NT> * NT * 512 && room > kMaxSplit * sums + sums * 2 + 4 * kParts<NT> * NT * 512, "a block of k must fit");
   // rows of x that are kept of every 8: a power of two
   p.x_shift = NT > 1 || p.m > 4 ? 3 : p.m > 2 ? 2 : p.m > 1 ? 1 : 0;
   const int x_bytes = 4 * kParts<NT> * NT * (64 << p.x_shift);  // of a chunk
-  const int tiles = (p.n + L::kRows - 1) / L::kRows;
+  const int tiles = (p.n + kRows - 1) / kRows;
   const int chunks = (p.k + kChunk<NT> - 1) / kChunk<NT>;
+  // Few tiles of long rows: as many blocks to a tile as leave each warp a chunk.
+  int split = 1;
+  while (split < kMaxSplit && tiles * split * 2 <= sms && chunks >= split * 2 * W) split *= 2;
+  p.ksplit = split;
+  p.rank_chunks = (chunks + split - 1) / split;
+  const int others = split > 1 ? split * sums : 0, left = room - others;
   // (a block of a group's width of k has to fit)
-  int S = tiles <= sms ? W : tiles <= 4 * sms ? 8 : 4;
-  while (S * x_bytes > room - room / 4) S /= 2;
+  int S = split > 1 || tiles <= sms ? W : tiles <= 4 * sms ? 8 : 4;
+  while (split == 1 && S * x_bytes > left - left / 4) S /= 2;
   p.split = S;
   const int groups = W / S;
-  const int whole = (chunks + S - 1) / S * S;
+  const int whole = (p.rank_chunks + S - 1) / S * S;
   p.blocks = 1;
   p.block_chunks = whole;
   p.batch = 0x3fffffff;
-  int smem = L::kFixed + whole * x_bytes;
-  if (whole > room / x_bytes) {  // blocks of k, as even as they come: a quarter of the room keeps sums
-    p.batch = std::max(1, room / 4 / (groups * sums));
-    const int fits = (room - p.batch * groups * sums) / (x_bytes * S) * S;
-    p.blocks = (chunks + fits - 1) / fits;
-    p.block_chunks = ((chunks + p.blocks - 1) / p.blocks + S - 1) / S * S;
-    p.blocks = (chunks + p.block_chunks - 1) / p.block_chunks;
-    smem = L::kFixed + p.batch * groups * sums + p.block_chunks * x_bytes;
+  int smem = L::kFixed + others + whole * x_bytes;
+  if (whole > left / x_bytes) {  // blocks of k, as even as they come: a quarter of the room keeps sums
+    p.batch = std::max(1, left / 4 / (groups * sums));
+    const int fits = (left - p.batch * groups * sums) / x_bytes;
+    p.blocks = (p.rank_chunks + fits - 1) / fits;
+    p.block_chunks = (p.rank_chunks + p.blocks - 1) / p.blocks;
+    if (p.block_chunks > S) p.block_chunks = std::min(fits, (p.block_chunks + S - 1) / S * S);
+    p.blocks = (p.rank_chunks + p.block_chunks - 1) / p.block_chunks;
+    smem = L::kFixed + others + p.batch * groups * sums + p.block_chunks * x_bytes;
   }
   CUtensorMap map = {};
   if (kAligned) {
     const auto encode = tensor_map_encoder();
     if (!encode) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
     const cuuint64_t dims[2] = {(cuuint64_t)p.row_bytes, (cuuint64_t)p.n}, strides[1] = {(cuuint64_t)p.row_bytes};
-    const cuuint32_t box[2] = {kPart / 2, L::kRows}, ones[2] = {1, 1};
+    const cuuint32_t box[2] = {kPart / 2, kRows}, ones[2] = {1, 1};
     const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p.w), dims, strides, box, ones,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, GS == 4 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_64B,
                               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   }
-  const cudaError_t e = launch_dependent(k, std::min(tiles, sms), W * 32, smem, st, p, map);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : std::min(tiles, sms)));
+  cfg.blockDim = dim3(W * 32);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)split, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = split > 1 ? 2 : 1;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, k, p, map);
+  if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "w4 launch");
 }
 

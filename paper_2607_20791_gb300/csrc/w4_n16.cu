@@ -1,4 +1,4 @@
-// The 4-bit products' kernel for 9 to 16 rows of x (a translation unit each, compiled in parallel).
+// The 4-bit products' kernel for more than 8 rows of x (a translation unit each, compiled in parallel).
 #include "w4_kernel.cuh"
 
 namespace rgd {
