@@ -106,14 +106,40 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
 
 // A chunk's scales and zeros as they lie in memory (a load must not be waited for before its
 // use).  Lane i has those of row i of the tile: one of every 128 weights, or of every group.
+// Where the rows' counts allow (scale_vec) they come by one or two vector loads, bf16 scales
+// two and zeros four to a word: a load of one scale from each of 32 rows looks up 32 lines,
+// and with groups of 32 that was the kernel's time twice over.
 template <int NL, bool kZeros>
 struct Scales {
   uint32_t s[NL], z[kZeros ? NL : 1];
 };
 
+template <int kBytes>
+__device__ __forceinline__ void load_bytes(const uint8_t* p, uint32_t* into) {
+  if (kBytes == 1) into[0] = __ldg(p);
+  if (kBytes == 2) into[0] = __ldg(reinterpret_cast<const uint16_t*>(p));
+  if (kBytes == 4) into[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+  if (kBytes == 8) {
+    const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+    into[0] = v.x, into[1] = v.y;
+  }
+#pragma unroll
+  for (int i = 0; i < kBytes / 16; ++i) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    into[4 * i] = v.x, into[4 * i + 1] = v.y, into[4 * i + 2] = v.z, into[4 * i + 3] = v.w;
+  }
+}
+
 template <int kEach, int GS, int NL, bool kZeros>
 __device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const uint8_t* row_scales,
                                             const uint8_t* row_zeros, int part) {
+  if (p.scale_vec) {
+    const int g = (part * kPart) >> p.group_shift;
+    if (p.scale_bytes == 2) load_bytes<2 * NL>(row_scales + 2 * g, c.s);
+    else load_bytes<4 * NL>(row_scales + 4 * g, c.s);
+    if (kZeros) load_bytes<NL>(row_zeros + g, c.z);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
     const int step = i % kEach * GS;
@@ -122,6 +148,21 @@ __device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros
     else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(row_scales) + g);
     if (kZeros) c.z[i] = __ldg(row_zeros + g);
   }
+}
+// Scale i as a number, and the zeros of a part, a byte each.
+template <int NL, bool kZeros>
+__device__ __forceinline__ float scale_of(const W4Params& p, const Scales<NL, kZeros>& c, int i) {
+  if (p.scale_bytes == 4) return __uint_as_float(c.s[i]);
+  if (!p.scale_vec) return __uint_as_float(c.s[i] << 16);
+  return __uint_as_float((i & 1) ? c.s[i / 2] & 0xffff0000u : c.s[i / 2] << 16);
+}
+template <int kEach, int NL, bool kZeros>
+__device__ __forceinline__ uint32_t zeros_of(const W4Params& p, const Scales<NL, kZeros>& c, int part) {
+  if (p.scale_vec) return kEach == 4 ? c.z[part] : c.z[0] >> (8 * kEach * part);
+  uint32_t z = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) z |= (c.z[part * kEach + i] & 15u) << (8 * i);
+  return z;
 }
 
 // Adds the products of a part of 16 rows (lo and hi: a lane's words of rows g and g + 8 by step)
@@ -258,7 +299,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   const int mine = tile0 < tiles ? (tiles - tile0 + stride - 1) / stride : 0;
   const int most = block < tiles ? (tiles - block + stride - 1) / stride : 0;  // of any group here
   const int my_chunks = min((p.k + kChunk<NT> - 1) / kChunk<NT>, (rank + 1) * p.rank_chunks);  // up to which this block goes
-  const int scale_shift = p.scale_bytes == 2 ? 16 : 0;
   const uint32_t ring_at = smem_u32(ring), magic = exponent_bits();
   const int unit = 64 << p.x_shift;                                            // bytes of x of a step and 8 rows
   const bool has_x = (lane >> 2) < (1 << p.x_shift);
@@ -356,10 +396,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
               float sc[NL];
               uint32_t z[P] = {};
 #pragma unroll
-              for (int i = 0; i < NL; ++i) {
-                sc[i] = __uint_as_float(c[s].s[i] << scale_shift);
-                if (kZeros) z[i / kEach] |= (c[s].z[i] & 15u) << (8 * (i % kEach));
-              }
+              for (int i = 0; i < NL; ++i) sc[i] = scale_of(p, c[s], i);
+              if constexpr (kZeros)
+#pragma unroll
+                for (int c2 = 0; c2 < P; ++c2) z[c2] = zeros_of<kEach>(p, c[s], c2);
               if (GS < 4) {
 #pragma unroll
                 for (int i = 0; i < NL; ++i)
@@ -474,6 +514,7 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
   constexpr int room = kW4Smem - L::kFixed;
   static_assert(room / 4 >= W / 4 * sums, "a tile of each group must be kept");
   static_assert(room - room / 4 >= 4 * 4 * kParts<NT> * NT * 512 && room > kMaxSplit * sums + sums * 2 + 4 * kParts<NT> * NT * 512, "a block of k must fit");
+  p.scale_vec = p.groups % (kParts<NT> * (GS == 4 ? 1 : L::kGroups)) == 0;
   // rows of x that are kept of every 8: a power of two
   p.x_shift = NT > 1 || p.m > 4 ? 3 : p.m > 2 ? 2 : p.m > 1 ? 1 : 0;
   const int x_bytes = 4 * kParts<NT> * NT * (64 << p.x_shift);  // of a chunk
