@@ -36,7 +36,7 @@ extern "C" int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size
   p.y_stride = y_stride;
   p.scale_bytes = scale_dtype == RGD_F32 ? 4 : 2;
   p.out_f32 = out_dtype == RGD_F32;
-  p.x_vec = k % 8 == 0;
+  p.x_vec = k % 8 == 0 ? 2 : k % 2 == 0 ? 1 : 0;
   p.dev_status = dev_status;
   cudaStream_t st = (cudaStream_t)stream;
   return m <= 8 ? launch_w4_n8(p, st) : launch_w4_n16(p, st);

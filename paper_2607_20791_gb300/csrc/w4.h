@@ -22,7 +22,8 @@ struct W4Params {
   const uint8_t* zeros;
   void* y;
   int64_t row_bytes, y_stride, total_bytes;
-  int32_t scale_bytes, out_f32, x_vec;
+  int32_t scale_bytes, out_f32;
+  int32_t x_vec;      // 2: rows of x lie on 16 bytes, 1: on 4
   int32_t scale_vec;  // a chunk's scales of a row are whole, aligned vectors
   int32_t x_shift;  // log2 of the rows of x that lie in shared memory of every 8
   int32_t* dev_status;

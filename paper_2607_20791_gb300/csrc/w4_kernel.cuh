@@ -21,8 +21,9 @@
 // so that the warp's 32 words lie in 32 banks.  A group's sum is scaled in fp32 after its
 // last MMA.
 //
-// Rows off 16 bytes have no box: a bulk copy a row brings the whole 16-byte vectors that
-// hold its part of a chunk, and a lane's word is cut from the two it lies in.
+// Rows off 16 bytes have no box: 16-byte asynchronous copies bring the whole vectors that
+// hold a row's part of a chunk, and a lane's word is cut from the two it lies in.  (A bulk
+// copy a row took 14 cycles each: 47 us for 13 x 2730 x 20011.)
 //
 // One block of 16 warps fills an SM, so that x lies there once.  Its warps form groups of S
 // that share a tile and whose sums meet in shared memory: few tiles want a wide group, many
@@ -58,7 +59,7 @@ constexpr int kChunk = kPart * kParts<NT>;
 
 // Shared memory: the warps' rings, every warp's sums of a tile, the sums kept between blocks of
 // k, the warps' scales (where groups are small), x.  GS: steps of 32 weights in a group.
-template <int NT, int GS, bool kAligned>
+template <int NT, int GS, bool kAligned, bool kZeros>
 struct Layout {
   static constexpr int kSums = kRows * 8 * NT;
   static constexpr int kJoin = kWarps * kSums * 4;
@@ -67,7 +68,8 @@ struct Layout {
   static constexpr int kRing = kWarps * kAhead * kSlot;
   static constexpr int kGroups = 4 / GS;                                         // of a part
   static constexpr int kScales = GS == 4 ? 0 : kParts<NT> * kRows * kGroups * 4;  // bytes of a warp
-  static constexpr int kFixed = kRing + kJoin + kWarps * kScales;
+  static constexpr int kZeroBytes = GS == 4 || !kZeros ? 0 : kParts<NT> * kRows * 2;
+  static constexpr int kFixed = kRing + kJoin + kWarps * (kScales + kZeroBytes);
 };
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -104,11 +106,12 @@ __device__ __forceinline__ void copy_box(uint32_t dst, const CUtensorMap* map, i
                : "memory");
 }
 
-// A chunk's scales and zeros as they lie in memory (a load must not be waited for before its
-// use).  Lane i has those of row i of the tile: one of every 128 weights, or of every group.
-// Where the rows' counts allow (scale_vec) they come by one or two vector loads, bf16 scales
-// two and zeros four to a word: a load of one scale from each of 32 rows looks up 32 lines,
-// and with groups of 32 that was the kernel's time twice over.
+// A chunk's scales and zeros (NL a row) as they lie in memory; a load must not be waited for
+// before its use.  Where the rows' counts allow (scale_vec) lane i has those of row i of the
+// tile, by one or two vector loads, bf16 scales two and zeros four to a word.  Else load i
+// brings those of rows 32 / NL i .. by one each: lane j that of row j / NL, group j % NL.  (A
+// load of one scale from each of 32 rows looks up 32 lines: with groups of 32 that was the
+// kernel's time twice over.)
 template <int NL, bool kZeros>
 struct Scales {
   uint32_t s[NL], z[kZeros ? NL : 1];
@@ -130,43 +133,66 @@ __device__ __forceinline__ void load_bytes(const uint8_t* p, uint32_t* into) {
   }
 }
 
-template <int kEach, int GS, int NL, bool kZeros>
-__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const uint8_t* row_scales,
-                                            const uint8_t* row_zeros, int part) {
+template <int NL, bool kZeros>
+__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, int tile, int part, int lane) {
+  const int g = (part * kPart) >> p.group_shift;
   if (p.scale_vec) {
-    const int g = (part * kPart) >> p.group_shift;
-    if (p.scale_bytes == 2) load_bytes<2 * NL>(row_scales + 2 * g, c.s);
-    else load_bytes<4 * NL>(row_scales + 4 * g, c.s);
-    if (kZeros) load_bytes<NL>(row_zeros + g, c.z);
+    const int64_t at = min((int64_t)tile * kRows + lane, (int64_t)p.n - 1) * p.groups + g;
+    if (p.scale_bytes == 2) load_bytes<2 * NL>(p.scales + 2 * at, c.s);
+    else load_bytes<4 * NL>(p.scales + 4 * at, c.s);
+    if (kZeros) load_bytes<NL>(p.zeros + at, c.z);
     return;
   }
+  const int mine = min(g + lane % NL, p.groups - 1);  // (past the row's end x is zero)
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    const int step = i % kEach * GS;
-    const int g = min(((part + i / kEach) * kPart + step * 32) >> p.group_shift, p.groups - 1);  // (past the row's end x is zero)
-    if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(row_scales) + g);
-    else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(row_scales) + g);
-    if (kZeros) c.z[i] = __ldg(row_zeros + g);
+    const int64_t at = min((int64_t)tile * kRows + i * (32 / NL) + lane / NL, (int64_t)p.n - 1) * p.groups + mine;
+    if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + at);
+    else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + at);
+    if (kZeros) c.z[i] = __ldg(p.zeros + at);
   }
 }
-// Scale i as a number, and the zeros of a part, a byte each.
+// Scale i as a number.
 template <int NL, bool kZeros>
 __device__ __forceinline__ float scale_of(const W4Params& p, const Scales<NL, kZeros>& c, int i) {
   if (p.scale_bytes == 4) return __uint_as_float(c.s[i]);
   if (!p.scale_vec) return __uint_as_float(c.s[i] << 16);
   return __uint_as_float((i & 1) ? c.s[i / 2] & 0xffff0000u : c.s[i / 2] << 16);
 }
+
+// Small groups' scales and zeros into the warp's place in shared memory: scales [part][row]
+// [group], zeros 4 bits a group in a word of 16 for each [part][row].
 template <int kEach, int NL, bool kZeros>
-__device__ __forceinline__ uint32_t zeros_of(const W4Params& p, const Scales<NL, kZeros>& c, int part) {
-  if (p.scale_vec) return kEach == 4 ? c.z[part] : c.z[0] >> (8 * kEach * part);
-  uint32_t z = 0;
+__device__ __forceinline__ void spread_scales(const W4Params& p, const Scales<NL, kZeros>& c, float* scales, uint16_t* zeros, int lane) {
+  if (p.scale_vec) {
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) z |= (c.z[part * kEach + i] & 15u) << (8 * i);
-  return z;
+    for (int i = 0; i < NL; ++i) scales[(i / kEach * kRows + lane) * kEach + i % kEach] = scale_of(p, c, i);
+    if constexpr (kZeros) {
+#pragma unroll
+      for (int c2 = 0; c2 < NL / kEach; ++c2) {
+        uint32_t z = kEach == 4 ? c.z[c2] : c.z[0] >> (16 * c2);
+        z = (z | z >> 4) & 0x00ff00ffu;  // (two zeros to a byte)
+        zeros[c2 * kRows + lane] = (uint16_t)(z | z >> 8);
+      }
+    }
+  } else {
+    const int row = lane / NL, i0 = lane % NL;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int r = i * (32 / NL) + row;
+      scales[(i0 / kEach * kRows + r) * kEach + i0 % kEach] = scale_of(p, c, i);
+      if constexpr (kZeros) {
+        uint32_t z = (c.z[i] & 15u) << (4 * (i0 % kEach));
+#pragma unroll
+        for (int o = 1; o < kEach; o <<= 1) z |= __shfl_xor_sync(0xffffffffu, z, o);
+        if (i0 % kEach == 0) zeros[i0 / kEach * kRows + r] = (uint16_t)z;
+      }
+    }
+  }
 }
 
 // Adds the products of a part of 16 rows (lo and hi: a lane's words of rows g and g + 8 by step)
-// to their sums.  s: the groups' scales of those rows; z: their zeros, a byte each.
+// to their sums.  s: the groups' scales of those rows; z: their zeros, 4 bits each.
 template <int NT, int GS, bool kZeros>
 __device__ __forceinline__ void multiply_rows(const uint32_t (&lo)[4], const uint32_t (&hi)[4], const float (&s0)[4 / GS],
                                               const float (&s1)[4 / GS], uint32_t z0, uint32_t z1, const uint8_t* xs, int unit,
@@ -175,8 +201,8 @@ __device__ __forceinline__ void multiply_rows(const uint32_t (&lo)[4], const uin
   for (int g = 0; g < 4 / GS; ++g) {
     uint32_t b0 = 0x43084308u, b1 = 0x43084308u;
     if (kZeros) {
-      b0 = 0x43004300u + 0x00010001u * (z0 >> (8 * g) & 15u);
-      b1 = 0x43004300u + 0x00010001u * (z1 >> (8 * g) & 15u);
+      b0 = 0x43004300u + 0x00010001u * (z0 >> (4 * g) & 15u);
+      b1 = 0x43004300u + 0x00010001u * (z1 >> (4 * g) & 15u);
     }
     float sum[NT][4];
 #pragma unroll
@@ -225,8 +251,14 @@ __device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int part
       r[f] = make_uint4(0, 0, 0, 0);
       if (u < units && m < p.m && k < p.k) {
         const uint16_t* src = p.x + (int64_t)m * p.k + k;
-        if (p.x_vec) {  // (k is then a multiple of 8)
+        if (p.x_vec == 2) {  // (k is then a multiple of 8)
           r[f] = __ldg(reinterpret_cast<const uint4*>(src));
+        } else if (p.x_vec == 1) {  // (... of 2)
+          const uint32_t* q = reinterpret_cast<const uint32_t*>(src);
+          r[f].x = __ldg(q);
+          if (k + 2 < p.k) r[f].y = __ldg(q + 1);
+          if (k + 4 < p.k) r[f].z = __ldg(q + 2);
+          if (k + 6 < p.k) r[f].w = __ldg(q + 3);
         } else {
           uint16_t e[8];
 #pragma unroll
@@ -244,6 +276,21 @@ __device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int part
             make_uint4(__byte_perm(r[f].x, r[f].z, 0x5410), __byte_perm(r[f].x, r[f].z, 0x7632),
                        __byte_perm(r[f].y, r[f].w, 0x5410), __byte_perm(r[f].y, r[f].w, 0x7632));
     }
+  }
+}
+
+// Rows off 16 bytes: starts the copies of the vectors that hold the tile's part (or two).
+// Nothing is read past the weights' end or for rows past the last: zeros fill its place.
+template <int P>
+__device__ __forceinline__ void copy_vectors(const W4Params& p, uint32_t to, int tile, int part, int lane) {
+  constexpr int kEach = P * 4 + 1;  // vectors of a row
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int u = i * 32 + lane, row = u / kEach, v = u % kEach;
+    const int64_t n = (int64_t)tile * kRows + row;
+    const int64_t at = ((n * p.row_bytes + (int64_t)part * (kPart / 2)) & ~int64_t(15)) + 16 * v;
+    const int bytes = n < p.n ? (int)max(int64_t(0), min(int64_t(16), p.total_bytes - at)) : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + u * 16), "l"(p.w + (bytes ? at : 0)), "r"(bytes) : "memory");
   }
 }
 
@@ -269,7 +316,7 @@ __device__ __forceinline__ void write_sum(const W4Params& p, int m, int64_t n, f
 
 template <int NT, int GS, bool kAligned, bool kZeros>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
-  using L = Layout<NT, GS, kAligned>;
+  using L = Layout<NT, GS, kAligned, kZeros>;
   constexpr bool kTurned = GS < 4 || !kAligned;  // a quad's words are of the same 16 bytes
   constexpr int kSums = L::kSums, R = kRows / 8, A = kAhead, P = kParts<NT>;
   constexpr int kEach = L::kGroups, NL = P * kEach;  // scales of a lane and part, and chunk
@@ -280,12 +327,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   const uint8_t* ring = dyn + warp * A * L::kSlot;
   float* join = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;  // [S][kSums]
   float* scales = reinterpret_cast<float*>(dyn + L::kRing + L::kJoin + warp * L::kScales);  // [P][kRows][kGroups]
+  uint16_t* zeros = reinterpret_cast<uint16_t*>(dyn + L::kRing + L::kJoin + kWarps * L::kScales + warp * L::kZeroBytes);  // [P][kRows]
   float* others = reinterpret_cast<float*>(dyn + L::kFixed);                                // [ksplit][kSums]
   float* kept = others + (p.ksplit > 1 ? p.ksplit * kSums : 0) + group * p.batch * kSums;   // [batch][kSums]
   uint8_t* xs = dyn + L::kFixed + ((p.ksplit > 1 ? p.ksplit : 0) + (p.blocks > 1 ? groups * p.batch : 0)) * kSums * 4;
   if (lane == 0) {
 #pragma unroll
-    for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], kAligned ? 1 : kRows);
+    for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], 1);
     fence_mbar_init();
     fence_proxy_async_smem();
   }
@@ -326,48 +374,30 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
         const int per = (chunks - member + S - 1) / S;  // chunks of this warp and a tile (none: the group's others have them)
         const int items = batch * max(per, 1);
         Scales<NL, kZeros> c[A];
-        // the next chunk to load, its tile, and the scales and zeros of the lane's row (of the last row for those past it)
-        int lt = 0, lc = member, load_tile = tile0 + first * stride;
-        const uint8_t *row_scales, *row_zeros;
-        auto at_row = [&] {
-          const int64_t g = min((int64_t)load_tile * kRows + lane, (int64_t)p.n - 1) * p.groups;
-          row_scales = p.scales + g * p.scale_bytes;
-          row_zeros = p.zeros + g;
-        };
-        at_row();
+        int lt = 0, lc = member, load_tile = tile0 + first * stride;  // the next chunk to load, and its tile
         auto load = [&](Scales<NL, kZeros>& into, int s) {
           if (lt < batch && lc < chunks) {
             const int part = (chunk0 + lc) * P;
-            if (alive) {
+            if (!kAligned) {
+              copy_vectors<P>(p, ring_at + s * L::kSlot, load_tile, part, lane);
+            } else if (alive) {
               ++flying;
-              if (kAligned && lane == 0) {
+              if (lane == 0) {
                 mbar_arrive_expect_tx(&landed[warp][s], L::kSlot);
 #pragma unroll
                 for (int c2 = 0; c2 < P; ++c2)  // (what lies past a row's end or the last row is filled with zeros)
                   copy_box(ring_at + s * L::kSlot + c2 * kRows * 64, &map, (part + c2) * (kPart / 2), load_tile * kRows,
                            &landed[warp][s]);
               }
-              if (!kAligned) {
-                // the vectors that hold the row's part, as far as they lie within the weights; the last
-                // bytes of those by themselves
-                const int64_t n = (int64_t)load_tile * kRows + lane;
-                const int64_t from = (n * p.row_bytes + (int64_t)part * (kPart / 2)) & ~int64_t(15);
-                const int64_t to = n < p.n && (int64_t)part * (kPart / 2) < p.row_bytes ? min(from + L::kPitch, p.total_bytes) : from;
-                const int64_t whole = max(from, min(to, p.total_bytes & ~int64_t(15)));
-                uint8_t* dst = const_cast<uint8_t*>(ring) + s * L::kSlot + lane * L::kPitch;
-                if (whole > from) bulk_load(dst, p.w + from, (uint32_t)(whole - from), &landed[warp][s]);
-                for (int64_t b = whole; b < to; ++b) dst[b - from] = p.w[b];
-                mbar_arrive_expect_tx(&landed[warp][s], (uint32_t)(whole - from));
-              }
             }
-            load_scales<kEach, GS, NL, kZeros>(p, into, row_scales, row_zeros, part);
+            load_scales(p, into, load_tile, part, lane);
           }
+          if (!kAligned) asm volatile("cp.async.commit_group;" ::: "memory");
           lc += S;
           if (lc < chunks) return;
           lc = member;
           ++lt;
           load_tile += stride;
-          at_row();
         };
 #pragma unroll
         for (int s = 0; s < A; ++s) load(c[s], s);
@@ -383,29 +413,25 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
           for (int s = 0; s < A; ++s) {
             if (it + s >= items) break;
             if (at < chunks) {
-              if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
-                if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
-                alive = false;  // (no more copies; those on their way are waited for at the end)
-                lost = s;
+              if (!kAligned) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copies of the chunk have landed
+                __syncwarp();
+              } else {
+                if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
+                  if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
+                  alive = false;  // (no more copies; those on their way are waited for at the end)
+                  lost = s;
+                }
+                if (alive) {
+                  parity ^= 1u << s;
+                  --flying;
+                }
               }
-              if (alive) {
-                parity ^= 1u << s;
-                --flying;
+              const Scales<NL, kZeros> now = c[s];
+              if constexpr (GS < 4) {
+                spread_scales<kEach>(p, now, scales, zeros, lane);
+                __syncwarp();
               }
-              // the lane's scales, as numbers; where groups are small through shared memory to the lanes of the rows
-              float sc[NL];
-              uint32_t z[P] = {};
-#pragma unroll
-              for (int i = 0; i < NL; ++i) sc[i] = scale_of(p, c[s], i);
-              if constexpr (kZeros)
-#pragma unroll
-                for (int c2 = 0; c2 < P; ++c2) z[c2] = zeros_of<kEach>(p, c[s], c2);
-              if (GS < 4) {
-#pragma unroll
-                for (int i = 0; i < NL; ++i)
-                  scales[(i / kEach * kRows + lane) * L::kGroups + i % kEach] = sc[i];
-              }
-              if (GS < 4) __syncwarp();
               const uint8_t* slot = ring + s * L::kSlot;
 #pragma unroll
               for (int c2 = 0; c2 < P; ++c2) {
@@ -435,18 +461,30 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                 for (int b = 0; b < kSub; ++b) {
                   const int row = 16 * b + (lane >> 2);
                   float s0[L::kGroups], s1[L::kGroups];
-                  if (GS == 4) {
-                    s0[0] = __shfl_sync(0xffffffffu, sc[c2], row);
-                    s1[0] = __shfl_sync(0xffffffffu, sc[c2], row + 8);
+                  uint32_t z0 = 0, z1 = 0;
+                  if constexpr (GS == 4) {
+                    // (rows 16 b .. are all of load b where a lane has one of two parts each)
+                    const bool apart = P == 2 && !p.scale_vec;
+                    const int from = apart ? row % 16 * 2 + c2 : row, step = apart ? 16 : 8;
+                    const float v = apart ? scale_of(p, now, b % NL) : scale_of(p, now, c2);
+                    s0[0] = __shfl_sync(0xffffffffu, v, from);
+                    s1[0] = __shfl_sync(0xffffffffu, v, from + step);
+                    if constexpr (kZeros) {
+                      const uint32_t z = apart ? now.z[b % NL] : p.scale_vec ? now.z[0] >> (8 * c2) : now.z[c2];
+                      z0 = __shfl_sync(0xffffffffu, z, from);
+                      z1 = __shfl_sync(0xffffffffu, z, from + step);
+                    }
                   } else {
 #pragma unroll
                     for (int g = 0; g < L::kGroups; ++g) {
                       s0[g] = scales[(c2 * kRows + row) * L::kGroups + g];
                       s1[g] = scales[(c2 * kRows + row + 8) * L::kGroups + g];
                     }
+                    if constexpr (kZeros) {
+                      z0 = zeros[c2 * kRows + row];
+                      z1 = zeros[c2 * kRows + row + 8];
+                    }
                   }
-                  const uint32_t z0 = kZeros ? __shfl_sync(0xffffffffu, z[c2], row) : 0;
-                  const uint32_t z1 = kZeros ? __shfl_sync(0xffffffffu, z[c2], row + 8) : 0;
                   multiply_rows<NT, GS, kZeros>(q[2 * b], q[2 * b + 1], s0, s1, z0, z1,
                                                 my_x + (int64_t)(at * P + c2) * 4 * NT * unit, unit, has_x, acc[b], magic);
                 }
@@ -499,6 +537,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
       }
     }
   }
+  if (!kAligned) asm volatile("cp.async.wait_all;" ::: "memory");
   if (!alive)
     for (int i = 0; i < flying; ++i) mbar_wait(&landed[warp][(lost + i) % A], (parity >> (lost + i) % A) & 1u);
 }
@@ -506,7 +545,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
 template <int NT, int GS, bool kAligned, bool kZeros>
 int launch_w4_as(W4Params& p, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
-  using L = Layout<NT, GS, kAligned>;
+  using L = Layout<NT, GS, kAligned, kZeros>;
   auto k = w4_kernel<NT, GS, kAligned, kZeros>;
   if (int rc = ensure_smem(k, kW4Smem, done)) return rc;
   constexpr int W = kWarps, sms = 152;
