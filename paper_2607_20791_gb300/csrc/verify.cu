@@ -40,7 +40,7 @@ namespace rgd {
 namespace {
 
 constexpr int kVerifyWarps = 8;
-constexpr int kVerifyThreads = (kVerifyWarps + 1) * 32;  // (the last warp looks after the parameters)
+constexpr int kVerifyThreads = kVerifyWarps * 32;
 constexpr int kGroups = 16;  // groups of a lane's vectors whose maxima it keeps
 constexpr int kFlight = 4;   // loads in flight per lane
 constexpr int kVerifyCluster = 16;                           // CTAs of a unit at most
@@ -523,7 +523,7 @@ __device__ __forceinline__ void push(const float* slot, float v, uint32_t rank) 
 }
 
 template <typename T, bool kAligned>
-__global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyParams p) {
+__global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyParams p) {
   constexpr int E = 16 / (int)sizeof(T);
   using V = Vec<T>;
   __shared__ VerifyShared sh;
@@ -563,16 +563,15 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
   const bool two = p.draft != nullptr && has_draft && !greedy;
   const int64_t trow = ((int64_t)row * (K + 1) + pos) * p.target_stride, qrow = ((int64_t)row * K + pos) * p.draft_stride;
 
-  // This warp's share (none for the last warp), in the order of the elements over the cluster.
-  const bool worker = warp < kVerifyWarps;
+  // This warp's share, in the order of the elements over the cluster.
   const int64_t share = (int64_t)p.stripes * 32 * E;
   const int64_t e0 = ((int64_t)rank * kVerifyWarps + warp) * share;
-  const int64_t count = worker ? min(share, p.vocab - e0) : 0;
+  const int64_t count = min(share, p.vocab - e0);
   const Share<T, kAligned> tv(p.target + trow, e0, count);
   const Share<T, kAligned> qv(two ? p.draft + qrow : p.target + trow, e0, two ? count : 0);
 
   // Pass 1: the maxima (NaN never wins).
-  if (!worker && lane == 0) {
+  if (warp == kVerifyWarps - 1 && lane == 0) {
     sh.tl = d_in && !greedy ? one_logit<T>(p.target + trow, d) : 0.f;
     sh.ql = d_in && two ? one_logit<T>(p.draft + qrow, d) : 0.f;
     sh.theta = scaled_log(temp, min_p);
@@ -581,7 +580,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
   {
     const float tm = find_maxima(tv, tkept, p.stripes, lane);
     const float qm = find_maxima(qv, qkept, two ? p.stripes : 0, lane);
-    if (worker && lane == 0) {
+    if (lane == 0) {
       sh.warp_top[0][warp] = tm;
       sh.warp_top[1][warp] = qm;
     }
@@ -619,7 +618,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
     for (int i = walk.next(); i >= 0; i = walk.next()) look(tv.get(i), i);
     look(tkept.rest, tv.whole);
     best = __reduce_min_sync(0xffffffffu, best);
-    if (worker && lane == 0) sh.warp_sum[0][warp] = best;
+    if (lane == 0) sh.warp_sum[0][warp] = best;
     __syncthreads();
     if (warp == 0) {
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.warp_sum[0][lane % kVerifyWarps]);
@@ -637,7 +636,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
 
   // A sum of every warp over the cluster: by warp for the CTA's own, by CTA for all.
   auto join = [&](int which, uint64_t mine) {
-    if (worker && lane == 0) sh.warp_sum[which][warp] = mine;
+    if (lane == 0) sh.warp_sum[which][warp] = mine;
   };
   auto exchange = [&](int first, int last) {
     __syncthreads();
@@ -725,7 +724,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {  // the parts' sums, then the element
 #pragma unroll 1
-    for (int s = 0; s < (worker ? stripes : 0); ++s) {
+    for (int s = 0; s < stripes; ++s) {
       const int i = (warp * stripes + s) * 32 + lane;
       uint4 a = V::nothing(), c = a;
       if (i < ot.whole) {
@@ -772,9 +771,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 3) verify_kernel(const VerifyP
       }
     }
     if (pass == 1) return;
-    if (worker && lane == 0) sh.part_sum[warp] = part;
+    if (lane == 0) sh.part_sum[warp] = part;
     __syncthreads();
-    if (!worker) return;
     before += warp_sum(lane < warp ? sh.part_sum[lane] : 0);
     if (!(before <= mark && mark < before + part)) return;
   }
