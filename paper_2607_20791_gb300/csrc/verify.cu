@@ -42,7 +42,9 @@ namespace {
 constexpr int kVerifyWarps = 8;
 constexpr int kVerifyThreads = kVerifyWarps * 32;
 constexpr int kGroups = 16;  // groups of a lane's vectors whose maxima it keeps
-constexpr int kFlight = 4;   // loads in flight per lane
+// Loads in flight per lane: a vector of a row off 16 bytes is five.
+template <bool kAligned>
+constexpr int kFlight = kAligned ? 8 : 4;
 constexpr int kVerifyCluster = 16;                           // CTAs of a unit at most
 constexpr int32_t kTaken = -1, kRejectedRow = -2;            // results of a unit other than a token
 
@@ -354,17 +356,17 @@ __device__ __forceinline__ float find_maxima(const Share<T, kAligned>& v, Kept& 
 #pragma unroll 1
   for (int s = 0; s < stripes; s += kGroups) {
 #pragma unroll
-    for (int g = 0; g < kGroups; g += kFlight) {
+    for (int g = 0; g < kGroups; g += kFlight<kAligned>) {
       if (s + g >= stripes) break;
-      uint4 w[kFlight];
+      uint4 w[kFlight<kAligned>];
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
+      for (int k = 0; k < kFlight<kAligned>; ++k) {
         const int i = (s + g + k) * 32 + lane;
         w[k] = V::nothing();
         if (i < v.whole) w[k] = v.get(i);
       }
 #pragma unroll
-      for (int k = 0; k < kFlight; k += 2) {
+      for (int k = 0; k < kFlight<kAligned>; k += 2) {
         const typename V::Max m0 = V::max_of(w[k], V::lowest()), m1 = V::max_of(w[k + 1], V::lowest());
         all = V::max_of(m0, m1, all);
         const __nv_bfloat162 m = __hmax2(V::up(m0, m1), *reinterpret_cast<const __nv_bfloat162*>(&kept.group[(g + k) / 2]));
@@ -436,15 +438,15 @@ __device__ __forceinline__ uint64_t sum_weights(const Share<T, kAligned>& v, con
   const int steps = (int)__reduce_max_sync(0xffffffffu, (uint32_t)__popc(mask)) * ((stripes + kGroups - 1) / kGroups);
   if (7 * steps > 4 * stripes) {  // all of the share, in order
 #pragma unroll 1
-    for (int i = lane; i < v.whole; i += 32 * kFlight) {
-      uint4 x[kFlight];
+    for (int i = lane; i < v.whole; i += 32 * kFlight<kAligned>) {
+      uint4 x[kFlight<kAligned>];
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
+      for (int k = 0; k < kFlight<kAligned>; ++k) {
         x[k] = V::nothing();
         if (i + 32 * k < v.whole) x[k] = v.get(i + 32 * k);
       }
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) add_weights<T>(x[k], side, cut, sum);
+      for (int k = 0; k < kFlight<kAligned>; ++k) add_weights<T>(x[k], side, cut, sum);
     }
     add_weights<T>(w, side, cut, sum);
   } else {  // the groups that reach the cutoff, two vectors on their way while one is worked on
@@ -786,14 +788,14 @@ int launch_verify(VerifyParams& p, cudaStream_t st) {
   const int64_t units = (int64_t)p.rows * (p.max_draft + 1);
   auto stripes = [&](int c) { return (int)((nvec + (int64_t)c * kVerifyWarps * 32 - 1) / ((int64_t)c * kVerifyWarps * 32)); };
   // CTAs of a unit.  A CTA pays for three exchanges however little it reads, and reads
-  // nothing meanwhile: its warps' shares are up to 40 stripes (20 KB), and shorter (16) only
-  // to have some three CTAs for each that fits the SMs at once (456), so that they are at
-  // different stages.  Measured: 400 units of 2 x 128256 bf16 46 us with 4, 52 with 2, 62 with
-  // 8; 2048 of 152064 216 us with 2, 234 with 4, 338 with 8; 192 of 262144 fp32 64 us with 8,
-  // 80 with 4.  Few units are cut further until the SMs have two CTAs each.
+  // nothing meanwhile: its warps' shares are up to 40 stripes (20 KB), shorter (16) only to
+  // have a few CTAs for each of the 608 that fit the SMs, so that they are at different
+  // stages, and 8 only to fill the SMs.  Measured: 400 units of 2 x 128256 bf16 40 us with 4,
+  // 47 with 2, 51 with 8; 1024 of 3 x 152064 192 us with 2, 196 with 4; 192 of 262144
+  // fp32 58 us with 8, 80 with 4.  Few units are cut further until the SMs have two CTAs each.
   int c = 1;
   while (c < kVerifyCluster && stripes(c) > 40) c *= 2;
-  while (c < kVerifyCluster && units * c < 3 * 456 && stripes(2 * c) >= 16) c *= 2;
+  while (c < 8 && ((units * c < 1600 && stripes(2 * c) >= 16) || (units * c < 608 && stripes(2 * c) >= 8))) c *= 2;
   while (c < kVerifyCluster && units * c < 304 && stripes(c) > 2) c *= 2;
   if (c > 8) {
     int dev = 0;
