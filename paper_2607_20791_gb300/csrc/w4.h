@@ -12,10 +12,9 @@ struct W4Params {
   int32_t group_shift;   // log2 of the group size
   int32_t block_chunks;  // chunks of a block of k
   int32_t blocks;        // blocks of k
-  int32_t split;         // warps of a group
   int32_t ksplit;        // blocks of a cluster that share a tile, each with rank_chunks chunks
   int32_t rank_chunks;
-  int32_t batch;         // tiles of a group between which k may go in blocks
+  int32_t batch;         // tiles of a block (or cluster) between which k may go in blocks
   const uint16_t* x;
   const uint8_t* w;
   const uint8_t* scales;

@@ -1,14 +1,14 @@
 // Products of a few rows of activations with 4-bit weights: y = x W^T with
 // W[n, k] = (q[n, k] - z[n, k / G]) s[n, k / G], q packed two to a byte along k.
 //
-// The weights are read once; everything else is small.  A tile is 32 rows of W; the warps
-// of its group take the chunks of those rows (256 weights for up
-// to 8 rows of x, else 128) in turn, so that together they read contiguous bytes of a row.
+// The weights are read once; everything else is small.  A tile is 32 rows of W, its k goes in
+// chunks of 256 weights (for up to 8 rows of x and groups of 64 or 128, else 128), and each
+// warp of a block takes an equal stretch of all its tiles' chunks, one tile after another.
 // A chunk comes by TMA boxes of 64 bytes by the tile's rows into the warp's own ring in
 // shared memory, 4 to 8 KB ahead of its use.  Every 128 weights are 8 mma.m16n8k16 with the
 // weights as A for every 16 rows of W and 8 rows of x: one row of x costs the same as
 // eight, and the tensor pipe does the sums over k in fp32.  (With 17 to 32 rows of x the
-// weights are read twice, 16 rows at a time: 166 us for 32 x 4096 x 128256 where one pass
+// weights are read twice, 16 rows at a time: 155 us for 32 x 4096 x 128256 where one pass
 // of 32 took 198, x coming from shared memory in blocks of k.)
 //
 // Which k a lane's A elements stand for is free as long as B agrees, so a lane feeds the
@@ -23,13 +23,19 @@
 //
 // Rows off 16 bytes have no box: 16-byte asynchronous copies bring the whole vectors that
 // hold a row's part of a chunk, and a lane's word is cut from the two it lies in.  (A bulk
-// copy a row took 14 cycles each: 47 us for 13 x 2730 x 20011.)
+// copy a row took 14 cycles each, half of the kernel's time.)
 //
-// One block of 16 warps fills an SM, so that x lies there once.  Its warps form groups of S
-// that share a tile and whose sums meet in shared memory: few tiles want a wide group, many
-// a narrow one, whose joins cost less.  Where x does not fit, k goes in blocks, with the sums
-// of a group's tiles kept in shared memory between them.  Few tiles of long rows are shared
-// by the blocks of a cluster, each with a stretch of k, whose sums the first one joins.
+// One block of 16 warps fills an SM, so that x lies there once.  A warp writes the sums of the
+// tiles it has whole; a tile that several warps have parts of is joined in shared memory at
+// the end, so that nothing waits in between (groups of 4 warps that shared each tile, with
+// two barriers a tile, took 61 us where this takes 56 for 5 x 4096 x 128256, and 33 where
+// this takes 29 for 13 x 2730 x 20011).  Where x does not fit, k goes in blocks, with the
+// sums of the block's tiles kept in shared memory between them.  Few tiles of long rows are
+// shared by the blocks of a cluster, each with a stretch of k, whose sums the first one joins.
+//
+// What bounds it: 5 x 4096 x 128256 in groups of 128 takes 56 us, 0.72 of the copy rate, with
+// 0.6 of the issue slots and of the integer pipe's cycles taken (7 integer operations and 4
+// subtractions for every 8 weights of 32 rows), the tensor pipe a quarter busy.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -51,24 +57,25 @@ constexpr int kRows = 16 * kSub;     // of a tile
 constexpr int kAhead = 2;            // chunks in flight
 constexpr int kMaxSplit = 8;         // blocks that share a tile's k
 
-// Parts of a chunk, for 8 NT rows of x.
-template <int NT>
-constexpr int kParts = NT == 1 ? 2 : 1;
-template <int NT>
-constexpr int kChunk = kPart * kParts<NT>;
+// Parts of a chunk (GS: steps of 32 weights in a group): two halve what a chunk costs besides its
+// products, but the scales of small groups would take more registers than there are.
+template <int NT, int GS>
+constexpr int kParts = NT == 1 && GS > 1 ? 2 : 1;
+template <int NT, int GS>
+constexpr int kChunk = kPart * kParts<NT, GS>;
 
 // Shared memory: the warps' rings, every warp's sums of a tile, the sums kept between blocks of
-// k, the warps' scales (where groups are small), x.  GS: steps of 32 weights in a group.
+// k, the warps' scales (where groups are small), x.
 template <int NT, int GS, bool kAligned, bool kZeros>
 struct Layout {
   static constexpr int kSums = kRows * 8 * NT;
   static constexpr int kJoin = kWarps * kSums * 4;
-  static constexpr int kPitch = kAligned ? 64 : kParts<NT> * 64 + 16;            // from a row to the next
-  static constexpr int kSlot = kRows * (kAligned ? kParts<NT> * 64 : kPitch);    // of a chunk
+  static constexpr int kPitch = kAligned ? 64 : kParts<NT, GS> * 64 + 16;            // from a row to the next
+  static constexpr int kSlot = kRows * (kAligned ? kParts<NT, GS> * 64 : kPitch);    // of a chunk
   static constexpr int kRing = kWarps * kAhead * kSlot;
   static constexpr int kGroups = 4 / GS;                                         // of a part
-  static constexpr int kScales = GS == 4 ? 0 : kParts<NT> * kRows * kGroups * 4;  // bytes of a warp
-  static constexpr int kZeroBytes = GS == 4 || !kZeros ? 0 : kParts<NT> * kRows * 2;
+  static constexpr int kScales = GS == 4 ? 0 : kParts<NT, GS> * kRows * kGroups * 4;  // bytes of a warp
+  static constexpr int kZeroBytes = GS == 4 || !kZeros ? 0 : kParts<NT, GS> * kRows * kGroups;
   static constexpr int kFixed = kRing + kJoin + kWarps * (kScales + kZeroBytes);
 };
 
@@ -134,10 +141,10 @@ __device__ __forceinline__ void load_bytes(const uint8_t* p, uint32_t* into) {
 }
 
 template <int NL, bool kZeros>
-__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, int tile, int part, int lane) {
+__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, int tile, int64_t row_at, int part, int lane) {
   const int g = (part * kPart) >> p.group_shift;
   if (p.scale_vec) {
-    const int64_t at = min((int64_t)tile * kRows + lane, (int64_t)p.n - 1) * p.groups + g;
+    const int64_t at = row_at + g;
     if (p.scale_bytes == 2) load_bytes<2 * NL>(p.scales + 2 * at, c.s);
     else load_bytes<4 * NL>(p.scales + 4 * at, c.s);
     if (kZeros) load_bytes<NL>(p.zeros + at, c.z);
@@ -160,76 +167,71 @@ __device__ __forceinline__ float scale_of(const W4Params& p, const Scales<NL, kZ
   return __uint_as_float((i & 1) ? c.s[i / 2] & 0xffff0000u : c.s[i / 2] << 16);
 }
 
-// Small groups' scales and zeros into the warp's place in shared memory: scales [part][row]
-// [group], zeros 4 bits a group in a word of 16 for each [part][row].
+// Small groups' scales and zeros into the warp's place in shared memory, as [part][row][group].
 template <int kEach, int NL, bool kZeros>
-__device__ __forceinline__ void spread_scales(const W4Params& p, const Scales<NL, kZeros>& c, float* scales, uint16_t* zeros, int lane) {
+__device__ __forceinline__ void spread_scales(const W4Params& p, const Scales<NL, kZeros>& c, float* scales, uint8_t* zeros, int lane) {
   if (p.scale_vec) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) scales[(i / kEach * kRows + lane) * kEach + i % kEach] = scale_of(p, c, i);
     if constexpr (kZeros) {
 #pragma unroll
       for (int c2 = 0; c2 < NL / kEach; ++c2) {
-        uint32_t z = kEach == 4 ? c.z[c2] : c.z[0] >> (16 * c2);
-        z = (z | z >> 4) & 0x00ff00ffu;  // (two zeros to a byte)
-        zeros[c2 * kRows + lane] = (uint16_t)(z | z >> 8);
+        uint8_t* to = zeros + (c2 * kRows + lane) * kEach;
+        if (kEach == 4) *reinterpret_cast<uint32_t*>(to) = c.z[c2];
+        else *reinterpret_cast<uint16_t*>(to) = (uint16_t)(c.z[0] >> (16 * c2));
       }
     }
   } else {
     const int row = lane / NL, i0 = lane % NL;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const int r = i * (32 / NL) + row;
-      scales[(i0 / kEach * kRows + r) * kEach + i0 % kEach] = scale_of(p, c, i);
-      if constexpr (kZeros) {
-        uint32_t z = (c.z[i] & 15u) << (4 * (i0 % kEach));
-#pragma unroll
-        for (int o = 1; o < kEach; o <<= 1) z |= __shfl_xor_sync(0xffffffffu, z, o);
-        if (i0 % kEach == 0) zeros[i0 / kEach * kRows + r] = (uint16_t)z;
-      }
+      const int at = (i0 / kEach * kRows + i * (32 / NL) + row) * kEach + i0 % kEach;
+      scales[at] = scale_of(p, c, i);
+      if constexpr (kZeros) zeros[at] = (uint8_t)c.z[i];
     }
   }
 }
 
-// Adds the products of a part of 16 rows (lo and hi: a lane's words of rows g and g + 8 by step)
-// to their sums.  s: the groups' scales of those rows; z: their zeros, 4 bits each.
+// Adds the products of a part of the tile's rows (q: a lane's words of rows g + 8 h by step) to
+// their sums.  s: the groups' scales of those rows; z: their zeros, a byte each.
 template <int NT, int GS, bool kZeros>
-__device__ __forceinline__ void multiply_rows(const uint32_t (&lo)[4], const uint32_t (&hi)[4], const float (&s0)[4 / GS],
-                                              const float (&s1)[4 / GS], uint32_t z0, uint32_t z1, const uint8_t* xs, int unit,
-                                              bool has_x, float (&acc)[NT][4], uint32_t magic) {
+__device__ __forceinline__ void multiply_part(const uint32_t (&q)[2 * kSub][4], const float (&s)[2 * kSub][4 / GS],
+                                              const uint32_t (&z)[2 * kSub], const uint8_t* xs, int unit,
+                                              float (&acc)[kSub][NT][4], uint32_t magic) {
 #pragma unroll
   for (int g = 0; g < 4 / GS; ++g) {
-    uint32_t b0 = 0x43084308u, b1 = 0x43084308u;
-    if (kZeros) {
-      b0 = 0x43004300u + 0x00010001u * (z0 >> (4 * g) & 15u);
-      b1 = 0x43004300u + 0x00010001u * (z1 >> (4 * g) & 15u);
-    }
-    float sum[NT][4];
+    uint32_t bias[2 * kSub];
 #pragma unroll
-    for (int s = 0; s < GS; ++s) {
-      const int j = g * GS + s;
-      uint32_t a[4], b[4];
+    for (int h = 0; h < 2 * kSub; ++h) bias[h] = kZeros ? __byte_perm(z[h], 0x43, 0x4040 + 0x101 * g) : 0x43084308u;
+    float sum[kSub][NT][4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        a[q] = weights2(lo[j], q, magic, b0);
-        b[q] = weights2(hi[j], q, magic, b1);
+    for (int i = 0; i < GS; ++i) {
+      const int j = g * GS + i;
+      uint4 x[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) x[n] = *reinterpret_cast<const uint4*>(xs + (j * NT + n) * unit);
+#pragma unroll
+      for (int b = 0; b < kSub; ++b) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          lo[e] = weights2(q[2 * b][j], e, magic, bias[2 * b]);
+          hi[e] = weights2(q[2 * b + 1][j], e, magic, bias[2 * b + 1]);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if (i == 0) mma16816_first(sum[b][n], lo[0], hi[0], lo[1], hi[1], x[n].x, x[n].y);
+          else mma16816(sum[b][n], lo[0], hi[0], lo[1], hi[1], x[n].x, x[n].y);
+          mma16816(sum[b][n], lo[2], hi[2], lo[3], hi[3], x[n].z, x[n].w);
+        }
       }
-#pragma unroll
-      for (int i = 0; i < NT; ++i) {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (NT > 1 || has_x) x = *reinterpret_cast<const uint4*>(xs + (j * NT + i) * unit);
-        if (s == 0) mma16816_first(sum[i], a[0], b[0], a[1], b[1], x.x, x.y);
-        else mma16816(sum[i], a[0], b[0], a[1], b[1], x.x, x.y);
-        mma16816(sum[i], a[2], b[2], a[3], b[3], x.z, x.w);
-      }
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      acc[i][0] = fmaf(s0[g], sum[i][0], acc[i][0]);
-      acc[i][1] = fmaf(s0[g], sum[i][1], acc[i][1]);
-      acc[i][2] = fmaf(s1[g], sum[i][2], acc[i][2]);
-      acc[i][3] = fmaf(s1[g], sum[i][3], acc[i][3]);
-    }
+    for (int b = 0; b < kSub; ++b)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[b][n][e] = fmaf(s[2 * b + (e >> 1)][g], sum[b][n][e], acc[b][n][e]);
   }
 }
 
@@ -294,11 +296,6 @@ __device__ __forceinline__ void copy_vectors(const W4Params& p, uint32_t to, int
   }
 }
 
-// The threads of a group of warps wait for one another.
-__device__ __forceinline__ void group_barrier(int group, int warps) {
-  asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(warps * 32) : "memory");
-}
-
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -318,19 +315,20 @@ template <int NT, int GS, bool kAligned, bool kZeros>
 __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, const __grid_constant__ CUtensorMap map) {
   using L = Layout<NT, GS, kAligned, kZeros>;
   constexpr bool kTurned = GS < 4 || !kAligned;  // a quad's words are of the same 16 bytes
-  constexpr int kSums = L::kSums, R = kRows / 8, A = kAhead, P = kParts<NT>;
+  constexpr int kSums = L::kSums, R = kRows / 8, A = kAhead, P = kParts<NT, GS>;
+  constexpr int H = GS == 4 ? 2 : 1;                 // chunks whose scales are on their way
   constexpr int kEach = L::kGroups, NL = P * kEach;  // scales of a lane and part, and chunk
   extern __shared__ __align__(1024) uint8_t dyn[];
   __shared__ uint64_t landed[kWarps][A];
+  __shared__ int begun[kWarps];  // the tile that a warp has the first of several parts of (as ~tile: in its ring), or -1
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = lane & 3;
-  const int S = p.split, groups = kWarps / S, group = warp / S, member = warp % S;
   const uint8_t* ring = dyn + warp * A * L::kSlot;
-  float* join = reinterpret_cast<float*>(dyn + L::kRing) + group * S * kSums;  // [S][kSums]
+  float* join = reinterpret_cast<float*>(dyn + L::kRing);                       // [kWarps][kSums]
   float* scales = reinterpret_cast<float*>(dyn + L::kRing + L::kJoin + warp * L::kScales);  // [P][kRows][kGroups]
-  uint16_t* zeros = reinterpret_cast<uint16_t*>(dyn + L::kRing + L::kJoin + kWarps * L::kScales + warp * L::kZeroBytes);  // [P][kRows]
+  uint8_t* zeros = dyn + L::kRing + L::kJoin + kWarps * L::kScales + warp * L::kZeroBytes;  // [P][kRows][kGroups]
   float* others = reinterpret_cast<float*>(dyn + L::kFixed);                                // [ksplit][kSums]
-  float* kept = others + (p.ksplit > 1 ? p.ksplit * kSums : 0) + group * p.batch * kSums;   // [batch][kSums]
-  uint8_t* xs = dyn + L::kFixed + ((p.ksplit > 1 ? p.ksplit : 0) + (p.blocks > 1 ? groups * p.batch : 0)) * kSums * 4;
+  float* kept = others + (p.ksplit > 1 ? p.ksplit * kSums : 0);                             // [batch][kSums]
+  uint8_t* xs = dyn + L::kFixed + ((p.ksplit > 1 ? p.ksplit : 0) + (p.blocks > 1 ? p.batch : 0)) * kSums * 4;
   if (lane == 0) {
 #pragma unroll
     for (int s = 0; s < A; ++s) mbar_init(&landed[warp][s], 1);
@@ -341,16 +339,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tiles = (p.n + kRows - 1) / kRows;
-  // group g of block (or cluster) b of B takes tiles b + B g, then every (B groups)-th
+  // block (or cluster) b of B takes tiles b, b + B, ...
   const int block = (int)blockIdx.x / p.ksplit, rank = (int)blockIdx.x % p.ksplit, blocks = (int)gridDim.x / p.ksplit;
-  const int tile0 = block + group * blocks, stride = blocks * groups;
-  const int mine = tile0 < tiles ? (tiles - tile0 + stride - 1) / stride : 0;
-  const int most = block < tiles ? (tiles - block + stride - 1) / stride : 0;  // of any group here
-  const int my_chunks = min((p.k + kChunk<NT> - 1) / kChunk<NT>, (rank + 1) * p.rank_chunks);  // up to which this block goes
+  const int mine = (tiles - block + blocks - 1) / blocks;
+  const int my_chunks = min((p.k + kChunk<NT, GS> - 1) / kChunk<NT, GS>, (rank + 1) * p.rank_chunks);  // up to which this block goes
   const uint32_t ring_at = smem_u32(ring), magic = exponent_bits();
   const int unit = 64 << p.x_shift;                                            // bytes of x of a step and 8 rows
-  const bool has_x = (lane >> 2) < (1 << p.x_shift);
-  const uint8_t* my_x = xs + (has_x ? lane * 16 : 0);
+  const uint8_t* my_x = xs + (lane & ((4 << p.x_shift) - 1)) * 16;             // (rows that are not there repeat others; their sums are dropped)
   // where a lane's words of a part lie: of row g, by step
   uint32_t word_at[4], cut[R];
   {
@@ -366,17 +361,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   int flying = 0, lost = 0;  // copies on their way, and the slot of the oldest once a wait has given up
   bool alive = true;         // no wait has given up
   for (int m0 = 0; m0 < p.m; m0 += 8 * NT) {
-    for (int first = 0; first < most; first += p.batch) {
-      const int batch = max(0, min(p.batch, mine - first));
+    for (int first = 0; first < mine; first += p.batch) {
+      const int batch = min(p.batch, mine - first);
       for (int kb = 0; kb < p.blocks; ++kb) {
+        // The chunks of the tiles, in order: each warp takes a stretch of them.
         const int chunk0 = rank * p.rank_chunks + kb * p.block_chunks;
         const int chunks = max(0, min(p.block_chunks, my_chunks - chunk0));
-        const int per = (chunks - member + S - 1) / S;  // chunks of this warp and a tile (none: the group's others have them)
-        const int items = batch * max(per, 1);
-        Scales<NL, kZeros> c[A];
-        int lt = 0, lc = member, load_tile = tile0 + first * stride;  // the next chunk to load, and its tile
-        auto load = [&](Scales<NL, kZeros>& into, int s) {
-          if (lt < batch && lc < chunks) {
+        const int items = batch * chunks, per = (items + kWarps - 1) / kWarps;
+        const int begin = min(warp * per, items), end = min(begin + per, items);
+        int tile = batch == 1 ? 0 : begin / max(chunks, 1), at = begin - tile * chunks;
+        int li = begin, lc = at, load_tile = block + (first + tile) * blocks;  // the next chunk to load, and its tile
+        auto load = [&](int s) {
+          if (li < end) {
             const int part = (chunk0 + lc) * P;
             if (!kAligned) {
               copy_vectors<P>(p, ring_at + s * L::kSlot, load_tile, part, lane);
@@ -390,149 +386,199 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                            &landed[warp][s]);
               }
             }
-            load_scales(p, into, load_tile, part, lane);
           }
           if (!kAligned) asm volatile("cp.async.commit_group;" ::: "memory");
-          lc += S;
-          if (lc < chunks) return;
-          lc = member;
-          ++lt;
-          load_tile += stride;
+          ++li;
+          if (++lc < chunks) return;
+          lc = 0;
+          load_tile += blocks;
+        };
+        // Scales are loaded ahead too: of the next chunk, or two where they take few registers.
+        Scales<NL, kZeros> ahead[H] = {};
+        int si = begin, sat = at, scale_tile = load_tile;
+        auto scales_of = [&](int of) { return min((int64_t)of * kRows + lane, (int64_t)p.n - 1) * p.groups; };  // (of this lane's row)
+        int64_t row_at = scales_of(scale_tile);
+        auto load_next = [&](Scales<NL, kZeros>& into) {
+          if (si < end) load_scales(p, into, scale_tile, row_at, (chunk0 + sat) * P, lane);
+          ++si;
+          if (++sat < chunks) return;
+          sat = 0;
+          scale_tile += blocks;
+          row_at = scales_of(scale_tile);
         };
 #pragma unroll
-        for (int s = 0; s < A; ++s) load(c[s], s);
+        for (int s = 0; s < A; ++s) load(s);
+#pragma unroll
+        for (int u = 0; u < H; ++u) load_next(ahead[u]);
         if (p.blocks > 1 || first == 0) {
           __syncthreads();  // (the x of the block before is no longer read)
           stage_x<NT, kTurned>(p, xs, chunk0 * P, chunks * P, m0);
           __syncthreads();
         }
+        // A sum of a tile over this block of k: kept for the next, or a result.
+        auto emit = [&](int of, int o, float v) {
+          if (kb > 0) v += kept[of * kSums + o];
+          if (kb + 1 < p.blocks) kept[of * kSums + o] = v;
+          else if (p.ksplit > 1) push_sum(others + rank * kSums + o, v);  // (into the cluster's first block)
+          else write_sum(p, m0 + o / kRows, (int64_t)(block + (first + of) * blocks) * kRows + o % kRows, v);
+        };
         float acc[kSub][NT][4] = {};
-        int tile = 0, at = member;
-        for (int it = 0; it < items; it += A) {
+        int from = at;        // where in the tile this warp's part begins
+        bool earlier = false;  // a part of another tile went before
+        if (lane == 0) begun[warp] = -1;
+        int s = 0;  // the ring's slot of the chunk
+#pragma unroll 1
+        for (int it = begin; it < end; it += H) {
 #pragma unroll
-          for (int s = 0; s < A; ++s) {
-            if (it + s >= items) break;
-            if (at < chunks) {
-              if (!kAligned) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copies of the chunk have landed
-                __syncwarp();
-              } else {
-                if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
-                  if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
-                  alive = false;  // (no more copies; those on their way are waited for at the end)
-                  lost = s;
-                }
-                if (alive) {
-                  parity ^= 1u << s;
-                  --flying;
-                }
-              }
-              const Scales<NL, kZeros> now = c[s];
-              if constexpr (GS < 4) {
-                spread_scales<kEach>(p, now, scales, zeros, lane);
-                __syncwarp();
-              }
-              const uint8_t* slot = ring + s * L::kSlot;
-#pragma unroll
-              for (int c2 = 0; c2 < P; ++c2) {
-                uint32_t q[R][4];
-#pragma unroll
-                for (int h = 0; h < R; ++h) {
-                  if (!kTurned) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(slot + c2 * kRows * 64 + h * 512 + lane * 16);
-                    q[h][0] = v.x, q[h][1] = v.y, q[h][2] = v.z, q[h][3] = v.w;
-                  } else if (kAligned) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                      q[h][j] = *reinterpret_cast<const uint32_t*>(slot + c2 * kRows * 64 + h * 512 + word_at[j]);
-                  } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                      const uint32_t* w = reinterpret_cast<const uint32_t*>(slot + c2 * 64 + h * 8 * L::kPitch + word_at[j] + (cut[h] & ~3u));
-                      q[h][j] = __funnelshift_r(w[0], w[1], 8 * (cut[h] & 3));
-                    }
-                  }
-                }
-                if (c2 + 1 == P) {
-                  __syncwarp();
-                  load(c[s], s);  // (over what the warp has just read)
-                }
-#pragma unroll
-                for (int b = 0; b < kSub; ++b) {
-                  const int row = 16 * b + (lane >> 2);
-                  float s0[L::kGroups], s1[L::kGroups];
-                  uint32_t z0 = 0, z1 = 0;
-                  if constexpr (GS == 4) {
-                    // (rows 16 b .. are all of load b where a lane has one of two parts each)
-                    const bool apart = P == 2 && !p.scale_vec;
-                    const int from = apart ? row % 16 * 2 + c2 : row, step = apart ? 16 : 8;
-                    const float v = apart ? scale_of(p, now, b % NL) : scale_of(p, now, c2);
-                    s0[0] = __shfl_sync(0xffffffffu, v, from);
-                    s1[0] = __shfl_sync(0xffffffffu, v, from + step);
-                    if constexpr (kZeros) {
-                      const uint32_t z = apart ? now.z[b % NL] : p.scale_vec ? now.z[0] >> (8 * c2) : now.z[c2];
-                      z0 = __shfl_sync(0xffffffffu, z, from);
-                      z1 = __shfl_sync(0xffffffffu, z, from + step);
-                    }
-                  } else {
-#pragma unroll
-                    for (int g = 0; g < L::kGroups; ++g) {
-                      s0[g] = scales[(c2 * kRows + row) * L::kGroups + g];
-                      s1[g] = scales[(c2 * kRows + row + 8) * L::kGroups + g];
-                    }
-                    if constexpr (kZeros) {
-                      z0 = zeros[c2 * kRows + row];
-                      z1 = zeros[c2 * kRows + row + 8];
-                    }
-                  }
-                  multiply_rows<NT, GS, kZeros>(q[2 * b], q[2 * b + 1], s0, s1, z0, z1,
-                                                my_x + (int64_t)(at * P + c2) * 4 * NT * unit, unit, has_x, acc[b], magic);
-                }
-              }
-              if (GS < 4) __syncwarp();  // (the scales have been read)
+          for (int u = 0; u < H; ++u) {
+            if (it + u >= end) break;
+            if (!kAligned) {
+              asm volatile("cp.async.wait_group %0;" ::"n"(A - 1) : "memory");  // this lane's copies of the chunk have landed
+              __syncwarp();
             } else {
-              load(c[s], s);
+              if (alive && !mbar_wait(&landed[warp][s], (parity >> s) & 1u)) {
+                if (p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
+                alive = false;  // (no more copies; those on their way are waited for at the end)
+                lost = s;
+              }
+              if (alive) {
+                parity ^= 1u << s;
+                --flying;
+              }
             }
-            at += S;
-            if (at < chunks) continue;
-            // the tile's sums: this warp's, once the group has read those of the tile before, then all of them
-            group_barrier(group, S);
-            float* mp = join + member * kSums + t * 2 * kRows + (lane >> 2);
+            const Scales<NL, kZeros> now = ahead[u];
+            const bool apart = P == 2 && !p.scale_vec;  // (groups of 128: a lane has one of two parts of rows 16 i .. in load i)
+            float own[NL];
+            if constexpr (GS == 4) {
+#pragma unroll
+              for (int i = 0; i < NL; ++i) own[i] = scale_of(p, now, i);
+            }
+            if constexpr (GS < 4) {
+              spread_scales<kEach>(p, now, scales, zeros, lane);
+              __syncwarp();
+            }
+            load_next(ahead[u]);
+            const uint8_t* slot = ring + s * L::kSlot;
+#pragma unroll
+            for (int c2 = 0; c2 < P; ++c2) {
+              uint32_t q[R][4];
+#pragma unroll
+              for (int h = 0; h < R; ++h) {
+                if (!kTurned) {
+                  const uint4 v = *reinterpret_cast<const uint4*>(slot + c2 * kRows * 64 + h * 512 + lane * 16);
+                  q[h][0] = v.x, q[h][1] = v.y, q[h][2] = v.z, q[h][3] = v.w;
+                } else if (kAligned) {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j)
+                    q[h][j] = *reinterpret_cast<const uint32_t*>(slot + c2 * kRows * 64 + h * 512 + word_at[j]);
+                } else {
+#pragma unroll
+                  for (int j = 0; j < 4; ++j) {
+                    const uint32_t* w = reinterpret_cast<const uint32_t*>(slot + c2 * 64 + h * 8 * L::kPitch + word_at[j] + (cut[h] & ~3u));
+                    q[h][j] = __funnelshift_r(w[0], w[1], 8 * (cut[h] & 3));
+                  }
+                }
+              }
+              if (c2 + 1 == P) {
+                __syncwarp();
+                load(s);  // (over what the warp has just read)
+              }
+              float sc[R][L::kGroups];
+              uint32_t z[R] = {};
+#pragma unroll
+              for (int h = 0; h < R; ++h) {
+                const int row = 8 * h + (lane >> 2);
+                if constexpr (GS == 4) {
+                  const int from = apart ? row % 16 * 2 + c2 : row;
+                  sc[h][0] = __shfl_sync(0xffffffffu, apart ? own[h / 2 % NL] : own[c2], from);
+                  if constexpr (kZeros)
+                    z[h] = __shfl_sync(0xffffffffu, apart ? now.z[h / 2 % NL] : p.scale_vec ? now.z[0] >> (8 * c2) : now.z[c2], from) & 15u;
+                } else {
+#pragma unroll
+                  for (int g = 0; g < L::kGroups; ++g) sc[h][g] = scales[(c2 * kRows + row) * L::kGroups + g];
+                  if constexpr (kZeros) {
+                    const uint8_t* at = zeros + (c2 * kRows + row) * L::kGroups;
+                    z[h] = (L::kGroups == 4 ? *reinterpret_cast<const uint32_t*>(at) : *reinterpret_cast<const uint16_t*>(at)) & 0x0f0f0f0fu;
+                  }
+                }
+              }
+              multiply_part<NT, GS, kZeros>(q, sc, z, my_x + (at * P + c2) * 4 * NT * unit, unit, acc, magic);
+            }
+            if (GS < 4) __syncwarp();  // (the scales have been read)
+            s = s + 1 == A ? 0 : s + 1;
+            if (++at < chunks && it + u + 1 < end) continue;
+            // The end of the tile, or of what this warp has of it: then its first part goes into its
+            // place for joins and its last one into its ring, which it no longer needs.
+            const bool all = from == 0 && at == chunks && p.ksplit == 1;
+            const int o0 = t * 2 * kRows + (lane >> 2);  // a lane's first sum
+            float* to = all ? kept + tile * kSums : earlier ? reinterpret_cast<float*>(dyn + warp * A * L::kSlot) : join + warp * kSums;
+            if (all && kb + 1 == p.blocks && p.ksplit == 1) {
+              const int64_t n0 = (int64_t)(block + (first + tile) * blocks) * kRows + (lane >> 2);
+#pragma unroll
+              for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2 * kSub; ++h)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    float v = acc[h / 2][i][(h & 1) * 2 + e];
+                    if (kb > 0) v += to[o0 + (i * 8 + e) * kRows + 8 * h];
+                    write_sum(p, m0 + i * 8 + t * 2 + e, n0 + 8 * h, v);
+                  }
+            } else {
+#pragma unroll
+              for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int h = 0; h < 2 * kSub; ++h)
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    float& v = to[o0 + (i * 8 + e) * kRows + 8 * h];
+                    v = (all && kb > 0 ? v : 0.f) + acc[h / 2][i][(h & 1) * 2 + e];
+                  }
+              if (!all && from == 0 && lane == 0) begun[warp] = earlier ? ~tile : tile;
+            }
 #pragma unroll
             for (int b = 0; b < kSub; ++b)
 #pragma unroll
               for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  mp[(i * 8 + (e & 1)) * kRows + b * 16 + (e >> 1) * 8] = acc[b][i][e];
-                  acc[b][i][e] = 0.f;
-                }
-            group_barrier(group, S);
-            for (int o = member * 32 + lane; o < kSums; o += S * 32) {
-              float v = kb > 0 ? kept[tile * kSums + o] : 0.f;
-#pragma unroll 4
-              for (int w = 0; w < S; ++w) v += join[w * kSums + o];
-              if (kb + 1 < p.blocks) {
-                kept[tile * kSums + o] = v;
-                continue;
-              }
-              if (p.ksplit > 1) push_sum(others + rank * kSums + o, v);  // (into the cluster's first block)
-              else write_sum(p, m0 + o / kRows, (int64_t)(tile0 + (first + tile) * stride) * kRows + o % kRows, v);
-            }
-            if (p.ksplit > 1 && kb + 1 == p.blocks) {  // (one tile and one group: the whole cluster comes here together)
-              cluster_sync();
-              if (rank == 0) {
-                for (int o = threadIdx.x; o < kSums; o += kWarps * 32) {
-                  float v = 0.f;
-                  for (int r = 0; r < p.ksplit; ++r) v += others[r * kSums + o];
-                  write_sum(p, m0 + o / kRows, (int64_t)tile0 * kRows + o % kRows, v);
-                }
-              }
-              cluster_sync();
-            }
-            at = member;
+                for (int e = 0; e < 4; ++e) acc[b][i][e] = 0.f;
+            earlier = true;
+            at = from = 0;
             ++tile;
           }
+        }
+        // The tiles that several warps had parts of, by the first of these warps.
+        __syncthreads();
+        constexpr int kAtOnce = kWarps * 32 / kSums;
+        uint32_t owners = __ballot_sync(0xffffffffu, begun[lane % kWarps] != -1) & ((1u << kWarps) - 1);
+        for (int i = 0; owners; ++i, owners &= owners - 1) {
+          if (i % kAtOnce != (int)threadIdx.x / kSums) continue;
+          const int w = __ffs(owners) - 1, o = threadIdx.x % kSums;
+          int of = begun[w];
+          const float* mp = of < 0 ? reinterpret_cast<const float*>(dyn + w * A * L::kSlot) : join + w * kSums;
+          of = of < 0 ? ~of : of;
+          float v = mp[o];
+          const int stop = (of + 1) * chunks;
+#pragma unroll
+          for (int i = 1; i < kWarps; ++i) v += w + i < kWarps && (w + i) * per < stop ? join[(w + i) * kSums + o] : 0.f;
+          emit(of, o, v);
+        }
+        if (chunks == 0)  // (a cluster's last block may have none in the last block of k)
+          for (int o = threadIdx.x; o < batch * kSums; o += kWarps * 32) emit(o / kSums, o % kSums, 0.f);
+        if (p.ksplit > 1 && kb + 1 == p.blocks) {  // (one tile)
+          cluster_sync();
+          if (rank == 0) {
+            for (int o = threadIdx.x; o < kSums; o += kWarps * 32) {
+              float v = 0.f;
+              for (int r = 0; r < p.ksplit; ++r) v += others[r * kSums + o];
+              write_sum(p, m0 + o / kRows, (int64_t)block * kRows + o % kRows, v);
+            }
+          }
+          cluster_sync();
+        }
+        if (kb + 1 < p.blocks || first + batch < mine || m0 + 8 * NT < p.m) {
+          if (kAligned) fence_proxy_async_smem();
+          __syncthreads();  // (rings, sums kept and parts have been read)
         }
       }
     }
@@ -551,38 +597,32 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
   constexpr int W = kWarps, sms = 152;
   constexpr int sums = L::kSums * 4;  // bytes
   constexpr int room = kW4Smem - L::kFixed;
-  static_assert(room / 4 >= W / 4 * sums, "a tile of each group must be kept");
-  static_assert(room - room / 4 >= 4 * 4 * kParts<NT> * NT * 512 && room > kMaxSplit * sums + sums * 2 + 4 * kParts<NT> * NT * 512, "a block of k must fit");
-  p.scale_vec = p.groups % (kParts<NT> * (GS == 4 ? 1 : L::kGroups)) == 0;
+  static_assert(room - kMaxSplit * sums >= 4 * sums && room - room / 4 - kMaxSplit * sums >= 4 * kParts<NT, GS> * NT * 512, "a tile's sums and a block of k must fit");
+  static_assert(kAhead * L::kSlot >= sums, "a part's sums must fit a warp's ring");
+  p.scale_vec = p.groups % (kParts<NT, GS> * (GS == 4 ? 1 : L::kGroups)) == 0;
   // rows of x that are kept of every 8: a power of two
   p.x_shift = NT > 1 || p.m > 4 ? 3 : p.m > 2 ? 2 : p.m > 1 ? 1 : 0;
-  const int x_bytes = 4 * kParts<NT> * NT * (64 << p.x_shift);  // of a chunk
+  const int x_bytes = 4 * kParts<NT, GS> * NT * (64 << p.x_shift);  // of a chunk
   const int tiles = (p.n + kRows - 1) / kRows;
-  const int chunks = (p.k + kChunk<NT> - 1) / kChunk<NT>;
+  const int chunks = (p.k + kChunk<NT, GS> - 1) / kChunk<NT, GS>;
   // Few tiles of long rows: as many blocks to a tile as leave each warp a chunk.
   int split = 1;
   while (split < kMaxSplit && tiles * split * 2 <= sms && chunks >= split * 2 * W) split *= 2;
   p.ksplit = split;
   p.rank_chunks = (chunks + split - 1) / split;
   const int others = split > 1 ? split * sums : 0, left = room - others;
-  // (a block of a group's width of k has to fit)
-  int S = split > 1 || tiles <= sms ? W : tiles <= 4 * sms ? 8 : 4;
-  while (split == 1 && S * x_bytes > left - left / 4) S /= 2;
-  p.split = S;
-  const int groups = W / S;
-  const int whole = (p.rank_chunks + S - 1) / S * S;
+  const int grid = split > 1 ? tiles * split : std::min(tiles, sms);
   p.blocks = 1;
-  p.block_chunks = whole;
+  p.block_chunks = p.rank_chunks;
   p.batch = 0x3fffffff;
-  int smem = L::kFixed + others + whole * x_bytes;
-  if (whole > left / x_bytes) {  // blocks of k, as even as they come: a quarter of the room keeps sums
-    p.batch = std::max(1, left / 4 / (groups * sums));
-    const int fits = (left - p.batch * groups * sums) / x_bytes;
+  int smem = L::kFixed + others + p.rank_chunks * x_bytes;
+  if (p.rank_chunks > left / x_bytes) {  // blocks of k, as even as they come: up to a quarter of the room keeps sums
+    p.batch = split > 1 ? 1 : std::min(left / 4 / sums, (tiles + grid - 1) / grid);
+    const int fits = (left - p.batch * sums) / x_bytes;
     p.blocks = (p.rank_chunks + fits - 1) / fits;
     p.block_chunks = (p.rank_chunks + p.blocks - 1) / p.blocks;
-    if (p.block_chunks > S) p.block_chunks = std::min(fits, (p.block_chunks + S - 1) / S * S);
     p.blocks = (p.rank_chunks + p.block_chunks - 1) / p.block_chunks;
-    smem = L::kFixed + others + p.batch * groups * sums + p.block_chunks * x_bytes;
+    smem = L::kFixed + others + p.batch * sums + p.block_chunks * x_bytes;
   }
   CUtensorMap map = {};
   if (kAligned) {
@@ -596,7 +636,7 @@ int launch_w4_as(W4Params& p, cudaStream_t st) {
     if (r != CUDA_SUCCESS) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
   }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : std::min(tiles, sms)));
+  cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(W * 32);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = st;
