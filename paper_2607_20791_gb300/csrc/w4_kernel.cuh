@@ -8,7 +8,7 @@
 // shared memory, 4 to 8 KB ahead of its use.  Every 128 weights are 8 mma.m16n8k16 with the
 // weights as A for every 16 rows of W and 8 rows of x: one row of x costs the same as
 // eight, and the tensor pipe does the sums over k in fp32.  (With 17 to 32 rows of x the
-// weights are read twice, 16 rows at a time: 155 us for 32 x 4096 x 128256 where one pass
+// weights are read twice, 16 rows at a time: 156 us for 32 x 4096 x 128256 where one pass
 // of 32 took 198, x coming from shared memory in blocks of k.)
 //
 // Which k a lane's A elements stand for is free as long as B agrees, so a lane feeds the
@@ -28,12 +28,12 @@
 // One block of 16 warps fills an SM, so that x lies there once.  A warp writes the sums of the
 // tiles it has whole; a tile that several warps have parts of is joined in shared memory at
 // the end, so that nothing waits in between (groups of 4 warps that shared each tile, with
-// two barriers a tile, took 61 us where this takes 56 for 5 x 4096 x 128256, and 33 where
+// two barriers a tile, took 61 us where this takes 57 for 5 x 4096 x 128256, and 33 where
 // this takes 29 for 13 x 2730 x 20011).  Where x does not fit, k goes in blocks, with the
 // sums of the block's tiles kept in shared memory between them.  Few tiles of long rows are
 // shared by the blocks of a cluster, each with a stretch of k, whose sums the first one joins.
 //
-// What bounds it: 5 x 4096 x 128256 in groups of 128 takes 56 us, 0.72 of the copy rate, with
+// What bounds it: 5 x 4096 x 128256 in groups of 128 takes 57 us, 0.71 of the copy rate, with
 // 0.6 of the issue slots and of the integer pipe's cycles taken (7 integer operations and 4
 // subtractions for every 8 weights of 32 rows), the tensor pipe a quarter busy.
 #pragma once
@@ -480,6 +480,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
                 }
               }
               if (c2 + 1 == P) {
+                if (kAligned) fence_proxy_async_smem();  // (without it a read was put off until the copy had overwritten its place)
                 __syncwarp();
                 load(s);  // (over what the warp has just read)
               }

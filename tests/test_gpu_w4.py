@@ -4,7 +4,7 @@ The bound, from the kernel's steps: a product of a bf16 with a whole number of 4
 exact in fp32; a group's products are summed in the tensor core's fp32 accumulator (at
 most 2^-23 of the sum of magnitudes for each of up to 128 terms), scaled (one rounding) and
 summed over the groups and the warps (at most K / 32 + 64 roundings of 2^-24): in all at
-most (129 + K / 64 + 32) 2^-23 sum |x| |w|; a bf16 result is rounded once more (2^-9 of it)."""
+most (129 + K / 64 + 32) 2^-23 sum |x| |w|; a bf16 result is the fp32 one, rounded."""
 import numpy as np
 import pytest
 
@@ -66,6 +66,31 @@ def test_rows(gpu_lib, m, n, k):
 @pytest.mark.parametrize("scales, out", [("bf16", "f32"), ("f32", "bf16")])
 def test_sizes(gpu_lib, m, n, k, group, scales, out):
     _run(m, n, k, group, k % 3 == 0, scales, out, seed=3, pad=5)
+
+
+@pytest.mark.parametrize("m, n, k, group", [(3, 60007, 200, 128), (5, 40000, 512, 64), (2, 50001, 600, 32), (12, 40003, 384, 128),
+                                            (9, 30000, 300, 32), (6, 60000, 1024, 128)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_warps_with_whole_tiles(gpu_lib, m, n, k, group, zeros):
+    """So many rows of W that a warp's share holds tiles of its own and parts of tiles shared with others."""
+    _run(m, n, k, group, zeros, seed=6)
+
+
+@pytest.mark.parametrize("m, n, k, group", [(5, 128256, 4096, 128), (1, 128256, 4096, 64), (12, 128256, 4096, 128),
+                                            (8, 128256, 4096, 32), (5, 128256, 2730, 128), (13, 20011, 2730, 32)])
+def test_same_result_every_time(gpu_lib, m, n, k, group):
+    """A place in the ring is copied over only once it has been read: what comes early gives other sums."""
+    import torch
+    x = torch.randn(m, k, device="cuda").to(torch.bfloat16)
+    w = torch.randint(0, 256, (n, (k + 1) // 2), device="cuda", dtype=torch.uint8)
+    s = torch.rand(n, -(-k // group), device="cuda").to(torch.bfloat16)
+    first, y = torch.empty(m, n, device="cuda"), torch.empty(m, n, device="cuda")
+    binding.rgd_w4_matvec(x, w, s, None, group, first)
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(200):
+        binding.rgd_w4_matvec(x, w, s, None, group, y)
+        wrong += (y != first).sum()
+    assert int(wrong.item()) == 0
 
 
 def test_every_weight_and_zero_point(gpu_lib):
