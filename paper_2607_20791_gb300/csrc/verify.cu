@@ -46,7 +46,7 @@ constexpr int kGroups = 16;  // groups of a lane's vectors whose maxima it keeps
 template <bool kAligned>
 constexpr int kFlight = kAligned ? 8 : 4;
 constexpr int kVerifyCluster = 16;                           // CTAs of a unit at most
-constexpr int32_t kTaken = -1, kRejectedRow = -2;            // results of a unit other than a token
+constexpr int32_t kTaken = -1, kRejectedRow = -2;            // results of a unit other than a token + 1
 
 struct VerifyParams {
   const uint8_t* target;
@@ -476,44 +476,60 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
 }
 
 // The whole warp: a row's finished unit is counted, and the last one to finish writes the row.
+// Results are never 0 and start at 0, so that the last one needs no other order than each
+// result's own: it reads them until all are there.  (A counter that released and acquired
+// them took 1 us more.)
 __device__ __noinline__ void finish_unit(const VerifyParams& p, int row, int pos, int n, int32_t result) {
   const int lane = threadIdx.x & 31;
   int32_t* res = p.result + (int64_t)row * (p.max_draft + 1);
+  const int32_t* drafts = p.tokens + (int64_t)row * p.max_draft;
+  const int32_t draft = lane < n ? drafts[lane] : -1;
   int last = 0;
   if (lane == 0) {
-    res[pos] = result;
+    asm volatile("st.relaxed.gpu.global.s32 [%0], %1;" ::"l"(res + pos), "r"(result) : "memory");
     int32_t old;
-    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(p.count + row) : "memory");
+    asm volatile("atom.relaxed.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(p.count + row) : "memory");
     last = old == n;
   }
   if (!__shfl_sync(0xffffffffu, last, 0)) return;
-  __syncwarp();
   int taken = n;
   int32_t token = kRejectedRow;
+  const uint64_t t0 = globaltimer_ns();
+  bool there = true;
   for (int base = 0; base <= n; base += 32) {
-    const int32_t v = base + lane <= n ? __ldcg(res + base + lane) : kTaken;
+    int32_t v = kTaken;
+    if (base + lane <= n) {
+      do {
+        asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(res + base + lane) : "memory");
+      } while (v == 0 && globaltimer_ns() - t0 < kWaitLimitNs);
+      asm volatile("st.relaxed.gpu.global.s32 [%0], 0;" ::"l"(res + base + lane) : "memory");
+    }
+    there = __all_sync(0xffffffffu, v != 0) && there;
     const uint32_t stop = __ballot_sync(0xffffffffu, v != kTaken);
-    if (stop) {
+    if (stop && taken == n && token == kRejectedRow) {
       const int at = __ffs(stop) - 1;
       taken = base + at;
       token = __shfl_sync(0xffffffffu, v, at);
-      break;
+      if (token == kRejectedRow) taken = -1;
     }
   }
-  __syncwarp();
-  for (int i = lane; i <= n; i += 32) res[i] = 0;  // (the workspace is all zero again: its next call may have another shape)
-  const bool good = token != kRejectedRow;
+  const bool good = there && taken >= 0;
   for (int i = lane; i <= p.max_draft; i += 32)
     p.token_out[(int64_t)row * (p.max_draft + 1) + i] =
-        !good || i > taken ? -1 : i < taken ? p.tokens[(int64_t)row * p.max_draft + i] : token;
+        !good || i > taken ? -1 : i < taken ? (i < 32 ? draft : drafts[i]) : token - 1;
   if (lane == 0) {
     p.accepted_out[row] = good ? taken : 0;
     p.count[row] = 0;
+    if (!there && p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
   }
 }
 
 // What the CTAs pushed before is seen by the whole cluster after it.
-__device__ __forceinline__ void cluster_exchange() {
+__device__ __forceinline__ void exchanged(uint32_t csize) {
+  if (csize == 1) {
+    __syncthreads();
+    return;
+  }
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -558,7 +574,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     return;
   }
   if (pos > n) return;
-  cluster_arrive_relaxed();
+  if (csize > 1) cluster_arrive_relaxed();
   const int32_t d = has_draft ? p.tokens[(int64_t)row * K + pos] : -1;
   const bool d_in = d >= 0 && d < p.vocab;  // (a draft outside the vocabulary is rejected, q = 0 everywhere)
   const float u = has_draft && !greedy ? p.accept_u[(int64_t)row * K + pos] : 0.f;
@@ -574,9 +590,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
 
   // Pass 1: the maxima (NaN never wins).
   if (warp == kVerifyWarps - 1 && lane == 0) {
+    sh.theta = scaled_log(temp, min_p);  // (the token is still on its way)
     sh.tl = d_in && !greedy ? one_logit<T>(p.target + trow, d) : 0.f;
     sh.ql = d_in && two ? one_logit<T>(p.draft + qrow, d) : 0.f;
-    sh.theta = scaled_log(temp, min_p);
   }
   Kept tkept, qkept;
   {
@@ -588,12 +604,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     }
   }
   __syncthreads();
-  cluster_wait();  // every CTA of the cluster has started
+  if (csize > 1) cluster_wait();  // every CTA of the cluster has started
   if (warp < 2) {
     const float m = warp_max(sh.warp_top[warp][lane % kVerifyWarps]);
     if (lane < (int)csize) push(&sh.top[warp][rank], m, lane);
   }
-  cluster_exchange();
+  exchanged(csize);
   Side t, q;
   t.top = warp_max(sh.top[0][lane % csize]);
   q.top = warp_max(sh.top[1][lane % csize]);
@@ -626,12 +642,12 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.warp_sum[0][lane % kVerifyWarps]);
       if (lane == 0) push(&sh.sum[0][rank], best, 0);
     }
-    cluster_exchange();
+    exchanged(csize);
     if (leader) {
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.sum[0][lane % csize]);
       const bool same = has_draft && (int32_t)best == d;
       if (lane == 0 && prob && has_draft) *prob = same ? 1.f : 0.f;
-      finish_unit(p, row, pos, n, same ? kTaken : (int32_t)best);
+      finish_unit(p, row, pos, n, same ? kTaken : (int32_t)best + 1);
     }
     return;
   }
@@ -646,7 +662,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
       const uint64_t v = warp_sum(lane < kVerifyWarps ? sh.warp_sum[warp][lane] : 0);
       if (lane < (int)csize) push(&sh.sum[warp][rank], v, lane);
     }
-    cluster_exchange();
+    exchanged(csize);
   };
   auto over_cluster = [&](int which) { return warp_sum(lane < (int)csize ? sh.sum[which][lane] : 0); };
 
@@ -766,7 +782,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
           if (upto > mark) token = (int32_t)o0 + i * E + e;
           upto -= w[e];
         }
-        finish_unit(p, row, pos, n, __shfl_sync(0xffffffffu, token, at));
+        finish_unit(p, row, pos, n, __shfl_sync(0xffffffffu, token, at) + 1);
         return;
       } else {
         before += stripe;
@@ -792,11 +808,12 @@ int launch_verify(VerifyParams& p, cudaStream_t st) {
   // have a few CTAs for each of the 608 that fit the SMs, so that they are at different
   // stages, and 8 only to fill the SMs.  Measured: 400 units of 2 x 128256 bf16 40 us with 4,
   // 47 with 2, 51 with 8; 1024 of 3 x 152064 192 us with 2, 196 with 4; 192 of 262144
-  // fp32 58 us with 8, 80 with 4.  Few units are cut further until the SMs have two CTAs each.
+  // fp32 58 us with 8, 80 with 4.  Few units are cut further until the SMs have two CTAs each, but
+  // a CTA on its own needs no cluster's barriers: 9 units of 4096 fp32 8.4 us with 1, 9.4 with 2.
   int c = 1;
   while (c < kVerifyCluster && stripes(c) > 40) c *= 2;
   while (c < 8 && ((units * c < 1600 && stripes(2 * c) >= 16) || (units * c < 608 && stripes(2 * c) >= 8))) c *= 2;
-  while (c < kVerifyCluster && units * c < 304 && stripes(c) > 2) c *= 2;
+  while (c < kVerifyCluster && units * c < 304 && stripes(c) > 4) c *= 2;
   if (c > 8) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
