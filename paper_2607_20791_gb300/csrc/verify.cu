@@ -75,6 +75,8 @@ struct VerifyShared {
   float warp_top[2][kVerifyWarps], top[2][kVerifyCluster];
   uint64_t warp_sum[3][kVerifyWarps], sum[3][kVerifyCluster];  // target's and draft's weights, max(0, p - q)
   uint64_t part_sum[kVerifyWarps];  // of the parts of the share that a draw falls into
+  uint64_t arrived[3];  // barriers of the exchanges: maxima; weights (or argmax); max(0, p - q)
+  int lost;             // a wait has given up
   float theta, tl, ql;  // T ln p_min, the drafted token's logits
 };
 
@@ -524,20 +526,47 @@ __device__ __noinline__ void finish_unit(const VerifyParams& p, int row, int pos
   }
 }
 
-// What the CTAs pushed before is seen by the whole cluster after it.
-__device__ __forceinline__ void exchanged(uint32_t csize) {
-  if (csize == 1) {
-    __syncthreads();
-    return;
+// An exchange over the cluster: every CTA pushes a value (or two) into every CTA, counted by
+// the receiver's barrier of that exchange.  (With stores and a cluster barrier instead, which
+// waits for the stores' return, 80 rows of 5 positions by 128256 bf16 took 38.2 us for 36.8.)
+__device__ __forceinline__ void push(VerifyShared& sh, int exchange, uint64_t* slot, uint64_t v, uint32_t csize, uint32_t to) {
+  if (csize == 1) *slot = v;
+  else
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(peer_addr(smem_u32(slot), to)),
+                 "l"(v), "r"(peer_addr(smem_u32(&sh.arrived[exchange]), to))
+                 : "memory");
+}
+__device__ __forceinline__ void push(VerifyShared& sh, int exchange, float* slot, float v, uint32_t csize, uint32_t to) {
+  if (csize == 1) *slot = v;
+  else
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(peer_addr(smem_u32(slot), to)),
+                 "r"(__float_as_uint(v)), "r"(peer_addr(smem_u32(&sh.arrived[exchange]), to))
+                 : "memory");
+}
+// The whole CTA: what is pushed into it has arrived; false after 2 s, once no CTA of the cluster
+// can push any more.
+__device__ __forceinline__ bool exchanged(VerifyShared& sh, int exchange, uint32_t csize, int32_t* dev_status) {
+  if (csize > 1 && threadIdx.x == 0) {
+    const uint64_t t0 = globaltimer_ns();
+    uint32_t done = 0;
+    for (uint32_t i = 1; !done; ++i) {
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], 0;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(done)
+          : "r"(smem_u32(&sh.arrived[exchange]))
+          : "memory");
+      if (!done && (i & 63u) == 0 && globaltimer_ns() - t0 > kWaitLimitNs) break;
+    }
+    if (!done) sh.lost = 1;
   }
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  __syncthreads();
+  if (csize == 1 || !sh.lost) return true;
+  if (threadIdx.x == 0 && dev_status) atomicOr(dev_status, RGD_DEV_WAIT_TIMEOUT);
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // (a CTA that has ended counts as arrived)
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void push(const uint64_t* slot, uint64_t v, uint32_t rank) {
-  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(peer_addr(smem_u32(slot), rank)), "l"(v) : "memory");
-}
-__device__ __forceinline__ void push(const float* slot, float v, uint32_t rank) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(peer_addr(smem_u32(slot), rank)), "f"(v) : "memory");
+  return false;
 }
 
 template <typename T, bool kAligned>
@@ -574,11 +603,23 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     return;
   }
   if (pos > n) return;
-  if (csize > 1) cluster_arrive_relaxed();
   const int32_t d = has_draft ? p.tokens[(int64_t)row * K + pos] : -1;
   const bool d_in = d >= 0 && d < p.vocab;  // (a draft outside the vocabulary is rejected, q = 0 everywhere)
   const float u = has_draft && !greedy ? p.accept_u[(int64_t)row * K + pos] : 0.f;
   const bool two = p.draft != nullptr && has_draft && !greedy;
+  if (csize > 1) {
+    if (threadIdx.x == 0) {
+      sh.lost = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) mbar_init(&sh.arrived[i], 1);
+      fence_mbar_init();
+      mbar_arrive_expect_tx(&sh.arrived[0], csize * 8);
+      mbar_arrive_expect_tx(&sh.arrived[1], csize * (two ? 16 : 8));
+      mbar_arrive_expect_tx(&sh.arrived[2], csize * 8);
+    }
+    __syncwarp();
+    cluster_arrive_relaxed();
+  }
   const int64_t trow = ((int64_t)row * (K + 1) + pos) * p.target_stride, qrow = ((int64_t)row * K + pos) * p.draft_stride;
 
   // This warp's share, in the order of the elements over the cluster.
@@ -607,9 +648,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   if (csize > 1) cluster_wait();  // every CTA of the cluster has started
   if (warp < 2) {
     const float m = warp_max(sh.warp_top[warp][lane % kVerifyWarps]);
-    if (lane < (int)csize) push(&sh.top[warp][rank], m, lane);
+    if (lane < (int)csize) push(sh, 0, &sh.top[warp][rank], m, csize, lane);
   }
-  exchanged(csize);
+  if (!exchanged(sh, 0, csize, p.dev_status)) return;
   Side t, q;
   t.top = warp_max(sh.top[0][lane % csize]);
   q.top = warp_max(sh.top[1][lane % csize]);
@@ -640,9 +681,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     __syncthreads();
     if (warp == 0) {
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.warp_sum[0][lane % kVerifyWarps]);
-      if (lane == 0) push(&sh.sum[0][rank], best, 0);
+      if (lane == 0) push(sh, 1, &sh.sum[0][rank], best, csize, 0);
     }
-    exchanged(csize);
+    if (rank != 0 || !exchanged(sh, 1, csize, p.dev_status)) return;
     if (leader) {
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.sum[0][lane % csize]);
       const bool same = has_draft && (int32_t)best == d;
@@ -660,9 +701,9 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     __syncthreads();
     if (warp >= first && warp <= last) {
       const uint64_t v = warp_sum(lane < kVerifyWarps ? sh.warp_sum[warp][lane] : 0);
-      if (lane < (int)csize) push(&sh.sum[warp][rank], v, lane);
+      if (lane < (int)csize) push(sh, first ? 2 : 1, &sh.sum[warp][rank], v, csize, lane);
     }
-    exchanged(csize);
+    return exchanged(sh, first ? 2 : 1, csize, p.dev_status);
   };
   auto over_cluster = [&](int which) { return warp_sum(lane < (int)csize ? sh.sum[which][lane] : 0); };
 
@@ -672,7 +713,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   q.cut = __fadd_rn(q.top, sh.theta);
   join(0, sum_weights(tv, tkept, t, p.stripes, lane));
   if (two) join(1, sum_weights(qv, qkept, q, p.stripes, lane));
-  exchange(0, two ? 1 : 0);
+  if (!exchange(0, two ? 1 : 0)) return;
   uint64_t total = over_cluster(0);
   t.inv = __fdiv_rn(1.f, __ull2float_rn(total) * 0x1p-31f);
   if (two) q.inv = __fdiv_rn(1.f, __ull2float_rn(over_cluster(1)) * 0x1p-31f);
@@ -719,7 +760,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
         a = a1, c = c1;
       }
       join(2, warp_sum(rest.total()));
-      exchange(2, 2);
+      if (!exchange(2, 2)) return;
       const uint64_t rz = over_cluster(2);
       if (rz > 0) {  // (p and q may be equal but for rounding: then p itself)
         which = 2;
@@ -739,19 +780,26 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   const Share<T, kAligned> ot(p.target + trow, o0, left), oq(two ? p.draft + qrow : p.target + trow, o0, two ? left : 0);
   const int stripes = (p.stripes + kVerifyWarps - 1) / kVerifyWarps;  // of a part
   uint64_t part = 0;
+  uint4 a1, c1;
+  auto fetch = [&](int s) {
+    const int i = (warp * stripes + s) * 32 + lane;
+    a1 = c1 = V::nothing();
+    if (i < ot.whole) {
+      a1 = ot.get(i);
+      if (two) c1 = oq.get(i);
+    } else if (i == ot.whole) {
+      a1 = ot.rest(lane);
+      if (two) c1 = oq.rest(lane);
+    }
+  };
+  fetch(0);
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {  // the parts' sums, then the element
 #pragma unroll 1
     for (int s = 0; s < stripes; ++s) {
       const int i = (warp * stripes + s) * 32 + lane;
-      uint4 a = V::nothing(), c = a;
-      if (i < ot.whole) {
-        a = ot.get(i);
-        if (two) c = oq.get(i);
-      } else if (i == ot.whole) {
-        a = ot.rest(lane);
-        if (two) c = oq.rest(lane);
-      }
+      const uint4 a = a1, c = c1;
+      fetch(s + 1 < stripes ? s + 1 : 0);  // (the next, or the first again)
       uint32_t w[E];
       uint64_t sum = 0;
 #pragma unroll
