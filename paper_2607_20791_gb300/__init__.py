@@ -10,6 +10,8 @@ from .binding import (  # noqa: F401
     AttnShape, GateState, RgdError, Trie, decode_gate_state, load_library, new_gate_state,
     rgd_gate_state_init, rgd_prefix_decode_attn, rgd_prefix_decode_attn_workspace_size,
     rgd_probe_gate, rgd_sample_head, rgd_trie_create, rgd_version,
+    CacheShape, rgd_cache_compact, rgd_cache_copy, rgd_cache_fork, rgd_cache_reserve, rgd_cache_trim,
+    rgd_cache_workspace_size, rgd_cache_write, rgd_verify_draft, rgd_verify_draft_workspace_size, rgd_w4_matvec,
     RGD_PENDING, RGD_REFUSAL, RGD_NON_REFUSAL, RGD_F32, RGD_BF16,
-    RGD_DEV_BAD_PAGE, RGD_DEV_BAD_TOKEN, RGD_DEV_WAIT_TIMEOUT, RGD_DEV_BAD_PARAM,
+    RGD_DEV_BAD_PAGE, RGD_DEV_BAD_TOKEN, RGD_DEV_WAIT_TIMEOUT, RGD_DEV_BAD_PARAM, RGD_DEV_NO_PAGE,
 )
