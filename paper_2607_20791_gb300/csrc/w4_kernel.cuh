@@ -140,23 +140,34 @@ __device__ __forceinline__ void load_bytes(const uint8_t* p, uint32_t* into) {
   }
 }
 
+// Where a tile's scales and zeros begin, and its last row that W has.
+struct TileScales {
+  const uint8_t *s, *z;
+  int last;
+  __device__ TileScales(const W4Params& p, int tile) {
+    const int64_t at = (int64_t)tile * kRows * p.groups;
+    s = p.scales + at * p.scale_bytes;
+    z = p.zeros + at;
+    last = min(kRows - 1, p.n - 1 - tile * kRows);
+  }
+};
 template <int NL, bool kZeros>
-__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, int tile, int64_t row_at, int part, int lane) {
+__device__ __forceinline__ void load_scales(const W4Params& p, Scales<NL, kZeros>& c, const TileScales& tile, int part, int lane) {
   const int g = (part * kPart) >> p.group_shift;
   if (p.scale_vec) {
-    const int64_t at = row_at + g;
-    if (p.scale_bytes == 2) load_bytes<2 * NL>(p.scales + 2 * at, c.s);
-    else load_bytes<4 * NL>(p.scales + 4 * at, c.s);
-    if (kZeros) load_bytes<NL>(p.zeros + at, c.z);
+    const int at = min(lane, tile.last) * p.groups + g;
+    if (p.scale_bytes == 2) load_bytes<2 * NL>(tile.s + 2 * (int64_t)at, c.s);
+    else load_bytes<4 * NL>(tile.s + 4 * (int64_t)at, c.s);
+    if (kZeros) load_bytes<NL>(tile.z + at, c.z);
     return;
   }
   const int mine = min(g + lane % NL, p.groups - 1);  // (past the row's end x is zero)
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
-    const int64_t at = min((int64_t)tile * kRows + i * (32 / NL) + lane / NL, (int64_t)p.n - 1) * p.groups + mine;
-    if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + at);
-    else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + at);
-    if (kZeros) c.z[i] = __ldg(p.zeros + at);
+    const int at = min(i * (32 / NL) + lane / NL, tile.last) * p.groups + mine;
+    if (p.scale_bytes == 2) c.s[i] = __ldg(reinterpret_cast<const uint16_t*>(tile.s) + at);
+    else c.s[i] = __ldg(reinterpret_cast<const uint32_t*>(tile.s) + at);
+    if (kZeros) c.z[i] = __ldg(tile.z + at);
   }
 }
 // Scale i as a number.
@@ -396,15 +407,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
         // Scales are loaded ahead too: of the next chunk, or two where they take few registers.
         Scales<NL, kZeros> ahead[H] = {};
         int si = begin, sat = at, scale_tile = load_tile;
-        auto scales_of = [&](int of) { return min((int64_t)of * kRows + lane, (int64_t)p.n - 1) * p.groups; };  // (of this lane's row)
-        int64_t row_at = scales_of(scale_tile);
+        TileScales tile_scales(p, scale_tile);
         auto load_next = [&](Scales<NL, kZeros>& into) {
-          if (si < end) load_scales(p, into, scale_tile, row_at, (chunk0 + sat) * P, lane);
+          if (si < end) load_scales(p, into, tile_scales, (chunk0 + sat) * P, lane);
           ++si;
           if (++sat < chunks) return;
           sat = 0;
           scale_tile += blocks;
-          row_at = scales_of(scale_tile);
+          tile_scales = TileScales(p, scale_tile);
         };
 #pragma unroll
         for (int s = 0; s < A; ++s) load(s);
