@@ -148,7 +148,7 @@ struct TileScales {
     const int64_t at = (int64_t)tile * kRows * p.groups;
     s = p.scales + at * p.scale_bytes;
     z = p.zeros + at;
-    last = min(kRows - 1, p.n - 1 - tile * kRows);
+    last = (int)min(int64_t(kRows - 1), p.n - 1 - (int64_t)tile * kRows);
   }
 };
 template <int NL, bool kZeros>
