@@ -246,48 +246,105 @@ __device__ __forceinline__ void multiply_part(const uint32_t (&q)[2 * kSub][4], 
   }
 }
 
+// Eight numbers of x from a place of any alignment: from the two aligned vectors they lie in, or
+// one by one where those reach past the end of x; `left` of them (or more) are the row's.
+struct Eight {
+  uint4 v[2];
+  __device__ __forceinline__ void load(const W4Params& p, const uint16_t* src, int left) {
+    const uint16_t* end = p.x + (int64_t)p.m * p.k;
+    const uint16_t* at = reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(src) & ~uintptr_t(15));
+    if (at + 16 <= end) {
+      v[0] = __ldg(reinterpret_cast<const uint4*>(at));
+      v[1] = __ldg(reinterpret_cast<const uint4*>(at) + 1);
+    } else {  // (as if they lay where `src` does in its vector)
+      uint16_t e[16];
+      const int off = (int)(src - at);
+#pragma unroll
+      for (int b = 0; b < 16; ++b) e[b] = b >= off && b < off + left && at + b < end ? __ldg(at + b) : 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        v[h] = make_uint4(e[8 * h] | (uint32_t)e[8 * h + 1] << 16, e[8 * h + 2] | (uint32_t)e[8 * h + 3] << 16,
+                          e[8 * h + 4] | (uint32_t)e[8 * h + 5] << 16, e[8 * h + 6] | (uint32_t)e[8 * h + 7] << 16);
+    }
+  }
+  __device__ __forceinline__ uint4 get(const uint16_t* src, int left) const {
+    const uint32_t by = (uint32_t)reinterpret_cast<uintptr_t>(src);
+    uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = (by & 8) ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = (by & 4) ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = __funnelshift_r(w[i], w[i + 1], (by & 2) * 8);
+      if (left < 2 * i + 2) w[i] = left > 2 * i ? w[i] & 0xffffu : 0;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
 // A block of x into shared memory: for every part and step the 8 numbers of each row and lane
-// of a quad, in the order of the nibbles; x_rows rows (a power of two up to 8) of every 8.
+// of a quad, in the order of the nibbles; a power of two up to 8 rows of every 8.
 template <int NT, bool kTurned>
 __device__ __forceinline__ void stage_x(const W4Params& p, uint8_t* xs, int part0, int parts, int m0) {
-  constexpr int kThreads = kWarps * 32, kBatch = 8;  // (loads in flight)
-  const int lanes = 2 + p.x_shift;                   // log2 of the lanes that have x
+  constexpr int kThreads = kWarps * 32;
+  const int lanes = 2 + p.x_shift;  // log2 of the lanes that have x
   const int units = (parts * 4 * NT) << lanes;
-  for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kBatch) {
-    uint4 r[kBatch];
+  auto place = [&](int u, int& m, int& k) {
+    const int v = u >> lanes, i = v % NT, j = v / NT & 3, c = v / (NT * 4), t = u & 3;
+    m = m0 + i * 8 + (u >> 2 & ((1 << p.x_shift) - 1));
+    k = (part0 + c) * kPart + (kTurned ? j * 32 + t * 8 : t * 32 + j * 8);
+  };
+  auto store = [&](int u, const uint4& r) {
+    if (u < units)
+      *reinterpret_cast<uint4*>(xs + (int64_t)u * 16) =
+          make_uint4(__byte_perm(r.x, r.z, 0x5410), __byte_perm(r.x, r.z, 0x7632), __byte_perm(r.y, r.w, 0x5410),
+                     __byte_perm(r.y, r.w, 0x7632));
+  };
+  if (p.x_vec) {
+    constexpr int kBatch = 8;  // loads in flight
+    for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kBatch) {
+      uint4 r[kBatch];
 #pragma unroll
-    for (int f = 0; f < kBatch; ++f) {
-      const int u = u0 + f * kThreads, v = u >> lanes;
-      const int i = v % NT, j = v / NT & 3, c = v / (NT * 4);
-      const int t = u & 3, m = m0 + i * 8 + (u >> 2 & ((1 << p.x_shift) - 1));
-      const int k = (part0 + c) * kPart + (kTurned ? j * 32 + t * 8 : t * 32 + j * 8);
-      r[f] = make_uint4(0, 0, 0, 0);
-      if (u < units && m < p.m && k < p.k) {
+      for (int f = 0; f < kBatch; ++f) {
+        int m, k;
+        place(u0 + f * kThreads, m, k);
+        r[f] = make_uint4(0, 0, 0, 0);
+        if (u0 + f * kThreads >= units || m >= p.m || k >= p.k) continue;
         const uint16_t* src = p.x + (int64_t)m * p.k + k;
-        if (p.x_vec == 2) {  // (k is then a multiple of 8)
+        if (p.x_vec == 2) {  // (p.k is a multiple of 8)
           r[f] = __ldg(reinterpret_cast<const uint4*>(src));
-        } else if (p.x_vec == 1) {  // (... of 2)
+        } else {  // (... of 2)
           const uint32_t* q = reinterpret_cast<const uint32_t*>(src);
           r[f].x = __ldg(q);
           if (k + 2 < p.k) r[f].y = __ldg(q + 1);
           if (k + 4 < p.k) r[f].z = __ldg(q + 2);
           if (k + 6 < p.k) r[f].w = __ldg(q + 3);
-        } else {
-          uint16_t e[8];
-#pragma unroll
-          for (int b = 0; b < 8; ++b) e[b] = k + b < p.k ? __ldg(src + b) : 0;
-          r[f] = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16,
-                            e[6] | (uint32_t)e[7] << 16);
         }
       }
+#pragma unroll
+      for (int f = 0; f < kBatch; ++f) store(u0 + f * kThreads, r[f]);
+    }
+    return;
+  }
+  // Odd p.k.  (Eight 2-byte loads took 36 us where this takes 32 for 16 x 4095 x 20011; 4-byte
+  // loads above are the faster where they will do, 28 us for 31 of 13 x 2730 x 20011.)
+  constexpr int kBatch = 4;
+#pragma unroll 1
+  for (int u0 = threadIdx.x; u0 < units; u0 += kThreads * kBatch) {
+    Eight r[kBatch];
+#pragma unroll
+    for (int f = 0; f < kBatch; ++f) {
+      int m, k;
+      place(u0 + f * kThreads, m, k);
+      r[f].v[0] = r[f].v[1] = make_uint4(0, 0, 0, 0);
+      if (u0 + f * kThreads < units && m < p.m && k < p.k) r[f].load(p, p.x + (int64_t)m * p.k + k, p.k - k);
     }
 #pragma unroll
     for (int f = 0; f < kBatch; ++f) {
-      const int u = u0 + f * kThreads;
-      if (u < units)
-        *reinterpret_cast<uint4*>(xs + (int64_t)u * 16) =
-            make_uint4(__byte_perm(r[f].x, r[f].z, 0x5410), __byte_perm(r[f].x, r[f].z, 0x7632),
-                       __byte_perm(r[f].y, r[f].w, 0x5410), __byte_perm(r[f].y, r[f].w, 0x7632));
+      int m, k;
+      place(u0 + f * kThreads, m, k);
+      store(u0 + f * kThreads, r[f].get(p.x + (int64_t)m * p.k + k, p.k - k));
     }
   }
 }

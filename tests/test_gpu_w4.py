@@ -122,6 +122,20 @@ def test_infinities_and_nan_stay_in_their_row_of_x(gpu_lib):
         assert torch.isinf(y[1]).all() and torch.isnan(y[2]).all()
 
 
+@pytest.mark.parametrize("k", [33, 201, 202, 203, 1111, 1114])
+def test_rows_of_x_off_alignment_end_where_they_end(gpu_lib, k):
+    """A vector of x that holds the end of a row holds the start of the next."""
+    import torch
+    x = torch.randn(5, k).to(torch.bfloat16)
+    x[1, 0], x[3, -1] = float("inf"), float("nan")
+    w = torch.randint(0, 256, (40, (k + 1) // 2), dtype=torch.uint8) | 0x11
+    y = torch.zeros(5, 40, device="cuda")
+    binding.rgd_w4_matvec(x.cuda(), w.cuda(), torch.ones(40, -(-k // 64), device="cuda"), None, 64, y)
+    y = y.cpu()
+    assert torch.isfinite(y[[0, 2, 4]]).all()
+    assert torch.isinf(y[1]).all() and torch.isnan(y[3]).all()
+
+
 def test_stream_graph_and_repeat(gpu_lib):
     import torch
     side = torch.cuda.Stream()
