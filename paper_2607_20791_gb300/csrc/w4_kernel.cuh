@@ -29,7 +29,7 @@
 // tiles it has whole; a tile that several warps have parts of is joined in shared memory at
 // the end, so that nothing waits in between (groups of 4 warps that shared each tile, with
 // two barriers a tile, took 61 us where this takes 57 for 5 x 4096 x 128256, and 33 where
-// this takes 29 for 13 x 2730 x 20011).  Where x does not fit, k goes in blocks, with the
+// this takes 28 for 13 x 2730 x 20011).  Where x does not fit, k goes in blocks, with the
 // sums of the block's tiles kept in shared memory between them.  Few tiles of long rows are
 // shared by the blocks of a cluster, each with a stretch of k, whose sums the first one joins.
 //
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) w4_kernel(const W4Params p, co
   using L = Layout<NT, GS, kAligned, kZeros>;
   constexpr bool kTurned = GS < 4 || !kAligned;  // a quad's words are of the same 16 bytes
   constexpr int kSums = L::kSums, R = kRows / 8, A = kAhead, P = kParts<NT, GS>;
-  constexpr int H = GS == 4 ? 2 : 1;                 // chunks whose scales are on their way
+  constexpr int H = GS == 4 ? 2 : 1;  // chunks whose scales are on their way (2 for groups of 32: 31.8 us for 28.8 in 13 x 2730 x 20011)
   constexpr int kEach = L::kGroups, NL = P * kEach;  // scales of a lane and part, and chunk
   extern __shared__ __align__(1024) uint8_t dyn[];
   __shared__ uint64_t landed[kWarps][A];

@@ -243,3 +243,23 @@ def test_workspace_reuse_stream_and_graph(gpu_lib):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(big.out, want)
+
+
+@pytest.mark.parametrize("rows, draft, vocab, dtype, certain", [(3, 3, 1000, "f32", False), (150, 4, 4096, "bf16", False),
+                                                                (40, 3, 32001, "f32", False), (4, 4, 128256, "bf16", True),
+                                                                (20, 5, 50000, "bf16", False)])
+def test_same_result_every_time(gpu_lib, rows, draft, vocab, dtype, certain):
+    """Calls back to back on one workspace: no result, sum or count of one is taken for another's."""
+    torch = _torch()
+    case = Case(rows, draft, vocab, dtype, seed=16, certain=certain).run()
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    args = (case.t.cuda(), None if case.q is None else case.q.cuda(), d(case.tokens), d(case.n), d(case.probe), d(case.temp),
+            d(case.min_p), d(case.au), d(case.du), d(case.active))
+    out, acc, prob = (torch.empty_like(x) for x in (case.out, case.acc, case.prob))
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(300):
+        binding.rgd_verify_draft(*args, out, acc, prob, case.ws, vocab=vocab, dev_status=case.status)
+        wrong += (out != case.out).sum() + (acc != case.acc).sum() + (prob != case.prob).sum()
+        out.fill_(-5)
+    assert int(wrong.item()) == 0 and int(case.status.item()) == 0
+    assert not bool(case.ws.any())
