@@ -7,10 +7,13 @@
 namespace rgd {
 namespace {
 
-// T ln p rounded to fp32, p in [0, 1].  FP64 is slow on this part (CUDA's log took 3 us of a
-// call on its own), so the logarithm is taken in pairs of floats, to about 2^-44: p = 2^k m
-// with m in [sqrt(1/2), sqrt(2)), ln m = 2 atanh(s) = 2 (s + s^3/3 + s^5/5 + ...) with
-// s = (m - 1) / (m + 1).
+// T ln p rounded once to fp32, p in [0, 1], T > 0: the same bits as (float)((double)T log((double)p)),
+// which the sample head takes.  FP64 is slow on this part (CUDA's log took 3 us of a call on
+// its own), so the logarithm is taken in pairs of floats: p = 2^k m with m in [sqrt(1/2),
+// sqrt(2)), ln m = 2 atanh(s) = 2 (s + s^3/3 + s^5/5 + ...) with s = (m - 1) / (m + 1).  The
+// product is off by less than 2^-45 of itself (the worst of 3e8 random ones, against 64 bits of
+// mantissa); where the nearest float could be another one for an error 16 times that, one case in
+// 65536, and where the pair's low half is out of fp32's range, FP64 decides.
 struct Float2 {
   float hi, lo;
 };
@@ -30,14 +33,12 @@ __device__ __forceinline__ Float2 mul(Float2 a, Float2 b) {
   const Float2 h = product_of(a.hi, b.hi);
   return sum_of(h.hi, __fadd_rn(h.lo, __fmaf_rn(a.hi, b.lo, __fmul_rn(a.lo, b.hi))));
 }
+__device__ __noinline__ float scaled_log_fp64(float temp, float p) { return (float)((double)temp * log((double)p)); }
 __device__ __forceinline__ float scaled_log(float temp, float p) {
   if (p == 0.f) return -INFINITY;
-  int k = 0;
-  if (p < 0x1p-100f) {  // (subnormals too)
-    p *= 0x1p60f;
-    k = -60;
-  }
-  const uint32_t bits = __float_as_uint(p);
+  const bool small = p < 0x1p-100f;  // (subnormals too)
+  const uint32_t bits = __float_as_uint(small ? p * 0x1p60f : p);
+  int k = small ? -60 : 0;
   k += (int)(bits >> 23) - 127;
   float m = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
   if (m > 1.4142135f) {
@@ -64,8 +65,10 @@ __device__ __forceinline__ float scaled_log(float temp, float p) {
   constexpr double kLn2 = 0.69314718055994530942;
   l = add(mul({(float)k, 0.f}, {(float)kLn2, (float)(kLn2 - (double)(float)kLn2)}), l);
   const Float2 v = product_of(l.hi, temp);
-  if (!(fabsf(v.hi) < INFINITY)) return v.hi;  // (the rest would be inf - inf)
-  return __fadd_rn(v.hi, __fmaf_rn(l.lo, temp, v.lo));
+  const float size = fabsf(v.hi);
+  const Float2 w = sum_of(v.hi, __fmaf_rn(l.lo, temp, v.lo));
+  const bool decided = size > 0x1p-96f && size < 0x1p127f && __fmaf_rn(w.lo, 1.f + 0x1p-16f, w.hi) == w.hi;
+  return decided || p == 1.f ? w.hi : scaled_log_fp64(temp, p);
 }
 
 }  // namespace

@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
 
   // Pass 1: the maxima (NaN never wins).
   if (warp == kVerifyWarps - 1 && lane == 0) {
-    sh.theta = scaled_log(temp, min_p);  // (the token is still on its way)
+    sh.theta = scaled_log(temp, greedy ? 1.f : min_p);  // (the token is still on its way)
     sh.tl = d_in && !greedy ? one_logit<T>(p.target + trow, d) : 0.f;
     sh.ql = d_in && two ? one_logit<T>(p.draft + qrow, d) : 0.f;
   }

@@ -19,3 +19,27 @@ def test_a_cutoff_past_fp32_keeps_everything(gpu_lib, certain):
     after = Case(24, 3, 600, "f32", seed=22)
     after.run(workspace=c.ws).check()
     assert not bool(c.ws.any())
+
+
+def test_the_cutoff_is_the_samplers_bit_for_bit(gpu_lib):
+    """A token at fl32(T ln p_min) below the largest logit is kept, one an ulp lower is not."""
+    import torch
+    rng = np.random.default_rng(23)
+    rows = 20000
+    near = np.array([[0x40cf8728, 0x3f3b5801], [0x4107e9cf, 0x3cafb2e0]], np.uint32).view(np.float32)
+    temp = np.concatenate([near[:, 0], rng.uniform(0.01, 20, rows - 2).astype(np.float32)])
+    min_p = np.concatenate([near[:, 1], rng.uniform(1e-5, 1 - 1e-5, rows - 2).astype(np.float32)])
+    cut = (temp.astype(np.float64) * np.log(min_p.astype(np.float64))).astype(np.float32)
+    logits = np.zeros((rows, 3, 4), np.float32)  # (the largest is 0)
+    logits[:, :, 1] = cut[:, None]
+    logits[:, :, 2] = np.nextafter(cut, np.float32(-np.inf))[:, None]
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    tokens = np.tile(np.array([1, 2], np.int32), (rows, 1))
+    out, acc = torch.empty(rows, 3, dtype=torch.int32, device="cuda"), torch.empty(rows, dtype=torch.int32, device="cuda")
+    prob, status = torch.empty(rows, 2, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.zeros(binding.rgd_verify_draft_workspace_size(rows, 2), dtype=torch.uint8, device="cuda")
+    binding.rgd_verify_draft(d(logits), None, d(tokens), None, None, d(temp), d(min_p), torch.rand(rows, 2, device="cuda"),
+                             torch.rand(rows, device="cuda"), None, out, acc, prob, ws, vocab=3, dev_status=status)
+    prob = prob.cpu().numpy()
+    assert int(status.item()) == 0
+    assert (prob[:, 0] > 0).all() and (prob[:, 1] == 0).all()

@@ -71,3 +71,18 @@ def test_the_ends_of_the_range(scaled_log):
     assert np.array_equal(scaled_log(temp, np.zeros(5)), np.full(5, -np.inf, np.float32))
     assert np.array_equal(scaled_log(temp, np.ones(5)), np.zeros(5, np.float32))
     assert not np.isnan(scaled_log(temp, np.full(5, 1e-45))).any()
+
+
+def test_rounded_once(scaled_log):
+    """Pairs whose product lies within 1e-6 of an ulp from half way between two floats, and random ones over the range."""
+    near = np.array([[0x40cf8728, 0x3f3b5801], [0x4107e9cf, 0x3cafb2e0]], np.uint32).view(np.float32)
+    assert np.array_equal(scaled_log(*near.T), _want(*near.T))
+    rng = np.random.default_rng(0)
+    n = 2_000_000
+    temp = np.concatenate([rng.uniform(0.01, 20, n), np.exp2(rng.uniform(-149, 128, n))]).astype(np.float32)
+    p = np.concatenate([rng.random(n), np.exp2(rng.uniform(-149, 0, n))]).astype(np.float32)
+    ok = np.isfinite(temp) & (temp > 0) & (p > 0) & (p <= 1)
+    temp, p = temp[ok], p[ok]
+    got, want = scaled_log(temp, p), _want(temp, p)
+    wrong = np.flatnonzero(got != want)
+    assert wrong.size == 0, [(float(temp[i]).hex(), float(p[i]).hex(), got[i], want[i]) for i in wrong[:5]]
