@@ -417,8 +417,9 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *   draft_logits   [rows, max_draft] rows of vocab logits of the same dtype,
  *                  draft_stride elements apart; NULL: every draft was certain
  *                  (q_k(d_k) = 1).  Rows that all start on 16 bytes are read fastest
- *   draft_tokens   int32 [rows, max_draft]; one outside [0, vocab) sets
- *                  RGD_DEV_BAD_TOKEN, is rejected, and the draw there is from p_k
+ *   draft_tokens   int32 [rows, max_draft]; one outside [0, vocab) is rejected, the
+ *                  draw there is from p_k, and it sets RGD_DEV_BAD_TOKEN, also at a
+ *                  position of finite logits that the row does not get to
  *   n_draft        int32 [rows], in [0, max_draft]; NULL: max_draft each
  *   is_probe       uint8 [rows] or NULL; temperature, min_p float [rows]
  *   accept_u       float [rows, max_draft], draw_u float [rows]: independent
@@ -436,9 +437,9 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *                  for the largest call serves calls of any shape.  Calls that share
  *                  it must not overlap.  (After RGD_DEV_WAIT_TIMEOUT - a row's results
  *                  were not all seen within 2 s, and the row is rejected - fill it anew)
- * A row with n_draft, temperature, min_p or a uniform out of range, or with a
- * position it gets to whose largest logit is not finite, is rejected and sets
- * RGD_DEV_BAD_PARAM.  NaN logits have no weight.  Weights are 2^((l - l_max)
+ * A row with n_draft, temperature, min_p or draw_u out of range, or with a position it
+ * gets to whose accept_u is out of range or whose largest logit is not finite, is rejected
+ * and sets RGD_DEV_BAD_PARAM.  NaN logits have no weight.  Weights are 2^((l - l_max)
  * log2(e)/T) in fp32, rounded to multiples of 2^-31 and summed exactly, so the
  * outputs do not depend on how a call is cut.  RGD_ERR_UNSUPPORTED above a vocab of
  * 2^20.  One kernel on `stream`. */

@@ -463,7 +463,8 @@ __device__ __noinline__ void finish_unit(const VerifyParams& p, int row, int pos
   if (lane == 0) {
     p.accepted_out[row] = good ? taken : 0;
     p.count[row] = 0;
-    if (!there && p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
+    // (a position that the row does not get to is nobody's error)
+    if (!good && p.dev_status) atomicOr(p.dev_status, there ? RGD_DEV_BAD_PARAM : RGD_DEV_WAIT_TIMEOUT);
   }
 }
 
@@ -598,7 +599,6 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   if (!two) q.top = 0.f;
   if (!(fabsf(t.top) < INFINITY && fabsf(q.top) < INFINITY && u >= 0.f && u < 1.f)) {
     if (leader) {
-      if (lane == 0 && p.dev_status) atomicOr(p.dev_status, RGD_DEV_BAD_PARAM);
       if (lane == 0 && prob) *prob = 0.f;
       finish_unit(p, row, pos, n, kRejectedRow);
     }

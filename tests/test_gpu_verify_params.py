@@ -43,3 +43,24 @@ def test_the_cutoff_is_the_samplers_bit_for_bit(gpu_lib):
     prob = prob.cpu().numpy()
     assert int(status.item()) == 0
     assert (prob[:, 0] > 0).all() and (prob[:, 1] == 0).all()
+
+
+@pytest.mark.parametrize("vocab", [200, 40000])
+@pytest.mark.parametrize("certain", [False, True])
+def test_positions_behind_a_rejection_set_no_status(gpu_lib, certain, vocab):
+    """Logits that are not finite and uniforms out of range at positions a row does not get to are no error."""
+    c = Case(6, 3, vocab, "f32", seed=24, certain=certain, temps=(1.0,), min_ps=(0.0,), probe_every=100)
+    c.active[:], c.n[:], c.probe[:] = 1, 3, [0, 0, 0, 0, 1, 1]
+    c.tokens[:, 0] = 5
+    c.t[:, 0, 5] = -np.inf  # (rejected in sample rows and greedy ones)
+    c.t[0:2, 1:], c.t[2, 2:], c.t[4:, 1:] = np.nan, np.inf, -np.inf
+    c.au[1, 1:], c.au[3, 2] = np.nan, 1.5
+    c.run()
+    assert int(c.status.item()) == 0
+    out, acc = c.out.cpu().numpy(), c.acc.cpu().numpy()
+    assert (acc == 0).all() and (out[:, 0] >= 0).all() and (out[:, 0] != 5).all() and (out[:, 1:] == -1).all()
+    # ... and are one where it gets to them
+    c.au[:], c.tokens[:, 0] = 0, np.nanargmax(c.t[:, 0].numpy(), -1)
+    c.run()
+    assert int(c.status.item()) == binding.RGD_DEV_BAD_PARAM
+    assert (c.out.cpu().numpy()[[0, 1, 4, 5]] == -1).all() and (c.acc.cpu().numpy()[[0, 1, 4, 5]] == 0).all()
