@@ -435,8 +435,9 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *   workspace      rgd_verify_draft_workspace_size() bytes, 4-byte aligned, zero-filled
  *                  before its first use; a call leaves it all zero again, so one sized
  *                  for the largest call serves calls of any shape.  Calls that share
- *                  it must not overlap.  (After RGD_DEV_WAIT_TIMEOUT - a row's results
- *                  were not all seen within 2 s, and the row is rejected - fill it anew)
+ *                  it must not overlap.  RGD_DEV_WAIT_TIMEOUT: a wait within the kernel
+ *                  gave up after 2 s, and the row it was for is rejected; rely on no
+ *                  output of the call then, and fill the workspace anew
  * A row with n_draft, temperature, min_p or draw_u out of range, or with a position it
  * gets to whose accept_u is out of range or whose largest logit is not finite, is rejected
  * and sets RGD_DEV_BAD_PARAM.  NaN logits have no weight.  Weights are 2^((l - l_max)

@@ -468,6 +468,19 @@ __device__ __noinline__ void finish_unit(const VerifyParams& p, int row, int pos
   }
 }
 
+// The whole CTA: a wait has run out, so the position has no result and no other one joins its row.
+// (Which row it is is read again, so that it costs the kernel no registers.)
+__device__ __noinline__ void give_up(const VerifyParams& p) {
+  uint32_t unit;
+  asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(unit));
+  const int K = p.max_draft, row = (int)unit / (K + 1), pos = (int)unit % (K + 1);
+  if (threadIdx.x >= 32) return;
+  for (int i = threadIdx.x; i <= K; i += 32) p.token_out[(int64_t)row * (K + 1) + i] = -1;
+  if (threadIdx.x != 0) return;
+  p.accepted_out[row] = 0;
+  if (pos < K && p.accept_prob) p.accept_prob[(int64_t)row * K + pos] = 0.f;
+}
+
 // An exchange over the cluster: every CTA pushes a value (or two) into every CTA, counted by
 // the receiver's barrier of that exchange.  (With stores and a cluster barrier instead, which
 // waits for the stores' return, 80 rows of 5 positions by 128256 bf16 took 38.2 us for 36.8.)
@@ -592,7 +605,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
     const float m = warp_max(sh.warp_top[warp][lane % kVerifyWarps]);
     if (lane < (int)csize) push(sh, 0, &sh.top[warp][rank], m, csize, lane);
   }
-  if (!exchanged(sh, 0, csize, p.dev_status)) return;
+  if (!exchanged(sh, 0, csize, p.dev_status)) return give_up(p);
   Side t, q;
   t.top = warp_max(sh.top[0][lane % csize]);
   q.top = warp_max(sh.top[1][lane % csize]);
@@ -624,7 +637,8 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.warp_sum[0][lane % kVerifyWarps]);
       if (lane == 0) push(sh, 1, &sh.sum[0][rank], best, csize, 0);
     }
-    if (rank != 0 || !exchanged(sh, 1, csize, p.dev_status)) return;
+    if (rank != 0) return;
+    if (!exchanged(sh, 1, csize, p.dev_status)) return give_up(p);
     if (leader) {
       best = __reduce_min_sync(0xffffffffu, (uint32_t)sh.sum[0][lane % csize]);
       const bool same = has_draft && (int32_t)best == d;
@@ -654,7 +668,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
   q.cut = __fadd_rn(q.top, sh.theta);
   join(0, sum_weights(tv, tkept, t, p.stripes, lane));
   if (two) join(1, sum_weights(qv, qkept, q, p.stripes, lane));
-  if (!exchange(0, two ? 1 : 0)) return;
+  if (!exchange(0, two ? 1 : 0)) return give_up(p);
   uint64_t total = over_cluster(0);
   t.inv = __fdiv_rn(1.f, __ull2float_rn(total) * 0x1p-31f);
   if (two) q.inv = __fdiv_rn(1.f, __ull2float_rn(over_cluster(1)) * 0x1p-31f);
@@ -701,7 +715,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 4) verify_kernel(const VerifyP
         a = a1, c = c1;
       }
       join(2, warp_sum(rest.total()));
-      if (!exchange(2, 2)) return;
+      if (!exchange(2, 2)) return give_up(p);
       const uint64_t rz = over_cluster(2);
       if (rz > 0) {  // (p and q may be equal but for rounding: then p itself)
         which = 2;
