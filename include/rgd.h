@@ -524,7 +524,8 @@ int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int32_t max_pa
  *   k_new, v_new  bf16, the Hkv x D values of (r, i) at r * row_stride + i *
  *                 token_stride elements (both multiples of 8): views of a fused
  *                 projection's output do
- *   n_new         int32 [rows], at most max_new
+ *   n_new         int32 [rows], in [0, max_new]; of a row of more, the first max_new
+ *                 are written and RGD_DEV_BAD_PAGE is set, as for one of less than 0
  *   row_active    uint8 [rows] or NULL: rows to write (rgd_cache_reserve's row_ok)
  * A token whose page is not listed is skipped and sets RGD_DEV_BAD_PAGE. */
 int rgd_cache_write(const rgd_cache_shape* shape, int32_t layer, int32_t rows, int32_t max_new, const rgd_bf16* k_new,

@@ -356,7 +356,9 @@ __global__ void __launch_bounds__(kCopyThreads) write_kernel(const WriteParams p
   const int32_t r = (int32_t)(w / p.tokens), i = (int32_t)(w % p.tokens);
   if (r >= p.rows) return;
   const int32_t n = p.n_new[r], len = p.length[r];
-  if (i >= n || (p.row_ok && !p.row_ok[r])) return;
+  if (p.row_ok && !p.row_ok[r]) return;
+  if (i == 0 && lane == 0 && (n < 0 || n > p.tokens)) flag(p.dev_status, RGD_DEV_BAD_PAGE);
+  if (i >= n) return;
   const int32_t per = p.c.dim / 8, vecs = p.c.heads * per;
   const int64_t at = r * p.row_stride + i * p.token_stride;
   const uint4* fresh[2] = {reinterpret_cast<const uint4*>(p.fresh[0] + at), reinterpret_cast<const uint4*>(p.fresh[1] + at)};
