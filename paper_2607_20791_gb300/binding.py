@@ -558,15 +558,19 @@ def rgd_cache_reserve(shape: CacheShape, block_table, length, n_new, row_active,
 
 
 def _new_tokens(t, name: str, shape: CacheShape):
-    """[rows, max_new, Hkv, D] whose last two dimensions are dense; its rows and tokens may be strided."""
+    """[rows, max_new, Hkv, D] whose last two dimensions are dense; its rows and tokens may be strided.  Returns the
+    pointer and those two strides (0 where there is one element: its stride is never used)."""
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
         raise TypeError(f"{name} must be a bfloat16 tensor")
     if t.dim() != 4 or t.shape[2] != shape.num_kv_heads or t.shape[3] != shape.head_dim:
         raise ValueError(f"{name} must be [rows, max_new, num_kv_heads, head_dim]")
-    if t.numel() and (t.stride(3) != 1 or t.stride(2) != shape.head_dim):
+    rows, tokens, heads, _ = t.shape
+    by_row, by_token, by_head, by_element = t.stride()
+    if t.numel() and (by_element != 1 or (by_head != shape.head_dim and heads > 1)):
         raise ValueError(f"{name}: heads and head_dim must be dense")
-    return t.data_ptr() if t.is_cuda else _HostTensor(name)
+    strides = (by_row if rows > 1 else 0, by_token if tokens > 1 else 0)
+    return (t.data_ptr() if t.is_cuda else _HostTensor(name)), strides
 
 
 def rgd_cache_write(shape: CacheShape, layer: int, k_new, v_new, n_new, block_table, length, row_active, k_pages,
@@ -574,12 +578,12 @@ def rgd_cache_write(shape: CacheShape, layer: int, k_new, v_new, n_new, block_ta
     """``k_new`` and ``v_new`` [rows, max_new, Hkv, D] have the same strides; views of a fused projection do."""
     import torch
     rows, cols = _table_size(block_table)
-    k, v = _new_tokens(k_new, "k_new", shape), _new_tokens(v_new, "v_new", shape)
-    if k_new.shape[0] != rows or v_new.shape != k_new.shape or v_new.stride() != k_new.stride():
+    (k, strides), (v, v_strides) = _new_tokens(k_new, "k_new", shape), _new_tokens(v_new, "v_new", shape)
+    if k_new.shape[0] != rows or v_new.shape != k_new.shape or v_strides != strides:
         raise ValueError("k_new and v_new must have block_table's rows and the same shape and strides")
     i32, pool = torch.int32, _pool_numel(shape)
     _check(_call(load_library().rgd_cache_write,
-        ctypes.byref(shape), int(layer), rows, k_new.shape[1], k, v, k_new.stride(0), k_new.stride(1),
+        ctypes.byref(shape), int(layer), rows, k_new.shape[1], k, v, *strides,
         _ptr(n_new, "n_new", i32, numel=rows), cols, _ptr(block_table, "block_table", i32),
         _ptr(length, "length", i32, numel=rows), _ptr(row_active, "row_active", torch.uint8, optional=True, numel=rows),
         _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
