@@ -511,8 +511,9 @@ size_t rgd_cache_workspace_size(const rgd_cache_shape* shape, int32_t rows);
  * Where the pool runs out, a row whose pages and those of the rows before it (those
  * refused included) exceed the free pages is left as it was, and RGD_DEV_NO_PAGE is
  * set.  A row of a negative length or n_new, or past the table, or with an entry >=
- * num_pages there, is left as it was and sets RGD_DEV_BAD_PAGE.  One kernel, and one for
- * the copies unless they are few. */
+ * num_pages there, is left as it was and sets RGD_DEV_BAD_PAGE.  RGD_ERR_UNSUPPORTED for
+ * rows * max_pages of 2^31 or more.  One kernel, and one for the copies unless they are
+ * few. */
 int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int32_t max_pages, int32_t* block_table,
                       const int32_t* length, const int32_t* n_new, const uint8_t* row_active, int32_t* page_refs,
                       rgd_bf16* k_pages, rgd_bf16* v_pages, uint8_t* row_ok, void* workspace, size_t workspace_bytes,
