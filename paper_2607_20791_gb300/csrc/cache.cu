@@ -556,11 +556,11 @@ int check_shape(const char* fn, const rgd_cache_shape* s, CacheView& c) {
   return RGD_OK;
 }
 
-int blocks_for(int64_t warps) { return (int)((warps + kCopyThreads / 32 - 1) / (kCopyThreads / 32)); }
+constexpr int kWarpsEach = kCopyThreads / 32;
 
 int launch_copies(const CopyParams& p, int64_t most, cudaStream_t st) {
   const int64_t warps = std::max(most * p.c.layers * 2 * p.c.heads, (p.entries[0] + p.entries[1] + 31) / 32);
-  const int grid = (int)std::min<int64_t>(blocks_for(std::max<int64_t>(warps, 1)), 152 * 8);
+  const int grid = blocks_for(std::max<int64_t>(warps, 1), kWarpsEach, 152 * 8);
   const cudaError_t e = launch_dependent(copy_kernel, grid, kCopyThreads, 0, st, p);
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache copy launch");
 }
@@ -673,7 +673,7 @@ extern "C" int rgd_cache_write(const rgd_cache_shape* shape, int32_t layer, int3
   p.row_ok = row_active;
   p.dev_status = dev_status;
   const cudaError_t e =
-      launch_dependent(write_kernel, blocks_for((int64_t)rows * max_new), kCopyThreads, 0, (cudaStream_t)stream, p);
+      launch_dependent(write_kernel, blocks_for((int64_t)rows * max_new, kWarpsEach), kCopyThreads, 0, (cudaStream_t)stream, p);
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache write launch");
 }
 
@@ -685,7 +685,7 @@ extern "C" int rgd_cache_trim(int32_t rows, int32_t max_pages, int32_t num_pages
   RGD_CHECK_ARG(rows >= 0 && max_pages >= 1 && num_pages >= 1, "%s: bad rows/max_pages/num_pages", fn);
   if (rows == 0) return RGD_OK;
   RGD_CHECK_ARG(block_table && length && page_refs, "%s: block_table/length/page_refs must be non-NULL", fn);
-  const cudaError_t e = launch_dependent(trim_kernel, blocks_for(rows), kCopyThreads, 0, (cudaStream_t)stream, rows,
+  const cudaError_t e = launch_dependent(trim_kernel, blocks_for(rows, kWarpsEach), kCopyThreads, 0, (cudaStream_t)stream, rows,
                                          max_pages, num_pages, block_table, length, row_active, page_refs, dev_status);
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache trim launch");
 }
@@ -699,7 +699,7 @@ extern "C" int rgd_cache_fork(int32_t pairs, const int32_t* parent, const int32_
   if (pairs == 0) return RGD_OK;
   RGD_CHECK_ARG(parent && child && block_table && length && page_refs,
                 "%s: parent/child/block_table/length/page_refs must be non-NULL", fn);
-  const cudaError_t e = launch_dependent(fork_kernel, blocks_for(pairs), kCopyThreads, 0, (cudaStream_t)stream, pairs,
+  const cudaError_t e = launch_dependent(fork_kernel, blocks_for(pairs, kWarpsEach), kCopyThreads, 0, (cudaStream_t)stream, pairs,
                                          rows, max_pages, num_pages, parent, child, block_table, length, page_refs,
                                          dev_status);
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache fork launch");

@@ -21,6 +21,12 @@ inline int cuda_error(cudaError_t e, const char* what) {
   return set_error(RGD_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
+// Blocks for a number of items, `each` of them in a block; at most `most`.
+inline int blocks_for(int64_t items, int each, int64_t most = 0x7fffffff) {
+  const int64_t n = (items + each - 1) / each;
+  return (int)(n < most ? n : most);
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // The driver's cuTensorMapEncodeTiled (NULL where it is missing).
