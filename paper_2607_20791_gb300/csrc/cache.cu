@@ -557,6 +557,8 @@ int check_shape(const char* fn, const rgd_cache_shape* s, CacheView& c) {
 }
 
 constexpr int kWarpsEach = kCopyThreads / 32;
+// Rows (or pairs, or tokens) at most: the numbers that a last block gives to those past the end are still an int.
+constexpr int32_t kMaxRows = 0x7fffffff - kPlanThreads;
 
 int launch_copies(const CopyParams& p, int64_t most, cudaStream_t st) {
   const int64_t warps = std::max(most * p.c.layers * 2 * p.c.heads, (p.entries[0] + p.entries[1] + 31) / 32);
@@ -591,6 +593,7 @@ extern "C" int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int
   if (int rc = check_shape(fn, shape, c)) return rc;
   RGD_CHECK_ARG(rows >= 0 && max_pages >= 1, "%s: bad rows/max_pages", fn);
   if (rows == 0) return RGD_OK;
+  RGD_CHECK_ARG(rows <= kMaxRows, "%s: too many rows", fn);
   // (the kernel adds up the pages that rows want in 32 bits)
   if ((int64_t)rows * max_pages > 0x7fffffff)
     return set_error(RGD_ERR_UNSUPPORTED, "%s: block_table must have fewer than 2^31 entries", fn);
@@ -655,7 +658,7 @@ extern "C" int rgd_cache_write(const rgd_cache_shape* shape, int32_t layer, int3
   RGD_CHECK_ARG(aligned16(k_new) && aligned16(v_new) && aligned16(k_pages) && aligned16(v_pages) &&
                     row_stride % 8 == 0 && token_stride % 8 == 0,
                 "%s: tensors must be 16-byte aligned and strides multiples of 8 elements", fn);
-  RGD_CHECK_ARG((int64_t)rows * max_new <= 0x7fffffff, "%s: too many tokens", fn);
+  RGD_CHECK_ARG((int64_t)rows * max_new <= kMaxRows, "%s: too many tokens", fn);
   WriteParams p{};
   p.c = c;
   p.pool[0] = k_pages + layer * c.layer_stride;
@@ -684,6 +687,7 @@ extern "C" int rgd_cache_trim(int32_t rows, int32_t max_pages, int32_t num_pages
   const char* fn = "rgd_cache_trim";
   RGD_CHECK_ARG(rows >= 0 && max_pages >= 1 && num_pages >= 1, "%s: bad rows/max_pages/num_pages", fn);
   if (rows == 0) return RGD_OK;
+  RGD_CHECK_ARG(rows <= kMaxRows, "%s: too many rows", fn);
   RGD_CHECK_ARG(block_table && length && page_refs, "%s: block_table/length/page_refs must be non-NULL", fn);
   const cudaError_t e = launch_dependent(trim_kernel, blocks_for(rows, kWarpsEach), kCopyThreads, 0, (cudaStream_t)stream, rows,
                                          max_pages, num_pages, block_table, length, row_active, page_refs, dev_status);
@@ -697,6 +701,7 @@ extern "C" int rgd_cache_fork(int32_t pairs, const int32_t* parent, const int32_
   const char* fn = "rgd_cache_fork";
   RGD_CHECK_ARG(pairs >= 0 && rows >= 0 && max_pages >= 1 && num_pages >= 1, "%s: bad pairs/rows/max_pages/num_pages", fn);
   if (pairs == 0) return RGD_OK;
+  RGD_CHECK_ARG(pairs <= kMaxRows, "%s: too many pairs", fn);
   RGD_CHECK_ARG(parent && child && block_table && length && page_refs,
                 "%s: parent/child/block_table/length/page_refs must be non-NULL", fn);
   const cudaError_t e = launch_dependent(fork_kernel, blocks_for(pairs, kWarpsEach), kCopyThreads, 0, (cudaStream_t)stream, pairs,

@@ -58,3 +58,17 @@ def test_blocks_of_more_work_than_32_bits_count(tmp_path):
     assert res.returncode == 0, res.stderr
     res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
     assert [int(x) for x in res.stdout.split()] == [1, 1, 2, 1216, 1216, 1216, 1216, 1216, 1216, 1216, 268435456]
+
+
+def test_rows_next_to_the_last_int_are_refused(lib):
+    """A kernel's last block has a few rows too many, whose numbers have to stay an int for it to leave them out."""
+    s = ctypes.byref(binding.CacheShape(num_layers=1, num_pages=10, num_kv_heads=1, page_size=16, head_dim=8))
+
+    def refused(rc):
+        assert rc == binding.RGD_ERR_INVALID_ARG and b"too many" in lib.rgd_last_error_string()
+    for rows in (0x7fffffff, 0x7fffffff - 1023):
+        refused(lib.rgd_cache_trim(rows, 1, 10, P, P, None, P, None, None))
+        refused(lib.rgd_cache_fork(rows, P, P, 2, 1, 10, P, P, P, None, None))
+        refused(lib.rgd_cache_write(s, 0, rows, 1, P, P, 0, 0, P, 1, P, P, None, P, P, None, None))
+        refused(lib.rgd_cache_reserve(s, rows, 1, P, P, P, None, P, P, P, None, P, 1 << 60, None, None))
+    refused(lib.rgd_cache_write(s, 0, 0x3fffffff, 2, P, P, 0, 0, P, 1, P, P, None, P, P, None, None))
