@@ -593,10 +593,10 @@ extern "C" int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int
   if (int rc = check_shape(fn, shape, c)) return rc;
   RGD_CHECK_ARG(rows >= 0 && max_pages >= 1, "%s: bad rows/max_pages", fn);
   if (rows == 0) return RGD_OK;
-  RGD_CHECK_ARG(rows <= kMaxRows, "%s: too many rows", fn);
   // (the kernel adds up the pages that rows want in 32 bits)
   if ((int64_t)rows * max_pages > 0x7fffffff)
     return set_error(RGD_ERR_UNSUPPORTED, "%s: block_table must have fewer than 2^31 entries", fn);
+  RGD_CHECK_ARG(rows <= kMaxRows, "%s: too many rows", fn);
   RGD_CHECK_ARG(block_table && length && n_new && page_refs && k_pages && v_pages && workspace,
                 "%s: block_table/length/n_new/page_refs/k_pages/v_pages/workspace must be non-NULL", fn);
   RGD_CHECK_ARG(aligned16(k_pages) && aligned16(v_pages) && aligned16(workspace),
