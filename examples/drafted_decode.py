@@ -81,7 +81,7 @@ class Decoder:
         self.verify_ws = torch.zeros(binding.rgd_verify_draft_workspace_size(self.R, draft), dtype=torch.uint8, device="cuda")
         self.last = torch.randint(0, vocab, (groups, 1), generator=g).expand(groups, rows_per_group).reshape(-1).int().cuda()
         self.status = torch.zeros(1, **i32)
-        self.gate_status = torch.zeros(1, **i32)  # (the gate skips the -1 behind a row's tokens, and says so)
+        self.gate_status = torch.zeros(1, **i32)  # (its RGD_DEV_BAD_TOKEN: the -1 behind a row's tokens, skipped)
         self.trie = binding.Trie(trie or [[1, 2]], 2)
         self.gate = binding.new_gate_state(groups)
         binding.rgd_gate_state_init(self.gate, groups)
@@ -164,8 +164,9 @@ class Decoder:
 
     def check(self):
         self.torch.cuda.synchronize()
-        if int(self.status.item()):
-            raise RuntimeError(f"device status {int(self.status.item())}")
+        status = int(self.status.item()) | (int(self.gate_status.item()) & ~binding.RGD_DEV_BAD_TOKEN)
+        if status:
+            raise RuntimeError(f"device status {status}")
 
 
 def run(draft=3, steps=8, seed=0, **sizes):
