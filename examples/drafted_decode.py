@@ -15,8 +15,9 @@ the target model then looks at all K + 1 positions at once:
 The attention takes a (row, position) as a row of its own: its block table is the row's, and
 its suffix ends with the position's token, which makes the K + 1 positions causal.
 
-Weights, embeddings and prompts are random; greedy rows produce exactly what they would
-without drafts.  Run: python examples/drafted_decode.py
+Weights, embeddings and prompts are random; greedy rows produce what they would without
+drafts, but for ties within rounding: the products' last bits go by how many rows they have.
+Run: python examples/drafted_decode.py
 """
 from __future__ import annotations
 

@@ -319,10 +319,10 @@ int rgd_sample_head_gated(int32_t rows, int32_t vocab, int32_t dtype, const void
 /* One whole decode step of the gated loop: rgd_prefix_decode_attn over the
  * step's rows, then rgd_sample_head_gated over the step's logits (two kernels
  * on `stream`; the head's blocks are scheduled while the attention finishes).
- * The logits are the caller's: the model between the attention output and the
- * next-token logits (projections, MLP, LM head) is not part of this library;
- * the head reads its inputs while the attention finishes (the attention writes
- * none of them).
+ * The logits are the caller's: this call has no part of the model between the
+ * attention output and the next-token logits (projections, MLP, LM head; for
+ * 4-bit weights there is rgd_w4_matvec); the head reads its inputs while the
+ * attention finishes (the attention writes none of them).
  * Arguments are those of the two calls, with rows = num_groups *
  * rows_per_group and one row_active shared by both (the attention reads it,
  * the gate updates it); out and lse receive the attention output.  The first
@@ -408,7 +408,9 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *   at the first that is not, the row's last token is drawn from max(0, p_k - q_k)
  *   (from p_k should that be 0 everywhere); if all are accepted it is drawn from p_n:
  *   token = the smallest i whose cumulative weight exceeds draw_u[r] times their sum.
- * The tokens that come out are distributed as p, whatever the draft.  Greedy rows
+ * The tokens that come out are distributed as p, up to rounding (see below), if d_k was
+ * drawn from q_k - that is with the row's temperature and min_p - or, without draft
+ * logits, was chosen in any way that does not look at the uniforms.  Greedy rows
  * (is_probe or temperature 0): d_k is accepted if it is the argmax (lowest index on
  * ties), and the last token is the argmax; draft_logits, min_p and the uniforms are
  * not read.
@@ -426,7 +428,9 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  *                  uniforms in [0, 1)
  *   row_active     uint8 [rows] or NULL (all active)
  *   token_out      int32 [rows, max_draft + 1]: the accepted drafts, the last token,
- *                  then -1; all -1 for inactive and rejected rows
+ *                  then -1; all -1 for inactive and rejected rows.  (rgd_probe_gate
+ *                  skips the -1 of a probe row that is given to it as it is, and sets
+ *                  RGD_DEV_BAD_TOKEN for them)
  *   accepted_out   int32 [rows]: accepted drafts (0 for inactive and rejected rows);
  *                  token_out[r] holds accepted_out[r] + 1 tokens
  *   accept_prob    float [rows, max_draft] or NULL: min(1, p_k(d_k) / q_k(d_k)) of
@@ -442,8 +446,15 @@ size_t rgd_verify_draft_workspace_size(int32_t rows, int32_t max_draft);
  * gets to whose accept_u is out of range or whose largest logit is not finite, is rejected
  * and sets RGD_DEV_BAD_PARAM.  NaN logits have no weight.  Weights are 2^((l - l_max)
  * log2(e)/T) in fp32, rounded to multiples of 2^-31 and summed exactly, so the
- * outputs do not depend on how a call is cut.  RGD_ERR_UNSUPPORTED above a vocab of
- * 2^20.  One kernel on `stream`. */
+ * outputs do not depend on how a call is cut.  (rgd_sample_head keeps 43 binary places
+ * of them: of the same uniform it can draw another token where the mark lies next to an
+ * edge.)  max(0, p_k - q_k) is rounded to multiples of 2^-31 as well - of probability 1,
+ * not of its own largest value: where p and q are flat and nearly the same, its small
+ * values lose digits or vanish.  The rest alone is then off by 0.4 % in total variation
+ * at a vocab of 262144, T = 10 and draft logits off by 0.05, by 4 % with 0.005, and 5e-5
+ * at T = 1 and 0.5; as such rests are drawn from as rarely, what is emitted is off by
+ * 1e-5 at most in each.  RGD_ERR_UNSUPPORTED above a vocab of 2^20.  One kernel on
+ * `stream`. */
 int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, int32_t dtype, const void* target_logits,
                      int64_t target_stride, const void* draft_logits, int64_t draft_stride,
                      const int32_t* draft_tokens, const int32_t* n_draft, const uint8_t* is_probe,
@@ -456,7 +467,8 @@ int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, int32_t dty
 /* ------------------------------------------------------------------------ */
 
 /* y[i, j] = sum_k x[i, k] W[j, k],  W[j, k] = (q[j, k] - z[j, k / G]) s[j, k / G],
- * for a few rows of activations (m up to some tens; any m is right).
+ * for a few rows of activations (any m is right; above 16 rows the weights are read and
+ * converted once more for every 16, so that many rows are better served as a dense product).
  *   x        bf16 [m, k]
  *   weights  uint8 [n, ceil(k / 2)]: q in 4 bits, the even k in the low half of its
  *            byte; the last high half of an odd k is not read as a weight
@@ -466,7 +478,9 @@ int rgd_verify_draft(int32_t rows, int32_t max_draft, int32_t vocab, int32_t dty
  *   y        [m] rows of n elements, y_stride elements apart (>= n; the rest of a row
  *            is left alone), out_dtype RGD_F32 or RGD_BF16
  * Products of bf16 activations with the whole numbers q - z are exact and are summed,
- * and scaled group by group, in fp32; the result is rounded once.  dev_status gets
+ * and scaled group by group, in fp32; the result is rounded once.  The order of the sums
+ * is the same for every call of the same m, n and k, but goes by all three: a row's y may
+ * differ in its last bits from that of a call with fewer or more rows.  dev_status gets
  * RGD_DEV_WAIT_TIMEOUT when a bounded wait on a copy gave up; y is then not valid.  One
  * kernel on `stream`. */
 int rgd_w4_matvec(int32_t m, int32_t n, int32_t k, int32_t group_size, const rgd_bf16* x, const uint8_t* weights,
@@ -502,15 +516,17 @@ size_t rgd_cache_workspace_size(const rgd_cache_shape* shape, int32_t rows);
  * tokens length .. length + n_new - 1 fall into is the row's own afterwards.  A table
  * entry < 0 there gets a free page; a page that other rows list too (count > 1) is
  * replaced by a free page, into which the row's tokens in it (length % page_size of
- * them) are copied in every layer.  Free pages are taken in order of their number,
- * by rows in order and within a row by column.
+ * them) are copied in every layer.  (So for every row of the call that writes it, the last
+ * one too: a page that all its rows write in one call is free afterwards.)  Free pages
+ * are taken in order of their number, by rows in order and within a row by column.
  *   block_table  int32 [rows, max_pages], updated; length, n_new int32 [rows]
  *   row_active   uint8 [rows] or NULL (all); other rows are left alone
  *   page_refs    updated; k_pages, v_pages every layer's pools
- *   row_ok       uint8 [rows] or NULL: 1 where an active row has its room, else 0
- * Where the pool runs out, a row whose pages and those of the rows before it (those
- * refused included) exceed the free pages is left as it was, and RGD_DEV_NO_PAGE is
- * set.  A row of a negative length or n_new, or past the table, or with an entry >=
+ *   row_ok       uint8 [rows] or NULL: 1 where an active row and those before it have
+ *                their room, else 0
+ * Rows are served in order: where the pool runs out, a row whose pages and those of the
+ * rows before it (those refused included) exceed the free pages is left as it was, also
+ * one that needs none itself, and RGD_DEV_NO_PAGE is set.  A row of a negative length or n_new, or past the table, or with an entry >=
  * num_pages there, is left as it was and sets RGD_DEV_BAD_PAGE.  RGD_ERR_UNSUPPORTED for
  * rows * max_pages of 2^31 or more.  One kernel, and one for the copies unless they are
  * few. */

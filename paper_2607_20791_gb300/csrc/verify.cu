@@ -27,7 +27,11 @@
 // weight 2^x <= 1 is rounded once to a whole number of 2^-31 and summed in 64 bits.  The
 // rounding is what a sum in fp32 does to a small weight too: it loses at most 2^-32 of
 // the largest weight, 3e-5 of the sum in the worst case over 131072 tokens, where each
-// is below 2.4e-10 of the largest.
+// is below 2.4e-10 of the largest.  max(0, p - q) goes by the same multiples, of probability
+// 1 (a scale of its own would take one exchange more, finer multiples a third sum).  A rest of small mass over many tokens
+// loses digits so (262144 tokens, T = 10, draft logits off by 0.05: a rest of mass 2e-3 is off by
+// 0.4 % in total variation; off by 0.005: 2e-4 and 4 %, a tenth of its tokens have no weight),
+// but is drawn from as rarely as its mass says: what is emitted is off by 8e-6 in both.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -810,7 +814,7 @@ int launch_verify(VerifyParams& p, cudaStream_t st) {
   // nothing meanwhile: its warps' shares are up to 40 stripes (20 KB), shorter (16) only to
   // have a few CTAs for each of the 608 that fit the SMs, so that they are at different
   // stages, and 8 only to fill the SMs.  Measured: 400 units of 2 x 128256 bf16 40 us with 4,
-  // 47 with 2, 51 with 8; 1024 of 3 x 152064 192 us with 2, 196 with 4; 192 of 262144
+  // 47 with 2, 51 with 8 (fp32: 55.4 with 4, 57.6 with 8); 1024 of 3 x 152064 192 us with 2, 196 with 4; 192 of 262144
   // fp32 58 us with 8, 80 with 4.  Few units are cut further until the SMs have two CTAs each, but
   // a CTA on its own needs no cluster's barriers: 9 units of 4096 fp32 8.4 us with 1, 9.4 with 2.
   int c = 1;
