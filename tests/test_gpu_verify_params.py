@@ -64,3 +64,22 @@ def test_positions_behind_a_rejection_set_no_status(gpu_lib, certain, vocab):
     c.run()
     assert int(c.status.item()) == binding.RGD_DEV_BAD_PARAM
     assert (c.out.cpu().numpy()[[0, 1, 4, 5]] == -1).all() and (c.acc.cpu().numpy()[[0, 1, 4, 5]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("certain", [False, True])
+def test_masks_of_the_types_lowest_value(gpu_lib, certain, dtype):
+    """Masked logits hold the lowest finite value; a position of nothing but masked ones is uniform over the vocabulary."""
+    import torch
+    c = Case(30, 2, 1500, dtype, seed=25, certain=certain, temps=(1.0, 0.5, 0.0, 3e38), min_ps=(0.0, 0.1), probe_every=9)
+    low = torch.finfo(c.t.dtype).min
+    c.t[:, :, 200:1400] = low
+    c.t[:, 2, 1400:] = low
+    if c.q is not None:
+        c.q[:, :, 100:1450] = low
+    c.t[::7, 0] = low
+    c.t[3::11, 1, 7] = -low  # (the largest logit the largest value: differences are past the range)
+    c.active[:] = 1
+    with np.errstate(over="ignore"):
+        c.run().check()
+    assert not bool(c.ws.any())
