@@ -25,6 +25,11 @@
  *   rgd_verify_draft        drafted tokens against the target's probabilities,
  *   rgd_cache_*             the pages of the KV cache: reserved and written for
  *                           new tokens, forked, trimmed, copied and compacted.
+ * Between a layer's hidden states and its attention:
+ *   rgd_fp8_quantize        activations or weights in 8-bit floating point,
+ *   rgd_fp8_matmul          products of them, for batches of rows and prompts,
+ *   rgd_qk_rope, _cache     norms of queries and keys and their rotation by
+ *                           position, the keys straight into the cache's pages.
  *
  * Conventions for every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller unless a comment
@@ -71,6 +76,17 @@ extern "C" {
 /* logits element types */
 #define RGD_F32 0
 #define RGD_BF16 1
+
+/* which values of a head are turned together: half the rotated part apart, or side by side */
+#define RGD_ROPE_HALF 0
+#define RGD_ROPE_PAIRS 1
+
+/* how rotary frequencies are scaled for positions past the trained length */
+#define RGD_ROPE_PLAIN 0
+#define RGD_ROPE_LINEAR 1
+#define RGD_ROPE_BASE 2
+#define RGD_ROPE_BANDS 3
+#define RGD_ROPE_RAMP 4
 
 /* gate decisions (Sec. 3 / Alg. 1 outcomes) */
 #define RGD_PENDING 0
@@ -582,6 +598,117 @@ int rgd_cache_compact(const rgd_cache_shape* shape, int32_t rows_a, int32_t max_
                       int32_t rows_b, int32_t max_pages_b, int32_t* block_table_b, int32_t* page_refs,
                       rgd_bf16* k_pages, rgd_bf16* v_pages, int32_t* num_live, void* workspace,
                       size_t workspace_bytes, int32_t* dev_status, rgd_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary positions, with the norms of queries and keys                       */
+/* ------------------------------------------------------------------------ */
+
+/* Heads of D = head_dim values each.  norm 1: a head x becomes w x / sqrt(mean(x^2) +
+ * eps) first.  Then pair i < rotary_dim / 2 of its values, (a, b), becomes
+ *   magnitude (a cos t - b sin t, b cos t + a sin t),  t = 2 pi turns[i] 2^-64 position;
+ * the pair is (x[i], x[i + rotary_dim / 2]) with RGD_ROPE_HALF, (x[2i], x[2i + 1]) with
+ * RGD_ROPE_PAIRS.  Values from rotary_dim on are not turned (they are normed). */
+typedef struct {
+  int32_t num_q_heads;  /* >= 0, at most 4096                                       */
+  int32_t num_k_heads;  /* >= 0, at most 4096                                       */
+  int32_t head_dim;     /* D >= 1, at most 1024                                     */
+  int32_t rotary_dim;   /* even, in [0, D]                                          */
+  int32_t layout;       /* RGD_ROPE_HALF or RGD_ROPE_PAIRS                          */
+  int32_t norm;         /* 0 or 1                                                   */
+  float eps;            /* of the norm                                              */
+  float magnitude;      /* on the rotated part (1 but for RGD_ROPE_RAMP)            */
+} rgd_rope_shape;
+
+/* HOST function: the frequencies of rotary_dim / 2 pairs as 64-bit fractions of a turn per
+ * position (turns, host, to be copied to the device by the caller), and the factor on the
+ * rotated part.  Pair i turns by f_i = base^(-2i / rotary_dim) radians per position, then
+ *   RGD_ROPE_PLAIN   no more
+ *   RGD_ROPE_LINEAR  f_i / factor
+ *   RGD_ROPE_BASE    with base factor^(rotary_dim / (rotary_dim - 2)) in place of base (base
+ *                    itself for a rotary_dim of 2)
+ *   RGD_ROPE_BANDS   f_i (s + (1 - s) / factor), s = (n_i - low) / (high - low) held to [0, 1],
+ *                    n_i = trained_length f_i / (2 pi): the turns over the trained length
+ *   RGD_ROPE_RAMP    the same with s = 1 - (i - a) / (b - a) held to [0, 1], a and b the pairs
+ *                    that turn `high` and `low` times over the trained length (rounded down
+ *                    and up, held to [0, rotary_dim - 1]); *magnitude = 0.1 ln(factor) + 1
+ * base >= 1, factor >= 1, trained_length > 0 and 0 < low < high where they are used. */
+int rgd_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double trained_length,
+                         double low, double high, uint64_t* turns, double* magnitude);
+
+/* Norms and rotation of the queries and keys of `tokens` tokens.
+ *   q, k           dtype RGD_F32 or RGD_BF16: token t's heads, densely, at t * q_stride (t *
+ *                  k_stride) elements; views of a fused projection's output do.  Aligned to
+ *                  their elements (16 bytes are fastest); not read where there are no heads
+ *   positions      int32 [tokens], any value
+ *   turns          device uint64 [rotary_dim / 2]
+ *   q_weight, k_weight  [D] of weight_dtype, or NULL (1); read with norm only
+ *   q_out, k_out   of the same dtype, token t's heads at t * q_out_stride (t * k_out_stride)
+ *                  elements, the strides no less than a token's heads.  They may be q and k
+ *                  themselves with the same strides, else must not overlap them
+ * Sums and products are taken in fp32 and rounded once; angles are exact to 2^-32 of a turn
+ * at any position.  No error is found on the device: dev_status is not written.  One kernel. */
+int rgd_qk_rope(const rgd_rope_shape* shape, int32_t tokens, int32_t dtype, const void* q, int64_t q_stride,
+                const void* k, int64_t k_stride, const int32_t* positions, const uint64_t* turns, int32_t weight_dtype,
+                const void* q_weight, const void* k_weight, void* q_out, int64_t q_out_stride, void* k_out,
+                int64_t k_out_stride, int32_t* dev_status, rgd_stream_t stream);
+
+/* The same for a step's new tokens, and their keys and values into reserved pages, in one
+ * pass (rgd_qk_rope, then rgd_cache_write): token i < n_new[r] of row r becomes token
+ * length[r] + i of the row, at position first_position[r] + length[r] + i.
+ *   q, k, v         bf16, the heads of (r, i) at r * row_stride + i * token_stride elements:
+ *                   views of a fused projection's output
+ *   first_position  int32 [rows]: tokens before the row's own (its prompt's), or NULL (0)
+ *   n_new, max_pages, block_table, length, row_active, k_pages, v_pages  as in
+ *                   rgd_cache_write
+ *   q_out           bf16 [rows, max_new, num_q_heads, D], not q itself
+ * The cache's num_kv_heads and head_dim are the shape's.  Tokens that are not written (rows
+ * with row_active 0, from n_new on, of a page that is not listed) leave q_out and the pages
+ * as they were; RGD_DEV_BAD_PAGE as in rgd_cache_write. */
+int rgd_qk_rope_cache(const rgd_rope_shape* shape, const rgd_cache_shape* cache, int32_t layer, int32_t rows,
+                      int32_t max_new, const rgd_bf16* q, const rgd_bf16* k, const rgd_bf16* v, int64_t row_stride,
+                      int64_t token_stride, const int32_t* first_position, const uint64_t* turns, int32_t weight_dtype,
+                      const void* q_weight, const void* k_weight, const int32_t* n_new, int32_t max_pages,
+                      const int32_t* block_table, const int32_t* length, const uint8_t* row_active, rgd_bf16* q_out,
+                      rgd_bf16* k_pages, rgd_bf16* v_pages, int32_t* dev_status, rgd_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Products in 8-bit floating point                                           */
+/* ------------------------------------------------------------------------ */
+
+/* Values in e4m3 (4 exponent, 3 mantissa bits, the largest 448, no infinities) and the scales
+ * that they stand for: of every 128 columns of a row (block_rows 1: activations) or of 128
+ * rows (block_rows 128: weights).  With most the largest magnitude of a block, scale = most /
+ * 448 and q = e4m3(x (448 / most)), each operation rounded to nearest in fp32; x is about q
+ * scale.  Blocks of zeros get 0 and 0; blocks whose largest is below 2^-100 are scaled as if it
+ * were that.  The last block of a row, and of rows, may be short.
+ *   x        [rows] rows of cols elements, x_stride elements apart (>= cols), dtype RGD_F32
+ *            or RGD_BF16, aligned to its elements
+ *   q        uint8 [rows] rows of cols, q_stride apart (>= cols; the rest of a row is left
+ *            alone).  rgd_fp8_matmul wants strides that are multiples of 16; those, with
+ *            x's rows on 16 bytes, are also written fastest
+ *   scales   float [ceil(rows / block_rows), ceil(cols / 128)]
+ * A block with an infinity or NaN gets that as its scale (products with it are NaN) and sets
+ * RGD_DEV_BAD_PARAM.  One kernel on `stream`. */
+int rgd_fp8_quantize(int32_t rows, int32_t cols, int32_t dtype, const void* x, int64_t x_stride, int32_t block_rows,
+                     uint8_t* q, int64_t q_stride, float* scales, int32_t* dev_status, rgd_stream_t stream);
+
+/* y[i, j] = sum_b x_scales[i, b] w_scales[j / 128, b] sum_{k in block b} x[i, k] w[j, k], b
+ * the blocks of 128 of k, for any number of rows (for a few rows and 4-bit weights there is
+ * rgd_w4_matvec).
+ *   x         e4m3 [m] rows of k values, x_stride bytes apart (>= k, a multiple of 16);
+ *             what lies behind a row's k is not read as a value
+ *   x_scales  float [m, ceil(k / 128)]
+ *   weights   e4m3 [n] rows of k, w_stride bytes apart (likewise)
+ *   w_scales  float [ceil(n / 128), ceil(k / 128)]
+ *   y         [m] rows of n elements, y_stride elements apart (>= n; the rest of a row is
+ *             left alone), out_dtype RGD_F32 or RGD_BF16
+ * A block's products are exact and summed by the tensor core in fp32; the blocks' sums are
+ * scaled and added in fp32 and the result is rounded once.  The order of the sums is the same
+ * for every call of the same m, n and k.  dev_status gets RGD_DEV_WAIT_TIMEOUT when a bounded
+ * wait gave up; y is then not valid.  k at most 2^24.  One kernel on `stream`. */
+int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x, int64_t x_stride, const float* x_scales,
+                   const uint8_t* weights, int64_t w_stride, const float* w_scales, int32_t out_dtype, void* y,
+                   int64_t y_stride, int32_t* dev_status, rgd_stream_t stream);
 
 #ifdef __cplusplus
 }

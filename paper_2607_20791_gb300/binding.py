@@ -21,6 +21,8 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "rgd.h")
 RGD_OK, RGD_ERR_INVALID_ARG, RGD_ERR_CUDA, RGD_ERR_UNSUPPORTED = 0, 1, 2, 3
 RGD_DEV_BAD_PAGE, RGD_DEV_BAD_TOKEN, RGD_DEV_WAIT_TIMEOUT, RGD_DEV_BAD_PARAM, RGD_DEV_NO_PAGE = 1, 2, 4, 8, 16
 RGD_F32, RGD_BF16 = 0, 1
+RGD_ROPE_HALF, RGD_ROPE_PAIRS = 0, 1
+RGD_ROPE_PLAIN, RGD_ROPE_LINEAR, RGD_ROPE_BASE, RGD_ROPE_BANDS, RGD_ROPE_RAMP = 0, 1, 2, 3, 4
 RGD_PENDING, RGD_REFUSAL, RGD_NON_REFUSAL = 0, 1, 2
 
 
@@ -42,6 +44,12 @@ class CacheShape(ctypes.Structure):
             ("layer_stride", ctypes.c_int64)]
 
 
+class RopeShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "num_q_heads", "num_k_heads", "head_dim", "rotary_dim", "layout", "norm")] + [
+            ("eps", ctypes.c_float), ("magnitude", ctypes.c_float)]
+
+
 class GateState(ctypes.Structure):
     _fields_ = [("node", ctypes.c_int32), ("length", ctypes.c_int32), ("steps", ctypes.c_int32),
                 ("decisive_step", ctypes.c_int32), ("decision", ctypes.c_uint8),
@@ -53,6 +61,7 @@ GATE_STATE_BYTES = ctypes.sizeof(GateState)  # 20
 _lib = None
 _P = ctypes.c_void_p
 _I32, _I64, _U64, _SZ, _F = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_size_t, ctypes.c_float
+_D = ctypes.c_double
 
 _SIGNATURES = {
     "rgd_last_error_string": (ctypes.c_char_p, []),
@@ -91,6 +100,13 @@ _SIGNATURES = {
     "rgd_cache_copy": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _P, _P, _P, _P, _P, _P]),
     "rgd_cache_compact": (ctypes.c_int, [ctypes.POINTER(CacheShape), _I32, _I32, _P, _I32, _I32, _P, _P, _P, _P, _P,
                                          _P, _SZ, _P, _P]),
+    "rgd_rope_frequencies": (ctypes.c_int, [_I32, _D, _I32, _D, _D, _D, _D, _P, ctypes.POINTER(_D)]),
+    "rgd_qk_rope": (ctypes.c_int, [ctypes.POINTER(RopeShape), _I32, _I32, _P, _I64, _P, _I64, _P, _P, _I32, _P, _P, _P, _I64,
+                                   _P, _I64, _P, _P]),
+    "rgd_qk_rope_cache": (ctypes.c_int, [ctypes.POINTER(RopeShape), ctypes.POINTER(CacheShape), _I32, _I32, _I32, _P, _P, _P,
+                                         _I64, _I64, _P, _P, _I32, _P, _P, _P, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "rgd_fp8_quantize": (ctypes.c_int, [_I32, _I32, _I32, _P, _I64, _I32, _P, _I64, _P, _P, _P]),
+    "rgd_fp8_matmul": (ctypes.c_int, [_I32, _I32, _I32, _P, _I64, _P, _P, _I64, _P, _I32, _P, _I64, _P, _P]),
 }
 
 
@@ -634,6 +650,156 @@ def rgd_cache_compact(shape: CacheShape, block_table_a, block_table_b, page_refs
         _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
         _ptr(num_live, "num_live", i32, numel=1), _ptr(workspace, "workspace"), _bytes_of(workspace),
         _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+_ROPE_SCALINGS = {"none": RGD_ROPE_PLAIN, "linear": RGD_ROPE_LINEAR, "base": RGD_ROPE_BASE, "bands": RGD_ROPE_BANDS,
+                  "ramp": RGD_ROPE_RAMP}
+
+
+def rgd_rope_frequencies(rotary_dim: int, base: float, scaling="none", factor: float = 1.0, trained_length: float = 0.0,
+                         low: float = 1.0, high: Optional[float] = None):
+    """Frequencies as 64-bit fractions of a turn (an int64 host tensor [rotary_dim / 2], to be moved to the device),
+    and the magnitude for :class:`RopeShape`.  ``high`` defaults to 4 for "bands" and 32 for "ramp"."""
+    import torch
+    kind = _ROPE_SCALINGS.get(scaling, scaling)
+    if not isinstance(kind, int):
+        raise ValueError(f"scaling must be one of {sorted(_ROPE_SCALINGS)}")
+    if high is None:
+        high = 32.0 if kind == RGD_ROPE_RAMP else 4.0
+    turns, magnitude = torch.zeros(max(int(rotary_dim), 0) // 2, dtype=torch.int64), ctypes.c_double()
+    _check(load_library().rgd_rope_frequencies(int(rotary_dim), float(base), kind, float(factor), float(trained_length),
+                                               float(low), float(high), turns.data_ptr(), ctypes.byref(magnitude)))
+    return turns, magnitude.value
+
+
+def _heads_of(t, name: str, lead: int, heads: int, dim: int, dtypes):
+    """[..., heads, head_dim] with `lead` leading dimensions, whose last two are dense; None where there are no heads.
+    Returns the pointer, the leading sizes and their strides (0 where there is one element: never used)."""
+    import torch
+    if t is None and heads == 0:
+        return None, None, (0,) * lead
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise TypeError(f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")
+    if t.dim() != lead + 2 or t.shape[lead] != heads or t.shape[lead + 1] != dim:
+        raise ValueError(f"{name} must have {lead} leading dimensions and then [{heads}, {dim}]")
+    stride = t.stride()
+    if t.numel() and ((stride[-1] != 1 and dim > 1) or (stride[-2] != dim and heads > 1)):
+        raise ValueError(f"{name}: heads and head_dim must be dense")
+    strides = tuple(stride[i] if t.shape[i] > 1 else 0 for i in range(lead))
+    return (t.data_ptr() if t.is_cuda else _HostTensor(name)), tuple(t.shape[:lead]), strides
+
+
+def _rope_weights(shape: RopeShape, q_weight, k_weight):
+    """Pointers of the norms' weights and their dtype code."""
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if not shape.norm or not weights:
+        return None, None, RGD_F32
+    code = _dtype_of(weights[0], "weights")
+    return tuple(_ptr(w, name, weights[0].dtype, optional=True, numel=shape.head_dim)
+                 for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight"))) + (code,)
+
+
+def rgd_qk_rope(shape: RopeShape, q, k, positions, turns, q_weight, k_weight, q_out, k_out, dev_status=None,
+                stream=None) -> None:
+    """``q`` and ``q_out`` [tokens, Hq, D], ``k`` and ``k_out`` [tokens, Hk, D] (None where the shape has no such heads);
+    tokens may be strided."""
+    import torch
+    first = q if shape.num_q_heads else k
+    kinds = (torch.bfloat16, torch.float32) if first is None or not hasattr(first, "dtype") else (
+        (first.dtype,) if first.dtype in (torch.bfloat16, torch.float32) else (torch.bfloat16, torch.float32))
+    hq, hk, d, tokens = shape.num_q_heads, shape.num_k_heads, shape.head_dim, positions.numel()
+    args = []
+    for t, name, heads in ((q, "q", hq), (k, "k", hk), (q_out, "q_out", hq), (k_out, "k_out", hk)):
+        ptr, lead, strides = _heads_of(t, name, 1, heads, d, kinds)
+        if heads and lead != (tokens,):
+            raise ValueError(f"{name} must have positions' {tokens} tokens")
+        if name.endswith("_out") and tokens <= 1:
+            strides = (heads * d,)
+        args += [ptr, strides[0]]
+    wq, wk, code = _rope_weights(shape, q_weight, k_weight)
+    _check(_call(load_library().rgd_qk_rope,
+        ctypes.byref(shape), tokens, RGD_F32 if kinds[0] is torch.float32 else RGD_BF16, *args[:4],
+        _ptr(positions, "positions", torch.int32), _ptr(turns, "turns", torch.int64, optional=shape.rotary_dim == 0,
+                                                        numel=shape.rotary_dim // 2),
+        code, wq, wk, *args[4:], _ptr(dev_status, "dev_status", torch.int32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_qk_rope_cache(shape: RopeShape, cache: CacheShape, layer: int, q, k, v, first_position, turns, q_weight, k_weight,
+                      n_new, block_table, length, row_active, q_out, k_pages, v_pages, dev_status=None,
+                      stream=None) -> None:
+    """``q`` [rows, max_new, Hq, D], ``k`` and ``v`` [rows, max_new, Hkv, D] with the same strides of rows and tokens (views
+    of a fused projection); ``q_out`` [rows, max_new, Hq, D], contiguous."""
+    import torch
+    bf, i32, pool = (torch.bfloat16,), torch.int32, _pool_numel(cache)
+    rows, cols = _table_size(block_table)
+    (kp, lead, strides), (vp, v_lead, v_strides) = (
+        _heads_of(t, name, 2, cache.num_kv_heads, cache.head_dim, bf) for t, name in ((k, "k"), (v, "v")))
+    qp, q_lead, q_strides = _heads_of(q, "q", 2, shape.num_q_heads, shape.head_dim, bf)
+    if lead[0] != rows or v_lead != lead or v_strides != strides or (q_lead is not None and (q_lead, q_strides) != (lead, strides)):
+        raise ValueError("q, k and v must have block_table's rows and the same leading sizes and strides")
+    wq, wk, code = _rope_weights(shape, q_weight, k_weight)
+    _check(_call(load_library().rgd_qk_rope_cache,
+        ctypes.byref(shape), ctypes.byref(cache), int(layer), rows, lead[1], qp, kp, vp, *strides,
+        _ptr(first_position, "first_position", i32, optional=True, numel=rows),
+        _ptr(turns, "turns", torch.int64, optional=shape.rotary_dim == 0, numel=shape.rotary_dim // 2), code, wq, wk,
+        _ptr(n_new, "n_new", i32, numel=rows), cols, _ptr(block_table, "block_table", i32),
+        _ptr(length, "length", i32, numel=rows), _ptr(row_active, "row_active", torch.uint8, optional=True, numel=rows),
+        _ptr(q_out, "q_out", torch.bfloat16, optional=shape.num_q_heads == 0,
+             numel=rows * lead[1] * shape.num_q_heads * shape.head_dim),
+        _ptr(k_pages, "k_pages", torch.bfloat16, numel=pool), _ptr(v_pages, "v_pages", torch.bfloat16, numel=pool),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
+
+
+def _rows_of(t, name: str, dtypes):
+    """[rows, columns] whose columns are dense: the pointer and the stride of its rows (that of one row: its width)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
+        raise TypeError(f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    rows, cols = t.shape
+    by_row, by_col = t.stride()
+    if t.numel() and by_col != 1 and cols > 1:
+        raise ValueError(f"{name}: columns must be dense")
+    return (t.data_ptr() if t.is_cuda else _HostTensor(name)), (by_row if rows > 1 else max(by_row, cols))
+
+
+def rgd_fp8_quantize(x, q, scales, block_rows: int = 1, dev_status=None, stream=None) -> None:
+    """``x`` [rows, cols] in e4m3 into the first cols columns of ``q`` [rows, W >= cols] (float8_e4m3fn or uint8); rows of
+    both may be strided."""
+    import torch
+    xp, x_stride = _rows_of(x, "x", (torch.float32, torch.bfloat16))
+    qp, q_stride = _rows_of(q, "q", (torch.float8_e4m3fn, torch.uint8))
+    rows, cols = x.shape
+    if q.shape[0] != rows or q.shape[1] < cols:
+        raise ValueError(f"q must be [{rows}, {cols}] (or wider)")
+    each = int(block_rows)
+    numel = -(-rows // each) * -(-cols // 128) if each > 0 else 0
+    _check(_call(load_library().rgd_fp8_quantize,
+        rows, cols, _dtype_of(x, "x"), xp, x_stride, each, qp, q_stride,
+        _ptr(scales, "scales", torch.float32, numel=numel),
+        _ptr(dev_status, "dev_status", torch.int32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_fp8_matmul(x, x_scales, weights, w_scales, y, k: Optional[int] = None, dev_status=None, stream=None) -> None:
+    """``y`` [m, W >= n] gets ``x`` [m, K] times ``weights`` [n, K'] over their first ``k`` columns (default: K) in its first
+    n columns.  e4m3 as float8_e4m3fn or uint8; rows of all three may be strided."""
+    import torch
+    bits = (torch.float8_e4m3fn, torch.uint8)
+    xp, x_stride = _rows_of(x, "x", bits)
+    wp, w_stride = _rows_of(weights, "weights", bits)
+    yp, y_stride = _rows_of(y, "y", (torch.float32, torch.bfloat16))
+    m, n = x.shape[0], weights.shape[0]
+    k = x.shape[1] if k is None else int(k)
+    if x.shape[1] < k or weights.shape[1] < k:
+        raise ValueError(f"x and weights must have at least k = {k} columns")
+    if y.shape[0] != m or y.shape[1] < n:
+        raise ValueError(f"y must be [{m}, {n}] (or wider)")
+    blocks = -(-k // 128)
+    _check(_call(load_library().rgd_fp8_matmul,
+        m, n, k, xp, x_stride, _ptr(x_scales, "x_scales", torch.float32, numel=m * blocks), wp, w_stride,
+        _ptr(w_scales, "w_scales", torch.float32, numel=-(-n // 128) * blocks), _dtype_of(y, "y"), yp, y_stride,
+        _ptr(dev_status, "dev_status", torch.int32, optional=True, numel=1), _stream(stream)))
 
 
 def new_gate_state(groups: int, device="cuda"):

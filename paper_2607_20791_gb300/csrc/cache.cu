@@ -11,20 +11,14 @@
 #include <algorithm>
 #include <cmath>
 
+#include "cache.h"
 #include "common.h"
 #include "ptx.cuh"
 
 namespace rgd {
 namespace {
 
-constexpr int kPageSize = 16;
-constexpr int kPlanThreads = 1024;
 constexpr int kCopyThreads = 256;
-
-struct CacheView {
-  int32_t layers, pages, heads, dim;
-  int64_t layer_stride;  // elements between a layer's pool and the next
-};
 
 __device__ __forceinline__ void begin_dependent() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
@@ -539,7 +533,17 @@ cudaError_t launch_plan(void (*kernel)(P...), int blocks, cudaStream_t st, A&&..
 // Blocks of a plan: one does for what it sees in a single sweep.
 int plan_blocks(int32_t rows, int32_t pages) { return rows <= kPlanThreads && pages <= kSweep ? 1 : kPlanBlocks; }
 
-int check_shape(const char* fn, const rgd_cache_shape* s, CacheView& c) {
+constexpr int kWarpsEach = kCopyThreads / 32;
+int launch_copies(const CopyParams& p, int64_t most, cudaStream_t st) {
+  const int64_t warps = std::max(most * p.c.layers * 2 * p.c.heads, (p.entries[0] + p.entries[1] + 31) / 32);
+  const int grid = blocks_for(std::max<int64_t>(warps, 1), kWarpsEach, 152 * 8);
+  const cudaError_t e = launch_dependent(copy_kernel, grid, kCopyThreads, 0, st, p);
+  return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache copy launch");
+}
+
+}  // namespace
+
+int check_cache_shape(const char* fn, const rgd_cache_shape* s, CacheView& c) {
   RGD_CHECK_ARG(s != nullptr, "%s: shape is NULL", fn);
   RGD_CHECK_ARG(s->num_layers >= 1 && s->num_pages >= 1 && s->num_kv_heads >= 1 && s->head_dim >= 1,
                 "%s: num_layers/num_pages/num_kv_heads/head_dim must be >= 1", fn);
@@ -556,18 +560,6 @@ int check_shape(const char* fn, const rgd_cache_shape* s, CacheView& c) {
   return RGD_OK;
 }
 
-constexpr int kWarpsEach = kCopyThreads / 32;
-// Rows (or pairs, or tokens) at most: the numbers that a last block gives to those past the end are still an int.
-constexpr int32_t kMaxRows = 0x7fffffff - kPlanThreads;
-
-int launch_copies(const CopyParams& p, int64_t most, cudaStream_t st) {
-  const int64_t warps = std::max(most * p.c.layers * 2 * p.c.heads, (p.entries[0] + p.entries[1] + 31) / 32);
-  const int grid = blocks_for(std::max<int64_t>(warps, 1), kWarpsEach, 152 * 8);
-  const cudaError_t e = launch_dependent(copy_kernel, grid, kCopyThreads, 0, st, p);
-  return e == cudaSuccess ? RGD_OK : cuda_error(e, "cache copy launch");
-}
-
-}  // namespace
 }  // namespace rgd
 
 using namespace rgd;
@@ -575,7 +567,7 @@ using namespace rgd;
 extern "C" size_t rgd_cache_workspace_size(const rgd_cache_shape* shape, int32_t rows) {
   clear_error();
   CacheView c;
-  if (check_shape("rgd_cache_workspace_size", shape, c)) return 0;
+  if (check_cache_shape("rgd_cache_workspace_size", shape, c)) return 0;
   if (rows < 0) {
     set_error(RGD_ERR_INVALID_ARG, "rgd_cache_workspace_size: rows < 0");
     return 0;
@@ -590,7 +582,7 @@ extern "C" int rgd_cache_reserve(const rgd_cache_shape* shape, int32_t rows, int
   clear_error();
   const char* fn = "rgd_cache_reserve";
   CacheView c;
-  if (int rc = check_shape(fn, shape, c)) return rc;
+  if (int rc = check_cache_shape(fn, shape, c)) return rc;
   RGD_CHECK_ARG(rows >= 0 && max_pages >= 1, "%s: bad rows/max_pages", fn);
   if (rows == 0) return RGD_OK;
   // (the kernel adds up the pages that rows want in 32 bits)
@@ -648,7 +640,7 @@ extern "C" int rgd_cache_write(const rgd_cache_shape* shape, int32_t layer, int3
   clear_error();
   const char* fn = "rgd_cache_write";
   CacheView c;
-  if (int rc = check_shape(fn, shape, c)) return rc;
+  if (int rc = check_cache_shape(fn, shape, c)) return rc;
   RGD_CHECK_ARG(rows >= 0 && max_new >= 0 && max_pages >= 1, "%s: bad rows/max_new/max_pages", fn);
   RGD_CHECK_ARG(layer >= 0 && layer < c.layers, "%s: layer outside [0, num_layers)", fn);
   RGD_CHECK_ARG(row_stride >= 0 && token_stride >= 0, "%s: strides must not be negative", fn);
@@ -715,7 +707,7 @@ extern "C" int rgd_cache_copy(const rgd_cache_shape* shape, int32_t n, const int
   clear_error();
   const char* fn = "rgd_cache_copy";
   CacheView c;
-  if (int rc = check_shape(fn, shape, c)) return rc;
+  if (int rc = check_cache_shape(fn, shape, c)) return rc;
   RGD_CHECK_ARG(n >= 0, "%s: n < 0", fn);
   if (n == 0) return RGD_OK;
   RGD_CHECK_ARG(src && dst && k_pages && v_pages, "%s: src/dst/k_pages/v_pages must be non-NULL", fn);
@@ -738,7 +730,7 @@ extern "C" int rgd_cache_compact(const rgd_cache_shape* shape, int32_t rows_a, i
   clear_error();
   const char* fn = "rgd_cache_compact";
   CacheView c;
-  if (int rc = check_shape(fn, shape, c)) return rc;
+  if (int rc = check_cache_shape(fn, shape, c)) return rc;
   RGD_CHECK_ARG(rows_a >= 0 && rows_b >= 0 && max_pages_a >= 0 && max_pages_b >= 0, "%s: bad rows/max_pages", fn);
   RGD_CHECK_ARG(page_refs && k_pages && v_pages && num_live && workspace,
                 "%s: page_refs/k_pages/v_pages/num_live/workspace must be non-NULL", fn);
