@@ -25,11 +25,13 @@
  *   rgd_verify_draft        drafted tokens against the target's probabilities,
  *   rgd_cache_*             the pages of the KV cache: reserved and written for
  *                           new tokens, forked, trimmed, copied and compacted.
- * Between a layer's hidden states and its attention:
+ * Between a layer's hidden states and its attention, and after the logits:
  *   rgd_fp8_quantize        activations or weights in 8-bit floating point,
  *   rgd_fp8_matmul          products of them, for batches of rows and prompts,
  *   rgd_qk_rope, _cache     norms of queries and keys and their rotation by
- *                           position, the keys straight into the cache's pages.
+ *                           position, the keys straight into the cache's pages,
+ *   rgd_sample_top          temperature, top-k, top-p and min-p from given
+ *                           uniforms.
  *
  * Conventions for every entry point
  *   - Tensor pointers are DEVICE pointers owned by the caller unless a comment
@@ -709,6 +711,40 @@ int rgd_fp8_quantize(int32_t rows, int32_t cols, int32_t dtype, const void* x, i
 int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x, int64_t x_stride, const float* x_scales,
                    const uint8_t* weights, int64_t w_stride, const float* w_scales, int32_t out_dtype, void* y,
                    int64_t y_stride, int32_t* dev_status, rgd_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Sampling with more filters, from given uniforms                            */
+/* ------------------------------------------------------------------------ */
+
+/* One token a row.  Tokens are ordered by their logits, the largest first, equal ones (0 and
+ * -0 are) by their index, and have weights 2^((l - l_max) log2(e) / T).  S: the first top_k of
+ * the tokens that min_p leaves, {l >= c} with c = fl32(l_max + fl32(T ln p_min)) as in
+ * rgd_sample_head.  The kept tokens: the shortest run of S from its front whose weights sum
+ * to at least top_p times those of S (one token at least; all of S for a top_p of 1).
+ * token = the smallest i whose kept tokens up to i, in order of the indices, have more weight
+ * than draw_u times that of all kept ones.  Greedy rows (is_probe or temperature 0): the
+ * argmax, lowest index on ties; the filters and draw_u are not read.
+ *   logits       [rows] rows of vocab logits, stride elements apart (>= vocab), RGD_F32 or
+ *                RGD_BF16; rows that all start on 16 bytes are read fastest
+ *   is_probe     uint8 [rows] or NULL; temperature float [rows]
+ *   top_k        int32 [rows] or NULL; no limit where it is <= 0 or >= vocab
+ *   top_p        float [rows] in [0, 1] or NULL (1); min_p float [rows] in [0, 1] or NULL (0)
+ *   draw_u       float [rows], in [0, 1)
+ *   row_active   uint8 [rows] or NULL (all active)
+ *   token_out    int32 [rows]: the token; -1 for inactive and rejected rows
+ *   kept_count   int32 [rows] or NULL: kept tokens (1 in greedy rows, 0 in inactive and
+ *                rejected ones)
+ *   prob_out     float [rows] or NULL: the token's weight over that of all kept tokens (1 in
+ *                greedy rows, 0 in inactive and rejected ones)
+ * NaN and -inf are never kept.  A row with a parameter out of range or a largest logit that is
+ * not finite is rejected and sets RGD_DEV_BAD_PARAM.  Weights are rounded to multiples of 2^-31 and
+ * summed exactly, and top_p's share is the smallest whole multiple not below top_p times the sum (rounded once in
+ * FP64): the outputs are the same however a call is cut.  RGD_ERR_UNSUPPORTED above a vocab
+ * of 2^20.  One kernel on `stream`. */
+int rgd_sample_top(int32_t rows, int32_t vocab, int32_t dtype, const void* logits, int64_t stride,
+                   const uint8_t* is_probe, const float* temperature, const int32_t* top_k, const float* top_p,
+                   const float* min_p, const float* draw_u, const uint8_t* row_active, int32_t* token_out,
+                   int32_t* kept_count, float* prob_out, int32_t* dev_status, rgd_stream_t stream);
 
 #ifdef __cplusplus
 }

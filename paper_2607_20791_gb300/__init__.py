@@ -12,7 +12,7 @@ from .binding import (  # noqa: F401
     rgd_probe_gate, rgd_sample_head, rgd_trie_create, rgd_version,
     CacheShape, rgd_cache_compact, rgd_cache_copy, rgd_cache_fork, rgd_cache_reserve, rgd_cache_trim,
     rgd_cache_workspace_size, rgd_cache_write, rgd_verify_draft, rgd_verify_draft_workspace_size, rgd_w4_matvec,
-    RopeShape, rgd_fp8_matmul, rgd_fp8_quantize, rgd_qk_rope, rgd_qk_rope_cache, rgd_rope_frequencies,
+    RopeShape, rgd_fp8_matmul, rgd_fp8_quantize, rgd_qk_rope, rgd_qk_rope_cache, rgd_rope_frequencies, rgd_sample_top,
     RGD_ROPE_HALF, RGD_ROPE_PAIRS,
     RGD_PENDING, RGD_REFUSAL, RGD_NON_REFUSAL, RGD_F32, RGD_BF16,
     RGD_DEV_BAD_PAGE, RGD_DEV_BAD_TOKEN, RGD_DEV_WAIT_TIMEOUT, RGD_DEV_BAD_PARAM, RGD_DEV_NO_PAGE,

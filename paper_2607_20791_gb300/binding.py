@@ -106,6 +106,7 @@ _SIGNATURES = {
     "rgd_qk_rope_cache": (ctypes.c_int, [ctypes.POINTER(RopeShape), ctypes.POINTER(CacheShape), _I32, _I32, _I32, _P, _P, _P,
                                          _I64, _I64, _P, _P, _I32, _P, _P, _P, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
     "rgd_fp8_quantize": (ctypes.c_int, [_I32, _I32, _I32, _P, _I64, _I32, _P, _I64, _P, _P, _P]),
+    "rgd_sample_top": (ctypes.c_int, [_I32, _I32, _I32, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "rgd_fp8_matmul": (ctypes.c_int, [_I32, _I32, _I32, _P, _I64, _P, _P, _I64, _P, _I32, _P, _I64, _P, _P]),
 }
 
@@ -800,6 +801,26 @@ def rgd_fp8_matmul(x, x_scales, weights, w_scales, y, k: Optional[int] = None, d
         m, n, k, xp, x_stride, _ptr(x_scales, "x_scales", torch.float32, numel=m * blocks), wp, w_stride,
         _ptr(w_scales, "w_scales", torch.float32, numel=-(-n // 128) * blocks), _dtype_of(y, "y"), yp, y_stride,
         _ptr(dev_status, "dev_status", torch.int32, optional=True, numel=1), _stream(stream)))
+
+
+def rgd_sample_top(logits, is_probe, temperature, top_k, top_p, min_p, draw_u, row_active, token_out, kept_count=None,
+                   prob_out=None, vocab: Optional[int] = None, dev_status=None, stream=None) -> None:
+    """``logits`` [rows, W], of which the first ``vocab`` of every row are logits (default: W); rows may be strided."""
+    import torch
+    lp, stride = _rows_of(logits, "logits", (torch.float32, torch.bfloat16))
+    rows, width = logits.shape
+    vocab = width if vocab is None else int(vocab)
+    if vocab > width:
+        raise ValueError(f"logits holds rows of {width}, the call needs {vocab}")
+    i32, f32, u8 = torch.int32, torch.float32, torch.uint8
+    _check(_call(load_library().rgd_sample_top,
+        rows, vocab, _dtype_of(logits, "logits"), lp, stride, _ptr(is_probe, "is_probe", u8, optional=True, numel=rows),
+        _ptr(temperature, "temperature", f32, numel=rows), _ptr(top_k, "top_k", i32, optional=True, numel=rows),
+        _ptr(top_p, "top_p", f32, optional=True, numel=rows), _ptr(min_p, "min_p", f32, optional=True, numel=rows),
+        _ptr(draw_u, "draw_u", f32, numel=rows), _ptr(row_active, "row_active", u8, optional=True, numel=rows),
+        _ptr(token_out, "token_out", i32, numel=rows), _ptr(kept_count, "kept_count", i32, optional=True, numel=rows),
+        _ptr(prob_out, "prob_out", f32, optional=True, numel=rows),
+        _ptr(dev_status, "dev_status", i32, optional=True, numel=1), _stream(stream)))
 
 
 def new_gate_state(groups: int, device="cuda"):

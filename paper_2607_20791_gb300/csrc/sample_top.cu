@@ -1,0 +1,852 @@
+// Sampling with temperature, top-k, top-p and min-p from given uniforms.  Tokens are ordered
+// by their logits, the largest first, equal ones by their index.  S is the first k of those
+// that min-p leaves; the kept tokens are the shortest run of S from its front whose weights
+// reach p times S's; the token is drawn from them in the order of their indices.
+//
+// Weights 2^((l - top) log2(e)/T) are whole multiples of 2^-31 and summed in 64 bits, so that
+// every sum, every cut and every token is the same whatever order it is worked out in.
+//
+// One cluster of CTAs a row, every warp with a contiguous share of it:
+//   1 the maximum, a stream from HBM; and a bound that enough tokens surely reach: a warp's
+//     r-th largest lane maximum, the smallest over all warps, is reached by r tokens of each;
+//   2 the tokens that reach the bound go into a list in the first CTA's shared memory (the
+//     row lies in L2 now, and only vectors whose group reaches the bound are read); top-p
+//     alone needs all the weights' sum as well.  The first CTA sorts the list.  Where k, or the
+//     mass p, lies within it the row is done: the usual case, two exchanges.
+//   3 else the cut is searched for: a range of logits, at first from a sample of the row, is
+//     divided into 512 by a histogram of counts or weights; the part that holds the cut is the
+//     next range, until what it holds fits the list or is one value.  Then a pass for the kept
+//     tokens' sums by warp, and one warp finds the token.
+// No sorting of whole rows, no limit on k or on how flat a row is.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "common.h"
+#include "log_pair.cuh"
+#include "logit_rows.cuh"
+#include "ptx.cuh"
+
+namespace rgd {
+namespace {
+
+constexpr int kTopWarps = 8;
+constexpr int kTopThreads = kTopWarps * 32;
+constexpr int kTopCluster = 16;  // CTAs of a row at most
+constexpr int kList = 2048;      // tokens that are sorted together at most
+constexpr int kEnough = 512;     // tokens that the first list shall hold at least for top-p
+constexpr int kBins = 512;
+constexpr int kSampleShift = 3;  // 1 stripe of 8 is sampled
+constexpr int kOctaves = 32;     // weights below 2^-32 are 0
+constexpr int kMargin = 4;       // bins to both sides of a sampled cut
+
+struct TopParams {
+  const uint8_t* logits;
+  int64_t stride;  // bytes
+  int32_t rows, vocab, stripes;
+  const uint8_t* is_probe;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* draw_u;
+  const uint8_t* row_active;
+  int32_t* token_out;
+  int32_t* kept_count;
+  float* prob_out;
+  int32_t* dev_status;
+};
+
+// What the first CTA tells the others to do next.
+enum Next { kDone, kRange, kDraw };
+struct Order {
+  int next;
+  int by_count;         // the cut is at a count, not a mass
+  uint32_t from, to;    // range of keys' distances from the largest
+  uint32_t last_key;    // the last kept value, and how many of it are kept (0: all)
+  uint32_t of_last;
+  uint64_t need;        // count or mass up to the cut, the last token included
+};
+static_assert(sizeof(Order) % 8 == 0, "");
+
+struct TopShared {
+  float warp_top[kTopWarps], warp_low[kTopWarps], top[kTopCluster], low[kTopCluster];
+  uint64_t warp_sum[kTopWarps], sum[kTopCluster], part_sum[kTopWarps];
+  uint32_t warp_count[kTopWarps], count[kTopCluster], part_count[kTopWarps];
+  uint64_t scan[kTopWarps];
+  uint32_t lo[kBins], hi[kBins];  // sums of the weights' low 16 bits and of the rest, or counts
+  uint32_t listed;                // tokens that belong into the list
+  Order order;
+  float theta;
+  int found;
+  uint64_t value;
+  uint64_t list[kList];
+};
+
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t load_peer(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_peer(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void store_peer(uint32_t addr, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+// Keys in the order of the logits; -0 and 0 have the same.
+__device__ __forceinline__ uint32_t key_of(float l) {
+  const uint32_t u = __float_as_uint(l == 0.f ? 0.f : l);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_key(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+}
+// The number of range t of 1/8 octave below the top.
+__device__ __forceinline__ int octave_bin(float octaves) { return (int)fminf(octaves * (float)(kBins / 2 / kOctaves), (float)(kBins / 2 - 1)); }
+
+// f(vector, its number) for every vector of a lane's part that may reach `bound`.
+template <typename T, bool kAligned, typename F>
+__device__ __forceinline__ void visit(const Share<T, kAligned>& v, const Kept& kept, float bound, int stripes, int lane, F&& f) {
+  using V = Vec<T>;
+  const uint32_t mask = groups_reaching(kept, bound);
+  const int steps = (int)__reduce_max_sync(0xffffffffu, (uint32_t)__popc(mask)) * ((stripes + kGroups - 1) / kGroups);
+  if (7 * steps > 4 * stripes) {  // all of them, in order
+#pragma unroll 1
+    for (int i = lane; i < v.whole; i += 32 * 4) {
+      uint4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[k] = V::nothing();
+        if (i + 32 * k < v.whole) x[k] = v.get(i + 32 * k);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f(x[k], i + 32 * k);
+    }
+  } else {
+    Walk walk(mask, stripes, v.whole, lane);
+    int i = walk.next();
+    uint4 w = V::nothing();
+    if (i >= 0) w = v.get(i);
+#pragma unroll 1
+    while (i >= 0) {
+      const int ahead = walk.next();
+      uint4 w1 = V::nothing();
+      if (ahead >= 0) w1 = v.get(ahead);
+      f(w, i);
+      w = w1;
+      i = ahead;
+    }
+  }
+  f(kept.rest, v.whole);
+}
+
+// Sorts n = 2^i numbers in shared memory, the largest first.  The whole CTA.
+__device__ __noinline__ void sort_down(uint64_t* a, int n) {
+  for (int size = 2; size <= n; size *= 2) {
+    for (int gap = size / 2; gap > 0; gap /= 2) {
+      __syncthreads();
+      for (int t = threadIdx.x; t < n / 2; t += kTopThreads) {
+        const int i = 2 * t - (t & (gap - 1)), j = i + gap;
+        const uint64_t x = a[i], y = a[j];
+        if ((x < y) == ((i & size) == 0)) {
+          a[i] = y;
+          a[j] = x;
+        }
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// Sum over the threads before this one, and over all.  The whole CTA.
+__device__ __forceinline__ uint64_t scan_before(TopShared& sh, uint64_t v, uint64_t& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t upto = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
+  }
+  __syncthreads();  // (may still be read from the scan before)
+  if (lane == 31) sh.scan[warp] = upto;
+  __syncthreads();
+  uint64_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kTopWarps; ++w) {
+    before += w < warp ? sh.scan[w] : 0;
+    all += sh.scan[w];
+  }
+  return before + upto - v;
+}
+
+__device__ __forceinline__ uint32_t whole_weight(const Side& side, float l) { return whole(side.weight(l)); }
+__device__ __forceinline__ uint64_t share_of(float p, uint64_t total) {  // ceil(p total), at least 1
+  const uint64_t need = (uint64_t)ceil((double)p * (double)total);
+  return need ? need : 1;
+}
+
+// The first CTA: the first `keep` tokens of the sorted list of n are kept; draws from them and
+// writes the row's results.
+__device__ __noinline__ void finish_list(const TopParams& p, TopShared& sh, const Side& side, int row, int keep, float u) {
+  int n = 32;
+  while (n < keep) n *= 2;
+  for (int i = threadIdx.x; i < n; i += kTopThreads) {
+    uint64_t e = 0;
+    if (i < keep) {
+      const uint64_t t = sh.list[i];
+      e = t << 32 | whole_weight(side, of_key((uint32_t)(t >> 32)));  // (the complement of the index, and the weight)
+    }
+    __syncwarp();
+    sh.list[i] = e;
+  }
+  sort_down(sh.list, n);  // by index
+  const int each = (n + kTopThreads - 1) / kTopThreads, first = threadIdx.x * each;
+  uint64_t mine = 0, total;
+  for (int i = 0; i < each; ++i)
+    if (first + i < keep) mine += (uint32_t)sh.list[first + i];
+  uint64_t before = scan_before(sh, mine, total);
+  const uint64_t mark = (uint64_t)((double)u * (double)total);
+  for (int i = 0; i < each; ++i) {
+    if (first + i >= keep) break;
+    const uint64_t e = sh.list[first + i];
+    const uint32_t w = (uint32_t)e;
+    if (before <= mark && mark < before + w) {
+      p.token_out[row] = (int32_t)~(uint32_t)(e >> 32);
+      if (p.prob_out) p.prob_out[row] = __fdiv_rn((float)w, __ull2float_rn(total));
+    }
+    before += w;
+  }
+  if (threadIdx.x == 0 && p.kept_count) p.kept_count[row] = keep;
+}
+
+template <typename T, bool kAligned>
+__global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopParams p) {
+  constexpr int E = 16 / (int)sizeof(T);
+  using V = Vec<T>;
+  __shared__ TopShared sh;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t rank, csize, urow;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(csize));
+  asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(urow));
+  const int row = (int)urow;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // The row's parameters; every thread of the cluster takes the same decisions.
+  const bool active = !p.row_active || p.row_active[row];
+  const float temp = p.temperature[row], u = p.draw_u[row];
+  const float min_p = p.min_p ? p.min_p[row] : 0.f, top_p = p.top_p ? p.top_p[row] : 1.f;
+  const bool greedy = (p.is_probe && p.is_probe[row]) || temp == 0.f;
+  const int k = p.top_k && p.top_k[row] > 0 && p.top_k[row] < p.vocab ? p.top_k[row] : 0;
+  bool good = true;
+  if (!greedy)
+    good = temp > 0.f && temp < INFINITY && min_p >= 0.f && min_p <= 1.f && top_p >= 0.f && top_p <= 1.f && u >= 0.f && u < 1.f;
+  auto nothing = [&](bool bad) {
+    if (rank != 0 || threadIdx.x != 0) return;
+    p.token_out[row] = -1;
+    if (p.kept_count) p.kept_count[row] = 0;
+    if (p.prob_out) p.prob_out[row] = 0.f;
+    if (bad && p.dev_status) atomicOr(p.dev_status, RGD_DEV_BAD_PARAM);
+  };
+  if (!active || !good) return nothing(active);
+  const bool cut_mass = !greedy && top_p < 1.f;
+
+  // This warp's share, in the order of the elements over the cluster.
+  const uint8_t* logits = p.logits + row * p.stride;
+  const int64_t share = (int64_t)p.stripes * 32 * E;
+  const int64_t e0 = ((int64_t)rank * kTopWarps + warp) * share;
+  const Share<T, kAligned> v(logits, e0, min(share, p.vocab - e0));
+  if (threadIdx.x == 0) {
+    sh.listed = 0;
+    sh.theta = scaled_log(greedy ? 1.f : temp, greedy ? 1.f : min_p);
+  }
+
+  // Pass 1: the maximum (NaN never wins), and a bound that `wanted` tokens reach.
+  Kept kept;
+  // (warps with a vector for every lane; the others' lanes would only lower the bound)
+  const int shares = (int)((p.vocab + share - 32 * E) / share);
+  const bool full_share = (int64_t)p.vocab - e0 >= 32 * E;
+  const int wanted = greedy ? 0 : k ? k : cut_mass ? min(kEnough, p.vocab) : 0;
+  const int each = shares ? (wanted + shares - 1) / shares : 0;  // of a warp (0: all tokens will do)
+  {
+    const float mine = find_lane_maxima(v, kept, p.stripes, lane), top = warp_max(mine);
+    float low = -INFINITY;
+    if (each > 0 && each <= 32 && full_share) {  // the each-th largest of the lanes' maxima
+      int larger = 0;
+#pragma unroll
+      for (int o = 0; o < 32; ++o) {
+        const float x = __shfl_sync(0xffffffffu, mine, o);
+        larger += x > mine || (x == mine && o < lane);
+      }
+      low = warp_max(larger == each - 1 ? mine : -INFINITY);
+    }
+    if (lane == 0) {
+      sh.warp_top[warp] = top;
+      sh.warp_low[warp] = full_share || !shares ? low : INFINITY;
+    }
+  }
+  __syncthreads();
+  cluster_arrive_relaxed();  // every CTA of the cluster has started
+  cluster_wait();
+  if (warp == 0) {
+    float t = sh.warp_top[lane % kTopWarps], l = -sh.warp_low[lane % kTopWarps];
+    t = warp_max(t);
+    l = -warp_max(l);
+    if (lane < (int)csize) {
+      store_peer(peer_addr(smem_u32(&sh.top[rank]), lane), __float_as_uint(t));
+      store_peer(peer_addr(smem_u32(&sh.low[rank]), lane), __float_as_uint(l));
+    }
+  }
+  cluster_barrier();
+  Side side;
+  side.top = warp_max(sh.top[lane % csize]);
+  const float low = -warp_max(-sh.low[lane % csize]);
+  if (!(fabsf(side.top) < INFINITY)) return nothing(true);
+
+  if (greedy) {  // the lowest index of the largest logit
+    uint32_t best = 0xffffffffu;
+    auto look = [&](const uint4& w, int i) {
+#pragma unroll
+      for (int e = E - 1; e >= 0; --e)
+        if (elem<T>(w, e) == side.top) best = min(best, (uint32_t)e0 + i * E + e);
+    };
+    Walk walk(groups_reaching(kept, side.top), p.stripes, v.whole, lane);
+#pragma unroll 1
+    for (int i = walk.next(); i >= 0; i = walk.next()) look(v.get(i), i);
+    look(kept.rest, v.whole);
+    best = __reduce_min_sync(0xffffffffu, best);
+    if (lane == 0) sh.warp_count[warp] = best;
+    __syncthreads();
+    if (warp == 0) {
+      best = __reduce_min_sync(0xffffffffu, sh.warp_count[lane % kTopWarps]);
+      if (lane == 0) store_peer(peer_addr(smem_u32(&sh.count[rank]), 0), best);
+    }
+    cluster_barrier();
+    if (rank == 0 && warp == 0) {
+      best = __reduce_min_sync(0xffffffffu, sh.count[lane % csize]);
+      if (lane == 0) {
+        p.token_out[row] = (int32_t)best;
+        if (p.kept_count) p.kept_count[row] = 1;
+        if (p.prob_out) p.prob_out[row] = 1.f;
+      }
+    }
+    return;
+  }
+  side.kexp = fminf(__fdiv_rn(1.4426950408889634f, temp), 3e38f);  // (finite: 0 times it is 0)
+  side.cut = fmaxf(__fadd_rn(side.top, sh.theta), -3.4028234663852886e38f);  // (-inf is never kept)
+  const uint32_t top_key = key_of(side.top);
+
+  const uint32_t list_count = peer_addr(smem_u32(&sh.listed), 0), list_at = peer_addr(smem_u32(&sh.list[0]), 0);
+  // (the lanes that come together count together; a lane that has seen the list full adds no more:
+  // the count is above kList then)
+  bool full = false;
+  auto enlist = [&](float l, uint32_t index) {
+    if (full) return;
+    const uint32_t with = __activemask();
+    const int first = __ffs(with) - 1;
+    uint32_t at = 0;
+    if (lane == first)
+      asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(at) : "r"(list_count), "r"(__popc(with)) : "memory");
+    at = __shfl_sync(with, at, first) + __popc(with & ((1u << lane) - 1));
+    if (at < kList) store_peer(list_at + 8 * at, (uint64_t)key_of(l) << 32 | (uint32_t)~index);
+    else full = true;
+  };
+  // Adds to a bin.  Where there are many tokens, they may all be of one value: lanes of the same
+  // bin add up first then.
+  auto add_to = [&](uint32_t* bins, uint32_t b, uint32_t x) {
+    if (full) {
+      const uint32_t with = __activemask();
+      int same;
+      __match_all_sync(with, b, &same);
+      if (same) {
+        x = __reduce_add_sync(with, x);
+        if (lane == __ffs(with) - 1) atomicAdd(&bins[b], x);
+        return;
+      }
+    }
+    atomicAdd(&bins[b], x);
+  };
+  // Every CTA's sum and count into every CTA.
+  auto exchange = [&](uint64_t sum, uint32_t count) {
+    if (lane == 0) {
+      sh.warp_sum[warp] = sum;
+      sh.warp_count[warp] = count;
+    }
+    __syncthreads();
+    if (warp == 0) {
+      const uint64_t s = warp_sum(lane < kTopWarps ? sh.warp_sum[lane] : 0);
+      const uint32_t c = __reduce_add_sync(0xffffffffu, lane < kTopWarps ? sh.warp_count[lane] : 0);
+      if (lane < (int)csize) {
+        store_peer(peer_addr(smem_u32(&sh.sum[rank]), lane), s);
+        store_peer(peer_addr(smem_u32(&sh.count[rank]), lane), c);
+      }
+    }
+    cluster_barrier();
+  };
+  auto sum_all = [&]() { return warp_sum(lane < (int)csize ? sh.sum[lane] : 0); };
+  auto count_all = [&]() { return __reduce_add_sync(0xffffffffu, lane < (int)csize ? sh.count[lane] : 0); };
+  // The first CTA's order into every CTA.
+  auto publish = [&]() {
+    __syncthreads();
+    if (warp == 0 && lane < (int)csize && lane > 0) {
+      const uint64_t* from = reinterpret_cast<const uint64_t*>(&sh.order);
+      const uint32_t to = peer_addr(smem_u32(&sh.order), lane);
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(Order) / 8; ++i) store_peer(to + 8 * i, from[i]);
+    }
+  };
+  auto clear_bins = [&]() {
+    for (int i = threadIdx.x; i < kBins; i += kTopThreads) sh.lo[i] = sh.hi[i] = 0;
+    __syncthreads();
+  };
+  // A bin's sum over the cluster (the first CTA).
+  auto bin_sum = [&](int b, bool high) {
+    uint64_t s = 0;
+    for (uint32_t r = 0; r < csize; ++r) {
+      s += load_peer(peer_addr(smem_u32(&sh.lo[b]), r));
+      if (high) s += (uint64_t)load_peer(peer_addr(smem_u32(&sh.hi[b]), r)) << 16;
+    }
+    return s;
+  };
+
+  uint64_t total = 0;  // of S's weights, once known
+  if (k || cut_mass) {
+    // Pass 2.
+    const float bound = each <= 32 ? fmaxf(low, side.cut) : INFINITY;
+    const bool sampled = !k || bound == INFINITY;
+    if (sampled) clear_bins();
+    WholeSum sum;
+    const float scale = side.kexp;
+    visit(v, kept, sampled ? side.cut : bound, p.stripes, lane, [&](const uint4& w, int i) {
+      if (!k) add_weights<T>(w, side, typename V::Bound(side.cut), sum);
+      const bool in_sample = sampled && ((i >> 5) & ((1 << kSampleShift) - 1)) == 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float l = elem<T>(w, e);
+        if (l >= bound) enlist(l, (uint32_t)e0 + i * E + e);
+        else if (in_sample && l >= side.cut)
+          atomicAdd(&sh.lo[octave_bin((side.top - l) * scale)], k ? 1u : whole_weight(side, l) >> 13);
+      }
+    });
+    exchange(k ? 0 : warp_sum(sum.total()), 0);
+    if (rank == 0) {
+      total = sum_all();
+      const uint32_t listed = sh.listed;
+      const int n = (int)min(listed, (uint32_t)kList);
+      int keep = -1;  // known to be cut within the list
+      uint64_t in_list = 0, need = k ? (uint64_t)k : share_of(top_p, total);
+      if (listed <= kList && bound < INFINITY) {
+        int n2 = 32;
+        while (n2 < n) n2 *= 2;
+        for (int i = n + threadIdx.x; i < n2; i += kTopThreads) sh.list[i] = 0;
+        sort_down(sh.list, n2);
+        const int m = k ? min(k, n) : n;  // of S
+        const int per = (n2 + kTopThreads - 1) / kTopThreads, first = threadIdx.x * per;
+        uint64_t mine = 0;
+        if (cut_mass) {
+          for (int i = 0; i < per; ++i)
+            if (first + i < m) mine += whole_weight(side, of_key((uint32_t)(sh.list[first + i] >> 32)));
+          uint64_t before = scan_before(sh, mine, in_list);
+          if (k) {
+            total = in_list;
+            need = share_of(top_p, total);
+          }
+          if (threadIdx.x == 0) sh.found = -1;
+          __syncthreads();
+          for (int i = 0; i < per; ++i) {
+            if (first + i >= m) break;
+            const uint32_t w = whole_weight(side, of_key((uint32_t)(sh.list[first + i] >> 32)));
+            if (before < need && need <= before + w) sh.found = first + i + 1;
+            before += w;
+          }
+          __syncthreads();
+          keep = sh.found;
+        } else {
+          keep = m;
+        }
+      }
+      if (threadIdx.x == 0) {
+        sh.order.next = keep >= 0 ? kDone : kRange;
+        sh.order.by_count = k > 0;
+        sh.order.need = need;
+        sh.order.from = 0;
+        sh.order.to = top_key - key_of(side.cut);
+        sh.found = -1;
+      }
+      __syncthreads();
+      if (keep < 0 && (k == 0 || bound == INFINITY) && (bound == INFINITY || listed <= kList)) {
+        // Where the cut is likely to be, from the sample: what it holds below the list stands for the rest.
+        const uint64_t mine = bin_sum(threadIdx.x, false);
+        uint64_t all;
+        const uint64_t before = scan_before(sh, mine, all);
+        const uint64_t rest = k ? 0 : total - in_list;
+        // (a stripe in 8, or in as many as a share has; what of k's sample stands for is not known better)
+        const double at = k ? (double)need / (double)min(1 << kSampleShift, p.stripes)
+                            : rest ? (double)(need - in_list) / (double)rest * (double)all : 0;
+        if (mine && (double)before < at && at <= (double)(before + mine)) {
+          const float octave = 1.f / (float)(kBins / 2 / kOctaves) / side.kexp;
+          const float hi = side.top - (float)max((int)threadIdx.x - kMargin, 0) * octave;
+          const float lo = side.top - (float)(threadIdx.x + 1 + kMargin) * octave;
+          sh.order.from = top_key - key_of(fminf(hi, side.top));
+          if (lo > side.cut && threadIdx.x + 1 + kMargin < kBins / 2) sh.order.to = top_key - key_of(lo);
+          if (sh.order.from > sh.order.to) sh.order.from = 0;
+        }
+      }
+      publish();
+      if (keep >= 0) {
+        cluster_barrier();
+        finish_list(p, sh, side, row, keep, u);
+        return;
+      }
+      if (threadIdx.x == 0) sh.listed = 0;
+    }
+    cluster_barrier();
+    if (sh.order.next == kDone) return;
+
+    // Pass 3, until the cut is found: what lies above the range, and in each of its parts.
+#pragma unroll 1
+    while (sh.order.next == kRange) {
+      const uint32_t from = sh.order.from, to = sh.order.to;
+      const bool by_count = sh.order.by_count;
+      int shift = 0;
+      while (((to - from) >> shift) >= (uint32_t)kBins) ++shift;
+      const float in_range = of_key(top_key - to);                          // the smallest of it,
+      const float above = from ? of_key(top_key - from + 1) : INFINITY;     // and of what lies above it
+      __syncthreads();
+      clear_bins();
+      WholeSum over;
+      full = false;
+      uint32_t count = 0;
+      visit(v, kept, in_range, p.stripes, lane, [&](const uint4& w, int i) {
+        if (from) add_weights<T>(w, side, typename V::Bound(above), over);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float l = elem<T>(w, e);
+          if (l >= above) {
+            ++count;
+          } else if (l >= in_range) {
+            const uint32_t b = (top_key - key_of(l) - from) >> shift;
+            if (by_count) {
+              add_to(sh.lo, b, 1);
+            } else {
+              const uint32_t x = whole_weight(side, l);
+              if (x & 0xffffu) add_to(sh.lo, b, x & 0xffffu);
+              if (x >> 16) add_to(sh.hi, b, x >> 16);
+            }
+            enlist(l, (uint32_t)e0 + i * E + e);
+          }
+        }
+      });
+      exchange(warp_sum(over.total()), __reduce_add_sync(0xffffffffu, count));
+      if (rank == 0) {
+        const uint64_t mass = sum_all();
+        const uint32_t counted = count_all(), listed = sh.listed;
+        const uint64_t before = by_count ? counted : mass, need = sh.order.need;
+        const uint64_t b0 = bin_sum(2 * threadIdx.x, !by_count), b1 = bin_sum(2 * threadIdx.x + 1, !by_count);
+        uint64_t inside;
+        uint64_t upto = before + scan_before(sh, b0 + b1, inside);
+        __syncthreads();  // (every thread has read the order)
+        bool cut = false;      // found, at (last_key, of_last), by this thread
+        uint32_t last_key = 0, of_last = 0;
+        uint32_t kept_here = 0;  // tokens of the range
+        uint64_t mass_upto = 0;  // up to the cut, known where the cut is at a count
+        if (need <= before) {
+          if (threadIdx.x == 0) {
+            sh.order.from = 0;
+            sh.order.to = from - 1;
+          }
+        } else if (need > before + inside) {  // (by a count: fewer than k tokens, if the range reaches down to the cutoff)
+          const uint32_t lowest = top_key - key_of(side.cut);
+          if (to < lowest) {
+            if (threadIdx.x == 0) {
+              sh.order.from = to + 1;
+              sh.order.to = lowest;
+            }
+          } else if (threadIdx.x == 0) {
+            sh.order.need = before + inside;  // all of them
+          }
+        } else if (from == to) {  // one value
+          if (threadIdx.x == 0) {
+            const uint64_t w = whole_weight(side, in_range), unit = by_count ? 1 : w;
+            cut = true;
+            last_key = top_key - to;
+            of_last = (uint32_t)((need - before + unit - 1) / unit);
+            kept_here = of_last;
+            mass_upto = mass + of_last * w;
+          }
+        } else if (listed <= kList) {
+          const int n = (int)listed;
+          int n2 = 32;
+          while (n2 < n) n2 *= 2;
+          for (int i = n + threadIdx.x; i < n2; i += kTopThreads) sh.list[i] = 0;
+          sort_down(sh.list, n2);
+          const int per = (n2 + kTopThreads - 1) / kTopThreads, first = threadIdx.x * per;
+          uint64_t mine = 0, all;
+          for (int i = 0; i < per; ++i)
+            if (first + i < n) mine += whole_weight(side, of_key((uint32_t)(sh.list[first + i] >> 32)));
+          uint64_t at = mass + scan_before(sh, mine, all);
+          for (int i = 0; i < per; ++i) {
+            const int j = first + i;
+            if (j >= n) break;
+            const uint32_t key = (uint32_t)(sh.list[j] >> 32), w = whole_weight(side, of_key(key));
+            if (by_count ? counted + j + 1 == need : at < need && need <= at + w) {
+              cut = true;
+              last_key = key;
+              int f = j;  // the first of this value
+              while (f > 0 && (uint32_t)(sh.list[f - 1] >> 32) == key) --f;
+              of_last = (uint32_t)(j - f + 1);
+              kept_here = (uint32_t)j + 1;
+              mass_upto = at + w;
+            }
+            at += w;
+          }
+        } else {  // the part that holds the cut
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint64_t b = i ? b1 : b0;
+            if (upto < need && need <= upto + b) {
+              const uint32_t start = from + ((uint32_t)(2 * threadIdx.x + i) << shift);
+              sh.order.from = start;
+              sh.order.to = min(to, start + ((1u << shift) - 1));
+            }
+            upto += b;
+          }
+        }
+        if (cut) {
+          if (by_count && cut_mass) {  // S is known now; next where its mass is cut
+            sh.order.by_count = 0;
+            sh.order.need = share_of(top_p, mass_upto);
+            sh.order.from = 0;
+            sh.order.to = top_key - last_key;
+          } else {
+            sh.order.next = kDraw;
+            sh.order.last_key = last_key;
+            sh.order.of_last = of_last;
+            if (p.kept_count) p.kept_count[row] = (int32_t)(counted + kept_here);
+          }
+        }
+        publish();
+        if (threadIdx.x == 0) sh.listed = 0;
+      }
+      cluster_barrier();
+    }
+  } else if (threadIdx.x == 0) {  // all that the cutoff leaves
+    sh.order.last_key = key_of(side.cut);
+    sh.order.of_last = 0;
+  }
+  __syncthreads();
+
+  // The kept tokens' sums by warp: those above the last kept value, and the lowest indices of it.
+  const uint32_t of_last = sh.order.of_last;
+  const float last = of_key(sh.order.last_key), above = of_last ? of_key(sh.order.last_key + 1) : side.cut;
+  const uint64_t last_weight = of_last ? whole_weight(side, last) : 0;
+  WholeSum sum;
+  uint32_t ties = 0, larger = 0;
+  visit(v, kept, of_last ? last : above, p.stripes, lane, [&](const uint4& w, int) {
+    add_weights<T>(w, side, typename V::Bound(above), sum);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float l = elem<T>(w, e);
+      larger += l >= above;
+      ties += l >= last && !(l >= above);
+    }
+  });
+  larger = __reduce_add_sync(0xffffffffu, larger);
+  exchange(warp_sum(sum.total()), of_last ? __reduce_add_sync(0xffffffffu, ties) : larger);
+  total = sum_all() + (uint64_t)of_last * last_weight;
+  if (rank == 0 && !of_last && p.kept_count) {  // (else it was known with the cut)
+    const uint32_t n = count_all();
+    if (threadIdx.x == 0) p.kept_count[row] = (int32_t)n;
+  }
+  // The CTA, then the share, that holds the mark.
+  const uint64_t mark = (uint64_t)((double)u * (double)total);
+  auto held = [&](uint64_t s, uint64_t before_ties, uint32_t n) {  // a stretch's mass, with the ties that are kept
+    const uint64_t left = before_ties < of_last ? of_last - before_ties : 0;
+    return s + (of_last ? min((uint64_t)n, left) * last_weight : 0);
+  };
+  uint64_t before = 0, tied = 0;
+  for (uint32_t r = 0; r < rank; ++r) {
+    before += held(sh.sum[r], tied, sh.count[r]);
+    tied += sh.count[r];
+  }
+  if (!(before <= mark && mark < before + held(sh.sum[rank], tied, sh.count[rank]))) return;
+  int owner = 0;
+  for (; owner + 1 < kTopWarps; ++owner) {
+    const uint64_t h = held(sh.warp_sum[owner], tied, sh.warp_count[owner]);
+    if (mark < before + h) break;
+    before += h;
+    tied += sh.warp_count[owner];
+  }
+  // Every warp takes a part of that share, and the one whose part holds the mark finds the token.
+  const int64_t o0 = ((int64_t)rank * kTopWarps + owner) * share;
+  const Share<T, kAligned> o(logits, o0, min(share, p.vocab - o0));
+  const int stripes = (p.stripes + kTopWarps - 1) / kTopWarps;
+  uint64_t part = 0;
+  uint32_t part_ties = 0;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll 1
+    for (int s = 0; s < stripes; ++s) {
+      const int i = (warp * stripes + s) * 32 + lane;
+      uint4 a = V::nothing();
+      if (s + warp * stripes < p.stripes) {
+        if (i < o.whole) a = o.get(i);
+        else if (i == o.whole) a = o.rest(lane);
+      }
+      uint64_t own = 0;
+      uint32_t n = 0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float l = elem<T>(a, e);
+        if (l >= above) own += whole_weight(side, l);
+        else if (of_last && l >= last) ++n;
+      }
+      const uint64_t stripe = warp_sum(own);
+      const uint32_t stripe_ties = __reduce_add_sync(0xffffffffu, n);
+      if (pass == 0) {
+        part += stripe;
+        part_ties += stripe_ties;
+        continue;
+      }
+      const uint64_t h = held(stripe, tied, stripe_ties);
+      if (!(mark < before + h)) {
+        before += h;
+        tied += stripe_ties;
+        continue;
+      }
+      uint32_t ties_upto = n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, ties_upto, d);
+        if (lane >= d) ties_upto += x;
+      }
+      uint64_t rank_of = tied + ties_upto - n;  // ties before this lane's
+      const uint64_t mine = held(own, rank_of, n);
+      uint64_t upto = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint64_t x = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += x;
+      }
+      uint64_t at = before + upto - mine;
+      if (at <= mark && mark < at + mine) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float l = elem<T>(a, e);
+          uint64_t w = 0;
+          if (l >= above) w = whole_weight(side, l);
+          else if (of_last && l >= last && rank_of++ < of_last) w = last_weight;
+          if (at <= mark && mark < at + w) {
+            p.token_out[row] = (int32_t)(o0 + (int64_t)i * E + e);
+            if (p.prob_out) p.prob_out[row] = __fdiv_rn((float)(uint32_t)w, __ull2float_rn(total));
+          }
+          at += w;
+        }
+      }
+      return;
+    }
+    if (pass == 1) return;
+    if (lane == 0) {
+      sh.part_sum[warp] = part;
+      sh.part_count[warp] = part_ties;
+    }
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) {
+      before += held(sh.part_sum[w], tied, sh.part_count[w]);
+      tied += sh.part_count[w];
+    }
+    if (!(before <= mark && mark < before + held(part, tied, part_ties))) return;
+  }
+}
+
+template <typename T, bool kAligned>
+int launch_top(TopParams& p, cudaStream_t st) {
+  static std::atomic<bool> wide[kMaxDevices];  // clusters of 16 are allowed
+  auto k = sample_top_kernel<T, kAligned>;
+  const int64_t nvec = ((int64_t)p.vocab * sizeof(T) + 15) / 16;
+  auto stripes = [&](int c) { return (int)((nvec + (int64_t)c * kTopWarps * 32 - 1) / ((int64_t)c * kTopWarps * 32)); };
+  // CTAs of a row: shares of up to 32 stripes (16 KB) a warp (and 65536 tokens a CTA at most: a bin's
+  // sums stay below 2^32), shorter only to have a few CTAs for every SM.
+  int c = 1;
+  while (c < kTopCluster && (stripes(c) > 32 || (int64_t)stripes(c) * kTopWarps * 32 * (16 / (int)sizeof(T)) > 65536)) c *= 2;
+  while (c < 8 && (int64_t)p.rows * c < 608 && stripes(2 * c) >= 4) c *= 2;
+  while (c < kTopCluster && (int64_t)p.rows * c < 304 && stripes(c) > 4) c *= 2;
+  if (c > 8) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return cuda_error(e, "cudaGetDevice");
+    if (dev >= kMaxDevices || !wide[dev].load(std::memory_order_acquire)) {
+      e = cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return cuda_error(e, "sampling attributes");
+      if (dev < kMaxDevices) wide[dev].store(true, std::memory_order_release);
+    }
+  }
+  p.stripes = stripes(c);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((int64_t)p.rows * c));
+  cfg.blockDim = dim3(kTopThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {(unsigned)c, 1, 1};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, k, p);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  return e == cudaSuccess ? RGD_OK : cuda_error(e, "sampling launch");
+}
+
+}  // namespace
+}  // namespace rgd
+
+using namespace rgd;
+
+extern "C" int rgd_sample_top(int32_t rows, int32_t vocab, int32_t dtype, const void* logits, int64_t stride,
+                              const uint8_t* is_probe, const float* temperature, const int32_t* top_k,
+                              const float* top_p, const float* min_p, const float* draw_u, const uint8_t* row_active,
+                              int32_t* token_out, int32_t* kept_count, float* prob_out, int32_t* dev_status,
+                              rgd_stream_t stream) {
+  clear_error();
+  const char* fn = "rgd_sample_top";
+  RGD_CHECK_ARG(rows >= 0, "%s: rows < 0", fn);
+  RGD_CHECK_ARG(vocab >= 1, "%s: vocab < 1", fn);
+  RGD_CHECK_ARG(dtype == RGD_F32 || dtype == RGD_BF16, "%s: dtype must be RGD_F32 or RGD_BF16", fn);
+  RGD_CHECK_ARG(stride >= vocab, "%s: stride is below vocab", fn);
+  if (rows == 0) return RGD_OK;
+  RGD_CHECK_ARG(logits && temperature && draw_u && token_out, "%s: logits/temperature/draw_u/token_out must be non-NULL", fn);
+  RGD_CHECK_ARG(aligned16(logits), "%s: logits must be 16-byte aligned", fn);
+  // (sums of a row's weights stay below 2^52 then, and are exact in FP64)
+  if (vocab > 1 << 20) return set_error(RGD_ERR_UNSUPPORTED, "%s: vocab %d too large (max %d)", fn, vocab, 1 << 20);
+  if (rows > 0x7fffffff / kTopCluster) return set_error(RGD_ERR_UNSUPPORTED, "%s: too many rows", fn);
+  const int es = dtype == RGD_F32 ? 4 : 2;
+  TopParams p{};
+  p.logits = static_cast<const uint8_t*>(logits);
+  p.stride = stride * es;
+  p.rows = rows;
+  p.vocab = vocab;
+  p.is_probe = is_probe;
+  p.temperature = temperature;
+  p.top_k = top_k;
+  p.top_p = top_p;
+  p.min_p = min_p;
+  p.draw_u = draw_u;
+  p.row_active = row_active;
+  p.token_out = token_out;
+  p.kept_count = kept_count;
+  p.prob_out = prob_out;
+  p.dev_status = dev_status;
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool aligned = p.stride % 16 == 0;
+  if (dtype == RGD_F32) return aligned ? launch_top<float, true>(p, st) : launch_top<float, false>(p, st);
+  return aligned ? launch_top<__nv_bfloat16, true>(p, st) : launch_top<__nv_bfloat16, false>(p, st);
+}
