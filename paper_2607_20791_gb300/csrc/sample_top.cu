@@ -39,6 +39,7 @@ constexpr int kEnough = 512;     // tokens that the first list shall hold at lea
 constexpr int kBins = 512;
 constexpr int kSampleShift = 3;  // 1 stripe of 8 is sampled
 constexpr int kOctaves = 32;     // weights below 2^-32 are 0
+constexpr int kMostRounds = 64;
 constexpr int kMargin = 4;       // bins to both sides of a sampled cut
 
 struct TopParams {
@@ -479,7 +480,6 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
         sh.order.need = need;
         sh.order.from = 0;
         sh.order.to = top_key - key_of(side.cut);
-        sh.found = -1;
       }
       __syncthreads();
       if (keep < 0 && (k == 0 || bound == INFINITY) && (bound == INFINITY || listed <= kList)) {
@@ -512,8 +512,16 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
     if (sh.order.next == kDone) return;
 
     // Pass 3, until the cut is found: what lies above the range, and in each of its parts.
+    // (A round leaves 1/512 of a range of less than 2^32, after one or two that find a sampled range
+    // wrong: no search takes kMostRounds.)
+    int rounds = 0;
 #pragma unroll 1
     while (sh.order.next == kRange) {
+      if (++rounds > kMostRounds) {  // (uniform over the cluster)
+        nothing(false);
+        if (rank == 0 && threadIdx.x == 0 && p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
+        return;
+      }
       const uint32_t from = sh.order.from, to = sh.order.to;
       const bool by_count = sh.order.by_count;
       int shift = 0;
