@@ -25,11 +25,12 @@
 namespace rgd {
 namespace {
 
-constexpr int kLanes = 128;              // rows of A a tile
+constexpr int kLanes = 128;              // rows of A a CTA's tile
 constexpr int kStep = 128;               // values of k that share a scale: one step
 constexpr int kABytes = kLanes * kStep;  // of a stage
 constexpr int kMostStages = 12;
-constexpr int kScaleSteps = 8;           // steps whose column scales are fetched together
+constexpr int kScaleSlots = 8;  // steps whose scales are on their way or in use
+constexpr int kMostSums = 8;    // steps whose sums are
 constexpr int kRoom = 227 * 1024 - 1024;
 
 struct Fp8Params {
@@ -46,7 +47,8 @@ struct Fp8Params {
 };
 
 struct Fp8Shared {
-  uint64_t full[kMostStages], empty[kMostStages], sum_full[2], sum_empty[2], drained;
+  uint64_t full[kMostStages], empty[kMostStages], sum_full[kMostSums], sum_empty[kMostSums];
+  uint64_t scale_full[kScaleSlots], scale_empty[kScaleSlots], drained;
   uint32_t tmem;
   int dead;
 };
@@ -108,36 +110,65 @@ __device__ __forceinline__ void write_rows(const Fp8Params& p, const uint32_t* w
   __syncwarp();
 }
 
+constexpr int kMostSplit = 8;  // CTAs that share a tile
 template <int NT>
-constexpr int kFp8Threads = NT > 128 ? 384 : 192;
+constexpr int kPartRow = NT + 4;  // floats of a lane's part (lanes on different banks)
+template <int NT>
+constexpr int kAdders = NT > 128 ? 256 : 128;  // threads that add up
+template <int NT>
+constexpr int kFp8Threads = kAdders<NT> + 128;
 
-// NT: columns of a tile at most.  kTurned: w's rows are the lanes, x's the columns.
-template <int NT, bool kTurned>
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// 4 bytes to shared memory, without a wait; zeros if not `on`.
+__device__ __forceinline__ void copy_async4(float* dst, const float* src, bool on) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 4 : 0) : "memory");
+}
+
+// NT: columns of a tile at most.  kTurned: w's rows are the lanes, x's the columns.  kPair: two
+// CTAs take 256 rows of x by 256 columns; each copies its own rows and half of the columns, so
+// that a value that is copied takes part in half as many copies again (48 KB a step by one CTA,
+// 32 by each of two), and the tensor cores read it from both CTAs' memory.
+template <int NT, bool kTurned, bool kPair>
 __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     fp8_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap) {
-  constexpr int kAdders = NT > 128 ? 256 : 128, kOwn = NT > 128 ? 128 : NT;  // threads that add up, columns of each
-  constexpr int kProducer = kAdders / 32, kIssuer = kProducer + 1;
-  constexpr uint32_t kTmemCols = 2 * NT < 32 ? 32 : 2 * NT;
+  static_assert(!kPair || (NT == 256 && !kTurned), "");
+  constexpr int kOwn = NT > 128 ? 128 : NT;  // columns of a thread
+  constexpr int kProducer = kAdders<NT> / 32, kIssuer = kProducer + 1, kScaler = kProducer + 2;
+  constexpr int kSums = 512 / NT < kMostSums ? 512 / NT : kMostSums;  // accumulators
+  constexpr uint32_t kTmemCols = kSums * NT;
+  constexpr int kRows = kTurned ? NT : kLanes;  // x's rows of a tile
   extern __shared__ uint8_t raw[];
   __shared__ Fp8Shared sh;
-  __shared__ __align__(16) float scale[kTurned ? 2 : 1][kTurned ? kScaleSteps : 1][kTurned ? NT : 4];
-  __shared__ uint32_t stage[kTurned ? 1 : kAdders * kStageWords];
+  __shared__ __align__(16) float x_scale[kScaleSlots][kRows];
+  __shared__ float w_scale[kScaleSlots][2];
+  __shared__ uint32_t stage[kTurned ? 1 : kAdders<NT> * kStageWords];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int stage_bytes = kABytes + p.cols * kStep;
+  const int b_rows = kPair ? p.cols / 2 : p.cols;  // of B that this CTA copies
+  const int stage_bytes = kABytes + b_rows * kStep;
   uint32_t rank = 0, tile0 = blockIdx.x, tile_step = gridDim.x;
-  if (p.split > 1) {
+  if (kPair || p.split > 1) {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%clusterid.x;" : "=r"(tile0));
-    tile_step = (uint32_t)p.tiles;
+    tile_step = kPair ? gridDim.x / 2 : (uint32_t)p.tiles;
   }
-  const int step0 = (int)((int64_t)p.steps * rank / p.split), steps = (int)((int64_t)p.steps * (rank + 1) / p.split) - step0;
+  const int parts = kPair ? 1 : p.split, part_rank = kPair ? 0 : (int)rank;
+  const int step0 = (int)((int64_t)p.steps * part_rank / parts), steps = (int)((int64_t)p.steps * (part_rank + 1) / parts) - step0;
   const int total = ((p.tiles - 1 - (int)tile0) / (int)tile_step + 1) * steps;
 
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
   if (warp == kIssuer) {
-    tmem_alloc(&sh.tmem, kTmemCols);
-    tmem_relinquish();
+    if (kPair) {
+      tmem_alloc_pair(&sh.tmem, kTmemCols);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(&sh.tmem, kTmemCols);
+      tmem_relinquish();
+    }
   }
   if (threadIdx.x == 0) {
     sh.dead = 0;
@@ -145,9 +176,13 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       mbar_init(&sh.full[i], 1);
       mbar_init(&sh.empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kSums; ++i) {
       mbar_init(&sh.sum_full[i], 1);
-      mbar_init(&sh.sum_empty[i], kAdders / 32);
+      mbar_init(&sh.sum_empty[i], kAdders<NT> / 32 * (kPair ? 2 : 1));
+    }
+    for (int i = 0; i < kScaleSlots; ++i) {
+      mbar_init(&sh.scale_full[i], 32);
+      mbar_init(&sh.scale_empty[i], kAdders<NT> / 32);
     }
     mbar_init(&sh.drained, 1);
     fence_mbar_init();
@@ -158,6 +193,10 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   }
   tc_fence_before();
   __syncthreads();
+  if (kPair) {  // (each signals the other's barriers)
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
   tc_fence_after();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t tmem = sh.tmem;
@@ -172,15 +211,24 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       int at = 0, s = 0;
       uint32_t turn = 0;
       for (; issued < total; ++issued) {
-        if (turn > 0 && !mbar_wait(&sh.empty[s], (turn - 1) & 1u)) {
+        if (turn > 0 && !(mbar_wait(&sh.empty[s], (turn - 1) & 1u))) {
           sh.dead = 1;
           break;
         }
         uint8_t* a = ring + s * stage_bytes;
         const int kx = (step0 + at) * kStep;
-        mbar_arrive_expect_tx(&sh.full[s], (uint32_t)stage_bytes);
-        tma_load_2d(a, &amap, &sh.full[s], kx, (int)(tile % (uint32_t)p.a_tiles) * kLanes);
-        tma_load_2d(a + kABytes, &bmap, &sh.full[s], kx, (int)(tile / (uint32_t)p.a_tiles) * p.cols);
+        const int ay = (int)(tile % (uint32_t)p.a_tiles) * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
+        const int by = (int)(tile / (uint32_t)p.a_tiles) * p.cols + (kPair ? (int)rank * b_rows : 0);
+        if (kPair) {  // (the first CTA's barrier counts both CTAs' copies)
+          const uint32_t bar = mapa_u32(smem_u32(&sh.full[s]), 0);
+          if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2u * (uint32_t)stage_bytes);
+          tma_load_2d_pair(a, &amap, bar, kx, ay);
+          tma_load_2d_pair(a + kABytes, &bmap, bar, kx, by);
+        } else {
+          mbar_arrive_expect_tx(&sh.full[s], (uint32_t)stage_bytes);
+          tma_load_2d(a, &amap, &sh.full[s], kx, ay);
+          tma_load_2d(a + kABytes, &bmap, &sh.full[s], kx, by);
+        }
         if (++at == steps) {
           at = 0;
           tile += tile_step;
@@ -191,13 +239,18 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
         }
       }
     }
-    if (warp == kIssuer && lane == 0) {
-      const uint32_t idesc = idesc_e4m3_f32(kLanes, p.cols);
+    if (warp == kIssuer && lane == 0 && (!kPair || rank == 0)) {
+      const uint32_t idesc = idesc_e4m3_f32(kPair ? 2 * kLanes : kLanes, p.cols);
       int s = 0;
       uint32_t turn = 0;
       for (int q = 0; q < total; ++q) {
-        const int b = q & 1;
-        if ((q > 1 && !mbar_wait(&sh.sum_empty[b], (uint32_t)((q >> 1) - 1) & 1u)) || !mbar_wait(&sh.full[s], turn & 1u)) {
+        const int b = q % kSums;
+        bool ok = true;
+        if (q >= kSums) {
+          const uint32_t parity = (uint32_t)(q / kSums - 1) & 1u;
+          ok = mbar_wait(&sh.sum_empty[b], parity);
+        }
+        if (!ok || !(mbar_wait(&sh.full[s], turn & 1u))) {
           sh.dead = 1;
           break;
         }
@@ -205,14 +258,50 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
         uint64_t ad = smem_desc(smem_u32(ring + s * stage_bytes), 16, 1024, 2);
         uint64_t bd = smem_desc(smem_u32(ring + s * stage_bytes + kABytes), 16, 1024, 2);
 #pragma unroll
-        for (int i = 0; i < kStep / 32; ++i, ad += 2, bd += 2) umma_e4m3(tmem + b * NT, ad, bd, idesc, i > 0);
-        umma_commit(&sh.empty[s]);
-        umma_commit(&sh.sum_full[b]);
+        for (int i = 0; i < kStep / 32; ++i, ad += 2, bd += 2) {
+          if (kPair) umma_e4m3_pair(tmem + b * NT, ad, bd, idesc, i > 0);
+          else umma_e4m3(tmem + b * NT, ad, bd, idesc, i > 0);
+        }
+        if (kPair) {
+          umma_commit_pair(&sh.empty[s]);
+          umma_commit_pair(&sh.sum_full[b]);
+        } else {
+          umma_commit(&sh.empty[s]);
+          umma_commit(&sh.sum_full[b]);
+        }
         if (++s == p.stages) {
           s = 0;
           ++turn;
         }
       }
+    }
+    if (warp == kScaler) {  // the scales of a step: x's rows', and those of the tile's blocks of w
+      uint32_t tile = tile0;
+      int at = 0;
+      for (int q = 0; q < total; ++q) {
+        const int slot = q % kScaleSlots;
+        if (q >= kScaleSlots && !__all_sync(0xffffffffu, mbar_wait(&sh.scale_empty[slot], (uint32_t)(q / kScaleSlots - 1) & 1u))) {
+          sh.dead = 1;
+          break;
+        }
+        const int ta = (int)(tile % (uint32_t)p.a_tiles), tb = (int)(tile / (uint32_t)p.a_tiles), b = step0 + at;
+        const int64_t r0 = kTurned ? 0 : (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
+#pragma unroll
+        for (int i = 0; i < kRows / 32; ++i) {
+          const int64_t r = r0 + i * 32 + lane;
+          copy_async4(&x_scale[slot][i * 32 + lane], r < p.m ? p.sx + r * p.steps + b : p.sx, r < p.m);
+        }
+        if (lane < 2) {
+          const int block = kTurned ? ta : min((int)(((int64_t)tb * p.cols + lane * 128) / 128), (p.n - 1) / 128);
+          copy_async4(&w_scale[slot][lane], p.sw + (int64_t)block * p.steps + b, true);
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.scale_full[slot])) : "memory");
+        if (++at == steps) {
+          at = 0;
+          tile += tile_step;
+        }
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
     __syncwarp();
   } else {
@@ -220,105 +309,74 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;  // of the tile's columns; the lane's row of A
     const int mine = kTurned ? min(max(p.cols - half * 128, 0), kOwn) : kOwn;
     const uint32_t at_tmem = tmem + ((uint32_t)(warp & 3) << 21) + half * 128;
+    const uint32_t free_sum = kPair ? mapa_u32(smem_u32(&sh.sum_empty[0]), 0) : 0;
     uint64_t acc[kOwn / 2];
 #pragma unroll
     for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
-    // Column scales (w's lanes): of kScaleSteps steps together, a column a thread.
-    float ahead[kScaleSteps];
-    int ahead_at = 0;
-    const float *ahead_x = p.sx + (int64_t)threadIdx.x * p.steps + step0, *ahead_w = p.sw + (int64_t)tile0 * p.steps + step0;
-    auto fetch = [&](int count) {
-#pragma unroll
-      for (int i = 0; i < kScaleSteps; ++i) {
-        ahead[i] = 0.f;
-        if (i >= count) continue;
-        if ((int)threadIdx.x < p.m) ahead[i] = __ldg(ahead_x + ahead_at) * __ldg(ahead_w + ahead_at);
-        if (++ahead_at == steps) {  // (one column of tiles: the next is the next of w's rows)
-          ahead_at = 0;
-          ahead_w += (int64_t)tile_step * p.steps;
-        }
-      }
-    };
-    // The lane's scale (x's lanes), a step ahead.
-    auto lane_scale = [&](int tile, int b) {
-      const int64_t r = (int64_t)(tile % p.a_tiles) * kLanes + row;
-      const int nb = min((int)(((int64_t)(tile / p.a_tiles) * p.cols + half * 128) / 128), (p.n - 1) / 128);
-      return r < p.m ? __ldg(p.sx + r * p.steps + b) * __ldg(p.sw + (int64_t)nb * p.steps + b) : 0.f;
-    };
-    if (kTurned) fetch(total);
     int tile = (int)tile0, at = 0;
-    float next = 0.f;
-    if (!kTurned && total > 0) next = lane_scale(tile, step0);
 #pragma unroll 1
     for (int q = 0; q < total; ++q) {
-      const int b = q & 1;
-      const float* columns = nullptr;
-      uint64_t by = 0;
-      if (kTurned) {
-        const int part = q / kScaleSteps;
-        if (q % kScaleSteps == 0) {
-          if ((int)threadIdx.x < NT) {
-#pragma unroll
-            for (int i = 0; i < kScaleSteps; ++i) scale[part & 1][i][threadIdx.x] = ahead[i];
-          }
-          asm volatile("bar.sync 1, %0;" ::"n"(kAdders) : "memory");
-          fetch(total - q - kScaleSteps);
-        }
-        columns = &scale[part & 1][q % kScaleSteps][half * 128];
-      } else {
-        by = pair2(next, next);
-        const bool more = at + 1 < steps;
-        if (q + 1 < total) next = lane_scale(more ? tile : tile + (int)tile_step, step0 + (more ? at + 1 : 0));
-      }
-      bool good = mbar_wait(&sh.sum_full[b], (uint32_t)(q >> 1) & 1u);
-      good = __all_sync(0xffffffffu, good);
-      if (!good) {
+      const int b = q % kSums, slot = q % kScaleSlots;
+      bool good = mbar_wait(&sh.scale_full[slot], (uint32_t)(q / kScaleSlots) & 1u);
+      const float sw = w_scale[slot][kTurned ? 0 : half];
+      const float own = kTurned ? sw : sw * x_scale[slot][row];
+      const uint64_t by = pair2(own, own);
+      const uint32_t parity = (uint32_t)(q / kSums) & 1u;
+      good = (mbar_wait(&sh.sum_full[b], parity)) && good;
+      if (!__all_sync(0xffffffffu, good)) {
         sh.dead = 1;
-        // (the others of this warp's barrier must not wait for it)
-        if (kTurned)
-          for (int c = (q / kScaleSteps + 1) * kScaleSteps; c < total; c += kScaleSteps) asm volatile("bar.sync 1, %0;" ::"n"(kAdders) : "memory");
         break;
       }
       tc_fence_after();
-      uint32_t d[2][16];
-      tmem_ld16(at_tmem + b * NT, d[0]);
+      uint32_t d[2][32];
+      tmem_ld32(at_tmem + b * NT, d[0]);
 #pragma unroll
-      for (int c = 0; c < kOwn / 16; ++c) {
-        if (c * 16 >= mine) break;
-        tmem_ld_wait16(d[c & 1]);
-        if ((c + 1) * 16 < mine && c + 1 < kOwn / 16) {
-          tmem_ld16(at_tmem + b * NT + (c + 1) * 16, d[(c + 1) & 1]);
+      for (int c = 0; c < kOwn / 32; ++c) {
+        if (c * 32 >= mine) break;
+        tmem_ld_wait32(d[c & 1]);
+        if ((c + 1) * 32 < mine && c + 1 < kOwn / 32) {
+          tmem_ld32(at_tmem + b * NT + (c + 1) * 32, d[(c + 1) & 1]);
         } else {
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(&sh.sum_empty[b]);
+          if (lane == 0) {
+            if (kPair) mbar_arrive_cluster(free_sum + 8 * b);
+            else mbar_arrive(&sh.sum_empty[b]);
+          }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 16; ++i) {
           uint64_t f = by;
-          if (kTurned) f = reinterpret_cast<const uint64_t*>(columns)[c * 8 + i];
+          if (kTurned) f = mul_pair(by, reinterpret_cast<const uint64_t*>(&x_scale[slot][half * 128])[c * 16 + i]);
           const uint64_t v = (uint64_t)d[c & 1][2 * i + 1] << 32 | d[c & 1][2 * i];
-          acc[c * 8 + i] = fma_pair(v, f, acc[c * 8 + i]);
+          acc[c * 16 + i] = fma_pair(v, f, acc[c * 16 + i]);
         }
       }
-      if (mine == 0) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.sum_empty[b]);
+      __syncwarp();  // (the step's scales have been read)
+      if (lane == 0) {
+        if (mine == 0) mbar_arrive(&sh.sum_empty[b]);
+        mbar_arrive(&sh.scale_empty[slot]);
       }
       if (++at < steps) continue;
       // The end of a tile.
       at = 0;
-      const int64_t a0 = (int64_t)(tile % p.a_tiles) * kLanes + row, b0 = (int64_t)(tile / p.a_tiles) * p.cols + half * 128;
+      const int64_t a0 = (int64_t)(tile % p.a_tiles) * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0) + row;
+      const int64_t b0 = (int64_t)(tile / p.a_tiles) * p.cols + half * 128;
       tile += (int)tile_step;
-      if (p.split > 1) {  // (the ring is free: every copy has been read)
-        float* part = reinterpret_cast<float*>(ring) + half * 128 * (kLanes + 1) + row;
+      if (!kPair && p.split > 1) {  // (the ring is free: every copy has been read)
+        float* part = reinterpret_cast<float*>(ring) + (kTurned ? half * 128 * kLanes + row : row * kPartRow<NT> + half * 128);
 #pragma unroll
-        for (int i = 0; i < kOwn / 2; ++i) {
-          if (2 * i >= mine) break;
-          float u, v;
-          unpair2(acc[i], u, v);
-          part[2 * i * (kLanes + 1)] = u;
-          part[(2 * i + 1) * (kLanes + 1)] = v;
+        for (int i = 0; i < kOwn / 4; ++i) {
+          if (4 * i >= mine) break;
+          float v[4];
+          unpair2(acc[2 * i], v[0], v[1]);
+          unpair2(acc[2 * i + 1], v[2], v[3]);
+          if (kTurned) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[(4 * i + j) * kLanes] = v[j];
+          } else {
+            reinterpret_cast<float4*>(part)[i] = make_float4(v[0], v[1], v[2], v[3]);
+          }
         }
         break;
       }
@@ -372,38 +430,59 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (p.split > 1) {  // the parts, in order of k, by the CTA whose columns they are
+  if (!kPair && p.split > 1) {  // the parts, in order of k, by the CTA whose columns they are
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    const int c0 = p.cols * (int)rank / p.split, c1 = p.cols * (int)(rank + 1) / p.split, width = c1 - c0;
+    // Of a CTA: some of w's lanes' columns, or of x's lanes.  Four sums at once, of every CTA together.
+    const int lines = kTurned ? p.cols : kLanes, line = kTurned ? kLanes : NT, pitch = kTurned ? kLanes : kPartRow<NT>;
+    const int l0 = lines * (int)rank / p.split, l1 = lines * (int)(rank + 1) / p.split;
     const int64_t a0 = (int64_t)(tile0 % (uint32_t)p.a_tiles) * kLanes, b0 = (int64_t)(tile0 / (uint32_t)p.a_tiles) * p.cols;
-    for (int e = threadIdx.x; e < width * kLanes; e += kFp8Threads<NT>) {
-      const int col = c0 + (kTurned ? e / kLanes : e % width), row = kTurned ? e % kLanes : e / width;
-      const uint32_t from = smem_u32(reinterpret_cast<float*>(ring) + col * (kLanes + 1) + row);
-      float v = 0.f;
-      for (int r = 0; r < p.split; ++r) {
+    for (int e = threadIdx.x; e < (l1 - l0) * (line / 4); e += kFp8Threads<NT>) {
+      const int at = l0 + e / (line / 4), x = e % (line / 4) * 4;
+      const uint32_t from = smem_u32(reinterpret_cast<float*>(ring) + at * pitch + x);
+      float4 v[kMostSplit];
+#pragma unroll
+      for (int r = 0; r < kMostSplit; ++r) {
+        if (r >= p.split) break;
         uint32_t there;
-        float x;
         asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(from), "r"(r));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(there) : "memory");
-        v += x;
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                     : "=f"(v[r].x), "=f"(v[r].y), "=f"(v[r].z), "=f"(v[r].w) : "r"(there) : "memory");
       }
-      if (kTurned) write_one(p, b0 + col, a0 + row, v);
-      else write_one(p, a0 + row, b0 + col, v);
+      float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+      for (int r = 1; r < kMostSplit; ++r) {
+        if (r >= p.split) break;
+        sum[0] += v[r].x, sum[1] += v[r].y, sum[2] += v[r].z, sum[3] += v[r].w;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (kTurned) write_one(p, b0 + at, a0 + x + j, sum[j]);
+        else write_one(p, a0 + at, b0 + x + j, sum[j]);
+      }
     }
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   }
   if (sh.dead) {  // copies and instructions in flight end before the memory that they use is given up
     if (threadIdx.x == 0 && p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
-    for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(&sh.full[i % p.stages], (uint32_t)(i / p.stages) & 1u);
-    if (warp == kIssuer && lane == 0) {
-      umma_commit(&sh.drained);
+    if (!kPair || rank == 0)  // (which counts both CTAs' copies)
+      for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(&sh.full[i % p.stages], (uint32_t)(i / p.stages) & 1u);
+    if (warp == kIssuer && lane == 0 && (!kPair || rank == 0)) {
+      if (kPair) umma_commit_pair(&sh.drained);
+      else umma_commit(&sh.drained);
       mbar_wait(&sh.drained, 0);
     }
     __syncthreads();
   }
-  if (warp == kIssuer) tmem_dealloc(tmem, kTmemCols);
+  if (kPair) {  // (the tensor cores read the other CTA's memory, and its barriers are signalled)
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  if (warp == kIssuer) {
+    if (kPair) tmem_dealloc_pair(tmem, kTmemCols);
+    else tmem_dealloc(tmem, kTmemCols);
+  }
 }
 
 int encode_rows(CUtensorMap* map, const void* base, int64_t k, int64_t rows, int64_t stride, int box_rows) {
@@ -423,29 +502,33 @@ struct Fp8Operands {
   int64_t x_stride, w_stride, k;
 };
 
-template <int NT, bool kTurned>
+template <int NT, bool kTurned, bool kPair = false>
 int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
-  auto k = fp8_kernel<NT, kTurned>;
-  constexpr int room = kRoom - (kTurned ? 2 * kScaleSteps * NT * 4 : (NT > 128 ? 256 : 128) * kStageWords * 4) - 512;
+  auto k = fp8_kernel<NT, kTurned, kPair>;
+  constexpr int fixed = kScaleSlots * 4 * (kTurned ? NT : kLanes) + (kTurned ? 0 : kAdders<NT> * kStageWords * 4) + 1024;
+  constexpr int room = kRoom - fixed;
   if (int rc = ensure_smem(k, room + 1024, done)) return rc;
   p.cols = kTurned ? (p.m + 15) / 16 * 16 : NT;
-  const int64_t a_tiles = ((int64_t)(kTurned ? p.n : p.m) + kLanes - 1) / kLanes;
+  const int lanes = kPair ? 2 * kLanes : kLanes, b_rows = kPair ? p.cols / 2 : p.cols;
+  const int64_t a_tiles = ((int64_t)(kTurned ? p.n : p.m) + lanes - 1) / lanes;
   const int64_t b_tiles = ((int64_t)(kTurned ? p.m : p.n) + p.cols - 1) / p.cols, tiles = a_tiles * b_tiles;
   if (tiles > 0x7fffffff / p.steps - 1) return set_error(RGD_ERR_UNSUPPORTED, "%s: too many tiles", fn);
   p.a_tiles = (int32_t)a_tiles;
   p.tiles = (int32_t)tiles;
-  const int stage = kABytes + p.cols * kStep;
+  const int stage = kABytes + b_rows * kStep;
   p.stages = std::min(kMostStages, room / stage);
-  // Too few tiles for the SMs: clusters of up to 8 CTAs share one, each with two steps at least.
+  // Too few tiles for the SMs: clusters of 2, 4 or 8 CTAs share one, each with two steps at least.
   constexpr int sms = 152;
-  p.split = (int)std::max<int64_t>(1, std::min<int64_t>({8, sms / tiles, p.steps / 2}));
-  const int grid = p.split > 1 ? p.tiles * p.split : (int)std::min<int64_t>(tiles, sms);
+  p.split = 1;
+  while (!kPair && p.split < kMostSplit && tiles * p.split * 2 <= sms && p.steps >= p.split * 4) p.split *= 2;
+  const int64_t ctas = kPair ? 2 * tiles : tiles;
+  const int grid = p.split > 1 ? p.tiles * p.split : (int)std::min<int64_t>(ctas, sms);
   CUtensorMap amap, bmap;
   const uint8_t *a = kTurned ? o.w : o.x, *b = kTurned ? o.x : o.w;
   const int64_t as = kTurned ? o.w_stride : o.x_stride, bs = kTurned ? o.x_stride : o.w_stride;
   if (int rc = encode_rows(&amap, a, o.k, kTurned ? p.n : p.m, as, kLanes)) return rc;
-  if (int rc = encode_rows(&bmap, b, o.k, kTurned ? p.m : p.n, bs, p.cols)) return rc;
+  if (int rc = encode_rows(&bmap, b, o.k, kTurned ? p.m : p.n, bs, b_rows)) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(kFp8Threads<NT>);
@@ -455,9 +538,9 @@ int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t 
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim = {(unsigned)p.split, 1, 1};
+  attr[1].val.clusterDim = {(unsigned)(kPair ? 2 : p.split), 1, 1};
   cfg.attrs = attr;
-  cfg.numAttrs = p.split > 1 ? 2 : 1;
+  cfg.numAttrs = kPair || p.split > 1 ? 2 : 1;
   cudaError_t e = cudaLaunchKernelEx(&cfg, k, p, amap, bmap);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "fp8 product launch");
@@ -501,6 +584,6 @@ extern "C" int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x,
   if (m <= 64) return launch_fp8<64, true>(fn, p, o, st);
   if (m <= 128) return launch_fp8<128, true>(fn, p, o, st);
   if (m <= 256) return launch_fp8<256, true>(fn, p, o, st);
-  if (((int64_t)m + 127) / 128 * (((int64_t)n + 255) / 256) >= 152) return launch_fp8<256, false>(fn, p, o, st);
+  if (((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256) >= 76) return launch_fp8<256, false, true>(fn, p, o, st);
   return launch_fp8<128, false>(fn, p, o, st);
 }
