@@ -29,7 +29,9 @@ constexpr int kLanes = 128;              // rows of A a CTA's tile
 constexpr int kStep = 128;               // values of k that share a scale: one step
 constexpr int kABytes = kLanes * kStep;  // of a stage
 constexpr int kMostStages = 12;
-constexpr int kScaleSlots = 8;  // steps whose scales are on their way or in use
+constexpr int kScaleSteps = 4;  // steps whose scales are fetched together: a slot
+constexpr int kScaleSlots = 4;  // on their way or in use
+constexpr int kScaleAhead = 2;  // on their way
 constexpr int kMostSums = 8;    // steps whose sums are
 constexpr int kRoom = 227 * 1024 - 1024;
 
@@ -143,8 +145,8 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   constexpr int kRows = kTurned ? NT : kLanes;  // x's rows of a tile
   extern __shared__ uint8_t raw[];
   __shared__ Fp8Shared sh;
-  __shared__ __align__(16) float x_scale[kScaleSlots][kRows];
-  __shared__ float w_scale[kScaleSlots][2];
+  __shared__ __align__(16) float x_scale[kScaleSlots * kScaleSteps][kRows];
+  __shared__ float w_scale[kScaleSlots * kScaleSteps][2];
   __shared__ uint32_t stage[kTurned ? 1 : kAdders<NT> * kStageWords];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -181,7 +183,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       mbar_init(&sh.sum_empty[i], kAdders<NT> / 32 * (kPair ? 2 : 1));
     }
     for (int i = 0; i < kScaleSlots; ++i) {
-      mbar_init(&sh.scale_full[i], 32);
+      mbar_init(&sh.scale_full[i], 1);
       mbar_init(&sh.scale_empty[i], kAdders<NT> / 32);
     }
     mbar_init(&sh.drained, 1);
@@ -208,17 +210,20 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     if (NT > 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if (warp == kProducer && lane == 0) {
       uint32_t tile = tile0;
-      int at = 0, s = 0;
+      int at = 0, s = 0, ay = 0, by = 0;
       uint32_t turn = 0;
+#pragma unroll 1
       for (; issued < total; ++issued) {
-        if (turn > 0 && !(mbar_wait(&sh.empty[s], (turn - 1) & 1u))) {
+        if (at == 0) {  // (a division takes longer than a step has)
+          ay = (int)(tile % (uint32_t)p.a_tiles) * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
+          by = (int)(tile / (uint32_t)p.a_tiles) * p.cols + (kPair ? (int)rank * b_rows : 0);
+        }
+        if (turn > 0 && !mbar_wait_soon(&sh.empty[s], (turn - 1) & 1u)) {
           sh.dead = 1;
           break;
         }
         uint8_t* a = ring + s * stage_bytes;
         const int kx = (step0 + at) * kStep;
-        const int ay = (int)(tile % (uint32_t)p.a_tiles) * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
-        const int by = (int)(tile / (uint32_t)p.a_tiles) * p.cols + (kPair ? (int)rank * b_rows : 0);
         if (kPair) {  // (the first CTA's barrier counts both CTAs' copies)
           const uint32_t bar = mapa_u32(smem_u32(&sh.full[s]), 0);
           if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2u * (uint32_t)stage_bytes);
@@ -248,9 +253,9 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
         bool ok = true;
         if (q >= kSums) {
           const uint32_t parity = (uint32_t)(q / kSums - 1) & 1u;
-          ok = mbar_wait(&sh.sum_empty[b], parity);
+          ok = mbar_wait_soon(&sh.sum_empty[b], parity);
         }
-        if (!ok || !(mbar_wait(&sh.full[s], turn & 1u))) {
+        if (!ok || !mbar_wait_soon(&sh.full[s], turn & 1u)) {
           sh.dead = 1;
           break;
         }
@@ -275,33 +280,49 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
         }
       }
     }
-    if (warp == kScaler) {  // the scales of a step: x's rows', and those of the tile's blocks of w
+    if (warp == kScaler) {  // x's rows' scales, and those of the tile's blocks of w, of a few steps at a time
       uint32_t tile = tile0;
-      int at = 0;
-      for (int q = 0; q < total; ++q) {
-        const int slot = q % kScaleSlots;
-        if (q >= kScaleSlots && !__all_sync(0xffffffffu, mbar_wait(&sh.scale_empty[slot], (uint32_t)(q / kScaleSlots - 1) & 1u))) {
+      int at = 0, chunks = (total + kScaleSteps - 1) / kScaleSteps, c = 0, rows = 0;
+      const int64_t x_stride = (int64_t)p.steps * 32;
+      const float *x_from = p.sx, *w_from = p.sw;
+      for (; c < chunks; ++c) {
+        const int slot = c % kScaleSlots;
+        if (c >= kScaleSlots && !__all_sync(0xffffffffu, mbar_wait_soon(&sh.scale_empty[slot], (uint32_t)(c / kScaleSlots - 1) & 1u))) {
           sh.dead = 1;
           break;
         }
-        const int ta = (int)(tile % (uint32_t)p.a_tiles), tb = (int)(tile / (uint32_t)p.a_tiles), b = step0 + at;
-        const int64_t r0 = kTurned ? 0 : (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
+#pragma unroll 1
+        for (int j = 0; j < kScaleSteps && c * kScaleSteps + j < total; ++j) {
+          if (at == 0) {
+            const int ta = (int)(tile % (uint32_t)p.a_tiles), tb = (int)(tile / (uint32_t)p.a_tiles);
+            const int64_t r0 = (kTurned ? 0 : (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0)) + lane;
+            rows = (int)max(int64_t(-1), min(int64_t(kRows), p.m - r0));
+            x_from = p.sx + r0 * p.steps + step0;
+            const int block = kTurned ? ta : min((int)(((int64_t)tb * p.cols + lane * 128) / 128), (p.n - 1) / 128);
+            w_from = p.sw + (int64_t)block * p.steps + step0;
+          }
+          float* to = &x_scale[slot * kScaleSteps + j][lane];
+          const float* from = x_from;
 #pragma unroll
-        for (int i = 0; i < kRows / 32; ++i) {
-          const int64_t r = r0 + i * 32 + lane;
-          copy_async4(&x_scale[slot][i * 32 + lane], r < p.m ? p.sx + r * p.steps + b : p.sx, r < p.m);
+          for (int i = 0; i < kRows; i += 32, from += x_stride) copy_async4(to + i, i < rows ? from : p.sx, i < rows);
+          if (lane < 2) copy_async4(&w_scale[slot * kScaleSteps + j][lane], w_from, true);
+          ++x_from, ++w_from;
+          if (++at == steps) {
+            at = 0;
+            tile += tile_step;
+          }
         }
-        if (lane < 2) {
-          const int block = kTurned ? ta : min((int)(((int64_t)tb * p.cols + lane * 128) / 128), (p.n - 1) / 128);
-          copy_async4(&w_scale[slot][lane], p.sw + (int64_t)block * p.steps + b, true);
-        }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.scale_full[slot])) : "memory");
-        if (++at == steps) {
-          at = 0;
-          tile += tile_step;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (c >= kScaleAhead) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kScaleAhead) : "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.scale_full[(c - kScaleAhead) % kScaleSlots]);
         }
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncwarp();
+      if (lane == 0)
+        for (int i = max(0, c - kScaleAhead); i < c; ++i) mbar_arrive(&sh.scale_full[i % kScaleSlots]);
     }
     __syncwarp();
   } else {
@@ -316,13 +337,14 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     int tile = (int)tile0, at = 0;
 #pragma unroll 1
     for (int q = 0; q < total; ++q) {
-      const int b = q % kSums, slot = q % kScaleSlots;
-      bool good = mbar_wait(&sh.scale_full[slot], (uint32_t)(q / kScaleSlots) & 1u);
+      const int b = q % kSums, slot = q % (kScaleSlots * kScaleSteps), chunk = q / kScaleSteps;
+      bool good = true;
+      if (q % kScaleSteps == 0) good = mbar_wait_soon(&sh.scale_full[chunk % kScaleSlots], (uint32_t)(chunk / kScaleSlots) & 1u);
       const float sw = w_scale[slot][kTurned ? 0 : half];
       const float own = kTurned ? sw : sw * x_scale[slot][row];
       const uint64_t by = pair2(own, own);
       const uint32_t parity = (uint32_t)(q / kSums) & 1u;
-      good = (mbar_wait(&sh.sum_full[b], parity)) && good;
+      good = mbar_wait_soon(&sh.sum_full[b], parity) && good;
       if (!__all_sync(0xffffffffu, good)) {
         sh.dead = 1;
         break;
@@ -352,10 +374,12 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
           acc[c * 16 + i] = fma_pair(v, f, acc[c * 16 + i]);
         }
       }
-      __syncwarp();  // (the step's scales have been read)
-      if (lane == 0) {
-        if (mine == 0) mbar_arrive(&sh.sum_empty[b]);
-        mbar_arrive(&sh.scale_empty[slot]);
+      if (mine == 0 || q % kScaleSteps == kScaleSteps - 1) {
+        __syncwarp();  // (the steps' scales have been read)
+        if (lane == 0) {
+          if (mine == 0) mbar_arrive(&sh.sum_empty[b]);
+          if (q % kScaleSteps == kScaleSteps - 1) mbar_arrive(&sh.scale_empty[chunk % kScaleSlots]);
+        }
       }
       if (++at < steps) continue;
       // The end of a tile.
@@ -506,7 +530,7 @@ template <int NT, bool kTurned, bool kPair = false>
 int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
   auto k = fp8_kernel<NT, kTurned, kPair>;
-  constexpr int fixed = kScaleSlots * 4 * (kTurned ? NT : kLanes) + (kTurned ? 0 : kAdders<NT> * kStageWords * 4) + 1024;
+  constexpr int fixed = kScaleSlots * kScaleSteps * 4 * (kTurned ? NT : kLanes) + (kTurned ? 0 : kAdders<NT> * kStageWords * 4) + 1024;
   constexpr int room = kRoom - fixed;
   if (int rc = ensure_smem(k, room + 1024, done)) return rc;
   p.cols = kTurned ? (p.m + 15) / 16 * 16 : NT;

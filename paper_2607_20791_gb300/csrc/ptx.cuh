@@ -83,6 +83,20 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
   }
 }
 
+// As mbar_wait, where the phase is often a few hundred cycles away: the clock, which takes a
+// microsecond to read, is not looked at before the 256th try.
+__device__ __forceinline__ bool mbar_wait_soon(uint64_t* bar, uint32_t parity) {
+  uint64_t t0 = 0;
+#pragma unroll 1
+  for (uint32_t i = 0;; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (i >= 256 && (i & 63u) == 0) {
+      const uint64_t t = globaltimer_ns();
+      if (t0 == 0) t0 = t;
+      else if (t - t0 > kWaitLimitNs) return false;
+    }
+  }
+}
 // An arrival at a barrier of any CTA of the cluster (a shared::cluster address).  It orders
 // nothing in memory between the CTAs: for what is handed over in TMEM.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
