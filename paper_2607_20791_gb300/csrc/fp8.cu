@@ -42,7 +42,7 @@ struct Fp8Params {
   uint8_t* y;
   int64_t y_stride;  // elements
   int32_t out_f32, vectors;
-  int32_t a_tiles, tiles, split;  // tile t: A's tile t % a_tiles, B's t / a_tiles
+  int32_t a_tiles, b_tiles, tiles, band, split;
   int32_t cols;                   // columns of a tile: the instructions' N
   int32_t stages;
   int32_t* dev_status;
@@ -67,6 +67,14 @@ __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
   uint64_t r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
+}
+
+// Tile t: `band` of A's tiles by all of B's, then the next band: what the SMs work on at a time
+// are few of either.
+__device__ __forceinline__ void tile_at(const Fp8Params& p, int t, int& ta, int& tb) {
+  const int first = t / (p.band * p.b_tiles) * p.band, high = min(p.band, p.a_tiles - first), r = t - first * p.b_tiles;
+  ta = first + r % high;
+  tb = r / high;
 }
 
 __device__ __forceinline__ void put(uint8_t* to, int f32, float v) {
@@ -115,6 +123,17 @@ __device__ __forceinline__ void write_rows(const Fp8Params& p, const uint32_t* w
 constexpr int kMostSplit = 8;  // CTAs that share a tile
 template <int NT>
 constexpr int kPartRow = NT + 4;  // floats of a lane's part (lanes on different banks)
+constexpr int kBox = 4096;  // 32 rows of 128 bytes
+// The whole warp: a box that it has filled goes to y at column x and row y0, as far as y has them.
+__device__ __forceinline__ void send_box(const Fp8Params& p, const CUtensorMap& map, const uint8_t* box, int x, int y0, int lane) {
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    if (y0 < p.m && x < p.n) tma_store_2d(&map, box, x, y0);
+    bulk_commit();
+  }
+}
+
 template <int NT>
 constexpr int kAdders = NT > 128 ? 256 : 128;  // threads that add up
 template <int NT>
@@ -136,7 +155,8 @@ __device__ __forceinline__ void copy_async4(float* dst, const float* src, bool o
 // 32 by each of two), and the tensor cores read it from both CTAs' memory.
 template <int NT, bool kTurned, bool kPair>
 __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
-    fp8_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap) {
+    fp8_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
+               const __grid_constant__ CUtensorMap ymap) {
   static_assert(!kPair || (NT == 256 && !kTurned), "");
   constexpr int kOwn = NT > 128 ? 128 : NT;  // columns of a thread
   constexpr int kProducer = kAdders<NT> / 32, kIssuer = kProducer + 1, kScaler = kProducer + 2;
@@ -147,8 +167,9 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   __shared__ Fp8Shared sh;
   __shared__ __align__(16) float x_scale[kScaleSlots * kScaleSteps][kRows];
   __shared__ float w_scale[kScaleSlots * kScaleSteps][2];
-  __shared__ uint32_t stage[kTurned ? 1 : kAdders<NT> * kStageWords];
+  __shared__ uint32_t stage[kTurned || kPair ? 1 : kAdders<NT> * kStageWords];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* out = ring + (kPair ? p.stages * (kABytes + 128 * kStep) : 0);  // boxes on their way to y
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int b_rows = kPair ? p.cols / 2 : p.cols;  // of B that this CTA copies
   const int stage_bytes = kABytes + b_rows * kStep;
@@ -215,8 +236,10 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
 #pragma unroll 1
       for (; issued < total; ++issued) {
         if (at == 0) {  // (a division takes longer than a step has)
-          ay = (int)(tile % (uint32_t)p.a_tiles) * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
-          by = (int)(tile / (uint32_t)p.a_tiles) * p.cols + (kPair ? (int)rank * b_rows : 0);
+          int ta, tb;
+          tile_at(p, (int)tile, ta, tb);
+          ay = ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
+          by = tb * p.cols + (kPair ? (int)rank * b_rows : 0);
         }
         if (turn > 0 && !mbar_wait_soon(&sh.empty[s], (turn - 1) & 1u)) {
           sh.dead = 1;
@@ -248,31 +271,27 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       const uint32_t idesc = idesc_e4m3_f32(kPair ? 2 * kLanes : kLanes, p.cols);
       int s = 0;
       uint32_t turn = 0;
+#pragma unroll 1
       for (int q = 0; q < total; ++q) {
         const int b = q % kSums;
-        bool ok = true;
-        if (q >= kSums) {
-          const uint32_t parity = (uint32_t)(q / kSums - 1) & 1u;
-          ok = mbar_wait_soon(&sh.sum_empty[b], parity);
-        }
-        if (!ok || !mbar_wait_soon(&sh.full[s], turn & 1u)) {
+        if ((q >= kSums && !mbar_wait_soon(&sh.sum_empty[b], (uint32_t)(q / kSums - 1) & 1u)) || !mbar_wait_soon(&sh.full[s], turn & 1u)) {
           sh.dead = 1;
           break;
         }
         tc_fence_after();
-        uint64_t ad = smem_desc(smem_u32(ring + s * stage_bytes), 16, 1024, 2);
-        uint64_t bd = smem_desc(smem_u32(ring + s * stage_bytes + kABytes), 16, 1024, 2);
+        const uint64_t ad = smem_desc(smem_u32(ring + s * stage_bytes), 16, 1024, 2);
+        const uint64_t bd = smem_desc(smem_u32(ring + s * stage_bytes + kABytes), 16, 1024, 2);
 #pragma unroll
-        for (int i = 0; i < kStep / 32; ++i, ad += 2, bd += 2) {
-          if (kPair) umma_e4m3_pair(tmem + b * NT, ad, bd, idesc, i > 0);
-          else umma_e4m3(tmem + b * NT, ad, bd, idesc, i > 0);
+        for (int i = 0; i < kStep / 32; ++i) {
+          if (kPair) umma_e4m3_pair(tmem + b * NT, ad + 2 * i, bd + 2 * i, idesc, i > 0);
+          else umma_e4m3(tmem + b * NT, ad + 2 * i, bd + 2 * i, idesc, i > 0);
         }
         if (kPair) {
-          umma_commit_pair(&sh.empty[s]);
           umma_commit_pair(&sh.sum_full[b]);
+          umma_commit_pair(&sh.empty[s]);
         } else {
-          umma_commit(&sh.empty[s]);
           umma_commit(&sh.sum_full[b]);
+          umma_commit(&sh.empty[s]);
         }
         if (++s == p.stages) {
           s = 0;
@@ -294,7 +313,8 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
 #pragma unroll 1
         for (int j = 0; j < kScaleSteps && c * kScaleSteps + j < total; ++j) {
           if (at == 0) {
-            const int ta = (int)(tile % (uint32_t)p.a_tiles), tb = (int)(tile / (uint32_t)p.a_tiles);
+            int ta, tb;
+            tile_at(p, (int)tile, ta, tb);
             const int64_t r0 = (kTurned ? 0 : (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0)) + lane;
             rows = (int)max(int64_t(-1), min(int64_t(kRows), p.m - r0));
             x_from = p.sx + r0 * p.steps + step0;
@@ -374,18 +394,17 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
           acc[c * 16 + i] = fma_pair(v, f, acc[c * 16 + i]);
         }
       }
-      if (mine == 0 || q % kScaleSteps == kScaleSteps - 1) {
+      if (q % kScaleSteps == kScaleSteps - 1) {
         __syncwarp();  // (the steps' scales have been read)
-        if (lane == 0) {
-          if (mine == 0) mbar_arrive(&sh.sum_empty[b]);
-          if (q % kScaleSteps == kScaleSteps - 1) mbar_arrive(&sh.scale_empty[chunk % kScaleSlots]);
-        }
+        if (lane == 0) mbar_arrive(&sh.scale_empty[chunk % kScaleSlots]);
       }
       if (++at < steps) continue;
       // The end of a tile.
       at = 0;
-      const int64_t a0 = (int64_t)(tile % p.a_tiles) * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0) + row;
-      const int64_t b0 = (int64_t)(tile / p.a_tiles) * p.cols + half * 128;
+      int ta, tb;
+      tile_at(p, tile, ta, tb);
+      const int64_t a0 = (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0) + row;
+      const int64_t b0 = (int64_t)tb * p.cols + half * 128;
       tile += (int)tile_step;
       if (!kPair && p.split > 1) {  // (the ring is free: every copy has been read)
         float* part = reinterpret_cast<float*>(ring) + (kTurned ? half * 128 * kLanes + row : row * kPartRow<NT> + half * 128);
@@ -414,6 +433,40 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
           unpair2(acc[i], v[0], v[1]);
 #pragma unroll
           for (int j = 0; j < 2; ++j, to += p.y_stride * es) put_if(2 * i + j < count, to, p.out_f32, v[j]);
+        }
+      } else if (kPair) {
+        // 128 bytes of each of the warp's rows make a box, which TMA writes while the next is filled.
+        uint8_t* box = out + warp * kBox;
+        const int x = (int)b0, y = (int)(a0 - lane);
+        if (p.out_f32) {
+#pragma unroll
+          for (int c = 0; c < kOwn / 32; ++c) {
+            if (lane == 0) bulk_wait_read();
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float v[4];
+              unpair2(acc[c * 16 + 2 * i], v[0], v[1]);
+              unpair2(acc[c * 16 + 2 * i + 1], v[2], v[3]);
+              *reinterpret_cast<float4*>(box + lane * 128 + ((i ^ lane) & 7) * 16) = make_float4(v[0], v[1], v[2], v[3]);
+            }
+            send_box(p, ymap, box, x + c * 32, y, lane);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < kOwn / 64; ++c) {
+            if (lane == 0) bulk_wait_read();
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float v[8];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) unpair2(acc[c * 32 + 4 * i + j], v[2 * j], v[2 * j + 1]);
+              *reinterpret_cast<uint4*>(box + lane * 128 + ((i ^ lane) & 7) * 16) =
+                  make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+            }
+            send_box(p, ymap, box, x + c * 64, y, lane);
+          }
         }
       } else {
         // 64 bytes of each of the warp's rows at a time, by way of shared memory.
@@ -449,6 +502,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
 #pragma unroll
       for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
     }
+    if (kPair && lane == 0) bulk_wait();
   }
   __syncwarp();
   tc_fence_before();
@@ -460,7 +514,9 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     // Of a CTA: some of w's lanes' columns, or of x's lanes.  Four sums at once, of every CTA together.
     const int lines = kTurned ? p.cols : kLanes, line = kTurned ? kLanes : NT, pitch = kTurned ? kLanes : kPartRow<NT>;
     const int l0 = lines * (int)rank / p.split, l1 = lines * (int)(rank + 1) / p.split;
-    const int64_t a0 = (int64_t)(tile0 % (uint32_t)p.a_tiles) * kLanes, b0 = (int64_t)(tile0 / (uint32_t)p.a_tiles) * p.cols;
+    int ta, tb;
+    tile_at(p, (int)tile0, ta, tb);
+    const int64_t a0 = (int64_t)ta * kLanes, b0 = (int64_t)tb * p.cols;
     for (int e = threadIdx.x; e < (l1 - l0) * (line / 4); e += kFp8Threads<NT>) {
       const int at = l0 + e / (line / 4), x = e % (line / 4) * 4;
       const uint32_t from = smem_u32(reinterpret_cast<float*>(ring) + at * pitch + x);
@@ -509,15 +565,19 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   }
 }
 
-int encode_rows(CUtensorMap* map, const void* base, int64_t k, int64_t rows, int64_t stride, int box_rows) {
+// Boxes of 128 bytes of each of some rows, swizzled.
+int encode_boxes(CUtensorMap* map, CUtensorMapDataType type, const void* base, int64_t cols, int64_t rows, int64_t stride,
+                 int box_cols, int box_rows) {
   const auto encode = tensor_map_encoder();
   if (!encode) return set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled is unavailable");
-  const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
-  const cuuint32_t box[2] = {kStep, (cuuint32_t)box_rows}, ones[2] = {1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, ones,
-                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  const CUresult r = encode(map, type, 2, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? RGD_OK : set_error(RGD_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
+}
+int encode_rows(CUtensorMap* map, const void* base, int64_t k, int64_t rows, int64_t stride, int box_rows) {
+  return encode_boxes(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, k, rows, stride, kStep, box_rows);
 }
 
 struct Fp8Operands {
@@ -530,16 +590,19 @@ template <int NT, bool kTurned, bool kPair = false>
 int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
   auto k = fp8_kernel<NT, kTurned, kPair>;
-  constexpr int fixed = kScaleSlots * kScaleSteps * 4 * (kTurned ? NT : kLanes) + (kTurned ? 0 : kAdders<NT> * kStageWords * 4) + 1024;
-  constexpr int room = kRoom - fixed;
-  if (int rc = ensure_smem(k, room + 1024, done)) return rc;
+  constexpr int fixed = kScaleSlots * kScaleSteps * 4 * (kTurned ? NT : kLanes) + (kTurned || kPair ? 0 : kAdders<NT> * kStageWords * 4) + 1024;
+  constexpr int boxes = kPair ? kAdders<NT> / 32 * kBox : 0;
+  constexpr int room = kRoom - fixed - boxes;
+  if (int rc = ensure_smem(k, room + boxes + 1024, done)) return rc;
   p.cols = kTurned ? (p.m + 15) / 16 * 16 : NT;
   const int lanes = kPair ? 2 * kLanes : kLanes, b_rows = kPair ? p.cols / 2 : p.cols;
   const int64_t a_tiles = ((int64_t)(kTurned ? p.n : p.m) + lanes - 1) / lanes;
   const int64_t b_tiles = ((int64_t)(kTurned ? p.m : p.n) + p.cols - 1) / p.cols, tiles = a_tiles * b_tiles;
   if (tiles > 0x7fffffff / p.steps - 1) return set_error(RGD_ERR_UNSUPPORTED, "%s: too many tiles", fn);
   p.a_tiles = (int32_t)a_tiles;
+  p.b_tiles = (int32_t)b_tiles;
   p.tiles = (int32_t)tiles;
+  p.band = 8;
   const int stage = kABytes + b_rows * kStep;
   p.stages = std::min(kMostStages, room / stage);
   // Too few tiles for the SMs: clusters of 2, 4 or 8 CTAs share one, each with two steps at least.
@@ -553,10 +616,14 @@ int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t 
   const int64_t as = kTurned ? o.w_stride : o.x_stride, bs = kTurned ? o.x_stride : o.w_stride;
   if (int rc = encode_rows(&amap, a, o.k, kTurned ? p.n : p.m, as, kLanes)) return rc;
   if (int rc = encode_rows(&bmap, b, o.k, kTurned ? p.m : p.n, bs, b_rows)) return rc;
+  CUtensorMap ymap = amap;  // (read by pairs only)
+  if (kPair)
+    if (int rc = encode_boxes(&ymap, p.out_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, p.y, p.n, p.m,
+                              p.y_stride * (p.out_f32 ? 4 : 2), p.out_f32 ? 32 : 64, 32)) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(kFp8Threads<NT>);
-  cfg.dynamicSmemBytes = (size_t)p.stages * stage + 1024;
+  cfg.dynamicSmemBytes = (size_t)p.stages * stage + boxes + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -565,7 +632,7 @@ int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t 
   attr[1].val.clusterDim = {(unsigned)(kPair ? 2 : p.split), 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = kPair || p.split > 1 ? 2 : 1;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, k, p, amap, bmap);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, k, p, amap, bmap, ymap);
   if (e == cudaSuccess) e = cudaGetLastError();
   return e == cudaSuccess ? RGD_OK : cuda_error(e, "fp8 product launch");
 }
@@ -608,6 +675,6 @@ extern "C" int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x,
   if (m <= 64) return launch_fp8<64, true>(fn, p, o, st);
   if (m <= 128) return launch_fp8<128, true>(fn, p, o, st);
   if (m <= 256) return launch_fp8<256, true>(fn, p, o, st);
-  if (((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256) >= 76) return launch_fp8<256, false, true>(fn, p, o, st);
+  if (p.vectors && ((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256) >= 76) return launch_fp8<256, false, true>(fn, p, o, st);
   return launch_fp8<128, false>(fn, p, o, st);
 }
