@@ -144,6 +144,22 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t from, uint32_t (&r)[N]) {
+  if constexpr (N == 32) tmem_ld32(from, r);
+  else tmem_ld16(from, r);
+}
+// Waits for all loads; those into r and s are not read before.
+template <int N>
+__device__ __forceinline__ void tmem_load_wait(uint32_t (&r)[N], uint32_t (&s)[N]) {
+  if constexpr (N == 32) {
+    tmem_ld_wait32(r);
+    tmem_after_wait32(s);
+  } else {
+    tmem_ld_wait16(r);
+    tmem_after_wait16(s);
+  }
+}
 // 4 bytes to shared memory, without a wait; zeros if not `on`.
 __device__ __forceinline__ void copy_async4(float* dst, const float* src, bool on) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(on ? 4 : 0) : "memory");
@@ -354,6 +370,12 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     uint64_t acc[kOwn / 2];
 #pragma unroll
     for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
+    // A step's sums come in chunks of columns: two together, the next two while these are added; one by
+    // one where two tiles' worth of registers hold sums (80 x 6144 x 4096: 14.9 us so, 16.4 one by one;
+    // 8192 x 14336 x 4096: 393 us one by one, 566 two together).
+    constexpr bool kTwo = NT <= 128;
+    constexpr int kChunk = kOwn > 32 ? 32 : 16, kChunks = kOwn / kChunk;
+    const int last = (mine + kChunk - 1) / kChunk - 1;
     int tile = (int)tile0, at = 0;
 #pragma unroll 1
     for (int q = 0; q < total; ++q) {
@@ -370,28 +392,47 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
         break;
       }
       tc_fence_after();
-      uint32_t d[2][32];
-      tmem_ld32(at_tmem + b * NT, d[0]);
+      uint32_t d[2][kChunk];
+      const uint32_t from = at_tmem + b * NT;
+      auto add = [&](int c) {
 #pragma unroll
-      for (int c = 0; c < kOwn / 32; ++c) {
-        if (c * 32 >= mine) break;
-        tmem_ld_wait32(d[c & 1]);
-        if ((c + 1) * 32 < mine && c + 1 < kOwn / 32) {
-          tmem_ld32(at_tmem + b * NT + (c + 1) * 32, d[(c + 1) & 1]);
-        } else {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (kPair) mbar_arrive_cluster(free_sum + 8 * b);
-            else mbar_arrive(&sh.sum_empty[b]);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < kChunk / 2; ++i) {
           uint64_t f = by;
-          if (kTurned) f = mul_pair(by, reinterpret_cast<const uint64_t*>(&x_scale[slot][half * 128])[c * 16 + i]);
+          if (kTurned) f = mul_pair(by, reinterpret_cast<const uint64_t*>(&x_scale[slot][half * 128])[c * (kChunk / 2) + i]);
           const uint64_t v = (uint64_t)d[c & 1][2 * i + 1] << 32 | d[c & 1][2 * i];
-          acc[c * 16 + i] = fma_pair(v, f, acc[c * 16 + i]);
+          acc[c * (kChunk / 2) + i] = fma_pair(v, f, acc[c * (kChunk / 2) + i]);
+        }
+      };
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (kPair) mbar_arrive_cluster(free_sum + 8 * b);
+          else mbar_arrive(&sh.sum_empty[b]);
+        }
+      };
+      tmem_load(from, d[0]);
+      if (kTwo && last >= 1) tmem_load(from + kChunk, d[1]);
+#pragma unroll
+      for (int c = 0; c < kChunks; c += kTwo ? 2 : 1) {
+        if (c > last) break;
+        if (kTwo) {
+          tmem_load_wait(d[0], d[1]);
+          if (c + 2 < kChunks && c + 2 <= last) {
+            add(c);
+            tmem_load(from + (c + 2) * kChunk, d[0]);
+            add(c + 1);
+            if (c + 3 < kChunks && c + 3 <= last) tmem_load(from + (c + 3) * kChunk, d[1]);
+          } else {
+            release();
+            add(c);
+            if (c + 1 < kChunks && c + 1 <= last) add(c + 1);
+          }
+        } else {
+          tmem_load_wait(d[c & 1], d[c & 1]);
+          if (c + 1 < kChunks && c + 1 <= last) tmem_load(from + (c + 1) * kChunk, d[(c + 1) & 1]);
+          else release();
+          add(c);
         }
       }
       if (q % kScaleSteps == kScaleSteps - 1) {
