@@ -34,13 +34,13 @@ namespace {
 constexpr int kTopWarps = 8;
 constexpr int kTopThreads = kTopWarps * 32;
 constexpr int kTopCluster = 16;  // CTAs of a row at most
-constexpr int kList = 2048;      // tokens that are sorted together at most
-constexpr int kEnough = 512;     // tokens that the first list shall hold at least for top-p
+constexpr int kList = 2048;      // tokens that the list holds at most,
+constexpr int kSorted = 1024;    // and that are sorted together
+constexpr int kEnough = 128;     // tokens that the first list shall hold at least for top-p
 constexpr int kBins = 512;
+constexpr int kCopies = 3, kCopyPitch = kBins + 8;  // (the same bin lies on another bank in each)
 constexpr int kSampleShift = 3;  // 1 stripe of 8 is sampled
-constexpr int kOctaves = 32;     // weights below 2^-32 are 0
 constexpr int kMostRounds = 64;
-constexpr int kMargin = 4;       // bins to both sides of a sampled cut
 
 struct TopParams {
   const uint8_t* logits;
@@ -64,9 +64,11 @@ enum Next { kDone, kRange, kDraw };
 struct Order {
   int next;
   int by_count;         // the cut is at a count, not a mass
+  int list;             // the range's tokens go into the list, in case that they fit
   uint32_t from, to;    // range of keys' distances from the largest
   uint32_t last_key;    // the last kept value, and how many of it are kept (0: all)
   uint32_t of_last;
+  int pad;
   uint64_t need;        // count or mass up to the cut, the last token included
 };
 static_assert(sizeof(Order) % 8 == 0, "");
@@ -75,14 +77,17 @@ struct TopShared {
   float warp_top[kTopWarps], warp_low[kTopWarps], top[kTopCluster], low[kTopCluster];
   uint64_t warp_sum[kTopWarps], sum[kTopCluster], part_sum[kTopWarps];
   uint32_t warp_count[kTopWarps], count[kTopCluster], part_count[kTopWarps];
+  uint32_t warp_larger[kTopWarps], larger[kTopCluster];  // (of the first CTA only)
   uint64_t scan[kTopWarps];
   uint32_t lo[kBins], hi[kBins];  // sums of the weights' low 16 bits and of the rest, or counts
   uint32_t listed;                // tokens that belong into the list
   Order order;
   float theta;
   int found;
-  uint64_t value;
-  uint64_t list[kList];
+  union {
+    uint64_t list[kList];
+    uint32_t copies[kCopies][kCopyPitch];  // of the bins, for counts while there is no list
+  };
 };
 
 __device__ __forceinline__ void cluster_barrier() {
@@ -101,16 +106,54 @@ __device__ __forceinline__ void store_peer(uint32_t addr, uint64_t v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
 
-// Keys in the order of the logits; -0 and 0 have the same.
+// Keys in the order of the logits, consecutive for consecutive values of the type; -0 and 0 have
+// the same.  key_of an fp32 that is no bf16: the key of the next bf16 above.
+template <typename T>
 __device__ __forceinline__ uint32_t key_of(float l) {
-  const uint32_t u = __float_as_uint(l == 0.f ? 0.f : l);
-  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  if (sizeof(T) == 2) l = __bfloat162float(__float2bfloat16_ru(l));
+  const uint32_t u = __float_as_uint(l == 0.f ? 0.f : l), key = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return sizeof(T) == 2 ? key >> 16 : key;
 }
+template <typename T>
 __device__ __forceinline__ float of_key(uint32_t k) {
+  if (sizeof(T) == 2) return __uint_as_float((k & 0x8000u) ? (k & 0x7fffu) << 16 : (~k & 0xffffu) << 16);
   return __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
 }
-// The number of range t of 1/8 octave below the top.
-__device__ __forceinline__ int octave_bin(float octaves) { return (int)fminf(octaves * (float)(kBins / 2 / kOctaves), (float)(kBins / 2 - 1)); }
+// The key of element e of a vector that is no NaN.
+template <typename T>
+__device__ __forceinline__ uint32_t key_at(const uint4& w, int e) {
+  if (sizeof(T) == 4) return key_of<T>(elem<T>(w, e));
+  const uint32_t pair = (e >> 1) == 0 ? w.x : (e >> 1) == 1 ? w.y : (e >> 1) == 2 ? w.z : w.w;
+  const uint32_t u = (e & 1) ? pair >> 16 : pair & 0xffffu, key = u ^ ((u & 0x8000u) ? 0xffffu : 0x8000u);
+  return key == 0x7fffu ? 0x8000u : key;
+}
+
+template <typename T>
+__device__ __forceinline__ bool one_value(const uint4& w) {
+  return w.x == w.y && w.x == w.z && w.x == w.w && (sizeof(T) == 4 || w.x >> 16 == (w.x & 0xffffu));
+}
+
+// The bins of a sample, by how many octaves a weight lies below the largest: 1/32 octave each for the
+// first eight (at high temperatures nearly all tokens are there), then 1/16; the last one holds the rest.
+constexpr int kFine = kBins / 2;
+__device__ __forceinline__ int octave_bin(float octaves) {
+  return (int)fminf(octaves < 8.f ? octaves * 32.f : kFine + (octaves - 8.f) * 16.f, (float)(kBins - 1));
+}
+__device__ __forceinline__ float octaves_of(int bin) {  // where it starts
+  return bin < kFine ? (float)bin * 0.03125f : 8.f + (float)(bin - kFine) * 0.0625f;
+}
+
+// Which elements of a vector are in [from, below), as bits (NaN is nowhere).
+template <typename T>
+__device__ __forceinline__ uint32_t elements_in(const uint4& w, float from, float below) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 16 / (int)sizeof(T); ++e) {
+    const float l = elem<T>(w, e);
+    m |= l >= from && !(l >= below) ? 1u << e : 0u;
+  }
+  return m;
+}
 
 // f(vector, its number) for every vector of a lane's part that may reach `bound`.
 template <typename T, bool kAligned, typename F>
@@ -148,22 +191,69 @@ __device__ __forceinline__ void visit(const Share<T, kAligned>& v, const Kept& k
   f(kept.rest, v.whole);
 }
 
-// Sorts n = 2^i numbers in shared memory, the largest first.  The whole CTA.
-__device__ __noinline__ void sort_down(uint64_t* a, int n) {
+// Sorts the first n = 256 R numbers or fewer (a power of two from 32 on) of a list in shared memory,
+// the largest first, those from `count` on taken as 0.  The whole CTA, R numbers a thread; they
+// pass through shared memory only from warp to warp.  (All in shared memory, with a barrier a
+// step, 1024 numbers took 12 us.)
+template <int R>
+__device__ __forceinline__ void sort_numbers(uint64_t* list, int n, int count) {
+  const int first = threadIdx.x * R;
+  uint64_t v[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) v[r] = first + r < count ? list[first + r] : 0;
+#pragma unroll 1
   for (int size = 2; size <= n; size *= 2) {
-    for (int gap = size / 2; gap > 0; gap /= 2) {
+#pragma unroll 1
+    for (int gap = size / 2; gap >= 32 * R; gap /= 2) {
       __syncthreads();
-      for (int t = threadIdx.x; t < n / 2; t += kTopThreads) {
-        const int i = 2 * t - (t & (gap - 1)), j = i + gap;
-        const uint64_t x = a[i], y = a[j];
-        if ((x < y) == ((i & size) == 0)) {
-          a[i] = y;
-          a[j] = x;
+#pragma unroll
+      for (int r = 0; r < R; ++r) list[first + r] = v[r];
+      __syncthreads();
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int i = first + r;
+        const uint64_t other = i < n ? list[i ^ gap] : 0;
+        const bool larger = ((i & gap) == 0) == ((i & size) == 0);  // this place gets the larger one
+        v[r] = larger == (v[r] > other) ? v[r] : other;
+      }
+    }
+#pragma unroll 1
+    for (int gap = min(size / 2, 16 * R); gap >= R; gap /= 2) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int i = first + r;
+        const uint64_t other = __shfl_xor_sync(0xffffffffu, v[r], gap / R);
+        const bool larger = ((i & gap) == 0) == ((i & size) == 0);
+        v[r] = larger == (v[r] > other) ? v[r] : other;
+      }
+    }
+#pragma unroll
+    for (int gap = R / 2; gap > 0; gap /= 2) {
+      if (gap >= size) continue;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (r & gap) continue;
+        const bool down = ((first + r) & size) == 0;
+        const uint64_t x = v[r], y = v[r | gap];
+        if ((x < y) == down) {
+          v[r] = y;
+          v[r | gap] = x;
         }
       }
     }
   }
   __syncthreads();
+#pragma unroll
+  for (int r = 0; r < R; ++r) list[first + r] = v[r];
+  __syncthreads();
+}
+// The whole CTA; at most kSorted numbers.
+__device__ __noinline__ void sort_down(uint64_t* list, int count) {
+  int n = 32;
+  while (n < count) n *= 2;
+  if (n <= 256) sort_numbers<1>(list, n, count);
+  else if (n <= 512) sort_numbers<2>(list, n, count);
+  else sort_numbers<4>(list, n, count);
 }
 
 // Sum over the threads before this one, and over all.  The whole CTA.
@@ -196,20 +286,35 @@ __device__ __forceinline__ uint64_t share_of(float p, uint64_t total) {  // ceil
 
 // The first CTA: the first `keep` tokens of the sorted list of n are kept; draws from them and
 // writes the row's results.
+template <typename T>
 __device__ __noinline__ void finish_list(const TopParams& p, TopShared& sh, const Side& side, int row, int keep, float u) {
-  int n = 32;
-  while (n < keep) n *= 2;
-  for (int i = threadIdx.x; i < n; i += kTopThreads) {
-    uint64_t e = 0;
-    if (i < keep) {
-      const uint64_t t = sh.list[i];
-      e = t << 32 | whole_weight(side, of_key((uint32_t)(t >> 32)));  // (the complement of the index, and the weight)
+  if (threadIdx.x == 0 && p.kept_count) p.kept_count[row] = keep;
+  if (keep <= 32) {  // one warp, a token a lane: the weights of lower indices are added up as they are
+    if (threadIdx.x >= 32) return;
+    const int lane = threadIdx.x;
+    const uint64_t t = lane < keep ? sh.list[lane] : 0;
+    const uint32_t index = ~(uint32_t)t, w = lane < keep ? whole_weight(side, of_key<T>((uint32_t)(t >> 32))) : 0;
+    uint64_t before = 0, total = 0;
+    for (int i = 0; i < keep; ++i) {
+      const uint32_t other = __shfl_sync(0xffffffffu, index, i), x = __shfl_sync(0xffffffffu, w, i);
+      total += x;
+      before += other < index ? x : 0;
     }
-    __syncwarp();
-    sh.list[i] = e;
+    const uint64_t mark = (uint64_t)((double)u * (double)total);
+    if (before <= mark && mark < before + w) {
+      p.token_out[row] = (int32_t)index;
+      if (p.prob_out) p.prob_out[row] = __fdiv_rn((float)w, __ull2float_rn(total));
+    }
+    return;
   }
-  sort_down(sh.list, n);  // by index
-  const int each = (n + kTopThreads - 1) / kTopThreads, first = threadIdx.x * each;
+  for (int i = threadIdx.x; i < keep; i += kTopThreads) {
+    const uint64_t t = sh.list[i];
+    // (the complement of the index, and the weight)
+    sh.list[i] = t << 32 | whole_weight(side, of_key<T>((uint32_t)(t >> 32)));
+  }
+  __syncthreads();
+  sort_down(sh.list, keep);  // by index
+  const int each = (keep + kTopThreads - 1) / kTopThreads, first = threadIdx.x * each;
   uint64_t mine = 0, total;
   for (int i = 0; i < each; ++i)
     if (first + i < keep) mine += (uint32_t)sh.list[first + i];
@@ -225,7 +330,6 @@ __device__ __noinline__ void finish_list(const TopParams& p, TopShared& sh, cons
     }
     before += w;
   }
-  if (threadIdx.x == 0 && p.kept_count) p.kept_count[row] = keep;
 }
 
 template <typename T, bool kAligned>
@@ -343,7 +447,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
   }
   side.kexp = fminf(__fdiv_rn(1.4426950408889634f, temp), 3e38f);  // (finite: 0 times it is 0)
   side.cut = fmaxf(__fadd_rn(side.top, sh.theta), -3.4028234663852886e38f);  // (-inf is never kept)
-  const uint32_t top_key = key_of(side.top);
+  const uint32_t top_key = key_of<T>(side.top);
 
   const uint32_t list_count = peer_addr(smem_u32(&sh.listed), 0), list_at = peer_addr(smem_u32(&sh.list[0]), 0);
   // (the lanes that come together count together; a lane that has seen the list full adds no more:
@@ -357,27 +461,13 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
     if (lane == first)
       asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(at) : "r"(list_count), "r"(__popc(with)) : "memory");
     at = __shfl_sync(with, at, first) + __popc(with & ((1u << lane) - 1));
-    if (at < kList) store_peer(list_at + 8 * at, (uint64_t)key_of(l) << 32 | (uint32_t)~index);
+    if (at < kList) store_peer(list_at + 8 * at, (uint64_t)key_of<T>(l) << 32 | (uint32_t)~index);
     else full = true;
   };
-  // Adds to a bin.  Where there are many tokens, they may all be of one value: lanes of the same
-  // bin add up first then.
-  auto add_to = [&](uint32_t* bins, uint32_t b, uint32_t x) {
-    if (full) {
-      const uint32_t with = __activemask();
-      int same;
-      __match_all_sync(with, b, &same);
-      if (same) {
-        x = __reduce_add_sync(with, x);
-        if (lane == __ffs(with) - 1) atomicAdd(&bins[b], x);
-        return;
-      }
-    }
-    atomicAdd(&bins[b], x);
-  };
   // Every CTA's sum and count into every CTA.
-  auto exchange = [&](uint64_t sum, uint32_t count) {
+  auto exchange = [&](uint64_t sum, uint32_t count, uint32_t larger) {
     if (lane == 0) {
+      sh.warp_larger[warp] = larger;
       sh.warp_sum[warp] = sum;
       sh.warp_count[warp] = count;
     }
@@ -385,6 +475,8 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
     if (warp == 0) {
       const uint64_t s = warp_sum(lane < kTopWarps ? sh.warp_sum[lane] : 0);
       const uint32_t c = __reduce_add_sync(0xffffffffu, lane < kTopWarps ? sh.warp_count[lane] : 0);
+      const uint32_t l = __reduce_add_sync(0xffffffffu, lane < kTopWarps ? sh.warp_larger[lane] : 0);
+      if (lane == 0) store_peer(peer_addr(smem_u32(&sh.larger[rank]), 0), l);
       if (lane < (int)csize) {
         store_peer(peer_addr(smem_u32(&sh.sum[rank]), lane), s);
         store_peer(peer_addr(smem_u32(&sh.count[rank]), lane), c);
@@ -426,18 +518,28 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
     if (sampled) clear_bins();
     WholeSum sum;
     const float scale = side.kexp;
+    // (What few tokens need is done one token after another, in code that is there once: unrolled
+    // into the stream of vectors it took seven times as long as the sums.)
+    const typename V::Bound at_bound(bound);
     visit(v, kept, sampled ? side.cut : bound, p.stripes, lane, [&](const uint4& w, int i) {
       if (!k) add_weights<T>(w, side, typename V::Bound(side.cut), sum);
-      const bool in_sample = sampled && ((i >> 5) & ((1 << kSampleShift) - 1)) == 0;
+      if (sampled && ((i >> 5) & ((1 << kSampleShift) - 1)) == 0) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float l = elem<T>(w, e);
-        if (l >= bound) enlist(l, (uint32_t)e0 + i * E + e);
-        else if (in_sample && l >= side.cut)
-          atomicAdd(&sh.lo[octave_bin((side.top - l) * scale)], k ? 1u : whole_weight(side, l) >> 13);
+        for (int e = 0; e < E; ++e) {
+          const float l = elem<T>(w, e);
+          if (l >= side.cut && !(l >= bound))
+            atomicAdd(&sh.lo[octave_bin((side.top - l) * scale)], k ? 1u : whole_weight(side, l) >> 13);
+        }
+      }
+      if (!V::reaches(V::max_of(w, V::lowest()), at_bound)) return;
+      uint32_t m = elements_in<T>(w, bound, INFINITY);
+#pragma unroll 1
+      for (; m; m &= m - 1) {
+        const int e = __ffs(m) - 1;
+        enlist(elem<T>(w, e), (uint32_t)e0 + i * E + e);
       }
     });
-    exchange(k ? 0 : warp_sum(sum.total()), 0);
+    exchange(k ? 0 : warp_sum(sum.total()), 0, 0);
     if (rank == 0) {
       total = sum_all();
       const uint32_t listed = sh.listed;
@@ -445,16 +547,20 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
       int keep = -1;  // known to be cut within the list
       uint64_t in_list = 0, need = k ? (uint64_t)k : share_of(top_p, total);
       if (listed <= kList && bound < INFINITY) {
-        int n2 = 32;
-        while (n2 < n) n2 *= 2;
-        for (int i = n + threadIdx.x; i < n2; i += kTopThreads) sh.list[i] = 0;
-        sort_down(sh.list, n2);
+        bool within = n <= kSorted;
+        if (!k) {
+          uint64_t mine = 0;
+          for (int i = threadIdx.x; i < n; i += kTopThreads) mine += whole_weight(side, of_key<T>((uint32_t)(sh.list[i] >> 32)));
+          scan_before(sh, mine, in_list);
+          within = within && need <= in_list;
+        }
+        if (within) sort_down(sh.list, n);
         const int m = k ? min(k, n) : n;  // of S
-        const int per = (n2 + kTopThreads - 1) / kTopThreads, first = threadIdx.x * per;
+        const int per = (n + kTopThreads - 1) / kTopThreads, first = threadIdx.x * per;
         uint64_t mine = 0;
-        if (cut_mass) {
+        if (cut_mass && within) {
           for (int i = 0; i < per; ++i)
-            if (first + i < m) mine += whole_weight(side, of_key((uint32_t)(sh.list[first + i] >> 32)));
+            if (first + i < m) mine += whole_weight(side, of_key<T>((uint32_t)(sh.list[first + i] >> 32)));
           uint64_t before = scan_before(sh, mine, in_list);
           if (k) {
             total = in_list;
@@ -464,46 +570,61 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
           __syncthreads();
           for (int i = 0; i < per; ++i) {
             if (first + i >= m) break;
-            const uint32_t w = whole_weight(side, of_key((uint32_t)(sh.list[first + i] >> 32)));
+            const uint32_t w = whole_weight(side, of_key<T>((uint32_t)(sh.list[first + i] >> 32)));
             if (before < need && need <= before + w) sh.found = first + i + 1;
             before += w;
           }
           __syncthreads();
           keep = sh.found;
-        } else {
+        } else if (within) {
           keep = m;
         }
       }
       if (threadIdx.x == 0) {
         sh.order.next = keep >= 0 ? kDone : kRange;
         sh.order.by_count = k > 0;
+        sh.order.list = 0;
         sh.order.need = need;
         sh.order.from = 0;
-        sh.order.to = top_key - key_of(side.cut);
+        // (weights 33 octaves down are 0)
+        sh.order.to = top_key - key_of<T>(k ? side.cut : fmaxf(side.cut, side.top - 33.f / side.kexp));
       }
       __syncthreads();
-      if (keep < 0 && (k == 0 || bound == INFINITY) && (bound == INFINITY || listed <= kList)) {
+      if (keep < 0 && bound < INFINITY && listed <= kList && (k || need <= in_list)) {  // within a long list
+        if (threadIdx.x == 0) sh.order.to = top_key - key_of<T>(bound);
+      } else if (keep < 0 && (k == 0 || bound == INFINITY) && (bound == INFINITY || listed <= kList)) {
         // Where the cut is likely to be, from the sample: what it holds below the list stands for the rest.
-        const uint64_t mine = bin_sum(threadIdx.x, false);
+        const uint64_t b0 = bin_sum(2 * threadIdx.x, false), b1 = bin_sum(2 * threadIdx.x + 1, false);
         uint64_t all;
-        const uint64_t before = scan_before(sh, mine, all);
+        uint64_t upto = scan_before(sh, b0 + b1, all);
         const uint64_t rest = k ? 0 : total - in_list;
         // (a stripe in 8, or in as many as a share has; what of k's sample stands for is not known better)
-        const double at = k ? (double)need / (double)min(1 << kSampleShift, p.stripes)
-                            : rest ? (double)(need - in_list) / (double)rest * (double)all : 0;
-        if (mine && (double)before < at && at <= (double)(before + mine)) {
-          const float octave = 1.f / (float)(kBins / 2 / kOctaves) / side.kexp;
-          const float hi = side.top - (float)max((int)threadIdx.x - kMargin, 0) * octave;
-          const float lo = side.top - (float)(threadIdx.x + 1 + kMargin) * octave;
-          sh.order.from = top_key - key_of(fminf(hi, side.top));
-          if (lo > side.cut && threadIdx.x + 1 + kMargin < kBins / 2) sh.order.to = top_key - key_of(lo);
-          if (sh.order.from > sh.order.to) sh.order.from = 0;
+        const float at = k ? (float)need / (float)min(1 << kSampleShift, p.stripes)
+                           : rest ? (float)(need - in_list) / (float)rest * (float)all : 0.f;
+        // A sum over a sample that each token is in by chance has the variance sum w^2 (of those in it).
+        // Bins from three deviations before the cut to three behind it are searched.
+        uint64_t squares;
+        scan_before(sh, k ? b0 + b1 : (uint64_t)((float)b0 * exp2f(18.f - octaves_of(2 * threadIdx.x)) + (float)b1 * exp2f(18.f - octaves_of(2 * threadIdx.x + 1))),
+                    squares);
+        const float off = (float)all * 0.005f + 3.f * sqrtf((float)squares);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int bin = 2 * threadIdx.x + i;
+          const float before = (float)upto, after = (float)(upto += i ? b1 : b0);
+          if (before <= at - off && at - off < after)
+            sh.order.from = top_key - key_of<T>(fminf(side.top - octaves_of(bin) / side.kexp, side.top));
+          if (before < at + off && at + off <= after && bin + 1 < kBins) {
+            const float lo = side.top - octaves_of(bin + 1) / side.kexp;
+            if (lo > side.cut) sh.order.to = top_key - key_of<T>(lo);
+          }
         }
+        __syncthreads();
+        if (threadIdx.x == 0 && sh.order.from > sh.order.to) sh.order.from = 0;
       }
       publish();
       if (keep >= 0) {
         cluster_barrier();
-        finish_list(p, sh, side, row, keep, u);
+        finish_list<T>(p, sh, side, row, keep, u);
         return;
       }
       if (threadIdx.x == 0) sh.listed = 0;
@@ -523,95 +644,120 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
         return;
       }
       const uint32_t from = sh.order.from, to = sh.order.to;
-      const bool by_count = sh.order.by_count;
+      const bool by_count = sh.order.by_count, list = sh.order.list;
       int shift = 0;
       while (((to - from) >> shift) >= (uint32_t)kBins) ++shift;
-      const float in_range = of_key(top_key - to);                          // the smallest of it,
-      const float above = from ? of_key(top_key - from + 1) : INFINITY;     // and of what lies above it
+      const float in_range = of_key<T>(top_key - to);                          // the smallest of it,
+      const float above = from ? of_key<T>(top_key - from + 1) : INFINITY;     // and of what lies above it
+      // Counts of few values meet at the same places: lanes take turns over four sets of bins.
+      const bool counts = by_count || shift == 0;  // (of a value, the count tells the mass)
+      const bool apart = counts && !list;
       __syncthreads();
+      if (apart)
+        for (int i = threadIdx.x; i < kCopies * kCopyPitch; i += kTopThreads) (&sh.copies[0][0])[i] = 0;
       clear_bins();
+      uint32_t* const my_bins = apart && (lane & 3) ? sh.copies[(lane & 3) - 1] : sh.lo;
       WholeSum over;
       full = false;
       uint32_t count = 0;
       visit(v, kept, in_range, p.stripes, lane, [&](const uint4& w, int i) {
-        if (from) add_weights<T>(w, side, typename V::Bound(above), over);
+        if (from) {
+          add_weights<T>(w, side, typename V::Bound(above), over);
+          count += __popc(elements_in<T>(w, above, INFINITY));
+        }
+        auto add = [&](float l, uint32_t key, uint32_t times) {
+          const uint32_t b = (top_key - key - from) >> shift;
+          if (counts) {
+            atomicAdd(&my_bins[b], times);
+          } else {
+            const uint32_t x = whole_weight(side, l);
+            if (x & 0xffffu) atomicAdd(&sh.lo[b], (x & 0xffffu) * times);
+            if (x >> 16) atomicAdd(&sh.hi[b], (x >> 16) * times);
+          }
+        };
+        if (one_value<T>(w) && !list) {  // (as in a row of few values: they would all wait for one bin)
+          const float l = elem<T>(w, 0);
+          if (l >= in_range && !(l >= above)) add(l, key_at<T>(w, 0), E);
+          return;
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float l = elem<T>(w, e);
-          if (l >= above) {
-            ++count;
-          } else if (l >= in_range) {
-            const uint32_t b = (top_key - key_of(l) - from) >> shift;
-            if (by_count) {
-              add_to(sh.lo, b, 1);
-            } else {
-              const uint32_t x = whole_weight(side, l);
-              if (x & 0xffffu) add_to(sh.lo, b, x & 0xffffu);
-              if (x >> 16) add_to(sh.hi, b, x >> 16);
-            }
-            enlist(l, (uint32_t)e0 + i * E + e);
-          }
+          if (l >= in_range && !(l >= above)) add(l, key_at<T>(w, e), 1);
+        }
+        if (!list || full) return;
+        uint32_t m = elements_in<T>(w, in_range, above);
+#pragma unroll 1
+        for (; m; m &= m - 1) {
+          const int e = __ffs(m) - 1;
+          enlist(elem<T>(w, e), (uint32_t)e0 + i * E + e);
         }
       });
-      exchange(warp_sum(over.total()), __reduce_add_sync(0xffffffffu, count));
+      if (apart) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kBins; i += kTopThreads)
+          for (int c = 0; c < kCopies; ++c) sh.lo[i] += sh.copies[c][i];
+      }
+      exchange(warp_sum(over.total()), __reduce_add_sync(0xffffffffu, count), 0);
       if (rank == 0) {
         const uint64_t mass = sum_all();
         const uint32_t counted = count_all(), listed = sh.listed;
         const uint64_t before = by_count ? counted : mass, need = sh.order.need;
-        const uint64_t b0 = bin_sum(2 * threadIdx.x, !by_count), b1 = bin_sum(2 * threadIdx.x + 1, !by_count);
+        const int bin = 2 * threadIdx.x;
+        uint64_t b0 = bin_sum(bin, !by_count && shift > 0), b1 = bin_sum(bin + 1, !by_count && shift > 0);
+        uint64_t mass_before = 0;  // of this thread's bins, where a count's cut needs it
+        if (shift == 0 && (cut_mass || !by_count)) {
+          const uint32_t key = top_key - from - bin;
+          const uint64_t m0 = b0 ? b0 * whole_weight(side, of_key<T>(key)) : 0, m1 = b1 ? b1 * whole_weight(side, of_key<T>(key - 1)) : 0;
+          if (by_count) {
+            uint64_t all;
+            mass_before = mass + scan_before(sh, m0 + m1, all);
+          } else {
+            b0 = m0;
+            b1 = m1;
+          }
+        }
         uint64_t inside;
         uint64_t upto = before + scan_before(sh, b0 + b1, inside);
         __syncthreads();  // (every thread has read the order)
         bool cut = false;      // found, at (last_key, of_last), by this thread
         uint32_t last_key = 0, of_last = 0;
-        uint32_t kept_here = 0;  // tokens of the range
         uint64_t mass_upto = 0;  // up to the cut, known where the cut is at a count
+        // (A sampled range that misses the cut: next to it, eight times as wide.)
+        const uint32_t wider = (to - from) < 0x0fffffffu ? 8 * (to - from) + 8 : 0xffffffffu;
         if (need <= before) {
           if (threadIdx.x == 0) {
-            sh.order.from = 0;
+            sh.order.from = from > wider ? from - wider : 0;
             sh.order.to = from - 1;
           }
         } else if (need > before + inside) {  // (by a count: fewer than k tokens, if the range reaches down to the cutoff)
-          const uint32_t lowest = top_key - key_of(side.cut);
+          const uint32_t lowest = top_key - key_of<T>(side.cut);
           if (to < lowest) {
             if (threadIdx.x == 0) {
               sh.order.from = to + 1;
-              sh.order.to = lowest;
+              sh.order.to = lowest - to > wider ? to + wider : lowest;
             }
           } else if (threadIdx.x == 0) {
             sh.order.need = before + inside;  // all of them
           }
-        } else if (from == to) {  // one value
-          if (threadIdx.x == 0) {
-            const uint64_t w = whole_weight(side, in_range), unit = by_count ? 1 : w;
-            cut = true;
-            last_key = top_key - to;
-            of_last = (uint32_t)((need - before + unit - 1) / unit);
-            kept_here = of_last;
-            mass_upto = mass + of_last * w;
-          }
-        } else if (listed <= kList) {
+        } else if (list && listed <= kSorted) {
           const int n = (int)listed;
-          int n2 = 32;
-          while (n2 < n) n2 *= 2;
-          for (int i = n + threadIdx.x; i < n2; i += kTopThreads) sh.list[i] = 0;
-          sort_down(sh.list, n2);
-          const int per = (n2 + kTopThreads - 1) / kTopThreads, first = threadIdx.x * per;
+          sort_down(sh.list, n);
+          const int per = (n + kTopThreads - 1) / kTopThreads, first = threadIdx.x * per;
           uint64_t mine = 0, all;
           for (int i = 0; i < per; ++i)
-            if (first + i < n) mine += whole_weight(side, of_key((uint32_t)(sh.list[first + i] >> 32)));
+            if (first + i < n) mine += whole_weight(side, of_key<T>((uint32_t)(sh.list[first + i] >> 32)));
           uint64_t at = mass + scan_before(sh, mine, all);
           for (int i = 0; i < per; ++i) {
             const int j = first + i;
             if (j >= n) break;
-            const uint32_t key = (uint32_t)(sh.list[j] >> 32), w = whole_weight(side, of_key(key));
+            const uint32_t key = (uint32_t)(sh.list[j] >> 32), w = whole_weight(side, of_key<T>(key));
             if (by_count ? counted + j + 1 == need : at < need && need <= at + w) {
               cut = true;
               last_key = key;
               int f = j;  // the first of this value
               while (f > 0 && (uint32_t)(sh.list[f - 1] >> 32) == key) --f;
               of_last = (uint32_t)(j - f + 1);
-              kept_here = (uint32_t)j + 1;
               mass_upto = at + w;
             }
             at += w;
@@ -620,10 +766,19 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const uint64_t b = i ? b1 : b0;
-            if (upto < need && need <= upto + b) {
-              const uint32_t start = from + ((uint32_t)(2 * threadIdx.x + i) << shift);
+            if (upto < need && need <= upto + b && shift == 0) {  // one value
+              last_key = top_key - from - (bin + i);
+              const uint64_t w = whole_weight(side, of_key<T>(last_key)), unit = by_count ? 1 : w;
+              cut = true;
+              of_last = (uint32_t)((need - upto + unit - 1) / unit);
+              mass_upto = mass_before + of_last * w;
+              if (i) mass_upto += b0 * whole_weight(side, of_key<T>(last_key + 1));  // (by a count: b0 is one)
+            } else if (upto < need && need <= upto + b) {
+              const uint32_t start = from + ((uint32_t)(bin + i) << shift);
               sh.order.from = start;
               sh.order.to = min(to, start + ((1u << shift) - 1));
+              // (bf16s are few values, found within another round; a mass does not tell of how many tokens)
+              sh.order.list = sizeof(T) == 4 && (!by_count || b <= kSorted);
             }
             upto += b;
           }
@@ -638,7 +793,6 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
             sh.order.next = kDraw;
             sh.order.last_key = last_key;
             sh.order.of_last = of_last;
-            if (p.kept_count) p.kept_count[row] = (int32_t)(counted + kept_here);
           }
         }
         publish();
@@ -647,32 +801,27 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
       cluster_barrier();
     }
   } else if (threadIdx.x == 0) {  // all that the cutoff leaves
-    sh.order.last_key = key_of(side.cut);
+    sh.order.last_key = key_of<T>(side.cut);
     sh.order.of_last = 0;
   }
   __syncthreads();
 
   // The kept tokens' sums by warp: those above the last kept value, and the lowest indices of it.
   const uint32_t of_last = sh.order.of_last;
-  const float last = of_key(sh.order.last_key), above = of_last ? of_key(sh.order.last_key + 1) : side.cut;
+  const float last = of_key<T>(sh.order.last_key), above = of_last ? of_key<T>(sh.order.last_key + 1) : side.cut;
   const uint64_t last_weight = of_last ? whole_weight(side, last) : 0;
   WholeSum sum;
   uint32_t ties = 0, larger = 0;
   visit(v, kept, of_last ? last : above, p.stripes, lane, [&](const uint4& w, int) {
     add_weights<T>(w, side, typename V::Bound(above), sum);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float l = elem<T>(w, e);
-      larger += l >= above;
-      ties += l >= last && !(l >= above);
-    }
+    larger += __popc(elements_in<T>(w, above, INFINITY));
+    if (of_last) ties += __popc(elements_in<T>(w, last, above));
   });
-  larger = __reduce_add_sync(0xffffffffu, larger);
-  exchange(warp_sum(sum.total()), of_last ? __reduce_add_sync(0xffffffffu, ties) : larger);
+  exchange(warp_sum(sum.total()), __reduce_add_sync(0xffffffffu, ties), __reduce_add_sync(0xffffffffu, larger));
   total = sum_all() + (uint64_t)of_last * last_weight;
-  if (rank == 0 && !of_last && p.kept_count) {  // (else it was known with the cut)
-    const uint32_t n = count_all();
-    if (threadIdx.x == 0) p.kept_count[row] = (int32_t)n;
+  if (rank == 0 && p.kept_count && warp == 0) {
+    const uint32_t n = __reduce_add_sync(0xffffffffu, lane < (int)csize ? sh.larger[lane] : 0);
+    if (lane == 0) p.kept_count[row] = (int32_t)(n + of_last);
   }
   // The CTA, then the share, that holds the mark.
   const uint64_t mark = (uint64_t)((double)u * (double)total);
