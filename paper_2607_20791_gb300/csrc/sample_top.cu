@@ -278,6 +278,18 @@ __device__ __forceinline__ uint64_t scan_before(TopShared& sh, uint64_t v, uint6
   return before + upto - v;
 }
 
+// The n-th largest (from 1) of the first `count` lanes' values, -inf if there are fewer.
+__device__ __forceinline__ float nth_largest(float v, int n, int count) {
+  const int lane = threadIdx.x & 31;
+  int larger = 0;
+#pragma unroll 8
+  for (int o = 0; o < count; ++o) {
+    const float x = __shfl_sync(0xffffffffu, v, o);
+    larger += x > v || (x == v && o < lane);
+  }
+  return warp_max(lane < count && larger == n - 1 ? v : -INFINITY);
+}
+
 __device__ __forceinline__ uint32_t whole_weight(const Side& side, float l) { return whole(side.weight(l)); }
 __device__ __forceinline__ uint64_t share_of(float p, uint64_t total) {  // ceil(p total), at least 1
   const uint64_t need = (uint64_t)ceil((double)p * (double)total);
@@ -376,35 +388,31 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
 
   // Pass 1: the maximum (NaN never wins), and a bound that `wanted` tokens reach.
   Kept kept;
-  // (warps with a vector for every lane; the others' lanes would only lower the bound)
-  const int shares = (int)((p.vocab + share - 32 * E) / share);
+  // (A bound that `wanted` tokens reach, by the lanes' maxima: the each-th largest of a warp; the fourth
+  // of a CTA's warps; the some-th of the CTAs.  So half of the row may hold nothing of interest.  A
+  // warp takes part if every lane has a vector.)
   const bool full_share = (int64_t)p.vocab - e0 >= 32 * E;
   const int wanted = greedy ? 0 : k ? k : cut_mass ? min(kEnough, p.vocab) : 0;
-  const int each = shares ? (wanted + shares - 1) / shares : 0;  // of a warp (0: all tokens will do)
+  const int half = ((int)csize + 1) / 2, each = min(max((wanted + 4 * half - 1) / (4 * half), 1), 32);
+  const int some = (wanted + 4 * each - 1) / (4 * each);
+  const bool bounded = some <= (int)csize;
   {
     const float mine = find_lane_maxima(v, kept, p.stripes, lane), top = warp_max(mine);
     float low = -INFINITY;
-    if (each > 0 && each <= 32 && full_share) {  // the each-th largest of the lanes' maxima
-      int larger = 0;
-#pragma unroll
-      for (int o = 0; o < 32; ++o) {
-        const float x = __shfl_sync(0xffffffffu, mine, o);
-        larger += x > mine || (x == mine && o < lane);
-      }
-      low = warp_max(larger == each - 1 ? mine : -INFINITY);
+    if (wanted && bounded && full_share) {  // the each-th largest of the lanes' maxima
+      low = nth_largest(mine, each, 32);
     }
     if (lane == 0) {
       sh.warp_top[warp] = top;
-      sh.warp_low[warp] = full_share || !shares ? low : INFINITY;
+      sh.warp_low[warp] = low;
     }
   }
   __syncthreads();
   cluster_arrive_relaxed();  // every CTA of the cluster has started
   cluster_wait();
   if (warp == 0) {
-    float t = sh.warp_top[lane % kTopWarps], l = -sh.warp_low[lane % kTopWarps];
-    t = warp_max(t);
-    l = -warp_max(l);
+    const float t = warp_max(sh.warp_top[lane % kTopWarps]);
+    const float l = nth_largest(lane < kTopWarps ? sh.warp_low[lane] : -INFINITY, 4, kTopWarps);
     if (lane < (int)csize) {
       store_peer(peer_addr(smem_u32(&sh.top[rank]), lane), __float_as_uint(t));
       store_peer(peer_addr(smem_u32(&sh.low[rank]), lane), __float_as_uint(l));
@@ -413,7 +421,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
   cluster_barrier();
   Side side;
   side.top = warp_max(sh.top[lane % csize]);
-  const float low = -warp_max(-sh.low[lane % csize]);
+  const float low = nth_largest(lane < (int)csize ? sh.low[lane] : -INFINITY, max(some, 1), (int)csize);
   if (!(fabsf(side.top) < INFINITY)) return nothing(true);
 
   if (greedy) {  // the lowest index of the largest logit
@@ -513,7 +521,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
   uint64_t total = 0;  // of S's weights, once known
   if (k || cut_mass) {
     // Pass 2.
-    const float bound = each <= 32 ? fmaxf(low, side.cut) : INFINITY;
+    const float bound = bounded ? fmaxf(low, side.cut) : INFINITY;
     const bool sampled = !k || bound == INFINITY;
     if (sampled) clear_bins();
     WholeSum sum;
