@@ -36,9 +36,9 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
 // stream: it is scheduled while that kernel finishes, and waits for it
 // (griddepcontrol.wait) before it reads or writes memory.
 template <typename... P, typename... A>
-cudaError_t launch_dependent(void (*kernel)(P...), int grid, int block, int smem, cudaStream_t st, A&&... args) {
+cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int block, int smem, cudaStream_t st, A&&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)block);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = st;

@@ -90,6 +90,7 @@ struct Values {
   }
 };
 
+// (of a token by itself)
 __device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
   const float x = a;
   a = fmaf(x, c, -b * s);
@@ -123,50 +124,102 @@ __device__ __forceinline__ float half_turns(const RopeParams& p, int64_t pos, in
   return (float)(int32_t)(t >> 32) * 0x1p-31f;
 }
 
-// kAcross: pair j of a lane is (a[j], b[j]) of its two vectors a, b; else a's values are
-// E / 2 pairs, and b's as many more.
+__device__ __forceinline__ uint64_t both(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void each_of(uint64_t v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t mul_both(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma_both(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// kAcross: pair j of a lane is (u[j], v[j]) of its two vectors u, v; else u's values are E / 2
+// pairs, side by side, and v's as many more.
+template <typename T, int E, bool kAcross>
+__device__ __forceinline__ void pairs_of(const Values<T, E>& u, const Values<T, E>& v, float (&a)[E], float (&b)[E]) {
+  float x[E], y[E];
+  u.get(x);
+  v.get(y);
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    a[j] = kAcross ? x[j] : j < E / 2 ? x[2 * j] : y[2 * j - E];
+    b[j] = kAcross ? y[j] : j < E / 2 ? x[2 * j + 1] : y[2 * j - E + 1];
+  }
+}
+template <typename T, int E, bool kAcross>
+__device__ __forceinline__ void put_pairs(Values<T, E>& u, Values<T, E>& v, const float (&a)[E], const float (&b)[E]) {
+  float x[E], y[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    (kAcross ? x[j] : j < E / 2 ? x[2 * j] : y[2 * j - E]) = a[j];
+    (kAcross ? y[j] : j < E / 2 ? x[2 * j + 1] : y[2 * j - E + 1]) = b[j];
+  }
+  u.set(x);
+  v.set(y);
+}
+
+// A lane's pairs as coefficients: (a, b) becomes by (a ca - b sb, b cb + a sa), the norm's weights
+// times the cosine and sine; `by` is the norm's factor.  Two pairs to an instruction.
+template <int E>
+struct Turns {
+  static constexpr int N = E > 1 ? E / 2 : 1;
+  uint64_t ca[N], sa[N], cb[N], sb[N];  // (sb negative)
+};
+
 template <typename T, int E, bool kAcross, bool kPages>
 __global__ void __launch_bounds__(kRopeWarps * 32) rope_kernel(const RopeParams p) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (a dependent waits for this kernel's end)
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const int64_t w = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
-  const int64_t t = w / p.chunks;
-  const int chunk = (int)(w - t * p.chunks);
-  const int32_t r = (int32_t)(t / p.tokens), i = (int32_t)(t - (int64_t)r * p.tokens);
-  if (r >= p.rows) return;
+  const int lane = threadIdx.x & 31, chunk = (int)blockIdx.y;
+  const uint32_t t = blockIdx.x * kRopeWarps + (threadIdx.x >> 5);  // token
+  const uint32_t r = kPages ? t / (uint32_t)p.tokens : t >= (uint32_t)p.tokens, i = kPages ? t - r * (uint32_t)p.tokens : t;
+  if (r >= (uint32_t)p.rows) return;
   int64_t pos, page_at = 0;
   if (kPages) {
-    if (!place(p, r, i, chunk == 0 && lane == 0, pos, page_at)) return;
+    if (!place(p, (int32_t)r, (int32_t)i, chunk == 0 && lane == 0, pos, page_at)) return;
   } else {
     pos = p.positions[t];
   }
   const int per = 32 / p.group, sub = lane / p.group, slot = lane & (p.group - 1);
   const bool on = slot < p.slots;
   const int half_slots = p.pairs ? 0 : p.rot / (2 * E);
-  int o0, o1;  // the lane's two vectors
-  if (slot < half_slots) {
-    o0 = slot * E;
-    o1 = o0 + p.rot / 2;
-  } else {
-    o0 = slot * 2 * E;
-    o1 = o0 + E;
-  }
+  const int o0 = slot < half_slots ? slot * E : slot * 2 * E;  // the lane's two vectors
+  const int o1 = slot < half_slots ? o0 + p.rot / 2 : o0 + E;
+  const int turned = on ? p.rot / 2 - slot * E : 0;  // of the lane's pairs
   float c[E], s[E];
+  if (E == 8 && p.group == 8 && p.rot == 128) {
+    // Four heads of 128 at once: every pair's angle is wanted by four lanes, each works out two of its eight.
+    float c2[2], s2[2];
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    c[j] = 1.f;
-    s[j] = 0.f;
-    const int pair = slot * E + j;
-    if (on && pair < p.rot / 2) {
-      sincospif(half_turns(p, pos, pair), &s[j], &c[j]);
-      c[j] *= p.magnitude;
-      s[j] *= p.magnitude;
+    for (int j = 0; j < 2; ++j) sincospif(half_turns(p, pos, slot * E + sub * 2 + j), &s2[j], &c2[j]);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      c[j] = __shfl_sync(0xffffffffu, c2[j & 1], (j >> 1) * 8 + slot) * p.magnitude;
+      s[j] = __shfl_sync(0xffffffffu, s2[j & 1], (j >> 1) * 8 + slot) * p.magnitude;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      c[j] = 1.f;
+      s[j] = 0.f;
+      if (j < turned) {
+        sincospif(half_turns(p, pos, slot * E + j), &s[j], &c[j]);
+        c[j] *= p.magnitude;
+        s[j] *= p.magnitude;
+      }
     }
   }
-  const int turned = p.rot / 2 - slot * E;  // of the lane's pairs
-  const bool whole = p.rot == p.dim;
-  float w0[E], w1[E];
+  Turns<E> by_pair;
   const int last = min((chunk + 1) * p.each, p.passes[0] + p.passes[1] + p.passes[2]);
   int kind_of_weights = -1;
 #pragma unroll 1
@@ -175,66 +228,105 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_kernel(const RopeParams 
     int kind = 0, q = first;
     while (q >= p.passes[kind]) q -= p.passes[kind++];
     const int count = min(min(last - first, p.passes[kind] - q), kInFlight);
-    const uint8_t* in = p.in[kind] + r * p.in_row[kind] + i * p.in_token[kind];
-    Values<T, E> a[kInFlight], b[kInFlight];
+    const int h0 = q * per + sub;
+    const T* from = reinterpret_cast<const T*>(p.in[kind] + r * p.in_row[kind] + i * p.in_token[kind]) + h0 * p.dim;
+    Values<T, E> u[kInFlight], v[kInFlight];
 #pragma unroll
     for (int k = 0; k < kInFlight; ++k) {
-      const int h = (q + k) * per + sub;
-      if (k < count && on && h < p.heads[kind]) {
-        const T* x = reinterpret_cast<const T*>(in) + (int64_t)h * p.dim;
-        a[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(x + o0);
-        b[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(x + o1);
+      if (k < count && on && h0 + k * per < p.heads[kind]) {
+        u[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(from + k * per * p.dim + o0);
+        v[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(from + k * per * p.dim + o1);
       }
     }
-    if (kind < 2 && p.norm && kind != kind_of_weights) {
+    if (kind < 2 && kind != kind_of_weights) {
       kind_of_weights = kind;
+      float wa[E], wb[E];
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        w0[j] = w1[j] = 1.f;
-        if (on && p.weight[kind]) {
-          w0[j] = weight_at(p, p.weight[kind], o0 + j);
-          w1[j] = weight_at(p, p.weight[kind], o1 + j);
+        wa[j] = wb[j] = 1.f;
+        if (p.norm && on && p.weight[kind]) {
+          wa[j] = weight_at(p, p.weight[kind], kAcross ? o0 + j : o0 + 2 * j);
+          wb[j] = weight_at(p, p.weight[kind], kAcross ? o1 + j : o0 + 2 * j + 1);
         }
       }
+      if (E > 1) {
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) {
+          const int x = 2 * j, y = E > 1 ? 2 * j + 1 : 0;
+          by_pair.ca[j] = both(wa[x] * c[x], wa[y] * c[y]);
+          by_pair.sa[j] = both(wa[x] * s[x], wa[y] * s[y]);
+          by_pair.cb[j] = both(wb[x] * c[x], wb[y] * c[y]);
+          by_pair.sb[j] = both(-wb[x] * s[x], -wb[y] * s[y]);
+        }
+      } else {
+        by_pair.ca[0] = both(wa[0] * c[0], 0.f);
+        by_pair.sa[0] = both(wa[0] * s[0], 0.f);
+        by_pair.cb[0] = both(wb[0] * c[0], 0.f);
+        by_pair.sb[0] = both(-wb[0] * s[0], 0.f);
+      }
     }
+    T* to = kPages && kind > 0 ? reinterpret_cast<T*>(p.out[kind]) + page_at + (int64_t)h0 * kPageSize * p.dim
+                               : reinterpret_cast<T*>(p.out[kind] + t * p.out_token[kind]) + h0 * p.dim;
+    const int64_t step = (int64_t)per * p.dim * (kPages && kind > 0 ? kPageSize : 1);
 #pragma unroll
     for (int k = 0; k < kInFlight; ++k) {
       if (k >= count) break;
-      const int h = (q + k) * per + sub;
-      const bool mine = on && h < p.heads[kind];
+      const bool mine = on && h0 + k * per < p.heads[kind];
       if (kind < 2) {
-        float x[E], y[E];
-        a[k].get(x);
-        b[k].get(y);
-        if (p.norm) {
-          float sum = 0.f;
-          if (mine) {
+        float a[E], b[E];
+        pairs_of<T, E, kAcross>(u[k], v[k], a, b);
+        uint64_t a2[Turns<E>::N], b2[Turns<E>::N];
 #pragma unroll
-            for (int j = 0; j < E; ++j) sum = fmaf(x[j], x[j], fmaf(y[j], y[j], sum));
-          }
+        for (int j = 0; j < Turns<E>::N; ++j) {
+          a2[j] = both(a[E > 1 ? 2 * j : 0], E > 1 ? a[E > 1 ? 2 * j + 1 : 0] : 0.f);
+          b2[j] = both(b[E > 1 ? 2 * j : 0], E > 1 ? b[E > 1 ? 2 * j + 1 : 0] : 0.f);
+        }
+        float by = 1.f;
+        if (p.norm) {
+          uint64_t squares = 0;
+#pragma unroll
+          for (int j = 0; j < Turns<E>::N; ++j) squares = fma_both(a2[j], a2[j], fma_both(b2[j], b2[j], squares));
+          float sum, high;
+          each_of(squares, sum, high);
+          sum = mine ? sum + high : 0.f;
           for (int o = p.group / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-          const float by = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+          by = rsqrtf(fmaf(sum, p.inv_dim, p.eps));
+        }
+        const uint64_t by2 = both(by, by);
+        if (turned >= E) {
+#pragma unroll
+          for (int j = 0; j < Turns<E>::N; ++j) {
+            const uint64_t x = fma_both(a2[j], by_pair.ca[j], mul_both(b2[j], by_pair.sb[j]));
+            const uint64_t y = fma_both(b2[j], by_pair.cb[j], mul_both(a2[j], by_pair.sa[j]));
+            float lo, hi;
+            each_of(mul_both(x, by2), lo, hi);
+            a[E > 1 ? 2 * j : 0] = lo;
+            if (E > 1) a[E > 1 ? 2 * j + 1 : 0] = hi;
+            each_of(mul_both(y, by2), lo, hi);
+            b[E > 1 ? 2 * j : 0] = lo;
+            if (E > 1) b[E > 1 ? 2 * j + 1 : 0] = hi;
+          }
+          put_pairs<T, E, kAcross>(u[k], v[k], a, b);
+        } else if (turned > 0 || p.norm) {
+          // (values behind the rotated part are not turned by 0: an infinity's partner would be NaN)
 #pragma unroll
           for (int j = 0; j < E; ++j) {
-            x[j] *= by * w0[j];
-            y[j] *= by * w1[j];
+            float ca, sa, cb, sb, other;
+            each_of(by_pair.ca[j / 2], E > 1 && (j & 1) ? other : ca, E > 1 && (j & 1) ? ca : other);
+            each_of(by_pair.sa[j / 2], E > 1 && (j & 1) ? other : sa, E > 1 && (j & 1) ? sa : other);
+            each_of(by_pair.cb[j / 2], E > 1 && (j & 1) ? other : cb, E > 1 && (j & 1) ? cb : other);
+            each_of(by_pair.sb[j / 2], E > 1 && (j & 1) ? other : sb, E > 1 && (j & 1) ? sb : other);
+            const float x = j < turned ? fmaf(a[j], ca, b[j] * sb) : a[j] * ca;
+            const float y = j < turned ? fmaf(b[j], cb, a[j] * sa) : b[j] * cb;
+            a[j] = x * by;
+            b[j] = y * by;
           }
+          put_pairs<T, E, kAcross>(u[k], v[k], a, b);
         }
-        // (values behind the rotated part are not turned by 0: an infinity's partner would be NaN)
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          float& u = kAcross ? x[j] : j < E / 2 ? x[2 * j] : y[2 * j - E];
-          float& v = kAcross ? y[j] : j < E / 2 ? x[2 * j + 1] : y[2 * j - E + 1];
-          if (whole || j < turned) turn(u, v, c[j], s[j]);
-        }
-        a[k].set(x);
-        b[k].set(y);
       }
       if (!mine) continue;
-      T* to = kPages && kind > 0 ? reinterpret_cast<T*>(p.out[kind]) + page_at + (int64_t)h * kPageSize * p.dim
-                                 : reinterpret_cast<T*>(p.out[kind] + t * p.out_token[kind]) + (int64_t)h * p.dim;
-      *reinterpret_cast<typename Values<T, E>::R*>(to + o0) = a[k].v;
-      *reinterpret_cast<typename Values<T, E>::R*>(to + o1) = b[k].v;
+      *reinterpret_cast<typename Values<T, E>::R*>(to + k * step + o0) = u[k].v;
+      *reinterpret_cast<typename Values<T, E>::R*>(to + k * step + o1) = v[k].v;
     }
     first += count;
   }
@@ -301,10 +393,9 @@ cudaError_t launch_vectors(RopeParams& p, cudaStream_t st) {
   p.chunks = (int)std::min<int64_t>(passes, std::max<int64_t>(1, (wanted + tokens - 1) / tokens));
   p.each = (passes + p.chunks - 1) / p.chunks;
   p.chunks = (passes + p.each - 1) / p.each;
-  const int64_t blocks = (tokens * p.chunks + kRopeWarps - 1) / kRopeWarps;
   const bool across = !p.pairs || E == 1;
   auto k = across ? rope_kernel<T, E, true, kPages> : rope_kernel<T, E, E == 1, kPages>;
-  return launch_dependent(k, (int)blocks, kRopeWarps * 32, 0, st, p);
+  return launch_dependent(k, dim3((unsigned)((tokens + kRopeWarps - 1) / kRopeWarps), (unsigned)p.chunks), kRopeWarps * 32, 0, st, p);
 }
 
 template <typename T, bool kPages>
