@@ -676,6 +676,12 @@ def rgd_rope_frequencies(rotary_dim: int, base: float, scaling="none", factor: f
 def _heads_of(t, name: str, lead: int, heads: int, dim: int, dtypes):
     """[..., heads, head_dim] with `lead` leading dimensions, whose last two are dense; None where there are no heads.
     Returns the pointer, the leading sizes and their strides (0 where there is one element: never used)."""
+    if type(t) is _Tensor and t.dtype in dtypes and t.is_cuda:  # (as in _ptr: what passes every check returns here)
+        shape, stride = t.shape, t.stride()
+        if len(shape) == lead + 2 and shape[lead] == heads and shape[-1] == dim and stride[-1] == 1 and stride[-2] == dim:
+            if lead == 1:
+                return t.data_ptr(), (shape[0],), (stride[0] if shape[0] > 1 else 0,)
+            return t.data_ptr(), (shape[0], shape[1]), (stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0)
     import torch
     if t is None and heads == 0:
         return None, None, (0,) * lead
@@ -753,6 +759,10 @@ def rgd_qk_rope_cache(shape: RopeShape, cache: CacheShape, layer: int, q, k, v, 
 
 def _rows_of(t, name: str, dtypes):
     """[rows, columns] whose columns are dense: the pointer and the stride of its rows (that of one row: its width)."""
+    if type(t) is _Tensor and t.dtype in dtypes and t.is_cuda:  # (as in _ptr)
+        shape, stride = t.shape, t.stride()
+        if len(shape) == 2 and stride[1] == 1:
+            return t.data_ptr(), (stride[0] if shape[0] > 1 else max(stride[0], shape[1]))
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise TypeError(f"{name} must be a tensor of {' or '.join(str(d) for d in dtypes)}")

@@ -184,18 +184,38 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_kernel(const RopeParams 
   const uint32_t t = blockIdx.x * kRopeWarps + (threadIdx.x >> 5);  // token
   const uint32_t r = kPages ? t / (uint32_t)p.tokens : t >= (uint32_t)p.tokens, i = kPages ? t - r * (uint32_t)p.tokens : t;
   if (r >= (uint32_t)p.rows) return;
-  int64_t pos, page_at = 0;
-  if (kPages) {
-    if (!place(p, (int32_t)r, (int32_t)i, chunk == 0 && lane == 0, pos, page_at)) return;
-  } else {
-    pos = p.positions[t];
-  }
   const int per = 32 / p.group, sub = lane / p.group, slot = lane & (p.group - 1);
   const bool on = slot < p.slots;
   const int half_slots = p.pairs ? 0 : p.rot / (2 * E);
   const int o0 = slot < half_slots ? slot * E : slot * 2 * E;  // the lane's two vectors
   const int o1 = slot < half_slots ? o0 + p.rot / 2 : o0 + E;
   const int turned = on ? p.rot / 2 - slot * E : 0;  // of the lane's pairs
+  // Passes of one kind together, from `first` on: the first ones' loads are under way while the page is
+  // looked up and the angles are worked out.
+  const int last = min((chunk + 1) * p.each, p.passes[0] + p.passes[1] + p.passes[2]);
+  int kind = 0, count = 0, h0 = 0;
+  Values<T, E> u[kInFlight], v[kInFlight];
+  auto load = [&](int first) {
+    int q = first;
+    for (kind = 0; q >= p.passes[kind];) q -= p.passes[kind++];
+    count = min(min(last - first, p.passes[kind] - q), kInFlight);
+    h0 = q * per + sub;
+    const T* from = reinterpret_cast<const T*>(p.in[kind] + r * p.in_row[kind] + i * p.in_token[kind]) + h0 * p.dim;
+#pragma unroll
+    for (int k = 0; k < kInFlight; ++k) {
+      if (k < count && on && h0 + k * per < p.heads[kind]) {
+        u[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(from + k * per * p.dim + o0);
+        v[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(from + k * per * p.dim + o1);
+      }
+    }
+  };
+  load(chunk * p.each);
+  int64_t pos, page_at = 0;
+  if (kPages) {
+    if (!place(p, (int32_t)r, (int32_t)i, chunk == 0 && lane == 0, pos, page_at)) return;
+  } else {
+    pos = p.positions[t];
+  }
   float c[E], s[E];
   if (E == 8 && p.group == 8 && p.rot == 128) {
     // Four heads of 128 at once: every pair's angle is wanted by four lanes, each works out two of its eight.
@@ -220,24 +240,9 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_kernel(const RopeParams 
     }
   }
   Turns<E> by_pair;
-  const int last = min((chunk + 1) * p.each, p.passes[0] + p.passes[1] + p.passes[2]);
   int kind_of_weights = -1;
 #pragma unroll 1
   for (int first = chunk * p.each; first < last;) {
-    // Passes of one kind together: their heads from h on.
-    int kind = 0, q = first;
-    while (q >= p.passes[kind]) q -= p.passes[kind++];
-    const int count = min(min(last - first, p.passes[kind] - q), kInFlight);
-    const int h0 = q * per + sub;
-    const T* from = reinterpret_cast<const T*>(p.in[kind] + r * p.in_row[kind] + i * p.in_token[kind]) + h0 * p.dim;
-    Values<T, E> u[kInFlight], v[kInFlight];
-#pragma unroll
-    for (int k = 0; k < kInFlight; ++k) {
-      if (k < count && on && h0 + k * per < p.heads[kind]) {
-        u[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(from + k * per * p.dim + o0);
-        v[k].v = *reinterpret_cast<const typename Values<T, E>::R*>(from + k * per * p.dim + o1);
-      }
-    }
     if (kind < 2 && kind != kind_of_weights) {
       kind_of_weights = kind;
       float wa[E], wb[E];
@@ -329,6 +334,7 @@ __global__ void __launch_bounds__(kRopeWarps * 32) rope_kernel(const RopeParams 
       *reinterpret_cast<typename Values<T, E>::R*>(to + k * step + o1) = v[k].v;
     }
     first += count;
+    if (first < last) load(first);
   }
 }
 
