@@ -135,7 +135,7 @@ __device__ __forceinline__ void send_box(const Fp8Params& p, const CUtensorMap& 
 }
 
 template <int NT>
-constexpr int kAdders = NT > 128 ? 256 : 128;  // threads that add up
+constexpr int kAdders = NT > 32 ? 256 : 128;  // threads that add up: two warps to 32 lanes, or one
 template <int NT>
 constexpr int kFp8Threads = kAdders<NT> + 128;
 
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     fp8_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
                const __grid_constant__ CUtensorMap ymap) {
   static_assert(!kPair || (NT == 256 && !kTurned), "");
-  constexpr int kOwn = NT > 128 ? 128 : NT;  // columns of a thread
+  constexpr int kOwn = NT / (kAdders<NT> / 128);  // columns of a thread
   constexpr int kProducer = kAdders<NT> / 32, kIssuer = kProducer + 1, kScaler = kProducer + 2;
   constexpr int kSums = 512 / NT < kMostSums ? 512 / NT : kMostSums;  // accumulators
   constexpr uint32_t kTmemCols = kSums * NT;
@@ -364,8 +364,8 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   } else {
     if (NT > 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;  // of the tile's columns; the lane's row of A
-    const int mine = kTurned ? min(max(p.cols - half * 128, 0), kOwn) : kOwn;
-    const uint32_t at_tmem = tmem + ((uint32_t)(warp & 3) << 21) + half * 128;
+    const int mine = kTurned ? min(max(p.cols - half * kOwn, 0), kOwn) : kOwn;
+    const uint32_t at_tmem = tmem + ((uint32_t)(warp & 3) << 21) + half * kOwn;
     const uint32_t free_sum = kPair ? mapa_u32(smem_u32(&sh.sum_empty[0]), 0) : 0;
     uint64_t acc[kOwn / 2];
 #pragma unroll
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     // A step's sums come in chunks of columns: two together, the next two while these are added; one by
     // one where two tiles' worth of registers hold sums (80 x 6144 x 4096: 14.9 us so, 16.4 one by one;
     // 8192 x 14336 x 4096: 393 us one by one, 566 two together).
-    constexpr bool kTwo = NT <= 128;
+    constexpr bool kTwo = kOwn < 128;
     constexpr int kChunk = kOwn > 32 ? 32 : 16, kChunks = kOwn / kChunk;
     const int last = (mine + kChunk - 1) / kChunk - 1;
     int tile = (int)tile0, at = 0;
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       const int b = q % kSums, slot = q % (kScaleSlots * kScaleSteps), chunk = q / kScaleSteps;
       bool good = true;
       if (q % kScaleSteps == 0) good = mbar_wait_soon(&sh.scale_full[chunk % kScaleSlots], (uint32_t)(chunk / kScaleSlots) & 1u);
-      const float sw = w_scale[slot][kTurned ? 0 : half];
+      const float sw = w_scale[slot][kTurned ? 0 : half * kOwn / 128];
       const float own = kTurned ? sw : sw * x_scale[slot][row];
       const uint64_t by = pair2(own, own);
       const uint32_t parity = (uint32_t)(q / kSums) & 1u;
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
 #pragma unroll
         for (int i = 0; i < kChunk / 2; ++i) {
           uint64_t f = by;
-          if (kTurned) f = mul_pair(by, reinterpret_cast<const uint64_t*>(&x_scale[slot][half * 128])[c * (kChunk / 2) + i]);
+          if (kTurned) f = mul_pair(by, reinterpret_cast<const uint64_t*>(&x_scale[slot][half * kOwn])[c * (kChunk / 2) + i]);
           const uint64_t v = (uint64_t)d[c & 1][2 * i + 1] << 32 | d[c & 1][2 * i];
           acc[c * (kChunk / 2) + i] = fma_pair(v, f, acc[c * (kChunk / 2) + i]);
         }
@@ -445,10 +445,10 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       int ta, tb;
       tile_at(p, tile, ta, tb);
       const int64_t a0 = (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0) + row;
-      const int64_t b0 = (int64_t)tb * p.cols + half * 128;
+      const int64_t b0 = (int64_t)tb * p.cols + half * kOwn;
       tile += (int)tile_step;
       if (!kPair && p.split > 1) {  // (the ring is free: every copy has been read)
-        float* part = reinterpret_cast<float*>(ring) + (kTurned ? half * 128 * kLanes + row : row * kPartRow<NT> + half * 128);
+        float* part = reinterpret_cast<float*>(ring) + (kTurned ? half * kOwn * kLanes + row : row * kPartRow<NT> + half * kOwn);
 #pragma unroll
         for (int i = 0; i < kOwn / 4; ++i) {
           if (4 * i >= mine) break;
