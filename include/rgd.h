@@ -707,7 +707,8 @@ int rgd_fp8_quantize(int32_t rows, int32_t cols, int32_t dtype, const void* x, i
  * A block's products are exact and summed by the tensor core in fp32; the blocks' sums are
  * scaled and added in fp32 and the result is rounded once.  The order of the sums is the same
  * for every call of the same m, n and k.  dev_status gets RGD_DEV_WAIT_TIMEOUT when a bounded
- * wait gave up; y is then not valid.  k at most 2^24.  One kernel on `stream`. */
+ * wait gave up; y is then not valid.  k at most 2^24.  RGD_ERR_UNSUPPORTED above 2^30 rows of
+ * either.  One kernel on `stream`. */
 int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x, int64_t x_stride, const float* x_scales,
                    const uint8_t* weights, int64_t w_stride, const float* w_scales, int32_t out_dtype, void* y,
                    int64_t y_stride, int32_t* dev_status, rgd_stream_t stream);

@@ -714,6 +714,8 @@ def rgd_qk_rope(shape: RopeShape, q, k, positions, turns, q_weight, k_weight, q_
     first = q if shape.num_q_heads else k
     kinds = (torch.bfloat16, torch.float32) if first is None or not hasattr(first, "dtype") else (
         (first.dtype,) if first.dtype in (torch.bfloat16, torch.float32) else (torch.bfloat16, torch.float32))
+    if not isinstance(positions, torch.Tensor):
+        raise TypeError("positions must be a tensor")
     hq, hk, d, tokens = shape.num_q_heads, shape.num_k_heads, shape.head_dim, positions.numel()
     args = []
     for t, name, heads in ((q, "q", hq), (k, "k", hk), (q_out, "q_out", hq), (k_out, "k_out", hk)):

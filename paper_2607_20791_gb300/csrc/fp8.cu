@@ -8,13 +8,14 @@
 // once to 128 products' sum, whatever its value.
 //
 // The tensor core takes 128 rows (TMEM lanes) by up to 256 columns.  Many rows of x: x's are
-// the lanes and w's the columns (a lane's scale is one number).  Few (up to 256): w's are the
-// lanes and all of x's rows the columns, so that the weights are read once; bound by them.
-// Where there are too few tiles for the SMs a cluster of CTAs shares one, each with a part
-// of k, and they add their parts up in order: the same sums in every call.
+// the lanes and w's the columns (a lane's scale is one number), 128 of them to a CTA or 256
+// to a pair of CTAs with 256 rows.  Few (up to 128): w's are the lanes and all of x's rows the
+// columns, so that the weights are read once; bound by them.  Where there are too few tiles
+// for the SMs a cluster of CTAs shares one, each with a part of k, and they add their parts
+// up in order: the same sums in every call.
 //
-// Warps: the first four (eight for 256 columns) add sums up, one copies tiles in by TMA, one
-// issues the tensor core's instructions.
+// Warps: the first eight (four for up to 32 columns) add sums up, one copies tiles in by TMA,
+// one issues the tensor core's instructions, one fetches scales.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -364,8 +365,10 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   } else {
     if (NT > 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     const int half = warp >> 2, row = (warp & 3) * 32 + lane;  // of the tile's columns; the lane's row of A
-    const int mine = kTurned ? min(max(p.cols - half * kOwn, 0), kOwn) : kOwn;
-    const uint32_t at_tmem = tmem + ((uint32_t)(warp & 3) << 21) + half * kOwn;
+    // Its columns, in whole 16s: of a tile that is not full, each half of the warps has about half.
+    const int off = half * (kTurned ? min((p.cols / 2 + 15) / 16 * 16, kOwn) : kOwn);
+    const int mine = !kTurned ? kOwn : kAdders<NT> == 128 || half ? p.cols - off : (p.cols / 2 + 15) / 16 * 16;
+    const uint32_t at_tmem = tmem + ((uint32_t)(warp & 3) << 21) + off;
     const uint32_t free_sum = kPair ? mapa_u32(smem_u32(&sh.sum_empty[0]), 0) : 0;
     uint64_t acc[kOwn / 2];
 #pragma unroll
@@ -396,11 +399,18 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       const uint32_t from = at_tmem + b * NT;
       auto add = [&](int c) {
 #pragma unroll
-        for (int i = 0; i < kChunk / 2; ++i) {
-          uint64_t f = by;
-          if (kTurned) f = mul_pair(by, reinterpret_cast<const uint64_t*>(&x_scale[slot][half * kOwn])[c * (kChunk / 2) + i]);
-          const uint64_t v = (uint64_t)d[c & 1][2 * i + 1] << 32 | d[c & 1][2 * i];
-          acc[c * (kChunk / 2) + i] = fma_pair(v, f, acc[c * (kChunk / 2) + i]);
+        for (int i = 0; i < kChunk / 2; i += 2) {
+          uint64_t f[2] = {by, by};
+          if (kTurned) {
+            const ulonglong2 of = *reinterpret_cast<const ulonglong2*>(&x_scale[slot][off + c * kChunk + 2 * i]);
+            f[0] = mul_pair(by, of.x);
+            f[1] = mul_pair(by, of.y);
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint64_t v = (uint64_t)d[c & 1][2 * (i + j) + 1] << 32 | d[c & 1][2 * (i + j)];
+            acc[c * (kChunk / 2) + i + j] = fma_pair(v, f[j], acc[c * (kChunk / 2) + i + j]);
+          }
         }
       };
       auto release = [&]() {
@@ -445,10 +455,10 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       int ta, tb;
       tile_at(p, tile, ta, tb);
       const int64_t a0 = (int64_t)ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0) + row;
-      const int64_t b0 = (int64_t)tb * p.cols + half * kOwn;
+      const int64_t b0 = (int64_t)tb * p.cols + off;
       tile += (int)tile_step;
       if (!kPair && p.split > 1) {  // (the ring is free: every copy has been read)
-        float* part = reinterpret_cast<float*>(ring) + (kTurned ? half * kOwn * kLanes + row : row * kPartRow<NT> + half * kOwn);
+        float* part = reinterpret_cast<float*>(ring) + (kTurned ? off * kLanes + row : row * kPartRow<NT> + off);
 #pragma unroll
         for (int i = 0; i < kOwn / 4; ++i) {
           if (4 * i >= mine) break;
@@ -621,6 +631,25 @@ int encode_rows(CUtensorMap* map, const void* base, int64_t k, int64_t rows, int
   return encode_boxes(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, k, rows, stride, kStep, box_rows);
 }
 
+// How many CTAs share a tile, and the time that all tiles take, in steps.  Clusters of 2, 4 or 8 share
+// one where that takes less: each round over the SMs costs the steps of its CTAs, and about eight more
+// where tiles are shared (their start and their joined sums are not behind another tile's).  152 CTAs
+// fit the SMs, as clusters of 4 144, of 8 120.
+constexpr int kSms = 152;
+struct Split {
+  int split;
+  int64_t cost;
+};
+Split best_split(int64_t tiles, int64_t steps) {
+  constexpr int fit[4] = {152, 152, 144, 120};
+  Split best{1, (tiles + kSms - 1) / kSms * steps};
+  for (int i = 1; i < 4 && steps >= 2 << i; ++i) {
+    const int64_t cost = ((tiles << i) + fit[i] - 1) / fit[i] * ((steps + (1 << i) - 1) / (1 << i) + 8);
+    if (cost < best.cost) best = Split{1 << i, cost};
+  }
+  return best;
+}
+
 struct Fp8Operands {
   const uint8_t* x;
   const uint8_t* w;
@@ -646,12 +675,9 @@ int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t 
   p.band = 8;
   const int stage = kABytes + b_rows * kStep;
   p.stages = std::min(kMostStages, room / stage);
-  // Too few tiles for the SMs: clusters of 2, 4 or 8 CTAs share one, each with two steps at least.
-  constexpr int sms = 152;
-  p.split = 1;
-  while (!kPair && p.split < kMostSplit && tiles * p.split * 2 <= sms && p.steps >= p.split * 4) p.split *= 2;
-  const int64_t ctas = kPair ? 2 * tiles : tiles;
-  const int grid = p.split > 1 ? p.tiles * p.split : (int)std::min<int64_t>(ctas, sms);
+  p.split = kPair ? 1 : best_split(tiles, p.steps).split;
+  if (p.split > 1 && tiles * p.split > 0x7fffffff) p.split = 1;
+  const int grid = p.split > 1 ? p.tiles * p.split : (int)std::min<int64_t>(kPair ? 2 * tiles : tiles, kSms);
   CUtensorMap amap, bmap;
   const uint8_t *a = kTurned ? o.w : o.x, *b = kTurned ? o.x : o.w;
   const int64_t as = kTurned ? o.w_stride : o.x_stride, bs = kTurned ? o.x_stride : o.w_stride;
@@ -692,6 +718,7 @@ extern "C" int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x,
   RGD_CHECK_ARG(out_dtype == RGD_F32 || out_dtype == RGD_BF16, "%s: out_dtype must be RGD_F32 or RGD_BF16", fn);
   RGD_CHECK_ARG(k <= 1 << 24, "%s: k too large (max 2^24)", fn);
   RGD_CHECK_ARG(x_stride >= k && w_stride >= k && y_stride >= n, "%s: x_stride or w_stride is below k, or y_stride below n", fn);
+  if (m > 1 << 30 || n > 1 << 30) return set_error(RGD_ERR_UNSUPPORTED, "%s: more than 2^30 rows", fn);
   if (m == 0 || n == 0) return RGD_OK;
   RGD_CHECK_ARG(x && x_scales && weights && w_scales && y, "%s: x/x_scales/weights/w_scales/y must be non-NULL", fn);
   RGD_CHECK_ARG(aligned16(x) && aligned16(weights) && aligned16(y) && x_stride % 16 == 0 && w_stride % 16 == 0,
@@ -715,7 +742,10 @@ extern "C" int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x,
   if (m <= 32) return launch_fp8<32, true>(fn, p, o, st);
   if (m <= 64) return launch_fp8<64, true>(fn, p, o, st);
   if (m <= 128) return launch_fp8<128, true>(fn, p, o, st);
-  if (m <= 256) return launch_fp8<256, true>(fn, p, o, st);
-  if (p.vectors && ((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256) >= 76) return launch_fp8<256, false, true>(fn, p, o, st);
+  // Pairs where that takes less time: a step of theirs is about 1.15 of a CTA's with 128 columns.
+  const int64_t pairs = ((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256);
+  const int64_t pair_cost = (pairs + kSms / 2 - 1) / (kSms / 2) * p.steps;
+  if (p.vectors && pair_cost * 23 / 20 < best_split(((int64_t)m + 127) / 128 * (((int64_t)n + 127) / 128), p.steps).cost)
+    return launch_fp8<256, false, true>(fn, p, o, st);
   return launch_fp8<128, false>(fn, p, o, st);
 }
