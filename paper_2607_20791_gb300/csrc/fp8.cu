@@ -742,10 +742,12 @@ extern "C" int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x,
   if (m <= 32) return launch_fp8<32, true>(fn, p, o, st);
   if (m <= 64) return launch_fp8<64, true>(fn, p, o, st);
   if (m <= 128) return launch_fp8<128, true>(fn, p, o, st);
-  // Pairs where that takes less time: a step of theirs is about 1.15 of a CTA's with 128 columns.
+  // Pairs where that takes less time: a step of theirs is about 1.15 of a CTA's with 128 columns.  Their
+  // results leave by TMA, which writes whole 16 bytes: rows of y start and end on them.
   const int64_t pairs = ((int64_t)m + 255) / 256 * (((int64_t)n + 255) / 256);
   const int64_t pair_cost = (pairs + kSms / 2 - 1) / (kSms / 2) * p.steps;
-  if (p.vectors && pair_cost * 23 / 20 < best_split(((int64_t)m + 127) / 128 * (((int64_t)n + 127) / 128), p.steps).cost)
+  const bool whole = p.vectors && (int64_t)n * (p.out_f32 ? 4 : 2) % 16 == 0;
+  if (whole && pair_cost * 23 / 20 < best_split(((int64_t)m + 127) / 128 * (((int64_t)n + 127) / 128), p.steps).cost)
     return launch_fp8<256, false, true>(fn, p, o, st);
   return launch_fp8<128, false>(fn, p, o, st);
 }
