@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   int issued = 0;  // steps whose copies are on their way, or were
   if (warp >= kProducer) {
     if (NT > 128) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    if (warp == kProducer && lane == 0) {
+    if (warp == kProducer) {
       uint32_t tile = tile0;
       int at = 0, s = 0, ay = 0, by = 0;
       uint32_t turn = 0;
@@ -258,22 +258,25 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
           ay = ta * (kPair ? 2 * kLanes : kLanes) + (kPair ? (int)rank * kLanes : 0);
           by = tb * p.cols + (kPair ? (int)rank * b_rows : 0);
         }
-        if (turn > 0 && !mbar_wait_soon(&sh.empty[s], (turn - 1) & 1u)) {
+        if (!__all_sync(0xffffffffu, turn == 0 || mbar_wait_soon(&sh.empty[s], (turn - 1) & 1u))) {
           sh.dead = 1;
           break;
         }
-        uint8_t* a = ring + s * stage_bytes;
-        const int kx = (step0 + at) * kStep;
-        if (kPair) {  // (the first CTA's barrier counts both CTAs' copies)
-          const uint32_t bar = mapa_u32(smem_u32(&sh.full[s]), 0);
-          if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2u * (uint32_t)stage_bytes);
-          tma_load_2d_pair(a, &amap, bar, kx, ay);
-          tma_load_2d_pair(a + kABytes, &bmap, bar, kx, by);
-        } else {
-          mbar_arrive_expect_tx(&sh.full[s], (uint32_t)stage_bytes);
-          tma_load_2d(a, &amap, &sh.full[s], kx, ay);
-          tma_load_2d(a + kABytes, &bmap, &sh.full[s], kx, by);
+        if (elect_one()) {
+          uint8_t* a = ring + s * stage_bytes;
+          const int kx = (step0 + at) * kStep;
+          if (kPair) {  // (the first CTA's barrier counts both CTAs' copies)
+            const uint32_t bar = mapa_u32(smem_u32(&sh.full[s]), 0);
+            if (rank == 0) mbar_arrive_expect_tx(&sh.full[s], 2u * (uint32_t)stage_bytes);
+            tma_load_2d_pair(a, &amap, bar, kx, ay);
+            tma_load_2d_pair(a + kABytes, &bmap, bar, kx, by);
+          } else {
+            mbar_arrive_expect_tx(&sh.full[s], (uint32_t)stage_bytes);
+            tma_load_2d(a, &amap, &sh.full[s], kx, ay);
+            tma_load_2d(a + kABytes, &bmap, &sh.full[s], kx, by);
+          }
         }
+        __syncwarp();
         if (++at == steps) {
           at = 0;
           tile += tile_step;
@@ -284,32 +287,40 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
         }
       }
     }
-    if (warp == kIssuer && lane == 0 && (!kPair || rank == 0)) {
+    // This warp, too, waits as one and a lane of it issues: these instructions take operands that are the
+    // same in a warp, and cost a lane that is alone in a branch more (8192 x 14336 x 4096: 353 us so, 362
+    // with the copies by lane 0, 390 with both).
+    if (warp == kIssuer && (!kPair || rank == 0)) {
       const uint32_t idesc = idesc_e4m3_f32(kPair ? 2 * kLanes : kLanes, p.cols);
+      const uint64_t ring_desc = smem_desc(smem_u32(ring), 16, 1024, 2);
+      const uint32_t sums = __shfl_sync(0xffffffffu, tmem, 0);  // (of shared memory: the same in each lane)
       int s = 0;
       uint32_t turn = 0;
 #pragma unroll 1
       for (int q = 0; q < total; ++q) {
         const int b = q % kSums;
-        if ((q >= kSums && !mbar_wait_soon(&sh.sum_empty[b], (uint32_t)(q / kSums - 1) & 1u)) || !mbar_wait_soon(&sh.full[s], turn & 1u)) {
+        const bool good = (q < kSums || mbar_wait_soon(&sh.sum_empty[b], (uint32_t)(q / kSums - 1) & 1u)) && mbar_wait_soon(&sh.full[s], turn & 1u);
+        if (!__all_sync(0xffffffffu, good)) {
           sh.dead = 1;
           break;
         }
         tc_fence_after();
-        const uint64_t ad = smem_desc(smem_u32(ring + s * stage_bytes), 16, 1024, 2);
-        const uint64_t bd = smem_desc(smem_u32(ring + s * stage_bytes + kABytes), 16, 1024, 2);
+        if (elect_one()) {
+          const uint64_t ad = ring_desc + (uint64_t)((uint32_t)(s * stage_bytes) >> 4), bd = ad + (kABytes >> 4);
 #pragma unroll
-        for (int i = 0; i < kStep / 32; ++i) {
-          if (kPair) umma_e4m3_pair(tmem + b * NT, ad + 2 * i, bd + 2 * i, idesc, i > 0);
-          else umma_e4m3(tmem + b * NT, ad + 2 * i, bd + 2 * i, idesc, i > 0);
+          for (int i = 0; i < kStep / 32; ++i) {
+            if (kPair) umma_e4m3_pair(sums + b * NT, ad + 2 * i, bd + 2 * i, idesc, i > 0);
+            else umma_e4m3(sums + b * NT, ad + 2 * i, bd + 2 * i, idesc, i > 0);
+          }
+          if (kPair) {
+            umma_commit_pair(&sh.sum_full[b]);
+            umma_commit_pair(&sh.empty[s]);
+          } else {
+            umma_commit(&sh.sum_full[b]);
+            umma_commit(&sh.empty[s]);
+          }
         }
-        if (kPair) {
-          umma_commit_pair(&sh.sum_full[b]);
-          umma_commit_pair(&sh.empty[s]);
-        } else {
-          umma_commit(&sh.sum_full[b]);
-          umma_commit(&sh.empty[s]);
-        }
+        __syncwarp();
         if (++s == p.stages) {
           s = 0;
           ++turn;
@@ -599,7 +610,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     if (threadIdx.x == 0 && p.dev_status) atomicOr(p.dev_status, RGD_DEV_WAIT_TIMEOUT);
     if (!kPair || rank == 0)  // (which counts both CTAs' copies)
       for (int i = max(0, issued - p.stages); i < issued; ++i) mbar_wait(&sh.full[i % p.stages], (uint32_t)(i / p.stages) & 1u);
-    if (warp == kIssuer && lane == 0 && (!kPair || rank == 0)) {
+    if (warp == kIssuer && (!kPair || rank == 0) && elect_one()) {  // (the lane that issued)
       if (kPair) umma_commit_pair(&sh.drained);
       else umma_commit(&sh.drained);
       mbar_wait(&sh.drained, 0);
