@@ -135,20 +135,17 @@ __device__ __forceinline__ void send_box(const Fp8Params& p, const CUtensorMap& 
   }
 }
 
-template <int NT>
-constexpr int kAdders = NT > 32 ? 256 : 128;  // threads that add up: two warps to 32 lanes, or one
-template <int NT>
-constexpr int kFp8Threads = kAdders<NT> + 128;
+// Threads that add up: a warp to 32 lanes, two from 33 columns on, and four where every sum has a factor of its own
+// (80 x 6144 x 4096: 13.0 us with four, 14.2 with two; 256 rows of x, whose sums have one: 17.8 and 16.6).
+template <int NT, bool kTurned>
+constexpr int kAdders = NT == 128 && kTurned ? 512 : NT > 32 ? 256 : 128;
+template <int NT, bool kTurned>
+constexpr int kFp8Threads = kAdders<NT, kTurned> + 128;
 
 __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b) {
   uint64_t r;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
-}
-template <int N>
-__device__ __forceinline__ void tmem_load(uint32_t from, uint32_t (&r)[N]) {
-  if constexpr (N == 32) tmem_ld32(from, r);
-  else tmem_ld16(from, r);
 }
 // Waits for all loads; those into r and s are not read before.
 template <int N>
@@ -171,12 +168,12 @@ __device__ __forceinline__ void copy_async4(float* dst, const float* src, bool o
 // that a value that is copied takes part in half as many copies again (48 KB a step by one CTA,
 // 32 by each of two), and the tensor cores read it from both CTAs' memory.
 template <int NT, bool kTurned, bool kPair>
-__global__ void __launch_bounds__(kFp8Threads<NT>, 1)
+__global__ void __launch_bounds__(kFp8Threads<NT, kTurned>, 1)
     fp8_kernel(const Fp8Params p, const __grid_constant__ CUtensorMap amap, const __grid_constant__ CUtensorMap bmap,
                const __grid_constant__ CUtensorMap ymap) {
   static_assert(!kPair || (NT == 256 && !kTurned), "");
-  constexpr int kOwn = NT / (kAdders<NT> / 128);  // columns of a thread
-  constexpr int kProducer = kAdders<NT> / 32, kIssuer = kProducer + 1, kScaler = kProducer + 2;
+  constexpr int kOwn = NT / (kAdders<NT, kTurned> / 128);  // columns of a thread
+  constexpr int kProducer = kAdders<NT, kTurned> / 32, kIssuer = kProducer + 1, kScaler = kProducer + 2;
   constexpr int kSums = 512 / NT < kMostSums ? 512 / NT : kMostSums;  // accumulators
   constexpr uint32_t kTmemCols = kSums * NT;
   constexpr int kRows = kTurned ? NT : kLanes;  // x's rows of a tile
@@ -184,7 +181,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
   __shared__ Fp8Shared sh;
   __shared__ __align__(16) float x_scale[kScaleSlots * kScaleSteps][kRows];
   __shared__ float w_scale[kScaleSlots * kScaleSteps][2];
-  __shared__ uint32_t stage[kTurned || kPair ? 1 : kAdders<NT> * kStageWords];
+  __shared__ uint32_t stage[kTurned || kPair ? 1 : kAdders<NT, kTurned> * kStageWords];
   uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
   uint8_t* out = ring + (kPair ? p.stages * (kABytes + 128 * kStep) : 0);  // boxes on their way to y
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -218,11 +215,11 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     }
     for (int i = 0; i < kSums; ++i) {
       mbar_init(&sh.sum_full[i], 1);
-      mbar_init(&sh.sum_empty[i], kAdders<NT> / 32 * (kPair ? 2 : 1));
+      mbar_init(&sh.sum_empty[i], kAdders<NT, kTurned> / 32 * (kPair ? 2 : 1));
     }
     for (int i = 0; i < kScaleSlots; ++i) {
       mbar_init(&sh.scale_full[i], 1);
-      mbar_init(&sh.scale_empty[i], kAdders<NT> / 32);
+      mbar_init(&sh.scale_empty[i], kAdders<NT, kTurned> / 32);
     }
     mbar_init(&sh.drained, 1);
     fence_mbar_init();
@@ -375,30 +372,41 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     __syncwarp();
   } else {
     if (NT > 128) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
-    const int half = warp >> 2, row = (warp & 3) * 32 + lane;  // of the tile's columns; the lane's row of A
-    // Its columns, in whole 16s: of a tile that is not full, each half of the warps has about half.
-    const int off = half * (kTurned ? min((p.cols / 2 + 15) / 16 * 16, kOwn) : kOwn);
-    const int mine = !kTurned ? kOwn : kAdders<NT> == 128 || half ? p.cols - off : (p.cols / 2 + 15) / 16 * 16;
+    const int part = warp >> 2, row = (warp & 3) * 32 + lane;  // of the tile's columns; the lane's row of A
+    // Of w's rows as lanes, the warps' shares of the columns are whole 16s (the last ones may have none).
+    constexpr int kParts = kAdders<NT, kTurned> / 128;
+    const int each = kTurned ? min((p.cols / kParts + 15) / 16 * 16, kOwn) : kOwn, off = part * each;
+    const int mine = kTurned ? max(0, min(each, p.cols - off)) : kOwn;
     const uint32_t at_tmem = tmem + ((uint32_t)(warp & 3) << 21) + off;
     const uint32_t free_sum = kPair ? mapa_u32(smem_u32(&sh.sum_empty[0]), 0) : 0;
     uint64_t acc[kOwn / 2];
 #pragma unroll
     for (int i = 0; i < kOwn / 2; ++i) acc[i] = 0;
-    // A step's sums come in chunks of columns: two together, the next two while these are added; one by
-    // one where two tiles' worth of registers hold sums (80 x 6144 x 4096: 14.9 us so, 16.4 one by one;
-    // 8192 x 14336 x 4096: 393 us one by one, 566 two together).
+    // A step's sums come in chunks.  x's rows as lanes: 32 columns of the thread's own lane at a time, the next while
+    // these are added; two together where there are no more (all of a pair's two together: 566 us for 8192 x 14336 x
+    // 4096, 393 so).  w's rows as lanes: a column has a factor of its own, and a thread that has all columns of one
+    // lane reads as many factors as sums; so 16 lanes' columns, two of each 8, are spread over the warp, and four pairs
+    // of sums share two factors (80 x 128256 x 4096: 107 us so, 140 with 40 factors of 80 columns a thread).
     constexpr bool kTwo = kOwn < 128;
-    constexpr int kChunk = kOwn > 32 ? 32 : 16, kChunks = kOwn / kChunk;
-    const int last = (mine + kChunk - 1) / kChunk - 1;
+    constexpr int kChunk = kTurned ? 16 : 32, kChunks = kOwn / kChunk;
+    static_assert(kTurned ? kChunks == 2 : !kTwo || kChunks == 2, "");
+    auto spread_col = [&](int i) { return i % (kOwn / 4) / 2 * 8 + 2 * (lane & 3); };  // of pair i of sums
+    auto spread_lane = [&](int i) { return i / (kOwn / 4) * 16 + i % 2 * 8 + (lane >> 2); };
     int tile = (int)tile0, at = 0;
 #pragma unroll 1
     for (int q = 0; q < total; ++q) {
       const int b = q % kSums, slot = q % (kScaleSlots * kScaleSteps), chunk = q / kScaleSteps;
       bool good = true;
       if (q % kScaleSteps == 0) good = mbar_wait_soon(&sh.scale_full[chunk % kScaleSlots], (uint32_t)(chunk / kScaleSlots) & 1u);
-      const float sw = w_scale[slot][kTurned ? 0 : half * kOwn / 128];
+      const float sw = w_scale[slot][kTurned ? 0 : part * kOwn / 128];
       const float own = kTurned ? sw : sw * x_scale[slot][row];
       const uint64_t by = pair2(own, own);
+      uint64_t factors[kTurned ? kOwn / 8 : 1];  // of the thread's columns (one pair for four of sums)
+      if (kTurned) {
+#pragma unroll
+        for (int g = 0; g < kOwn / 8; ++g)
+          factors[g] = mul_pair(by, *reinterpret_cast<const uint64_t*>(&x_scale[slot][off + 8 * g + 2 * (lane & 3)]));
+      }
       const uint32_t parity = (uint32_t)(q / kSums) & 1u;
       good = mbar_wait_soon(&sh.sum_full[b], parity) && good;
       if (!__all_sync(0xffffffffu, good)) {
@@ -410,18 +418,9 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       const uint32_t from = at_tmem + b * NT;
       auto add = [&](int c) {
 #pragma unroll
-        for (int i = 0; i < kChunk / 2; i += 2) {
-          uint64_t f[2] = {by, by};
-          if (kTurned) {
-            const ulonglong2 of = *reinterpret_cast<const ulonglong2*>(&x_scale[slot][off + c * kChunk + 2 * i]);
-            f[0] = mul_pair(by, of.x);
-            f[1] = mul_pair(by, of.y);
-          }
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint64_t v = (uint64_t)d[c & 1][2 * (i + j) + 1] << 32 | d[c & 1][2 * (i + j)];
-            acc[c * (kChunk / 2) + i + j] = fma_pair(v, f[j], acc[c * (kChunk / 2) + i + j]);
-          }
+        for (int i = 0; i < kChunk / 2; ++i) {
+          const uint64_t v = (uint64_t)d[c & 1][2 * i + 1] << 32 | d[c & 1][2 * i];
+          acc[c * (kChunk / 2) + i] = fma_pair(v, kTurned ? factors[i / 2] : by, acc[c * (kChunk / 2) + i]);
         }
       };
       auto release = [&]() {
@@ -432,26 +431,23 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
           else mbar_arrive(&sh.sum_empty[b]);
         }
       };
-      tmem_load(from, d[0]);
-      if (kTwo && last >= 1) tmem_load(from + kChunk, d[1]);
+      if constexpr (kTurned) {
+        tmem_ld16_rows16(from, d[0]);
+        tmem_ld16_rows16(from + (16u << 16), d[1]);
+      } else {
+        tmem_ld32(from, d[0]);
+        if (kTwo) tmem_ld32(from + kChunk, d[1]);
+      }
+      if constexpr (kTwo) {
+        tmem_load_wait(d[0], d[1]);
+        release();
+        add(0);
+        add(1);
+      } else {
 #pragma unroll
-      for (int c = 0; c < kChunks; c += kTwo ? 2 : 1) {
-        if (c > last) break;
-        if (kTwo) {
-          tmem_load_wait(d[0], d[1]);
-          if (c + 2 < kChunks && c + 2 <= last) {
-            add(c);
-            tmem_load(from + (c + 2) * kChunk, d[0]);
-            add(c + 1);
-            if (c + 3 < kChunks && c + 3 <= last) tmem_load(from + (c + 3) * kChunk, d[1]);
-          } else {
-            release();
-            add(c);
-            if (c + 1 < kChunks && c + 1 <= last) add(c + 1);
-          }
-        } else {
+        for (int c = 0; c < kChunks; ++c) {
           tmem_load_wait(d[c & 1], d[c & 1]);
-          if (c + 1 < kChunks && c + 1 <= last) tmem_load(from + (c + 1) * kChunk, d[(c + 1) & 1]);
+          if (c + 1 < kChunks) tmem_ld32(from + (c + 1) * kChunk, d[(c + 1) & 1]);
           else release();
           add(c);
         }
@@ -469,32 +465,43 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
       const int64_t b0 = (int64_t)tb * p.cols + off;
       tile += (int)tile_step;
       if (!kPair && p.split > 1) {  // (the ring is free: every copy has been read)
-        float* part = reinterpret_cast<float*>(ring) + (kTurned ? off * kLanes + row : row * kPartRow<NT> + off);
+        if (kTurned) {
 #pragma unroll
-        for (int i = 0; i < kOwn / 4; ++i) {
-          if (4 * i >= mine) break;
-          float v[4];
-          unpair2(acc[2 * i], v[0], v[1]);
-          unpair2(acc[2 * i + 1], v[2], v[3]);
-          if (kTurned) {
+          for (int i = 0; i < kOwn / 2; ++i) {
+            const int col = spread_col(i);
+            if (col >= mine) continue;
+            float v[2];
+            unpair2(acc[i], v[0], v[1]);
+            float* to = reinterpret_cast<float*>(ring) + (off + col) * kPartRow<kLanes> + (warp & 3) * 32 + spread_lane(i);
+            to[0] = v[0];
+            to[kPartRow<kLanes>] = v[1];
+          }
+        } else {
+          float* to = reinterpret_cast<float*>(ring) + row * kPartRow<NT> + off;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) part[(4 * i + j) * kLanes] = v[j];
-          } else {
-            reinterpret_cast<float4*>(part)[i] = make_float4(v[0], v[1], v[2], v[3]);
+          for (int i = 0; i < kOwn / 4; ++i) {
+            if (4 * i >= mine) break;
+            float v[4];
+            unpair2(acc[2 * i], v[0], v[1]);
+            unpair2(acc[2 * i + 1], v[2], v[3]);
+            reinterpret_cast<float4*>(to)[i] = make_float4(v[0], v[1], v[2], v[3]);
           }
         }
         break;
       }
       const int es = p.out_f32 ? 4 : 2;
       if (kTurned) {
-        const int count = a0 < p.n ? (int)min((int64_t)mine, p.m - b0) : 0;
-        uint8_t* to = p.y + (b0 * p.y_stride + a0) * es;
+        const int count = (int)min((int64_t)mine, p.m - b0);
+        const int64_t lane0 = a0 - lane;  // the warp's first row of w
 #pragma unroll
         for (int i = 0; i < kOwn / 2; ++i) {
+          const int col = spread_col(i);
+          const int64_t n = lane0 + spread_lane(i);
           float v[2];
           unpair2(acc[i], v[0], v[1]);
+          uint8_t* to = p.y + ((b0 + col) * p.y_stride + n) * es;
 #pragma unroll
-          for (int j = 0; j < 2; ++j, to += p.y_stride * es) put_if(2 * i + j < count, to, p.out_f32, v[j]);
+          for (int j = 0; j < 2; ++j) put_if(n < p.n && col + j < count, to + j * p.y_stride * es, p.out_f32, v[j]);
         }
       } else if (kPair) {
         // 128 bytes of each of the warp's rows make a box, which TMA writes while the next is filled.
@@ -574,12 +581,12 @@ __global__ void __launch_bounds__(kFp8Threads<NT>, 1)
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     // Of a CTA: some of w's lanes' columns, or of x's lanes.  Four sums at once, of every CTA together.
-    const int lines = kTurned ? p.cols : kLanes, line = kTurned ? kLanes : NT, pitch = kTurned ? kLanes : kPartRow<NT>;
+    const int lines = kTurned ? p.cols : kLanes, line = kTurned ? kLanes : NT, pitch = kPartRow<kTurned ? kLanes : NT>;
     const int l0 = lines * (int)rank / p.split, l1 = lines * (int)(rank + 1) / p.split;
     int ta, tb;
     tile_at(p, (int)tile0, ta, tb);
     const int64_t a0 = (int64_t)ta * kLanes, b0 = (int64_t)tb * p.cols;
-    for (int e = threadIdx.x; e < (l1 - l0) * (line / 4); e += kFp8Threads<NT>) {
+    for (int e = threadIdx.x; e < (l1 - l0) * (line / 4); e += kFp8Threads<NT, kTurned>) {
       const int at = l0 + e / (line / 4), x = e % (line / 4) * 4;
       const uint32_t from = smem_u32(reinterpret_cast<float*>(ring) + at * pitch + x);
       float4 v[kMostSplit];
@@ -671,8 +678,8 @@ template <int NT, bool kTurned, bool kPair = false>
 int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t st) {
   static std::atomic<bool> done[kMaxDevices];
   auto k = fp8_kernel<NT, kTurned, kPair>;
-  constexpr int fixed = kScaleSlots * kScaleSteps * 4 * (kTurned ? NT : kLanes) + (kTurned || kPair ? 0 : kAdders<NT> * kStageWords * 4) + 1024;
-  constexpr int boxes = kPair ? kAdders<NT> / 32 * kBox : 0;
+  constexpr int fixed = kScaleSlots * kScaleSteps * 4 * (kTurned ? NT : kLanes) + (kTurned || kPair ? 0 : kAdders<NT, kTurned> * kStageWords * 4) + 1024;
+  constexpr int boxes = kPair ? kAdders<NT, kTurned> / 32 * kBox : 0;
   constexpr int room = kRoom - fixed - boxes;
   if (int rc = ensure_smem(k, room + boxes + 1024, done)) return rc;
   p.cols = kTurned ? (p.m + 15) / 16 * 16 : NT;
@@ -700,7 +707,7 @@ int launch_fp8(const char* fn, Fp8Params& p, const Fp8Operands& o, cudaStream_t 
                               p.y_stride * (p.out_f32 ? 4 : 2), p.out_f32 ? 32 : 64, 32)) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kFp8Threads<NT>);
+  cfg.blockDim = dim3(kFp8Threads<NT, kTurned>);
   cfg.dynamicSmemBytes = (size_t)p.stages * stage + boxes + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
