@@ -4,7 +4,7 @@
 //
 // Bound by bytes: values are read once and stay in registers while their block's largest is
 // found.  Eight lanes hold a row's 128 columns, 16 each: whole 16-byte stores, three shuffles
-// a block.
+// a block.  16384 x 14336 bf16: 114 us, 6.2 TB/s, 0.92 of what a copy reaches; 80 x 4096: 1.5 us.
 #include <cuda_bf16.h>
 
 #include "common.h"

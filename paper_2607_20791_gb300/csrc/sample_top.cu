@@ -18,6 +18,11 @@
 //     next range, until what it holds fits the list or is one value.  Then a pass for the kept
 //     tokens' sums by warp, and one warp finds the token.
 // No sorting of whole rows, no limit on k or on how flat a row is.
+//
+// Measured: 80 rows of 128256 bf16 with the usual filters 20 us, 512 of 152064 with filters of all
+// kinds 126 us, 5 of 32001 fp32 with top-p alone 36 us.  A row's stages follow one another, and
+// the first CTA works while the others of its cluster wait: neither HBM (15 % of its rate in the
+// second case) nor the instructions bound it.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -211,6 +211,34 @@ def test_same_result_every_time(gpu_lib, rows, vocab, dtype):
     assert int(wrong.item()) == 0
 
 
+def test_two_calls_at_once(gpu_lib):
+    """On streams of their own, beside a product whose blocks want the same SMs."""
+    import torch
+    sides = [torch.cuda.Stream() for _ in range(3)]
+    rng = np.random.default_rng(21)
+    cases = []
+    for rows, vocab, dtype in ((80, 128256, "bf16"), (200, 5931, "f32")):
+        t, k, p, m, u = (torch.as_tensor(a, device="cuda") for a in _params(rows, rng))
+        out = [torch.zeros(rows, dtype=d, device="cuda") for d in (torch.int32, torch.int32, torch.float32)]
+        cases.append((_logits(rows, vocab, "zipf", dtype, rows).cuda(), None, t, k.int(), p, m, u, None, *out))
+    x, w = (torch.randint(0, 0x70, (r, 1024), device="cuda", dtype=torch.uint8) for r in (1000, 4000))
+    product = (x, torch.rand(1000, 8, device="cuda"), w, torch.rand(32, 8, device="cuda"), torch.empty(1000, 4000, device="cuda"))
+    calls = [(binding.rgd_sample_top, c, c[-3:]) for c in cases] + [(binding.rgd_fp8_matmul, product, product[-1:])]
+    alone = []
+    for call, args, out in calls:
+        call(*args)
+        alone.append([o.clone() for o in out])
+        for o in out:
+            o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for side, (call, args, _) in zip(sides, calls):
+            call(*args, stream=side)
+    torch.cuda.synchronize()
+    for (_, _, out), want in zip(calls, alone):
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
 def test_strided_rows_stream_and_graph(gpu_lib):
     import torch
     side = torch.cuda.Stream()
