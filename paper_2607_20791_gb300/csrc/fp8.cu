@@ -403,23 +403,37 @@ __global__ void __launch_bounds__(kFp8Threads<NT, kTurned>, 1)
     static_assert(kTurned ? kChunks == 2 : !kTwo || kChunks == 2, "");
     auto spread_col = [&](int i) { return i % (kOwn / 4) / 2 * 8 + 2 * (lane & 3); };  // of pair i of sums
     auto spread_lane = [&](int i) { return i / (kOwn / 4) * 16 + i % 2 * 8 + (lane >> 2); };
+    // With factors a step's scales are read while the sums of the step before are on their way (13.0 and 102 us
+    // for 13.3 and 107; without, as lanes' scales are, that takes longer, and so does any branch between a load of
+    // sums and its wait).
+    uint64_t scales[kTurned ? kOwn / 8 : 1];  // of the thread's columns
+    float block_scale = 0.f;
+    auto read_scales = [&](int slot) {
+      block_scale = w_scale[slot][0];
+#pragma unroll
+      for (int g = 0; g < kOwn / 8; ++g) scales[g] = *reinterpret_cast<const uint64_t*>(&x_scale[slot][off + 8 * g + 2 * (lane & 3)]);
+    };
+    auto wait_scales = [&](int chunk) {
+      return mbar_wait_soon(&sh.scale_full[chunk % kScaleSlots], (uint32_t)(chunk / kScaleSlots) & 1u);
+    };
+    bool good = !kTurned || wait_scales(0);
+    if constexpr (kTurned) read_scales(0);
     int tile = (int)tile0, at = 0;
 #pragma unroll 1
     for (int q = 0; q < total; ++q) {
       const int b = q % kSums, slot = q % (kScaleSlots * kScaleSteps), chunk = q / kScaleSteps;
-      bool good = true;
-      if (q % kScaleSteps == 0) good = mbar_wait_soon(&sh.scale_full[chunk % kScaleSlots], (uint32_t)(chunk / kScaleSlots) & 1u);
-      const float sw = w_scale[slot][kTurned ? 0 : part * kOwn / 128];
-      const float own = kTurned ? sw : sw * x_scale[slot][row];
-      const uint64_t by = pair2(own, own);
-      uint64_t factors[kTurned ? kOwn / 8 : 1];  // of the thread's columns (one pair for four of sums)
-      if (kTurned) {
+      uint64_t by, factors[kTurned ? kOwn / 8 : 1];
+      if constexpr (kTurned) {
+        const uint64_t block = pair2(block_scale, block_scale);
 #pragma unroll
-        for (int g = 0; g < kOwn / 8; ++g)
-          factors[g] = mul_pair(by, *reinterpret_cast<const uint64_t*>(&x_scale[slot][off + 8 * g + 2 * (lane & 3)]));
+        for (int g = 0; g < kOwn / 8; ++g) factors[g] = mul_pair(block, scales[g]);
+      } else {
+        good = q % kScaleSteps != 0 || wait_scales(chunk);
+        const float own = w_scale[slot][part * kOwn / 128] * x_scale[slot][row];
+        by = pair2(own, own);
       }
-      const uint32_t parity = (uint32_t)(q / kSums) & 1u;
-      good = mbar_wait_soon(&sh.sum_full[b], parity) && good;
+      good = mbar_wait_soon(&sh.sum_full[b], (uint32_t)(q / kSums) & 1u) && good;
+      if (kTurned && (q + 1) % kScaleSteps == 0 && q + 1 < total) good = wait_scales(chunk + 1) && good;
       if (!__all_sync(0xffffffffu, good)) {
         sh.dead = 1;
         break;
@@ -445,6 +459,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT, kTurned>, 1)
       if constexpr (kTurned) {
         tmem_ld16_rows16(from, d[0]);
         tmem_ld16_rows16(from + (16u << 16), d[1]);
+        read_scales((q + 1) % (kScaleSlots * kScaleSteps));  // (behind the last step: what is there, unused)
       } else {
         tmem_ld32(from, d[0]);
         if (kTwo) tmem_ld32(from + kChunk, d[1]);
