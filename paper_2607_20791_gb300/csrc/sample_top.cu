@@ -948,6 +948,9 @@ int launch_top(TopParams& p, cudaStream_t st) {
   int c = 1;
   while (c < kTopCluster && (stripes(c) > 32 || (int64_t)stripes(c) * kTopWarps * 32 * (16 / (int)sizeof(T)) > 65536)) c *= 2;
   while (c < 8 && (int64_t)p.rows * c < 608 && stripes(2 * c) >= 4) c *= 2;
+  // A row whose cut is searched for takes several times as long as the others, so that four CTAs pay for up to 3.5
+  // rounds of them (512 x 128256 bf16, two and four: filters of all kinds 166 and 109 us, the usual ones 45 and 50).
+  if (c == 2 && p.rows <= 532 && stripes(4) >= 8) c = 4;
   while (c < kTopCluster && (int64_t)p.rows * c < 304 && stripes(c) > 4) c *= 2;
   if (c > 8) {
     int dev = 0;
