@@ -86,6 +86,7 @@ struct TopShared {
   uint64_t scan[kTopWarps];
   uint32_t lo[kBins], hi[kBins];  // sums of the weights' low 16 bits and of the rest, or counts
   uint32_t listed;                // tokens that belong into the list
+  uint32_t list_from;             // where this CTA's go in the first one's
   Order order;
   float theta;
   int found;
@@ -194,6 +195,30 @@ __device__ __forceinline__ void visit(const Share<T, kAligned>& v, const Kept& k
     }
   }
   f(kept.rest, v.whole);
+}
+
+// The same with code for one vector alone, two on their way.  (A range's pass, unrolled four times, does not
+// stay in the instruction cache: 45 us of a row of 152064 among 512, 29 so.)
+template <typename T, bool kAligned, typename F>
+__device__ __forceinline__ void visit_each(const Share<T, kAligned>& v, const Kept& kept, float bound, int stripes, int lane, F&& f) {
+  using V = Vec<T>;
+  Walk walk(groups_reaching(kept, bound), stripes, v.whole, lane);
+  int i = walk.next(), i1 = walk.next();
+  uint4 w = V::nothing(), w1 = w;
+  if (i >= 0) w = v.get(i);
+  if (i1 >= 0) w1 = v.get(i1);
+#pragma unroll 1
+  for (;;) {
+    const int i2 = walk.next();
+    uint4 w2 = V::nothing();
+    if (i2 >= 0) w2 = v.get(i2);
+    const bool end = i < 0;
+    if (end) w = kept.rest;
+    f(w, end ? v.whole : i);
+    if (end) break;
+    w = w1, w1 = w2;
+    i = i1, i1 = i2;
+  }
 }
 
 // Sorts the first n = 256 R numbers or fewer (a power of two from 32 on) of a list in shared memory,
@@ -463,19 +488,31 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
   const uint32_t top_key = key_of<T>(side.top);
 
   const uint32_t list_count = peer_addr(smem_u32(&sh.listed), 0), list_at = peer_addr(smem_u32(&sh.list[0]), 0);
-  // (the lanes that come together count together; a lane that has seen the list full adds no more:
-  // the count is above kList then)
+  // Every CTA lists its own tokens, and what the others have listed then goes to the first one together (a count
+  // there for each token's sake takes 0.5 us a token and warp).  The lanes that come together count together; a
+  // lane that has seen the list full adds no more: the count is above kList then.
   bool full = false;
   auto enlist = [&](float l, uint32_t index) {
     if (full) return;
     const uint32_t with = __activemask();
     const int first = __ffs(with) - 1;
     uint32_t at = 0;
-    if (lane == first)
-      asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(at) : "r"(list_count), "r"(__popc(with)) : "memory");
+    if (lane == first) at = atomicAdd(&sh.listed, __popc(with));
     at = __shfl_sync(with, at, first) + __popc(with & ((1u << lane) - 1));
-    if (at < kList) store_peer(list_at + 8 * at, (uint64_t)key_of<T>(l) << 32 | (uint32_t)~index);
+    if (at < kList) sh.list[at] = (uint64_t)key_of<T>(l) << 32 | (uint32_t)~index;
     else full = true;
+  };
+  auto hand_over = [&]() {
+    if (rank == 0) return;
+    __syncthreads();
+    const uint32_t n = sh.listed;
+    if (n == 0) return;
+    if (threadIdx.x == 0)
+      asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(sh.list_from) : "r"(list_count), "r"(n) : "memory");
+    __syncthreads();
+    const uint32_t to = sh.list_from;
+    for (uint32_t i = threadIdx.x; i < n && to + i < kList; i += kTopThreads) store_peer(list_at + 8 * (to + i), sh.list[i]);
+    if (threadIdx.x == 0) sh.listed = 0;
   };
   // Every CTA's sum and count into every CTA.
   auto exchange = [&](uint64_t sum, uint32_t count, uint32_t larger) {
@@ -552,6 +589,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
         enlist(elem<T>(w, e), (uint32_t)e0 + i * E + e);
       }
     });
+    hand_over();
     exchange(k ? 0 : warp_sum(sum.total()), 0, 0);
     if (rank == 0) {
       total = sum_all();
@@ -665,6 +703,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
       // Counts of few values meet at the same places: lanes take turns over four sets of bins.
       const bool counts = by_count || shift == 0;  // (of a value, the count tells the mass)
       const bool apart = counts && !list;
+      const bool masses = !by_count || cut_mass;
       __syncthreads();
       if (apart)
         for (int i = threadIdx.x; i < kCopies * kCopyPitch; i += kTopThreads) (&sh.copies[0][0])[i] = 0;
@@ -673,10 +712,10 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
       WholeSum over;
       full = false;
       uint32_t count = 0;
-      visit(v, kept, in_range, p.stripes, lane, [&](const uint4& w, int i) {
+      visit_each(v, kept, in_range, p.stripes, lane, [&](const uint4& w, int i) {
         if (from) {
-          add_weights<T>(w, side, typename V::Bound(above), over);
-          count += __popc(elements_in<T>(w, above, INFINITY));
+          if (masses) add_weights<T>(w, side, typename V::Bound(above), over);
+          if (by_count) count += __popc(elements_in<T>(w, above, INFINITY));
         }
         auto add = [&](float l, uint32_t key, uint32_t times) {
           const uint32_t b = (top_key - key - from) >> shift;
@@ -711,6 +750,7 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
         for (int i = threadIdx.x; i < kBins; i += kTopThreads)
           for (int c = 0; c < kCopies; ++c) sh.lo[i] += sh.copies[c][i];
       }
+      if (list) hand_over();
       exchange(warp_sum(over.total()), __reduce_add_sync(0xffffffffu, count), 0);
       if (rank == 0) {
         const uint64_t mass = sum_all();
