@@ -569,26 +569,44 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
     WholeSum sum;
     const float scale = side.kexp;
     // (What few tokens need is done one token after another, in code that is there once: unrolled
-    // into the stream of vectors it took seven times as long as the sums.)
+    // into the stream of vectors it took seven times as long as the sums.  And where all vectors are
+    // streamed, only after it, for the vectors of a lane that reach the bound: two warps in three have
+    // one among 32, a lane one in 30.)
     const typename V::Bound at_bound(bound);
-    visit(v, kept, sampled ? side.cut : bound, p.stripes, lane, [&](const uint4& w, int i) {
-      if (!k) add_weights<T>(w, side, typename V::Bound(side.cut), sum);
-      if (sampled && ((i >> 5) & ((1 << kSampleShift) - 1)) == 0) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float l = elem<T>(w, e);
-          if (l >= side.cut && !(l >= bound))
-            atomicAdd(&sh.lo[octave_bin((side.top - l) * scale)], k ? 1u : whole_weight(side, l) >> 13);
-        }
-      }
-      if (!V::reaches(V::max_of(w, V::lowest()), at_bound)) return;
+    auto list_vector = [&](const uint4& w, int i) {
       uint32_t m = elements_in<T>(w, bound, INFINITY);
 #pragma unroll 1
       for (; m; m &= m - 1) {
         const int e = __ffs(m) - 1;
         enlist(elem<T>(w, e), (uint32_t)e0 + i * E + e);
       }
-    });
+    };
+    if (sampled) {
+      uint64_t hits = 0;  // the lane's stripes (64 at most)
+      visit(v, kept, side.cut, p.stripes, lane, [&](const uint4& w, int i) {
+        if (!k) add_weights<T>(w, side, typename V::Bound(side.cut), sum);
+        if (((i >> 5) & ((1 << kSampleShift) - 1)) == 0) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float l = elem<T>(w, e);
+            if (l >= side.cut && !(l >= bound))
+              atomicAdd(&sh.lo[octave_bin((side.top - l) * scale)], k ? 1u : whole_weight(side, l) >> 13);
+          }
+        }
+        if (i < v.whole && V::reaches(V::max_of(w, V::lowest()), at_bound)) hits |= 1ull << (i >> 5);
+      });
+      list_vector(kept.rest, v.whole);
+#pragma unroll 1
+      while (hits) {
+        const int i = (__ffsll(hits) - 1) * 32 + lane;
+        hits &= hits - 1;
+        list_vector(v.get(i), i);
+      }
+    } else {
+      visit_each(v, kept, bound, p.stripes, lane, [&](const uint4& w, int i) {
+        if (V::reaches(V::max_of(w, V::lowest()), at_bound)) list_vector(w, i);
+      });
+    }
     hand_over();
     exchange(k ? 0 : warp_sum(sum.total()), 0, 0);
     if (rank == 0) {
