@@ -100,7 +100,8 @@ def test_distributions(gpu_lib, rows, vocab, pad, kind, dtype):
     _check(_logits(rows, vocab, kind, dtype, rows, pad).cuda(), *_params(rows, rng), vocab=vocab, name=f"{rows} x {vocab} {dtype} {kind}")
 
 
-@pytest.mark.parametrize("rows, vocab, dtype", [(300, 5931, "bf16"), (700, 1000, "f32"), (150, 20000, "bf16"), (3, 500000, "f32"), (2, 1 << 20, "bf16")])
+@pytest.mark.parametrize("rows, vocab, dtype", [(300, 5931, "bf16"), (700, 1000, "f32"), (150, 20000, "bf16"), (3, 500000, "f32"), (2, 1 << 20, "bf16"),
+                                                (2, 1 << 20, "f32"), (310, 70001, "bf16")])
 def test_batches(gpu_lib, rows, vocab, dtype):
     rng = np.random.default_rng(rows)
     _check(_logits(rows, vocab, "zipf", dtype, 1).cuda(), *_params(rows, rng), name=f"{rows} x {vocab} {dtype}")
