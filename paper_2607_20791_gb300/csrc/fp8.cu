@@ -113,21 +113,37 @@ constexpr int kStageWords = 17;  // of a row: 16 and one that spreads rows over 
 template <int kSize>
 __device__ __forceinline__ void write_rows(const Fp8Params& p, const uint32_t* words, uint8_t* to, int rows, int count, int lane) {
   __syncwarp();
-  const int part = lane & 3;
-  const bool whole = p.vectors && (part + 1) * (16 / kSize) <= count;
+  if (p.vectors) {  // rows of y on 16 bytes
+    const int part = lane & 3;
+    const bool whole = (part + 1) * (16 / kSize) <= count;
 #pragma unroll 1
-  for (int r = lane >> 2; r < rows; r += 8) {
-    const uint32_t* w = words + r * kStageWords + part * 4;
-    uint8_t* at = to + r * p.y_stride * kSize + part * 16;
-    if (whole) {
-      *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
+    for (int r = lane >> 2; r < rows; r += 8) {
+      const uint32_t* w = words + r * kStageWords + part * 4;
+      uint8_t* at = to + r * p.y_stride * kSize + part * 16;
+      if (whole) {
+        *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
 #pragma unroll 1
-      for (int i = 0; i < 16 / kSize && part * (16 / kSize) + i < count; ++i) {
-        if (kSize == 4) reinterpret_cast<uint32_t*>(at)[i] = w[i];
-        else reinterpret_cast<uint16_t*>(at)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        for (int i = 0; i < 16 / kSize && part * (16 / kSize) + i < count; ++i) {
+          if (kSize == 4) reinterpret_cast<uint32_t*>(at)[i] = w[i];
+          else reinterpret_cast<uint16_t*>(at)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+        }
       }
     }
+  } else if (p.y_stride * kSize % 4 == 0) {  // on 4: words, lanes side by side (6860 x 7494 x 144, fp32: 73 us, 174 as above)
+    const int i = lane & 15, n = (i + 1) * (4 / kSize) - count;  // (elements of the word that are not y's)
+    uint8_t* at = to + (lane >> 4) * p.y_stride * kSize + i * 4;
+    const uint32_t* w = words + (lane >> 4) * kStageWords + i;
+#pragma unroll 4
+    for (int r = lane >> 4; r < rows; r += 2, at += 2 * p.y_stride * kSize, w += 2 * kStageWords) {
+      if (n <= 0) *reinterpret_cast<uint32_t*>(at) = *w;
+      else if (kSize == 2 && n == 1) *reinterpret_cast<uint16_t*>(at) = (uint16_t)*w;
+    }
+  } else {
+    uint8_t* at = to + lane * 2;
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r, at += p.y_stride * 2)
+      if (lane < count) *reinterpret_cast<uint16_t*>(at) = (uint16_t)(words[r * kStageWords + lane / 2] >> (16 * (lane & 1)));
   }
   __syncwarp();
 }
