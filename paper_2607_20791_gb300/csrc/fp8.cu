@@ -23,10 +23,10 @@
 //                                                         960 clocks, 640 if its sums are not read
 //   4096    4096 x 4096    61 us    2.25 PFLOP/s          the same
 //   200     128256 x 4096  111 us   4.7 TB/s of weights   the steps of 128 x 128 tiles
-//   80      128256 x 4096  107 us   4.9 TB/s              reading sums, a factor to each
+//   80      128256 x 4096  103 us   5.1 TB/s              adding sums, with factors of their own
 //   64      128256 x 4096  90 us    5.8 TB/s              weights
 //   16      128256 x 4096  92 us    5.7 TB/s              weights
-//   80      6144 x 4096    13.1 us  1.9 TB/s              16 steps one after another on 96 SMs, start and join
+//   80      6144 x 4096    12.9 us  2.0 TB/s              16 steps one after another on 96 SMs, start and join
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kFp8Threads<NT, kTurned>, 1)
     // these are added; two together where there are no more (all of a pair's two together: 566 us for 8192 x 14336 x
     // 4096, 393 so).  w's rows as lanes: a column has a factor of its own, and a thread that has all columns of one
     // lane reads as many factors as sums; so 16 lanes' columns, two of each 8, are spread over the warp, and four pairs
-    // of sums share two factors (80 x 128256 x 4096: 107 us so, 140 with 40 factors of 80 columns a thread).
+    // of sums share two factors (80 x 128256 x 4096: 107 us so, 140 with a factor of its own to each).
     constexpr bool kTwo = kOwn < 128;
     constexpr int kChunk = kTurned ? 16 : 32, kChunks = kOwn / kChunk;
     static_assert(kTurned ? kChunks == 2 : !kTwo || kChunks == 2, "");

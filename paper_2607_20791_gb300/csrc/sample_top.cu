@@ -9,8 +9,8 @@
 // One cluster of CTAs a row, every warp with a contiguous share of it:
 //   1 the maximum, a stream from HBM; and a bound that enough tokens surely reach: a warp's
 //     r-th largest lane maximum, the smallest over all warps, is reached by r tokens of each;
-//   2 the tokens that reach the bound go into a list in the first CTA's shared memory (the
-//     row lies in L2 now, and only vectors whose group reaches the bound are read); top-p
+//   2 the tokens that reach the bound are listed, and the lists meet in the first CTA's shared
+//     memory (the row lies in L2 now, and only vectors whose group reaches the bound are read); top-p
 //     alone needs all the weights' sum as well.  The first CTA sorts the list.  Where k, or the
 //     mass p, lies within it the row is done: the usual case, two exchanges.
 //   3 else the cut is searched for: a range of logits, at first from a sample of the row, is
@@ -19,10 +19,11 @@
 //     tokens' sums by warp, and one warp finds the token.
 // No sorting of whole rows, no limit on k or on how flat a row is.
 //
-// Measured: 80 rows of 128256 bf16 with the usual filters 20 us, 512 of 152064 with filters of all
-// kinds 126 us, 5 of 32001 fp32 with top-p alone 36 us.  A row's stages follow one another, and
-// the first CTA works while the others of its cluster wait: neither HBM (15 % of its rate in the
-// second case) nor the instructions bound it.
+// Measured: 80 rows of 128256 bf16 with the usual filters 19 us, 512 of 152064 with filters of all
+// kinds 106 us, with top-p alone 158 us, 5 of 32001 fp32 with top-p alone 34 us.  A row's stages
+// follow one another, and the first CTA works while the others of its cluster wait: that bounds
+// few rows and rows whose list suffices (15 % of HBM in the second case); rows that are searched
+// are bound by the instructions for every token's weight and place, three times each.
 #include <cuda_bf16.h>
 
 #include <algorithm>
