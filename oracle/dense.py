@@ -7,9 +7,11 @@
   (sign, 4 bits of exponent with bias 7, 3 of mantissa, no infinities), block scales in
   fp32 as stated, products in fp64.
 * :func:`sample` -- temperature, min-p, top-k, top-p and a draw from a given uniform, token by
-  token over a sorted list.
+  token over a sorted list; :func:`admitted` -- which results the roundings of fp32 weights leave
+  open for a row, also where a cut or the draw lies next to its threshold.
 
-Pinned by ``tests/test_oracle_dense.py`` against closed forms and hand cases.
+Pinned by ``tests/test_oracle_dense.py`` and ``tests/test_oracle_thresholds.py`` against closed forms and hand
+cases.
 """
 from __future__ import annotations
 
@@ -149,3 +151,60 @@ def sample(row, temperature: float, top_k: int, top_p: float, min_p: float, u: f
     edges = upto[w > 0]
     near = near or bool(np.abs(edges - mark).min() <= band * upto[-1] or mark <= band * upto[-1])
     return Drawn(int(index[i]), len(order), float(w[i] / upto[-1]), near)
+
+
+class Admitted:
+    """What a row's kept count, token and probability may be, for weights that are rounded.
+
+    Exact weights w_i = 2^x_i, x_i = (l_i - top) log2(e) / T <= 0, the largest 1.  Rounded ones differ by at most
+      e_i = w_i (4 * 2^-24 ln 2 |x_i| + 2^-22) + 2^-32:
+    x's difference, quotient and product and its constant are rounded (four times 2^-24 of x), the power is good
+    to 2^-22, and the weight becomes a whole multiple of 2^-31.  A threshold is a share of one such sum, rounded to
+    a whole multiple, and is compared with another: both are off by the sum of S's e_i at most, and by 2^-31.
+    """
+
+    def __init__(self, row, temperature: float, top_k: int, top_p: float, min_p: float):
+        row = np.asarray(row, np.float32)
+        fine = np.where(np.isnan(row), np.float32(-np.inf), row)
+        top = fine.max()
+        low = sampling.cutoff32(top, temperature, min_p)
+        at = np.nonzero((fine >= low) & (fine > -np.inf))[0]
+        order = at[np.argsort(-fine[at], kind="stable")]  # (equal logits, 0 and -0 too, by index)
+        if top_k > 0:
+            order = order[:top_k]
+        self.order = order
+        x = (fine[order].astype(np.float64) - float(top)) / (float(np.float32(temperature)) * math.log(2))
+        self.w = np.exp2(x)
+        self.e = self.w * (4 * 2.0 ** -24 * math.log(2) * -x + 2.0 ** -22) + 2.0 ** -32
+        upto, slack = np.cumsum(self.w), 2 * self.e.sum() + 2.0 ** -30
+        self.fewest = self.most = len(order)
+        if top_p < 1:
+            want = float(np.float32(top_p)) * upto[-1]
+            # n tokens are kept if they reach the threshold and n - 1 do not
+            self.fewest = min(int(np.searchsorted(upto, want - slack)) + 1, len(order))
+            self.most = min(int(np.searchsorted(upto, want + slack)) + 1, len(order))
+
+    def fault(self, kept: int, token: int, prob: float, u: float) -> str:
+        """Why a result cannot be; empty if it can."""
+        if not self.fewest <= kept <= self.most:
+            return f"kept {kept}, not {self.fewest} to {self.most}"
+        back = np.argsort(self.order[:kept])
+        index, w, e = self.order[:kept][back], self.w[:kept][back], self.e[:kept][back]
+        i = int(np.searchsorted(index, token))
+        if i == kept or index[i] != token:
+            return f"token {token} is not kept"
+        if w[i] + e[i] < 2.0 ** -31:
+            return f"token {token} has no weight"
+        upto, slack = np.cumsum(w), 2 * e.sum() + 2.0 ** -30
+        mark = float(np.float32(u)) * upto[-1]
+        if not upto[i] - w[i] - slack <= mark <= upto[i] + slack:
+            return f"token {token} from {upto[i] - w[i]} to {upto[i]}, not at {mark}"
+        want = w[i] / upto[-1]
+        # (the weight and the sum as above, and three roundings of 2^-24: both to fp32, and the quotient)
+        off = e[i] / upto[-1] + want * (e.sum() / upto[-1] + 3 * 2.0 ** -24)
+        return "" if abs(prob - want) <= 1.01 * off else f"probability {prob}, not {want}"
+
+
+def admitted(row, temperature: float, top_k: int, top_p: float, min_p: float) -> Admitted:
+    """Of a row that is not greedy."""
+    return Admitted(row, temperature, top_k, top_p, min_p)
