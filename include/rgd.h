@@ -647,8 +647,10 @@ int rgd_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, doubl
  *   q_out, k_out   of the same dtype, token t's heads at t * q_out_stride (t * k_out_stride)
  *                  elements, the strides no less than a token's heads.  They may be q and k
  *                  themselves with the same strides, else must not overlap them
- * Sums and products are taken in fp32 and rounded once; angles are exact to 2^-32 of a turn
- * at any position.  No error is found on the device: dev_status is not written.  One kernel. */
+ * Sums and products are taken in fp32 and rounded once.  An angle is turns[i] times the
+ * position, modulo one turn in whole numbers, cut to 2^-32 of a turn and rounded to fp32 (2^-26
+ * of a turn at most), at any position.  No error is found on the device: dev_status is not
+ * written.  One kernel. */
 int rgd_qk_rope(const rgd_rope_shape* shape, int32_t tokens, int32_t dtype, const void* q, int64_t q_stride,
                 const void* k, int64_t k_stride, const int32_t* positions, const uint64_t* turns, int32_t weight_dtype,
                 const void* q_weight, const void* k_weight, void* q_out, int64_t q_out_stride, void* k_out,

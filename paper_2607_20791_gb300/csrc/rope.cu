@@ -5,8 +5,9 @@
 // rotated part apart.
 //
 // Angles.  A frequency is a fraction of a turn in 64 bits, so the position times it, modulo
-// 2^64, is the angle modulo one turn without any loss, however far the position (in fp32 a
-// position of 500000 would leave four decimals of it).  Its top 32 bits go to sincospif.
+// 2^64, is the angle modulo one turn without any loss, however far the position (an fp32 angle
+// of 500000 radians is good to 0.016).  Its top 32 bits go to sincospif as an fp32, rounded by
+// 2^-26 of a turn (1e-7 radians) at most.
 //
 // Bound by bytes: every value is read once and written once.  A lane holds two vectors of E
 // values whose pairs it can turn by itself: side by side for adjacent pairs, half the rotated
