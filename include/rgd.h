@@ -71,8 +71,9 @@ extern "C" {
 /* device status bits (ORed into *dev_status) */
 #define RGD_DEV_BAD_PAGE 1      /* block-table entry outside [0, num_pages): read as zeros */
 #define RGD_DEV_BAD_TOKEN 2     /* negative probe token that is not the stop token: skipped */
-#define RGD_DEV_WAIT_TIMEOUT 4  /* a bounded wait on a copy gave up; outputs of that block are missing */
-#define RGD_DEV_BAD_PARAM 8     /* temperature < 0 or not finite, min_p outside [0, 1], or non-finite logits max */
+#define RGD_DEV_WAIT_TIMEOUT 4  /* a bounded wait or search gave up; outputs of that block or row are missing */
+#define RGD_DEV_BAD_PARAM 8     /* temperature < 0 or not finite, min_p outside [0, 1], or non-finite logits max;
+                                 * else as the entry point says */
 #define RGD_DEV_NO_PAGE 16      /* the pool has fewer free pages than rgd_cache_reserve was asked for */
 
 /* logits element types */
@@ -740,7 +741,9 @@ int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x, int64_t x_
  *   prob_out     float [rows] or NULL: the token's weight over that of all kept tokens (1 in
  *                greedy rows, 0 in inactive and rejected ones)
  * NaN and -inf are never kept.  A row with a parameter out of range or a largest logit that is
- * not finite is rejected and sets RGD_DEV_BAD_PARAM.  Weights are rounded to multiples of 2^-31 and
+ * not finite is rejected and sets RGD_DEV_BAD_PARAM.  A row whose cut is not found within 64 passes gets the
+ * results of a rejected one and sets RGD_DEV_WAIT_TIMEOUT (21 passes are enough for any logits that
+ * are not written during the call).  Weights are rounded to multiples of 2^-31 and
  * summed exactly, and top_p's share is the smallest whole multiple not below top_p times the sum (rounded once in
  * FP64): the outputs are the same however a call is cut.  RGD_ERR_UNSUPPORTED above a vocab
  * of 2^20.  One kernel on `stream`. */

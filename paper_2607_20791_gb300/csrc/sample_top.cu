@@ -720,8 +720,9 @@ __global__ void __launch_bounds__(kTopThreads, 4) sample_top_kernel(const TopPar
     if (sh.order.next == kDone) return;
 
     // Pass 3, until the cut is found: what lies above the range, and in each of its parts.
-    // (A round leaves 1/512 of a range of less than 2^32, after one or two that find a sampled range
-    // wrong: no search takes kMostRounds.)
+    // (A round leaves 1/512 of a range of less than 2^32: four, and four more for the mass of what a count leaves.
+    // Before them, a sampled range that misses the cut is followed by one next to it, at least eight times as wide:
+    // eleven reach over every key.  No search of a row that stays as it is takes kMostRounds.)
     int rounds = 0;
 #pragma unroll 1
     while (sh.order.next == kRange) {
