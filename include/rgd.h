@@ -707,9 +707,10 @@ int rgd_fp8_quantize(int32_t rows, int32_t cols, int32_t dtype, const void* x, i
  *   w_scales  float [ceil(n / 128), ceil(k / 128)]
  *   y         [m] rows of n elements, y_stride elements apart (>= n; the rest of a row is
  *             left alone), out_dtype RGD_F32 or RGD_BF16
- * A block's products are exact and summed by the tensor core in fp32; the blocks' sums are
- * scaled and added in fp32 and the result is rounded once.  The order of the sums is the same
- * for every call of the same m, n and k.  dev_status gets RGD_DEV_WAIT_TIMEOUT when a bounded
+ * A block's products are exact and summed by the tensor core in fp32; a block's sum times the
+ * fp32 product of its two scales (which over- or underflows as such) is added in fp32, and the
+ * result is rounded once.  The order of the sums is the same for every call of the same m, n,
+ * k, out_dtype and y_stride.  dev_status gets RGD_DEV_WAIT_TIMEOUT when a bounded
  * wait gave up; y is then not valid.  k at most 2^24.  RGD_ERR_UNSUPPORTED above 2^30 rows of
  * either.  One kernel on `stream`. */
 int rgd_fp8_matmul(int32_t m, int32_t n, int32_t k, const uint8_t* x, int64_t x_stride, const float* x_scales,
