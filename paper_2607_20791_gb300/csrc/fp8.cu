@@ -17,16 +17,17 @@
 // Warps: the first 4, 8 or 16 add sums up, one copies tiles in by TMA, one issues the tensor
 // core's instructions, one fetches scales.
 //
-// Measured back to back (a copy runs at 6.75 TB/s, bf16 products at 1.93 PFLOP/s):
+// Measured back to back, with inputs that change (a copy runs at 6.75 TB/s, bf16 products at 1.93 PFLOP/s):
 //   x rows  n x k          time     rate                  bound by
-//   8192    14336 x 4096   372 us   2.6 PFLOP/s           reading sums: a pair's step of 256 x 256 x 128 takes
-//                                                         960 clocks, 640 if its sums are not read
-//   4096    4096 x 4096    61 us    2.25 PFLOP/s          the same
-//   200     128256 x 4096  111 us   4.7 TB/s of weights   the steps of 128 x 128 tiles
-//   80      128256 x 4096  103 us   5.1 TB/s              adding sums, with factors of their own
-//   64      128256 x 4096  90 us    5.8 TB/s              weights
-//   16      128256 x 4096  92 us    5.7 TB/s              weights
-//   80      6144 x 4096    12.9 us  2.0 TB/s              16 steps one after another on 96 SMs, start and join
+//   8192    14336 x 4096   387 us   2.49 PFLOP/s          reading sums: a pair's step of 256 x 256 x 128 takes
+//                                                         960 clocks, 640 if its sums are not read; at length
+//                                                         power (353 us for a short run over one set of inputs)
+//   4096    4096 x 4096    62 us    2.22 PFLOP/s          the same
+//   200     128256 x 4096  118 us   4.4 TB/s of weights   the steps of 128 x 128 tiles
+//   80      128256 x 4096  102 us   5.1 TB/s              adding sums, with factors of their own
+//   64      128256 x 4096  88 us    6.0 TB/s              weights
+//   16      128256 x 4096  88 us    6.0 TB/s              weights
+//   80      6144 x 4096    13.0 us  1.9 TB/s              16 steps one after another on 96 SMs, start and join
 #include <cuda_bf16.h>
 
 #include <algorithm>

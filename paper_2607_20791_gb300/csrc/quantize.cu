@@ -4,7 +4,9 @@
 //
 // Bound by bytes: values are read once and stay in registers while their block's largest is
 // found.  Eight lanes hold a row's 128 columns, 16 each: whole 16-byte stores, three shuffles
-// a block.  16384 x 14336 bf16: 114 us, 6.2 TB/s, 0.92 of what a copy reaches; 80 x 4096: 1.5 us.
+// a block.  16384 x 14336 bf16: 115 us, 6.1 TB/s, 0.91 of what a copy reaches; fp32: 166 us, 7.1 TB/s;
+// 80 x 4096: 1.5 us.  Blocks of 128 rows, 14336 x 4096: bf16 54 us, 3.3 TB/s, fp32 46 us, 6.3 TB/s.  Rows
+// off 16 bytes go value by value: 16384 x 14333 bf16 434 us.
 #include <cuda_bf16.h>
 
 #include "common.h"

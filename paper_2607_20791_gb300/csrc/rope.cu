@@ -16,11 +16,11 @@
 // spread over more warps, each with a share of the heads (and sines of its own).
 //
 // Measured: 16384 tokens of 32 + 8 heads of 128, normed, bf16: 62 us, 5.4 TB/s, 0.80 of what a
-// copy reaches; 16384 tokens of 32 + 8 + 8 heads, half turned, keys and values into pages: 68 us,
-// 4.8 TB/s (0.72).  Four loads a lane on their way are what that takes (three 63 us, two 62 to 65,
+// copy reaches, fp32 103 us, 6.5 TB/s (0.96); 16384 tokens of 32 + 8 + 8 heads, half turned, keys and
+// values into pages: 69 us, 4.8 TB/s (0.71).  Four loads a lane on their way are what that takes (three 63 us, two 62 to 65,
 // one 78), and the registers that the compiler wants for them: held to 102 for a fifth CTA on an
 // SM the prompt takes 62 us and the pages 76, held to 80 for a sixth 66 and 83.  Single steps are
-// latency: 80 rows 3.8 us.
+// latency: 80 rows 3.7 us.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -19,8 +19,9 @@
 //     tokens' sums by warp, and one warp finds the token.
 // No sorting of whole rows, no limit on k or on how flat a row is.
 //
-// Measured: 80 rows of 128256 bf16 with the usual filters 19 us, 512 of 152064 with filters of all
-// kinds 106 us, with top-p alone 158 us, 5 of 32001 fp32 with top-p alone 34 us.  A row's stages
+// Measured: 80 rows of 128256 with the usual filters 19 us (bf16) and 21 us (fp32), fp32 with top-p
+// alone 92 us; 512 of 152064 bf16 with filters of all kinds 106 us, with top-p alone 158 us; 5 of
+// 32001 fp32 with top-p alone 34 us.  A row's stages
 // follow one another, and the first CTA works while the others of its cluster wait: that bounds
 // few rows and rows whose list suffices (15 % of HBM in the second case); rows that are searched
 // are bound by the instructions for every token's weight and place, three times each.
@@ -1036,8 +1037,11 @@ int launch_top(TopParams& p, cudaStream_t st) {
   int c = 1;
   while (c < kTopCluster && (stripes(c) > 32 || (int64_t)stripes(c) * kTopWarps * 32 * (16 / (int)sizeof(T)) > 65536)) c *= 2;
   while (c < 8 && (int64_t)p.rows * c < 608 && stripes(2 * c) >= 4) c *= 2;
-  // A row whose cut is searched for takes several times as long as the others, so that four CTAs pay for up to 3.5
-  // rounds of them (512 x 128256 bf16, two and four: filters of all kinds 166 and 109 us, the usual ones 45 and 50).
+  // A row whose cut is searched for takes several times as long as the others, so that four CTAs pay where a call has
+  // such rows, and cost where it has none (us, two and four; the usual filters, then filters of all kinds: 310 x 128256
+  // bf16 25 and 31, 133 and 67; 512 x 128256 43 and 49, 145 and 89; 512 x 70001 41 and 54, 101 and 92; 512 x 50257 fp32
+  // 39 and 50, 129 and 97).  Only the device knows the filters; up to 3.5 rounds of four (beyond, 560 x 128256: 45 and
+  // 52, 143 and 102).
   if (c == 2 && p.rows <= 532 && stripes(4) >= 8) c = 4;
   while (c < kTopCluster && (int64_t)p.rows * c < 304 && stripes(c) > 4) c *= 2;
   if (c > 8) {
